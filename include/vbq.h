@@ -59,7 +59,8 @@ enum {
     VBQ_ERR_CUDA        = -6,  /* a CUDA runtime call or launch failed          */
     VBQ_ERR_UNSUPPORTED = -7,  /* batch outside 1..16, or a size over a limit   */
     VBQ_ERR_TIMEOUT     = -8,  /* a bounded device wait gave up                 */
-    VBQ_ERR_NOMEM       = -9   /* device or host allocation failed              */
+    VBQ_ERR_NOMEM       = -9,  /* device or host allocation failed              */
+    VBQ_ERR_RANGE       = -10  /* a position or page outside the cache (device) */
 };
 
 /* Opaque packed matrix: host descriptor plus one device allocation. */
@@ -356,6 +357,159 @@ vbq_status_t vbq_gemv_static(const vbq_layout* layout, const uint16_t* x, float*
                              void* stream);
 
 /*
+ * ---------------------------------------------------------------------------
+ * The rest of a decode step: what stands between the packed products. (The
+ * paper has no counterpart; its decode loops run on another runtime, §6.)
+ *
+ * Types: a `type` argument is VBQ_BF16 (BF16 bit patterns) or VBQ_F32.
+ * Arrays of int32 (tables, positions) and the sampler's per-row parameters
+ * need 4-byte alignment only. All of these calls are enqueued on `stream`,
+ * allocate nothing and can be captured in a CUDA graph; their kernels are
+ * launched with programmatic dependent launch and read nothing before the
+ * previous kernel on the stream has finished.
+ * ---------------------------------------------------------------------------
+ */
+enum { VBQ_BF16 = 0, VBQ_F32 = 1 };
+
+/*
+ * A key-value cache in 4 bits, in pages of 64 tokens. The caller owns its
+ * device memory: n_pages pages of vbq_kv_page_bytes each (VBQ_ERR_SHAPE for
+ * kv_heads outside 1..1024 or a head_dim other than 64, 128 or 256). A page
+ * needs no initialisation: what no append has written is never used.
+ *
+ * A key (value) of one head is cut into groups of 64. A group is held as Eq. 1
+ * holds weights at 4 bits: s = FP16(max|x| / 7), rounded to nearest even and
+ * saturating at 65504, codes q = round-half-even(x / s) clipped to -7..7, and
+ * stands for s * q. A NaN value counts as 0. The arrangement within a page is
+ * the library's own; vbq_kv_read gives the values back.
+ *
+ * Sequences are rows of a page table: sequence b's tokens 64 i .. 64 i + 63
+ * are in page table[b * table_stride + i], i < table_pages. Rows of tokens are
+ * given as batch x rows positions `pos` (row (b, t) is a token of sequence b);
+ * a negative position marks an unused row. A position or page outside the
+ * cache is not touched: such a row is skipped (append), reads as zeros (read)
+ * or gives an undefined output (attend), and vbq_device_status reports
+ * VBQ_ERR_RANGE.
+ */
+typedef struct vbq_kv_cache {
+    void*   pages;       /* device, n_pages * page bytes */
+    int64_t n_pages;     /* 1 .. 2^31 - 1 */
+    int     kv_heads;
+    int     head_dim;
+} vbq_kv_cache;
+
+vbq_status_t vbq_kv_page_bytes(int kv_heads, int head_dim, size_t* bytes);
+
+/*
+ * vbq_kv_append — rotate, quantise and write the keys and values of new tokens.
+ *   table, table_stride, table_pages   as above (stride in entries).
+ *   pos        device, batch x rows int32. Two rows of one call must not be the
+ *              same token.
+ *   k, v       device; row r's kv_heads x head_dim values, dense, start at
+ *              r * k_stride (v_stride) elements, r = b * rows + t.
+ *   q          device, rows of heads x head_dim values, or NULL (then q_out is
+ *              NULL too).
+ *   type       of q, k and v. Pointers and row starts are 16-byte aligned.
+ *   rot_cos, rot_sin   device, rot_rows x (rot_dim / 2) float, or both NULL for
+ *              no rotation. Row p turns the first rot_dim dimensions of every
+ *              head of q and k at position p, the pairs (i, i + rot_dim / 2):
+ *              (a, c) -> (a cos - c sin, c cos + a sin), in fp32. rot_dim is a
+ *              multiple of 16 up to head_dim. A position >= rot_rows counts as
+ *              outside the cache.
+ *   q_out      device, batch x rows x heads x head_dim BF16, dense: q, rotated.
+ *              Unused rows get zeros. Must not overlap q.
+ * Batch and rows >= 0 (0 does nothing), batch * rows < 2^31.
+ */
+vbq_status_t vbq_kv_append(const vbq_kv_cache* cache, const int32_t* table, int64_t table_stride, int table_pages,
+                           const int32_t* pos, int batch, int rows, const void* q, int64_t q_stride, int heads,
+                           const void* k, int64_t k_stride, const void* v, int64_t v_stride, int type,
+                           const float* rot_cos, const float* rot_sin, int rot_dim, int64_t rot_rows,
+                           uint16_t* q_out, void* stream);
+
+/*
+ * vbq_kv_read — the values that the cache holds (the inverse of the append):
+ * k_out and v_out are device arrays of batch x rows x kv_heads x head_dim
+ * float; either may be NULL.
+ */
+vbq_status_t vbq_kv_read(const vbq_kv_cache* cache, const int32_t* table, int64_t table_stride, int table_pages,
+                         const int32_t* pos, int batch, int rows, float* k_out, float* v_out, void* stream);
+
+/*
+ * vbq_kv_attend — attention of new rows over the cache:
+ *   out[b, t, h] = sum_j p_j v_j,  p = softmax_j(scale * q[b, t, h] . k_j),
+ * over the keys j of sequence b with pos[b, t] - window < j <= pos[b, t]
+ * (window 0: every j from 0). The row's own token is among them, so append
+ * first. Query head h reads key-value head h / (heads / kv_heads). A row with
+ * no keys (unused) gives zeros.
+ *   rows       1..16 new rows per sequence, as the products' batches
+ *              (VBQ_ERR_UNSUPPORTED otherwise); batch 0..1024. Rows of one
+ *              sequence share its keys' reads, in any order of positions.
+ *   q, out     device, batch x rows x heads x head_dim BF16, dense. |q| below
+ *              2^64.
+ *   heads      a multiple of kv_heads (VBQ_ERR_SHAPE otherwise), at most 64 of
+ *              them per key-value head.
+ *   workspace  device, vbq_kv_workspace_bytes of these sizes, 16-byte aligned,
+ *              zero before its first use; every call leaves it ready for the
+ *              next. Calls that share one must not overlap on the GPU. It
+ *              serves every call of at most these sizes (each of batch, rows,
+ *              heads) on a cache of the same shape.
+ * Scores, softmax statistics and sums are fp32; queries and probabilities
+ * enter the tensor cores in FP16, scaled by powers of two (11 significant
+ * bits: finer than the BF16 of q and out). Results do not vary between calls.
+ */
+vbq_status_t vbq_kv_workspace_bytes(const vbq_kv_cache* cache, int batch, int rows, int heads, size_t* bytes);
+vbq_status_t vbq_kv_attend(const vbq_kv_cache* cache, const int32_t* table, int64_t table_stride, int table_pages,
+                           const int32_t* pos, int batch, int rows, const uint16_t* q, int heads, float scale,
+                           int window, uint16_t* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * vbq_residual_norm — the residual addition and the root-mean-square norm
+ * before a product, per row of `width` values:
+ *   r' = type(residual + x)   (x itself when residual is NULL)
+ *   out = BF16(r' * rsqrt(mean(r'^2) + eps) * weight)
+ * The sum is fp32, rounded to the residual's type; the norm is of the rounded
+ * values, in fp32.
+ *   x             device, rows x width of x_type (a product's y).
+ *   residual      device, rows x width of residual_type, or NULL.
+ *   weight        device, width float.
+ *   eps           >= 0 and finite (VBQ_ERR_ARG otherwise).
+ *   rows, width   rows >= 0 (0 does nothing), width 1..2^20.
+ *   out           device, rows x width BF16 bit patterns: the next product's x.
+ *   residual_out  device, as residual; may be residual itself (in place). NULL
+ *                 exactly when residual is.
+ */
+vbq_status_t vbq_residual_norm(const void* x, int x_type, const void* residual, int residual_type,
+                               const float* weight, float eps, int64_t rows, int width, uint16_t* out,
+                               void* residual_out, void* stream);
+
+/*
+ * vbq_sample — draw one token per row of logits from given random numbers.
+ * Per row, with l the logits (a NaN counts as -inf) and m their maximum:
+ *   e_i = exp((l_i - m) / temperature) in fp32, and w_i = e_i rounded to a whole
+ *   multiple of 2^-32 (so sums are exact and do not depend on their order);
+ *   top_k   keeps the k largest logits (0 or less: all);
+ *   top_p   of those, the shortest run from the largest down whose weight is at
+ *           least top_p times theirs, at least one (1 or more: all);
+ *   min_p   of those, the ones with e_i >= min_p (at most 1 counts);
+ *   the draw takes the least index i for which the kept weights of tokens
+ *   0..i sum to more than u times the kept weights.
+ * Logits equal at a cut are kept from the lowest index up. A temperature that
+ * is not positive takes the first largest logit. A row without a logit above
+ * -inf gives token -1 (probability 0, 0 kept).
+ *   logits      device, row b at b * stride elements of `type` (element
+ *               alignment).
+ *   batch       0..65535; vocab 1..2^18 (VBQ_ERR_UNSUPPORTED above).
+ *   temperature, top_k, top_p, min_p, u   device, one per row; u in [0, 1).
+ *   tokens      device, batch int32.
+ *   probs       device, batch float: the drawn token's e over the kept weights;
+ *               or NULL.
+ *   kept        device, batch int32: how many tokens the filters left; or NULL.
+ */
+vbq_status_t vbq_sample(const void* logits, int64_t stride, int type, int batch, int vocab, const float* temperature,
+                        const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
+                        int32_t* tokens, float* probs, int32_t* kept, void* stream);
+
+/*
  * vbq_device_status — report (and clear) a bounded wait that gave up.
  * (The paper has no counterpart; this is the library's failure report.)
  *
@@ -366,8 +520,11 @@ vbq_status_t vbq_gemv_static(const vbq_layout* layout, const uint16_t* x, float*
  * copies in flight, so the CUDA context stays usable; the affected y is
  * undefined. This call synchronises `stream`, then reads and clears the word.
  *
- *   Returns VBQ_OK, VBQ_ERR_TIMEOUT (some product since the last call gave
- *   up), or VBQ_ERR_CUDA.
+ * A cache call (vbq_kv_*) that met a position or page outside its cache has
+ * recorded VBQ_ERR_RANGE the same way.
+ *
+ *   Returns VBQ_OK, VBQ_ERR_TIMEOUT (some kernel since the last call gave
+ *   up), VBQ_ERR_RANGE, or VBQ_ERR_CUDA.
  */
 vbq_status_t vbq_device_status(void* stream);
 

@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "../../include/vbq.h"
+#include "vbq_decode.h"
 #include "vbq_kernels.h"
 
 struct vbq_layout {
@@ -29,13 +30,7 @@ namespace {
 
 thread_local char g_err[512] = "";
 
-vbq_status_t fail(vbq_status_t st, const char* fmt, ...) {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_err, sizeof(g_err), fmt, ap);
-    va_end(ap);
-    return st;
-}
+using vbq::fail;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -70,6 +65,20 @@ vbq_status_t check_layout(const vbq_layout* L) {
 
 }  // namespace
 
+namespace vbq {
+
+vbq_status_t fail(vbq_status_t st, const char* fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    va_end(ap);
+    return st;
+}
+
+void clear_error() { g_err[0] = 0; }
+
+}  // namespace vbq
+
 extern "C" {
 
 const char* vbq_status_string(vbq_status_t st) {
@@ -84,6 +93,7 @@ const char* vbq_status_string(vbq_status_t st) {
         case VBQ_ERR_UNSUPPORTED: return "VBQ_ERR_UNSUPPORTED";
         case VBQ_ERR_TIMEOUT: return "VBQ_ERR_TIMEOUT";
         case VBQ_ERR_NOMEM: return "VBQ_ERR_NOMEM";
+        case VBQ_ERR_RANGE: return "VBQ_ERR_RANGE";
         default: return "VBQ_ERR_UNKNOWN";
     }
 }
@@ -503,7 +513,13 @@ vbq_status_t vbq_chain_free(vbq_chain* C) {
 vbq_status_t vbq_device_status(void* stream) {
     g_err[0] = 0;
     uint32_t word = 0;
+    uint32_t kv = 0, attend = 0;
     VBQ_CUDA(vbq::read_device_status(&word, static_cast<cudaStream_t>(stream)));
+    VBQ_CUDA(vbq::read_device_status_kv(&kv));
+    VBQ_CUDA(vbq::read_device_status_attend(&attend));
+    word |= kv | attend;
+    if (word == vbq::VBQ_DEVICE_RANGE)
+        return fail(VBQ_ERR_RANGE, "a position or page of a cache call lay outside the cache");
     if (word) return fail(VBQ_ERR_TIMEOUT, "a bounded device wait gave up (status word 0x%x)", word);
     return VBQ_OK;
 }

@@ -19,6 +19,7 @@ STATUS_NAMES = {
     0: "VBQ_OK", -1: "VBQ_ERR_ARG", -2: "VBQ_ERR_SHAPE", -3: "VBQ_ERR_WIDTH",
     -4: "VBQ_ERR_CODE_RANGE", -5: "VBQ_ERR_ALIGN", -6: "VBQ_ERR_CUDA",
     -7: "VBQ_ERR_UNSUPPORTED", -8: "VBQ_ERR_TIMEOUT", -9: "VBQ_ERR_NOMEM",
+    -10: "VBQ_ERR_RANGE",
 }
 
 # Every symbol include/vbq.h declares, with (restype, argtypes).
@@ -44,6 +45,14 @@ SIGNATURES = {
     "vbq_chain_run": (_I, [_P, _P]),
     "vbq_chain_free": (_I, [_P]),
     "vbq_gemv_group": (_I, [ctypes.POINTER(_P), ctypes.POINTER(_P), ctypes.POINTER(_P), _I, _P]),
+    "vbq_kv_page_bytes": (_I, [_I, _I, _SZP]),
+    "vbq_kv_append": (_I, [_P, _P, _I64, _I, _P, _I, _I, _P, _I64, _I, _P, _I64, _P, _I64, _I, _P, _P, _I, _I64,
+                           _P, _P]),
+    "vbq_kv_read": (_I, [_P, _P, _I64, _I, _P, _I, _I, _P, _P, _P]),
+    "vbq_kv_workspace_bytes": (_I, [_P, _I, _I, _I, _SZP]),
+    "vbq_kv_attend": (_I, [_P, _P, _I64, _I, _P, _I, _I, _P, _I, ctypes.c_float, _I, _P, _P, ctypes.c_size_t, _P]),
+    "vbq_residual_norm": (_I, [_P, _I, _P, _I, _P, ctypes.c_float, _I64, _I, _P, _P, _P]),
+    "vbq_sample": (_I, [_P, _I64, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
     "vbq_device_status": (_I, [_P]),
     "vbq_selftest_timeout": (_I, [_I, _P]),
     "vbq_free": (_I, [_P]),
@@ -292,7 +301,8 @@ def vbq_gemm_small(layout: Layout, X, Y, B: Optional[int] = None, stream=None) -
 
 def vbq_device_status(stream=None) -> None:
     """Synchronise the stream; raise VbqError(VBQ_ERR_TIMEOUT) if a bounded
-    device wait gave up since the last call (the record is cleared)."""
+    device wait gave up since the last call, VbqError(VBQ_ERR_RANGE) if a cache
+    call met a position or page outside its cache (the record is cleared)."""
     _check(load().vbq_device_status(_stream(stream)))
 
 
