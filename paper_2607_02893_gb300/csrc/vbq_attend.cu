@@ -1,9 +1,45 @@
-// vbq_attend.cu — attention over the 4-bit cache.
+// vbq_attend.cu — attention over the 4-bit cache, for one to sixteen new rows
+// per sequence.
 //
 // out = sum_j softmax_j(scale q.k_j) v_j over the keys j in (p - window, p] of
-// a row at position p. One block per (sequence, row, query head); groups of
-// d / 8 lanes take a key each, a lane 8 of its dimensions, with a running
-// maximum and sum per group, joined through shared memory at the end.
+// a row at position p, in one pass over the cache with a running maximum and
+// sum. The query rows that share a key-value head (its group of heads, times
+// the sequence's new rows) go through the cache together, 8 * NT at a time.
+//
+// Bound: the cache's bytes (136 B per token and head at d = 128) at HBM speed,
+// which leaves under three thread instructions per code at full issue: the
+// decode has to be nearly free. So the codes go to the tensor cores
+// (mma.m16n8k16, f16) as they are: a masked nibble at bits 2..5 of a half is the
+// denormal u * 2^-22 exactly, one at bits 6..9 is u * 2^-18, so one mask makes
+// two operands, with a byte swap for every second pair (kv_turned). The MMA
+// aligns its products by their operands' exponents, and a denormal's is that of
+// 2^-14: the fp32 sum resolves 2^-16 of a code's step from bits 2..5 and 2^-20
+// from bits 6..9. Keys take both (a score's error is then below 2^-16 of
+// sum |q| in units of the key's scale); values are shifted up to bits 6..9
+// first, so that a large probability on a zero code leaves nothing behind.
+//   - S^T = K Q^T: keys are the MMA's 16 rows, query rows its 8 columns. The
+//     middle of the codes (8) enters as the accumulators' start, -8 times the
+//     group's sum of q; the key's scale multiplies the group's result in fp32.
+//     q enters in f16, scaled per row by a power of two so that its largest
+//     value is in [2^12, 2^13): exact for BF16 values down to 2^-27 of it.
+//   - O^T = V^T P^T: a value's word holds 8 dimensions of one key, so pairing
+//     the words of two keys (a byte permute per 4 operands) gives A fragments
+//     whose rows are dimensions. P^T is S^T's accumulators times the key's
+//     value scale, rounded to f16 (11 bits) and turned by movmatrix; scales are
+//     taken relative to a running power of two, as the maximum is, so that f16
+//     never runs out of range. The codes' middle is subtracted at the end: one
+//     more MMA with ones sums the rounded P, so what is subtracted is exactly
+//     what the rounded probabilities added.
+// Weights as the A operand make every decoded nibble pair serve 8 query rows
+// and keep the accumulators' columns (rows of q) in the same lanes for S, P and
+// O: no shuffles but the maximum's.
+//
+// A warp takes whole pages (64 keys of one head, one contiguous blob) through
+// its own ring of shared-memory stages filled by bulk copies: no barrier in the
+// steady state. The pages of all (sequence, head) segments form one list that
+// is cut evenly over the blocks, one per SM, whatever the lengths; a segment
+// that crosses blocks is joined through the workspace by the block that
+// finishes last, in block order, so results do not depend on timing.
 #include <cuda_bf16.h>
 
 #include "vbq_decode.h"
@@ -12,74 +48,657 @@
 namespace vbq {
 namespace {
 
-constexpr int AT_THREADS = 128;
+constexpr uint32_t FULL = 0xffffffffu;
+constexpr uint32_t LOW = 0x003c003cu, HIGH = 0x03c003c0u;    // codes at bits 2..5 and 6..9 of each half
 
-__global__ void __launch_bounds__(AT_THREADS) kv_attend_kernel(KvView c, KvAttend a) {
-    extern __shared__ float sh[];
+// D: head dimension, NT: 8-row tiles of query rows per pass, W: warps, S: stages per warp.
+template <int D_, int NT_, int W_, int S_>
+struct Shape {
+    static constexpr int D = D_, NT = NT_, W = W_, S = S_;
+    static constexpr int ROWS = 8 * NT;
+    static constexpr int GR = D / 64;            // scale groups
+    static constexpr int KW = D / 32;            // words of a key per lane
+    static constexpr int TILES = D / 16;         // output tiles of 16 dimensions
+    static constexpr int BLOB = 68 * D;
+    static constexpr int THREADS = 32 * W;
+    static constexpr int UNITS = ROWS * D / 8;   // 8 outputs each
+    // shared memory
+    static constexpr int BARS = W * S * BLOB;                    // full barriers
+    static constexpr int ML = BARS + W * S * 8;                  // (maximum, sum) per warp and row
+    static constexpr int CUM = ML + W * ROWS * 8;                // pages before each sequence
+    static constexpr int LO = CUM + (KV_MAX_BATCH + 2) * 8;      // first page of each sequence
+    static constexpr int MISC = LO + KV_MAX_BATCH * 4;
+    static constexpr int SMEM = MISC + 64 + 4 * W;
+    static constexpr int PART = ROWS * D + 2 * ROWS;             // floats of a partial result
+};
+
+struct __align__(16) Misc {
+    int64_t quantum;
+    int abort, last;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }   // e in -126..127
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t a) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                    uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The words at a shared address (16, 8 or 4 bytes at a time).
+template <int N>
+__device__ __forceinline__ void lds_words(uint32_t (&w)[N], uint32_t at) {
+    if constexpr (N == 1) {
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at));
+    } else if constexpr (N == 2) {
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3])
+                         : "r"(at + 4 * i));
+    }
+}
+
+// One (sequence, row tile, key-value head): its place in the list of pages.
+struct Segment {
+    int b, rt, h;
+    int64_t start, pages;                        // in the list
+    int64_t index;                               // among all segments
+};
+
+struct List {
+    const int64_t* cum;                          // shared: pages of one head before each sequence
+    const int* lo;
+    int batch, kv_heads, per_seq;                // segments per sequence
+    __device__ Segment at(int64_t p) const {
+        int b = 0, e = batch;                    // the last b with cum[b] * per_seq <= p (it has pages: p is in the list)
+        while (e - b > 1) {
+            const int m = (b + e) >> 1;
+            if (cum[m] * per_seq <= p) b = m; else e = m;
+        }
+        Segment s;
+        s.b = b;
+        s.pages = cum[b + 1] - cum[b];
+        const int64_t in = p - cum[b] * per_seq, k = in / s.pages;
+        s.start = cum[b] * per_seq + k * s.pages;
+        s.rt = (int)(k / kv_heads);
+        s.h = (int)(k - (int64_t)s.rt * kv_heads);
+        s.index = (int64_t)b * per_seq + k;
+        return s;
+    }
+};
+
+template <class C>
+__global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAttend a, int row_tiles, uint32_t* counts,
+                                                                 float* parts) {
+    constexpr int D = C::D, NT = C::NT, W = C::W, S = C::S, GR = C::GR, KW = C::KW;
+    extern __shared__ __align__(128) uint8_t smem[];
+    const uint32_t sbase = smem_u32(smem);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int g = lane >> 2, t4 = lane & 3;
+    float2* ml = reinterpret_cast<float2*>(smem + C::ML);
+    int64_t* cum = reinterpret_cast<int64_t*>(smem + C::CUM);
+    int* lo_page = reinterpret_cast<int*>(smem + C::LO);
+    Misc* misc = reinterpret_cast<Misc*>(smem + C::MISC);
+    int* kept_in = reinterpret_cast<int*>(smem + C::MISC + 64);          // the stage a warp's partial result is in
+    const uint32_t abort_addr = sbase + C::MISC + 8;
+    const int group = a.heads / c.kv_heads, rows_all = group * a.rows, per_seq = row_tiles * c.kv_heads;
+
+    if (tid < W * S) mbar_init(sbase + C::BARS + 8 * tid, 1);
+    if (tid == 0) {
+        misc->abort = 0;
+        misc->last = 0;
+    }
+    fence_barrier_init();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int d = c.head_dim, lanes = d / 8, teams = AT_THREADS / lanes;
-    const int team = threadIdx.x / lanes, ch = threadIdx.x % lanes;
-    const int64_t row = blockIdx.x / a.heads;
-    const int head = (int)(blockIdx.x % a.heads), h = head / (a.heads / c.kv_heads);
-    const int64_t b = row / a.rows;
-    int64_t p = a.pos[row];
-    if (p >= (int64_t)c.table_pages * KV_PAGE) {
-        if (threadIdx.x == 0) atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
-        p = (int64_t)c.table_pages * KV_PAGE - 1;
-    }
-    const int64_t lo = a.window && p >= a.window ? p - a.window + 1 : 0;
-    float q[8], o[8] = {}, m = -INFINITY, l = 0.f;
-    for (int e = 0; e < 8; ++e)
-        q[e] = __uint_as_float((uint32_t)a.q[(row * a.heads + head) * d + ch * 8 + e] << 16) * a.scale;
-    for (int64_t j0 = lo; j0 <= p; j0 += teams) {
-        const int64_t j = j0 + team;
-        const bool live = j <= p;
-        const int64_t jj = live ? j : p;
-        int64_t page = c.table[b * c.table_stride + jj / KV_PAGE];
-        if (page < 0 || page >= c.n_pages) {
-            atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
-            page = 0;
+
+    // Every sequence's range of pages.
+    const int64_t table_keys = (int64_t)c.table_pages * KV_PAGE;
+    for (int b = tid; b < a.batch; b += C::THREADS) {
+        int hi = -1, mn = 0x7fffffff;
+        for (int t = 0; t < a.rows; ++t) {
+            const int p = a.pos[b * a.rows + t];
+            hi = max(hi, p);
+            if (p >= 0) mn = min(mn, p);
         }
-        const int slot = (int)(jj % KV_PAGE), krow = kv_key_row(slot);
-        const uint8_t* blob = c.pages + (page * c.kv_heads + h) * kv_blob_bytes(d);
-        const uint32_t kw = *reinterpret_cast<const uint32_t*>(blob + krow * (d / 2) + 4 * kv_key_word(ch, d));
-        const uint32_t vw = *reinterpret_cast<const uint32_t*>(blob + kv_values_at(d) + slot * (d / 2) +
-                                                               4 * kv_value_word(ch, slot, d));
-        const __half* sc = reinterpret_cast<const __half*>(blob + kv_scales_at(d) + krow * (d / 16));
-        const float ks = __half2float(sc[ch >> 3]), vs = __half2float(sc[d / 64 + (ch >> 3)]);
-        float s = 0.f;
-        for (int e = 0; e < 8; ++e) s = fmaf(q[e], (float)((int)((kw >> (4 * e)) & 15u) - 8), s);
-        s *= ks;
-        for (int x = lanes / 2; x; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-        if (!live) continue;
-        const float mn = fmaxf(m, s), f = expf(m - mn), w = expf(s - mn);
-        l = l * f + w;
-        m = mn;
-        for (int e = 0; e < 8; ++e) o[e] = o[e] * f + w * vs * (float)((int)((vw >> (4 * e)) & 15u) - 8);
+        if (hi >= table_keys) {
+            if (blockIdx.x == 0) atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
+            hi = (int)(table_keys - 1);
+            mn = min(mn, hi);
+        }
+        const int lo = hi >= 0 && a.window > 0 && mn >= a.window ? mn - a.window + 1 : 0;
+        lo_page[b] = lo / KV_PAGE;
+        cum[b + 1] = hi < 0 ? 0 : hi / KV_PAGE - lo / KV_PAGE + 1;
     }
-    float* sm = sh + teams * d;
-    for (int e = 0; e < 8; ++e) sh[team * d + ch * 8 + e] = o[e];
-    if (ch == 0) { sm[2 * team] = m; sm[2 * team + 1] = l; }
+    if (tid == 0) cum[0] = 0;
     __syncthreads();
-    float mx = -INFINITY, ls = 0.f;
-    for (int t = 0; t < teams; ++t) mx = fmaxf(mx, sm[2 * t]);
-    for (int t = 0; t < teams; ++t) ls += sm[2 * t + 1] > 0.f ? sm[2 * t + 1] * expf(sm[2 * t] - mx) : 0.f;
-    for (int i = threadIdx.x; i < d; i += AT_THREADS) {
-        float v = 0.f;
-        for (int t = 0; t < teams; ++t)
-            if (sm[2 * t + 1] > 0.f) v += sh[t * d + i] * expf(sm[2 * t] - mx);
-        a.out[(row * a.heads + head) * d + i] = __bfloat16_as_ushort(__float2bfloat16_rn(ls > 0.f ? v / ls : 0.f));
+    if (warp == 0) {
+        int64_t before = 0, most = 0;
+        for (int b0 = 0; b0 < a.batch; b0 += 32) {
+            const int b = b0 + lane;
+            int64_t x = b < a.batch ? cum[b + 1] : 0;
+            most = max(most, x);
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t y = __shfl_up_sync(FULL, x, o);
+                if (lane >= o) x += y;
+            }
+            x += before;
+            before = __shfl_sync(FULL, x, 31);
+            if (b < a.batch) cum[b + 1] = x;
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) most = max(most, (int64_t)__shfl_xor_sync(FULL, most, o));
+        if (lane == 0) {
+            // an even share of the pages; short segments are not cut where a block's warps take them at once
+            int64_t q = (before * per_seq + gridDim.x - 1) / gridDim.x;
+            if (most <= W && q < most) q = most;
+            misc->quantum = q > 0 ? q : 1;
+        }
     }
+    __syncthreads();
+    const List list{cum, lo_page, a.batch, c.kv_heads, per_seq};
+    const int64_t total = cum[a.batch] * per_seq, quantum = misc->quantum;
+    const int64_t p0 = min(total, (int64_t)blockIdx.x * quantum), p1 = min(total, p0 + quantum);
+
+    // Sequences without keys: zeros.
+    for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
+        if (cum[b + 1] != cum[b]) continue;
+        uint4* o = reinterpret_cast<uint4*>(a.out + (int64_t)b * a.rows * a.heads * D);
+        for (int64_t i = tid; i < (int64_t)a.rows * a.heads * (D / 8); i += C::THREADS) o[i] = make_uint4(0, 0, 0, 0);
+    }
+
+    // The warp's own pages: p0 + warp, + W, ...; the k-th uses stage k % S.
+    const uint8_t* src = nullptr;                 // lane i: of the page 32 * n + i
+    int64_t issued = 0, used = 0, landed = 0;     // landed: copies waited for
+    bool ok = true;
+    const int64_t mine = p1 - p0 > warp ? (p1 - p0 - warp + W - 1) / W : 0;
+    auto issue = [&]() {                          // the next page's copy
+        if (issued >= mine || !ok) return;
+        if ((issued & 31) == 0) {
+            const int64_t k = issued + lane;
+            if (k < mine) {
+                const int64_t p = p0 + warp + k * W;
+                const Segment s = list.at(p);
+                int64_t page = c.table[s.b * c.table_stride + lo_page[s.b] + (p - s.start)];
+                if (page < 0 || page >= c.n_pages) {
+                    atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
+                    page = 0;
+                }
+                src = c.pages + (page * c.kv_heads + s.h) * C::BLOB;
+            }
+        }
+        const int st = (int)(issued % S);
+        if (lane == (int)(issued & 31))
+            bulk_load(sbase + (warp * S + st) * C::BLOB, src, C::BLOB, sbase + C::BARS + 8 * (warp * S + st));
+        ++issued;
+    };
+    for (int i = 0; i < S; ++i) issue();
+
+    for (int64_t cur = p0; cur < p1;) {
+        const Segment s = list.at(cur);
+        const int64_t end = min(p1, s.start + s.pages);
+        const int hi_key = [&] {                  // the sequence's last key
+            int hi = -1;
+            for (int t = 0; t < a.rows; ++t) hi = max(hi, a.pos[s.b * a.rows + t]);
+            return (int)min((int64_t)hi, table_keys - 1);
+        }();
+
+        // Query fragments of the tile's rows, and the rows' parameters per accumulator column.
+        uint32_t qb[NT][KW][4];
+        float corr[NT][GR][2], f[NT][2];
+        int pos[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int r = s.rt * C::ROWS + 8 * n + g;
+            const bool live = r < rows_all;
+            const int t = live ? r / group : 0, hq = live ? s.h * group + r % group : 0;
+            const uint16_t* q = a.q + (((int64_t)s.b * a.rows + t) * a.heads + hq) * D;
+            uint4 w[KW];
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < KW; ++j) {
+                w[j] = live ? *reinterpret_cast<const uint4*>(q + 64 * (j / 2) + 32 * (j & 1) + 8 * t4) : make_uint4(0, 0, 0, 0);
+                const uint32_t v[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = max(top, max(v[i] << 16 & 0x7fff0000u, v[i] & 0x7fff0000u));
+            }
+            top = max(top, __shfl_xor_sync(FULL, top, 1));
+            top = max(top, __shfl_xor_sync(FULL, top, 2));
+            const int e = max((int)(top >> 23), 13);                     // biased exponent of the row's largest value
+            const float up = pow2(139 - e);                              // to [2^12, 2^13)
+            const float fr = a.scale * 1.44269504f * 0x1p22f * pow2(e - 139);
+            float sum[GR];
+#pragma unroll
+            for (int i = 0; i < GR; ++i) sum[i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < KW; ++j) {
+                const uint32_t v[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[2 * i] = __uint_as_float(v[i] << 16) * up;
+                    x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u) * up;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {                            // nibbles i and i + 4; odd ones carry a factor 16
+                    const float by = i & 1 ? 0.0625f : 1.f;
+                    qb[n][j][i] = half2_bits(x[i] * by, x[i + 4] * by);
+                    const __half2 h = *reinterpret_cast<const __half2*>(&qb[n][j][i]);
+                    sum[j / 2] += (__low2float(h) + __high2float(h)) * (i & 1 ? 16.f : 1.f);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < GR; ++i) {
+                sum[i] += __shfl_xor_sync(FULL, sum[i], 1);
+                sum[i] += __shfl_xor_sync(FULL, sum[i], 2);
+                corr[n][i][0] = -8.f * 0x1p-22f * __shfl_sync(FULL, sum[i], 8 * t4);
+                corr[n][i][1] = -8.f * 0x1p-22f * __shfl_sync(FULL, sum[i], 8 * t4 + 4);
+            }
+            f[n][0] = __shfl_sync(FULL, fr, 8 * t4);
+            f[n][1] = __shfl_sync(FULL, fr, 8 * t4 + 4);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int rc = s.rt * C::ROWS + 8 * n + 2 * t4 + i;
+                pos[n][i] = rc < rows_all ? a.pos[s.b * a.rows + rc / group] : 0x7fffffff;
+            }
+        }
+        // Keys that every row of the tile attends to: (open, close].
+        int close = 0x7fffffff, open = -1;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                close = min(close, pos[n][i]);
+                if (a.window > 0 && pos[n][i] != 0x7fffffff) open = max(open, pos[n][i] - a.window);
+            }
+        close = min(__reduce_min_sync(FULL, close), hi_key);
+        open = __reduce_max_sync(FULL, open);
+
+        float acc[C::TILES][NT][4], ones[GR][NT][4], m[NT][2], l[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) { m[n][i] = -INFINITY; l[n][i] = 0.f; }
+#pragma unroll
+            for (int k = 0; k < C::TILES; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[k][n][i] = 0.f;
+#pragma unroll
+            for (int k = 0; k < GR; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ones[k][n][i] = 0.f;
+        }
+        int vexp = -13;                           // value scales are taken in units of 2^(vexp - 14)
+        bool any = false;
+
+        for (int64_t p = p0 + warp + used * W; p < end; p += W) {
+            if (any) { __syncwarp(); issue(); }   // into the stage of the page before
+            any = true;
+            const int st = (int)(used % S);
+            const uint32_t stage = sbase + (warp * S + st) * C::BLOB;
+            if (ok && !warp_wait(sbase + C::BARS + 8 * (warp * S + st), (uint32_t)(used / S) & 1u, abort_addr)) {
+                if (lane == 0) raise_abort(&misc->abort);
+                ok = false;
+            }
+            ++used;
+            if (!ok) continue;
+            landed = used;
+            const int key0 = (int)((lo_page[s.b] + (p - s.start)) * KV_PAGE);
+            const int subs = min(4, (hi_key - key0) / 16 + 1);
+            const bool edge = key0 + KV_PAGE - 1 > close || key0 <= open;
+
+            float sc[4][NT][4];
+            __half2 vtop = __float2half2_rn(0.f);
+#pragma unroll
+            for (int sub = 0; sub < 4; ++sub) {
+                if (sub < subs) {
+                    uint32_t k0[KW], k1[KW], sw0[GR], sw1[GR];           // keys g and g + 8 (in row order), their scales
+                    const uint32_t krow = stage + (sub * 16 + g) * (D / 2) + t4 * (D / 8);
+                    const uint32_t srow = stage + kv_scales_at(D) + (sub * 16 + g) * (D / 16);
+                    lds_words<KW>(k0, krow);
+                    lds_words<KW>(k1, krow + 8 * (D / 2));
+                    lds_words<GR>(sw0, srow);
+                    lds_words<GR>(sw1, srow + 8 * (D / 16));
+                    const __half* s0 = reinterpret_cast<const __half*>(sw0);
+                    const __half* s1 = reinterpret_cast<const __half*>(sw1);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sc[sub][n][i] = 0.f;
+#pragma unroll
+                    for (int q = 0; q < GR; ++q) {
+                        float d[NT][4];
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            d[n][0] = d[n][2] = corr[n][q][0];
+                            d[n][1] = d[n][3] = corr[n][q][1];
+                        }
+#pragma unroll
+                        for (int j = 2 * q; j < 2 * q + 2; ++j) {
+                            const uint32_t x0 = k0[j], x1 = k1[j], y0 = prmt(x0, 0, 0x2301), y1 = prmt(x1, 0, 0x2301);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) {
+                                mma(d[n], x0 & LOW, x1 & LOW, x0 & HIGH, x1 & HIGH,
+                                    qb[n][j][0], qb[n][j][1]);
+                                mma(d[n], y0 & LOW, y1 & LOW, y0 & HIGH, y1 & HIGH,
+                                    qb[n][j][2], qb[n][j][3]);
+                            }
+                        }
+                        const float e0 = __half2float(s0[q]), e1 = __half2float(s1[q]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            sc[sub][n][0] = fmaf(d[n][0], e0, sc[sub][n][0]);
+                            sc[sub][n][1] = fmaf(d[n][1], e0, sc[sub][n][1]);
+                            sc[sub][n][2] = fmaf(d[n][2], e1, sc[sub][n][2]);
+                            sc[sub][n][3] = fmaf(d[n][3], e1, sc[sub][n][3]);
+                        }
+                    }
+                    const int key = key0 + sub * 16 + (g >> 1) + (g & 1) * 4;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            sc[sub][n][i] *= f[n][i & 1];
+                            if (edge) {
+                                const int k = key + (i >> 1) * 8, p_ = pos[n][i & 1];
+                                if (k > p_ || k > hi_key || (a.window > 0 && k <= p_ - a.window)) sc[sub][n][i] = -INFINITY;
+                            }
+                        }
+                    // the largest value scale among keys that exist
+#pragma unroll
+                    for (int q = 0; q < GR; ++q) {
+                        const __half z = __float2half(0.f);
+                        vtop = __hmax2(vtop, __halves2half2(edge && key > hi_key ? z : s0[GR + q],
+                                                            edge && key + 8 > hi_key ? z : s1[GR + q]));
+                    }
+                } else {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sc[sub][n][i] = -INFINITY;
+                }
+            }
+
+            // Running maximum per row, running power of two of the value scales.
+            const uint32_t vb = __reduce_max_sync(
+                FULL, max((uint32_t)__half_as_ushort(__low2half(vtop)), (uint32_t)__half_as_ushort(__high2half(vtop))));
+            const int vnew = max(vexp, max((int)(vb >> 10), 1) - 14);    // scales below 2^vnew
+            const float shrink = pow2(vexp - vnew);
+            bool moved = vnew != vexp;
+            vexp = vnew;
+            float mu[NT][2], fac[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float x = m[n][i];
+#pragma unroll
+                    for (int sub = 0; sub < 4; ++sub) x = fmaxf(x, fmaxf(sc[sub][n][i], sc[sub][n][i + 2]));
+                    x = fmaxf(x, __shfl_xor_sync(FULL, x, 4));
+                    x = fmaxf(x, __shfl_xor_sync(FULL, x, 8));
+                    x = fmaxf(x, __shfl_xor_sync(FULL, x, 16));
+                    mu[n][i] = x == -INFINITY ? 0.f : x;
+                    fac[n][i] = ex2(m[n][i] - mu[n][i]);
+                    moved |= x != m[n][i];
+                    m[n][i] = x;
+                    l[n][i] *= fac[n][i];
+                    fac[n][i] *= shrink;
+                }
+            if (__any_sync(FULL, moved)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int k = 0; k < C::TILES; ++k)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[k][n][i] *= fac[n][i & 1];
+#pragma unroll
+                    for (int k = 0; k < GR; ++k)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) ones[k][n][i] *= fac[n][i & 1];
+                }
+            }
+            const float vup = pow2(14 - vexp);
+
+#pragma unroll
+            for (int sub = 0; sub < 4; ++sub) {
+                if (sub >= subs) break;
+                uint32_t sw0[GR], sw1[GR], vw[4][GR];
+                const uint32_t srow = stage + kv_scales_at(D) + (sub * 16 + g) * (D / 16);
+                lds_words<GR>(sw0, srow);
+                lds_words<GR>(sw1, srow + 8 * (D / 16));
+                const uint32_t turn = D == 64 ? g : D == 128 ? g ^ ((t4 >> 1) << 2) : g ^ (t4 << 1);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    lds_words<GR>(vw[j], stage + kv_values_at(D) + (sub * 16 + 4 * j + t4) * (D / 2) + turn * (D / 16));
+                const __half* s0 = reinterpret_cast<const __half*>(sw0);
+                const __half* s1 = reinterpret_cast<const __half*>(sw1);
+                const int key = key0 + sub * 16 + (g >> 1) + (g & 1) * 4;
+                float pr[NT][4];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pr[n][i] = ex2(sc[sub][n][i] - mu[n][i & 1]);
+                    l[n][0] += pr[n][0] + pr[n][2];
+                    l[n][1] += pr[n][1] + pr[n][3];
+                }
+#pragma unroll
+                for (int q = 0; q < GR; ++q) {
+                    float e0 = __half2float(s0[GR + q]) * vup, e1 = __half2float(s1[GR + q]) * vup;
+                    if (edge) {                   // what was never written may be anything
+                        if (key > hi_key) e0 = 0.f;
+                        if (key + 8 > hi_key) e1 = 0.f;
+                    }
+                    uint32_t b0[NT], b1[NT];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        b0[n] = transposed(half2_bits(pr[n][0] * e0, pr[n][1] * e0));
+                        b1[n] = transposed(half2_bits(pr[n][2] * e1, pr[n][3] * e1));
+                    }
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {                     // dimensions 0..3 and 4..7 of the words
+                        // codes 0, 1 and (bytes swapped) 2, 3 of the half: two keys' side by side
+                        const uint32_t sel = hf ? 0x7632u : 0x5410u, swp = hf ? 0x6723u : 0x4501u;
+                        const uint32_t x0 = prmt(vw[0][q], vw[1][q], sel), x2 = prmt(vw[2][q], vw[3][q], sel);
+                        const uint32_t y0 = prmt(vw[0][q], vw[1][q], swp), y2 = prmt(vw[2][q], vw[3][q], swp);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            mma(acc[4 * q + 2 * hf][n], x0 << 4 & HIGH, y0 << 4 & HIGH, x2 << 4 & HIGH, y2 << 4 & HIGH, b0[n],
+                                b1[n]);
+                            mma(acc[4 * q + 2 * hf + 1][n], x0 & HIGH, y0 & HIGH, x2 & HIGH, y2 & HIGH, b0[n], b1[n]);
+                        }
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        mma(ones[q][n], 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, b0[n], b1[n]);
+                }
+            }
+        }
+
+        // The warp's part of the segment, into the stage it has just read.
+        if (any) {
+            const int st = (int)((used - 1) % S);
+            float* buf = reinterpret_cast<float*>(smem + (warp * S + st) * C::BLOB);
+            const float down = pow2(vexp - 14);
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < C::TILES; ++k)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        buf[((k * NT + n) * 4 + i) * 32 + lane] =
+                            (acc[k][n][i] * 0x1p18f - 8.f * ones[k / 4][n][i]) * down;
+            if (lane == 0) kept_in[warp] = st;
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float x = l[n][i];
+                x += __shfl_xor_sync(FULL, x, 4);
+                x += __shfl_xor_sync(FULL, x, 8);
+                x += __shfl_xor_sync(FULL, x, 16);
+                if (g == 0) ml[warp * C::ROWS + 8 * n + 2 * t4 + i] = make_float2(m[n][i], x);
+            }
+        __syncthreads();
+
+        // Join the warps: a unit is 8 neighbouring dimensions of a row.
+        const bool whole = s.start >= cur && s.start + s.pages <= end;
+        const int64_t slot = 2 * (int64_t)blockIdx.x + (s.start <= p0 ? 0 : 1);
+        for (int u = tid; u < C::UNITS; u += C::THREADS) {
+            const int par = u >> 5 & 1, n = (u >> 6) % NT, q = (u >> 6) / NT, ln = u & 31;
+            const int row = 8 * n + 2 * (ln & 3) + par;
+            float mx = -INFINITY, sum = 0.f, v[8] = {};
+#pragma unroll
+            for (int w = 0; w < W; ++w) mx = fmaxf(mx, ml[w * C::ROWS + row].x);
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float2 x = ml[w * C::ROWS + row];
+                if (x.y == 0.f) continue;
+                const float fw = ex2(x.x - mx);
+                sum = fmaf(x.y, fw, sum);
+                const float* buf = reinterpret_cast<const float*>(smem + (w * S + kept_in[w]) * C::BLOB);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int tile = 4 * q + (i >> 2) * 2 + (i & 1), hf = i >> 1 & 1;
+                    v[i] = fmaf(buf[((tile * NT + n) * 4 + 2 * hf + par) * 32 + ln], fw, v[i]);
+                }
+            }
+            if (!whole) {
+                float4* o = reinterpret_cast<float4*>(parts + slot * C::PART) + 2 * u;
+                o[0] = make_float4(v[0], v[1], v[2], v[3]);
+                o[1] = make_float4(v[4], v[5], v[6], v[7]);
+                if (q == 0 && ln < 4) reinterpret_cast<float2*>(parts + slot * C::PART + C::ROWS * D)[row] = make_float2(mx, sum);
+                continue;
+            }
+            const int r = s.rt * C::ROWS + row;
+            if (r >= rows_all) continue;
+            const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;     // no keys: zeros; NaN stays
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i] * inv, v[2 * i + 1] * inv);
+                w[i] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            *reinterpret_cast<uint4*>(a.out + (((int64_t)s.b * a.rows + r / group) * a.heads + s.h * group + r % group) * D +
+                                      64 * q + 8 * (ln >> 2)) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        if (!whole) {
+            // The last of the segment's blocks joins their parts, in order.
+            const int64_t b0 = s.start / quantum, b1 = (s.start + s.pages - 1) / quantum;
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) misc->last = atomicAdd(&counts[s.index], 1u) == (uint32_t)(b1 - b0);
+            __syncthreads();
+            if (misc->last) {
+                __threadfence();
+                if (tid == 0) counts[s.index] = 0;
+                for (int u = tid; u < C::UNITS; u += C::THREADS) {
+                    const int par = u >> 5 & 1, n = (u >> 6) % NT, q = (u >> 6) / NT, ln = u & 31;
+                    const int row = 8 * n + 2 * (ln & 3) + par;
+                    const int r = s.rt * C::ROWS + row;
+                    if (r >= rows_all) continue;
+                    float mx = -INFINITY, sum = 0.f, v[8] = {};
+                    for (int64_t k = b0; k <= b1; ++k) {
+                        const float* part = parts + (2 * k + (s.start <= k * quantum ? 0 : 1)) * C::PART;
+                        const float2 x = __ldcg(reinterpret_cast<const float2*>(part + C::ROWS * D) + row);
+                        const float4 y0 = __ldcg(reinterpret_cast<const float4*>(part) + 2 * u),
+                                     y1 = __ldcg(reinterpret_cast<const float4*>(part) + 2 * u + 1);
+                        if (x.y == 0.f) continue;
+                        const float mn = fmaxf(mx, x.x), f0 = ex2(mx - mn), f1 = ex2(x.x - mn);
+                        mx = mn;
+                        sum = sum * f0 + x.y * f1;
+                        v[0] = v[0] * f0 + y0.x * f1; v[1] = v[1] * f0 + y0.y * f1;
+                        v[2] = v[2] * f0 + y0.z * f1; v[3] = v[3] * f0 + y0.w * f1;
+                        v[4] = v[4] * f0 + y1.x * f1; v[5] = v[5] * f0 + y1.y * f1;
+                        v[6] = v[6] * f0 + y1.z * f1; v[7] = v[7] * f0 + y1.w * f1;
+                    }
+                    const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i] * inv, v[2 * i + 1] * inv);
+                        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+                    }
+                    *reinterpret_cast<uint4*>(a.out + (((int64_t)s.b * a.rows + r / group) * a.heads + s.h * group + r % group) * D +
+                                              64 * q + 8 * (ln >> 2)) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+        }
+        __syncthreads();                          // the parts are read: their stages may be filled again
+        if (any) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            issue();
+        }
+        cur = end;
+    }
+    // A wait that ran out: let every copy land before the block's memory goes.
+    if (!ok)
+        for (; landed < issued; ++landed)
+            mbar_wait_bounded(sbase + C::BARS + 8 * (warp * S + (int)(landed % S)), (uint32_t)(landed / S) & 1u);
+}
+
+using Shape64a = Shape<64, 1, 12, 4>;
+using Shape64b = Shape<64, 2, 12, 4>;
+using Shape128a = Shape<128, 1, 12, 2>;
+using Shape128b = Shape<128, 2, 8, 3>;
+using Shape256a = Shape<256, 1, 6, 2>;
+
+// Query rows per pass: 16 where there are more than 8 (the registers for 16
+// rows of 256 dimensions are not there).
+int tile_rows(int rows, int head_dim) { return rows > 8 && head_dim <= 128 ? 16 : 8; }
+
+size_t parts_bytes(int head_dim, int sms) {       // of the largest tile, so that it does not move between calls
+    const size_t rows = head_dim <= 128 ? 16 : 8;
+    return (2 * (size_t)sms * (rows * head_dim + 2 * rows) * sizeof(float) + 255) / 256 * 256;
+}
+
+template <class C>
+cudaError_t launch(const KvView& c, const KvAttend& a, int row_tiles, cudaStream_t s) {
+    static LaunchPrep prep;
+    int sms = 0;
+    const cudaError_t e = prep.get(kv_attend_kernel<C>, C::SMEM, &sms);
+    if (e != cudaSuccess) return e;
+    uint32_t* counts = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.workspace) + parts_bytes(C::D, sms));
+    return launch_dependent(kv_attend_kernel<C>, dim3(sms), C::THREADS, C::SMEM, s, c, a, row_tiles, counts,
+                            static_cast<float*>(a.workspace));
 }
 
 }  // namespace
 
-size_t kv_workspace_bytes(int, int, int, int, int, int) { return 256; }
+// Two partial results per block (its first and its last segment), then a count
+// per segment.
+size_t kv_workspace_bytes(int batch, int rows, int heads, int kv_heads, int head_dim, int sms) {
+    const int64_t rows_all = (int64_t)(heads / kv_heads) * rows;
+    const int64_t tiles = (rows_all + 7) / 8;
+    return parts_bytes(head_dim, sms) + (size_t)batch * (size_t)kv_heads * (size_t)tiles * sizeof(uint32_t) + 256;
+}
 
 cudaError_t launch_kv_attend(const KvView& c, const KvAttend& a, cudaStream_t s) {
-    const size_t smem = (size_t)(AT_THREADS / (c.head_dim / 8)) * (c.head_dim + 2) * sizeof(float);
-    return launch_dependent(kv_attend_kernel, dim3((unsigned)(a.batch * a.rows * a.heads)), AT_THREADS, smem, s, c, a);
+    const int rows_all = a.heads / c.kv_heads * a.rows, tile = tile_rows(rows_all, c.head_dim);
+    const int tiles = (rows_all + tile - 1) / tile;
+    if (c.head_dim == 256) return launch<Shape256a>(c, a, tiles, s);
+    if (c.head_dim == 128) return tile == 16 ? launch<Shape128b>(c, a, tiles, s) : launch<Shape128a>(c, a, tiles, s);
+    return tile == 16 ? launch<Shape64b>(c, a, tiles, s) : launch<Shape64a>(c, a, tiles, s);
 }
 
 cudaError_t read_device_status_attend(uint32_t* status) {

@@ -27,9 +27,9 @@ void clear_error();
 //           token's d/64 FP16 key scales, then its d/64 FP16 value scales
 //
 // = 68 d bytes. A row is d/8 words of 8 codes; word c (codes 8c .. 8c + 7, the
-// lowest nibble first, offset binary: 8 is zero) sits at kv_key_word /
-// kv_value_word. The orders are those the attention kernel's fragments read
-// from shared memory without bank conflicts (vbq_attend.cu).
+// lowest nibble first, offset binary: 8 is zero; then kv_turned) sits at
+// kv_key_word / kv_value_word. The orders are those the attention kernel's
+// fragments read from shared memory without bank conflicts (vbq_attend.cu).
 // ---------------------------------------------------------------------------
 constexpr int KV_PAGE = 64;
 constexpr int KV_GROUP = 64;                    // codes that share a scale
@@ -46,6 +46,12 @@ struct KvView {
 __host__ __device__ constexpr int64_t kv_blob_bytes(int d) { return 68ll * d; }
 __host__ __device__ constexpr int kv_values_at(int d) { return 32 * d; }
 __host__ __device__ constexpr int kv_scales_at(int d) { return 64 * d; }
+
+// Each 16-bit half of a word is turned left by 2: codes 0 and 1 of a half are
+// then at bits 2..5 and 6..9, the high bits of an f16's fraction, and codes 2
+// and 3 are after a swap of the half's bytes.
+__host__ __device__ constexpr uint32_t kv_turned(uint32_t w) { return (w << 2 & 0xfffcfffcu) | (w >> 14 & 0x00030003u); }
+__host__ __device__ constexpr uint32_t kv_unturned(uint32_t w) { return (w >> 2 & 0x3fff3fffu) | (w << 14 & 0xc000c000u); }
 
 // Row of a token's keys (and scales) within the page: within each 8 tokens the
 // first four take the even rows, the last four the odd ones.

@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(KA_THREADS) kv_append_kernel(KvView c, KvAppen
         const int krow = kv_key_row(slot);
         uint8_t* dst = is_k ? blob + krow * (d / 2) + 4 * kv_key_word(ch, d)
                             : blob + kv_values_at(d) + slot * (d / 2) + 4 * kv_value_word(ch, slot, d);
-        *reinterpret_cast<uint32_t*>(dst) = w;
+        *reinterpret_cast<uint32_t*>(dst) = kv_turned(w);
         if ((ch & 7) == 0)
             *reinterpret_cast<__half*>(blob + kv_scales_at(d) + krow * (d / 16) + (is_k ? 0 : d / 32) + 2 * (ch >> 3)) = sh;
     }
@@ -185,9 +185,9 @@ __global__ void __launch_bounds__(KA_THREADS) kv_read_kernel(KvView c, const int
             } else {
                 const int slot = (int)(p % KV_PAGE), krow = kv_key_row(slot);
                 const uint8_t* blob = c.pages + (page * c.kv_heads + h) * kv_blob_bytes(d);
-                w = *reinterpret_cast<const uint32_t*>(
+                w = kv_unturned(*reinterpret_cast<const uint32_t*>(
                     is_k ? blob + krow * (d / 2) + 4 * kv_key_word(ch, d)
-                         : blob + kv_values_at(d) + slot * (d / 2) + 4 * kv_value_word(ch, slot, d));
+                         : blob + kv_values_at(d) + slot * (d / 2) + 4 * kv_value_word(ch, slot, d)));
                 s = __half2float(*reinterpret_cast<const __half*>(blob + kv_scales_at(d) + krow * (d / 16) +
                                                                   (is_k ? 0 : d / 32) + 2 * (ch >> 3)));
             }
