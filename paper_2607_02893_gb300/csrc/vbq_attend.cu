@@ -49,6 +49,8 @@ namespace vbq {
 namespace {
 
 constexpr uint32_t FULL = 0xffffffffu;
+constexpr int JOIN = 8;
+constexpr int CUT = 6;                           // pages a block takes at least of a segment that is cut
 constexpr uint32_t LOW = 0x003c003cu, HIGH = 0x03c003c0u;    // codes at bits 2..5 and 6..9 of each half
 
 // D: head dimension, NT: 8-row tiles of query rows per pass, W: warps, S: stages per warp.
@@ -207,9 +209,11 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
 #pragma unroll
         for (int o = 16; o; o >>= 1) most = max(most, (int64_t)__shfl_xor_sync(FULL, most, o));
         if (lane == 0) {
-            // an even share of the pages; short segments are not cut where a block's warps take them at once
+            // an even share of the pages; segments that a block's warps take at once are not cut, and no
+            // segment into parts that cost more to join than to read
             int64_t q = (before * per_seq + gridDim.x - 1) / gridDim.x;
-            if (most <= W && q < most) q = most;
+            const int64_t least = most <= W ? most : CUT;
+            if (q < least) q = least;
             misc->quantum = q > 0 ? q : 1;
         }
     }
@@ -611,35 +615,47 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             if (misc->last) {
                 __threadfence();
                 if (tid == 0) counts[s.index] = 0;
-                for (int u = tid; u < C::UNITS; u += C::THREADS) {
-                    const int par = u >> 5 & 1, n = (u >> 6) % NT, q = (u >> 6) / NT, ln = u & 31;
+                // half a unit per thread, JOIN parts' loads in flight
+                for (int v = tid; v < 2 * C::UNITS; v += C::THREADS) {
+                    const int u = v >> 1, par = u >> 5 & 1, n = (u >> 6) % NT, q = (u >> 6) / NT, ln = u & 31;
                     const int row = 8 * n + 2 * (ln & 3) + par;
                     const int r = s.rt * C::ROWS + row;
                     if (r >= rows_all) continue;
-                    float mx = -INFINITY, sum = 0.f, v[8] = {};
-                    for (int64_t k = b0; k <= b1; ++k) {
-                        const float* part = parts + (2 * k + (s.start <= k * quantum ? 0 : 1)) * C::PART;
-                        const float2 x = __ldcg(reinterpret_cast<const float2*>(part + C::ROWS * D) + row);
-                        const float4 y0 = __ldcg(reinterpret_cast<const float4*>(part) + 2 * u),
-                                     y1 = __ldcg(reinterpret_cast<const float4*>(part) + 2 * u + 1);
-                        if (x.y == 0.f) continue;
-                        const float mn = fmaxf(mx, x.x), f0 = ex2(mx - mn), f1 = ex2(x.x - mn);
+                    float mx = -INFINITY, sum = 0.f;
+                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int64_t k0 = b0; k0 <= b1; k0 += JOIN) {
+                        float2 x[JOIN];
+                        float4 y[JOIN];
+#pragma unroll
+                        for (int j = 0; j < JOIN; ++j) {
+                            const int64_t k = min(k0 + j, b1);
+                            const float* part = parts + (2 * k + (s.start <= k * quantum ? 0 : 1)) * C::PART;
+                            x[j] = __ldcg(reinterpret_cast<const float2*>(part + C::ROWS * D) + row);
+                            y[j] = __ldcg(reinterpret_cast<const float4*>(part) + v);
+                            if (k0 + j > b1) x[j] = make_float2(-INFINITY, 0.f);
+                        }
+                        float mn = mx;
+#pragma unroll
+                        for (int j = 0; j < JOIN; ++j) mn = fmaxf(mn, x[j].x);
+                        const float f0 = sum == 0.f ? 0.f : ex2(mx - mn);
                         mx = mn;
-                        sum = sum * f0 + x.y * f1;
-                        v[0] = v[0] * f0 + y0.x * f1; v[1] = v[1] * f0 + y0.y * f1;
-                        v[2] = v[2] * f0 + y0.z * f1; v[3] = v[3] * f0 + y0.w * f1;
-                        v[4] = v[4] * f0 + y1.x * f1; v[5] = v[5] * f0 + y1.y * f1;
-                        v[6] = v[6] * f0 + y1.z * f1; v[7] = v[7] * f0 + y1.w * f1;
+                        sum *= f0;
+                        o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+#pragma unroll
+                        for (int j = 0; j < JOIN; ++j) {
+                            const float fj = x[j].y == 0.f ? 0.f : ex2(x[j].x - mn);
+                            if (x[j].y == 0.f) y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            sum = fmaf(x[j].y, fj, sum);
+                            o.x = fmaf(y[j].x, fj, o.x); o.y = fmaf(y[j].y, fj, o.y);
+                            o.z = fmaf(y[j].z, fj, o.z); o.w = fmaf(y[j].w, fj, o.w);
+                        }
                     }
                     const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
-                    uint32_t w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i] * inv, v[2 * i + 1] * inv);
-                        w[i] = *reinterpret_cast<const uint32_t*>(&h);
-                    }
-                    *reinterpret_cast<uint4*>(a.out + (((int64_t)s.b * a.rows + r / group) * a.heads + s.h * group + r % group) * D +
-                                              64 * q + 8 * (ln >> 2)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    const __nv_bfloat162 h0 = __floats2bfloat162_rn(o.x * inv, o.y * inv),
+                                         h1 = __floats2bfloat162_rn(o.z * inv, o.w * inv);
+                    *reinterpret_cast<uint2*>(a.out + (((int64_t)s.b * a.rows + r / group) * a.heads + s.h * group + r % group) * D +
+                                              64 * q + 8 * (ln >> 2) + 4 * (v & 1)) =
+                        make_uint2(*reinterpret_cast<const uint32_t*>(&h0), *reinterpret_cast<const uint32_t*>(&h1));
                 }
             }
         }
