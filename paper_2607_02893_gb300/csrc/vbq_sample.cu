@@ -5,18 +5,20 @@
 // sums of whole numbers do not depend on their order, so neither the cuts nor
 // the draw depend on how the row is split or when an addition arrives.
 //
-// A cluster of up to 8 blocks holds a row's e in registers (16 or 32 per
-// thread), so the logits are read once; everything after that is a few rounds
-// of "add up locally, exchange through distributed shared memory, decide", and
-// the number of rounds is what bounds it (a row of 128256 is 0.5 MB: 0.08 us of
-// HBM bandwidth). A cut (top-k by count, top-p by weight) is found in two rounds
-// from one histogram over 2048 bins of e, 64 to an octave: 32 octave sums, then
-// the 64 bins of the octave that holds the cut. If no more than LIST tokens lie
-// in or above the cut's bin, one block gathers them in index order, sorts them
-// by (logit, lowest index first) and finishes alone. Otherwise only the bin's own
-// tokens are gathered and sorted, by every block, for the exact cut; a bin that
-// holds more (equal logits by the thousand) is narrowed 5 bits of (logit,
-// index) a round first. The draw then adds up in index order.
+// A cluster of up to 8 blocks holds a row in shared memory, so the logits are
+// read once; everything after that is a few rounds of "add up locally,
+// exchange through distributed shared memory, decide", and those rounds are
+// what bounds it (a row of 128256 is 0.5 MB: 0.08 us of HBM bandwidth). A cut
+// (top-k by count, top-p by weight) is found in two rounds from one histogram
+// of 2048 bins, 64 to a factor of 2 in weight: 32 sums of 64 bins, then the 64
+// bins that hold the cut. For top-k the bins are of the logits themselves and no
+// exponential is taken but of the tokens that remain. If no more than LIST
+// tokens lie in or above the cut's bin, one block gathers them, sorts them by
+// (logit, lowest index first), applies the filters as a prefix, sorts what is
+// left by index and draws. Otherwise only the bin's own tokens are gathered and
+// sorted, by every block, for the exact cut; a bin that holds more than LIST
+// (equal logits by the thousand) is narrowed 5 bits of (logit, index) a round
+// first. The draw then adds up in index order over the whole row.
 #include <cooperative_groups.h>
 
 #include "vbq_decode.h"
@@ -29,29 +31,37 @@ namespace cg = cooperative_groups;
 typedef unsigned long long u64;
 
 constexpr uint32_t ALL = 0xffffffffu;
-constexpr int SA_THREADS = 1024;
+constexpr int SA_THREADS = 512;
 constexpr int SA_WARPS = SA_THREADS / 32;
 constexpr int SA_BLOCKS = 8;              // most blocks of a cluster
 constexpr int BINS = 2048;
-constexpr int LIST = 1024;                // tokens a block sorts, one per thread
+constexpr int LIST = SA_THREADS;          // tokens a block sorts, one per thread
 
 struct Sum { u64 w; uint32_t n, pad; };   // weight and count
+
+struct Found {                            // where a cut lies
+    int at;                               // bin, or -1: nothing reaches it
+    uint32_t in, above_n;                 // tokens in the bin, and above it
+    u64 above;                            // count or weight above it
+};
 
 struct Shared {
     union {
         struct { uint32_t n[BINS], lo[BINS], hi[BINS]; } hist;   // counts; weights' low 16 and high bits
         u64 sorted[LIST];
     };
-    u64 list[LIST];                       // gathered tokens, in index order
+    u64 list[LIST];                       // gathered tokens
     Sum coarse[SA_BLOCKS][32];            // written by the blocks of the cluster; the rounds that narrow a
     Sum fine[SA_BLOCKS][64];              // bin take the two in turn, each free since the exchange before
-    u64 table[8][SA_WARPS];               // per (quad, warp) sums in index order
     u64 top[SA_BLOCKS];
     Sum total[SA_BLOCKS];
-    u64 part[SA_WARPS];
-    u64 pick[4];
-    int done;
+    uint32_t count[SA_BLOCKS];            // tokens each block gathers
+    u64 part[SA_WARPS], warp_w[SA_WARPS];
+    u64 mass, pick[2];
+    Found found;
+    uint32_t next;
 };
+constexpr int SHARED_BYTES = (sizeof(Shared) + 15) / 16 * 16;    // the row's slice follows
 
 __device__ __forceinline__ uint32_t key_of(float v) {
     const uint32_t u = __float_as_uint(v);
@@ -68,7 +78,7 @@ __device__ __forceinline__ float chance(float v, float top, float t) {
     return v == top ? 1.f : v == -INFINITY ? 0.f : expf(__fdiv_rn(__fsub_rn(v, top), t));
 }
 __device__ __forceinline__ u64 weight(float e) { return (u64)rintf(__fmul_rn(e, 0x1p32f)); }
-// Bin of a token: its weight's octave (2^-32 and below: 0) and 6 bits; tokens without weight are bin 0.
+// Bin of a weight: its factor of 2 (2^-32 and below: the first) and 6 bits; no weight: bin 0.
 __device__ __forceinline__ int bin_of(float e) {
     const int b = (int)(__float_as_uint(e) >> 17) - 95 * 64;
     return e <= 0x1p-33f ? 0 : min(max(b, 1), BINS - 1);
@@ -100,7 +110,7 @@ __device__ __forceinline__ u64 block_scan(u64 v, u64* part, u64* all) {
     __syncthreads();
     if (lane == 31) part[warp] = x;
     __syncthreads();
-    const u64 y = warp_scan(part[lane]);
+    const u64 y = warp_scan(lane < SA_WARPS ? part[lane] : 0);
     *all = __shfl_sync(ALL, y, 31);
     const u64 before = __shfl_sync(ALL, y, max(warp, 1) - 1);
     return x + (warp ? before : 0);
@@ -122,15 +132,40 @@ __device__ __forceinline__ T* in_block(T* p, int rank) {
     return cg::this_cluster().map_shared_rank(p, rank);
 }
 
-// The kept set so far: tokens at or above `order` in (logit, index) order; a token's
-// bin decides unless it is the cut's own bin.
-struct Cut {
-    int bin;                              // -1: every token
-    u64 order;
-};
+// One warp: the cut's place among PER * 32 bins, from the highest down, whose
+// sums are the C blocks' added up; above counts what lies above all of them.
+template <int C, int PER>
+__device__ __forceinline__ void find_cut(const Sum* tab, int width, bool by_weight, double enough, Found* f) {
+    const int lane = threadIdx.x & 31, hi = PER * (32 - lane) - 1;       // this lane's bins: hi, hi - 1
+    Sum a = {0, 0, 0}, z = {0, 0, 0};
+#pragma unroll
+    for (int r = 0; r < C; ++r) {
+        const Sum x = tab[r * width + hi];
+        a.n += x.n; a.w += x.w;
+        if (PER == 2) {
+            const Sum y = tab[r * width + hi - 1];
+            z.n += y.n; z.w += y.w;
+        }
+    }
+    const u64 own_a = by_weight ? a.w : a.n, own_z = by_weight ? z.w : z.n;
+    const u64 upto = f->above + warp_scan(own_a + own_z);
+    const uint32_t n = f->above_n + (uint32_t)warp_scan((u64)(a.n + z.n));
+    const bool hit_a = (double)(upto - own_z) >= enough && a.n > 0;
+    const bool hit_z = PER == 2 && (double)upto >= enough && z.n > 0;
+    const uint32_t hits = __ballot_sync(ALL, hit_a || hit_z);
+    __syncwarp();                         // every lane has read *f
+    if (hits == 0) {
+        if (lane == 0) f->at = -1;
+    } else if (lane == __ffs(hits) - 1) {
+        f->at = hit_a ? hi : hi - 1;
+        f->in = hit_a ? a.n : z.n;
+        f->above = hit_a ? upto - own_z - own_a : upto - own_z;
+        f->above_n = hit_a ? n - z.n - a.n : n - z.n;
+    }
+}
 
-// Descending bitonic sort of LIST or fewer values, one per thread below size (a
-// power of two of at least 32); the others pass through.
+// Descending bitonic sort of one value per thread below size (a power of two,
+// 32..LIST); the others pass through.
 __device__ u64 sort_down(u64 v, int size, u64* buf) {
     const int t = threadIdx.x;
     for (int k = 2; k <= size; k <<= 1) {
@@ -151,67 +186,66 @@ __device__ u64 sort_down(u64 v, int size, u64* buf) {
     return v;
 }
 
-// C blocks per row, QUADS x 4 tokens per thread: thread t of block r holds tokens
-// (r * QUADS + j) * 4096 + 4 t + 0..3.
-template <int C, int QUADS>
-__global__ void __launch_bounds__(SA_THREADS, 1) sample_kernel(Sample p) {
-    __shared__ Shared sh;
+// C blocks per row, each with `slice` neighbouring tokens (a multiple of 4).
+template <int C>
+__global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    Shared& sh = *reinterpret_cast<Shared*>(smem);
+    float* x = reinterpret_cast<float*>(smem + SHARED_BYTES);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = C == 1 ? 0 : (int)(blockIdx.x % C);
     const int64_t row = blockIdx.x / C;
     if constexpr (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // this block has started
+    const auto clear_hist = [&] {
+        uint4* h = reinterpret_cast<uint4*>(&sh.hist);
+        for (int i = tid; i < (int)(sizeof(sh.hist) / 16); i += SA_THREADS) h[i] = make_uint4(0, 0, 0, 0);
+    };
+    clear_hist();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int V = p.vocab;
+    const int V = p.vocab, first = rank * slice, n = max(0, min(V - first, slice));
     const void* logits = static_cast<const uint8_t*>(p.logits) + row * p.stride * (p.f32 ? 4 : 2);
-    const int first = rank * QUADS * 4096 + 4 * tid;
     const float T = p.temperature[row];
     const int top_k = p.top_k[row];
     const float top_p = p.top_p[row], mp = p.min_p[row], min_p = mp > 0.f ? fminf(mp, 1.f) : 0.f, u = p.u[row];
 
-    // The logits, and the largest with its first index.
-    float e[QUADS * 4];
-    const bool vec = (reinterpret_cast<uintptr_t>(logits) & (p.f32 ? 15 : 7)) == 0;
-#pragma unroll
-    for (int j = 0; j < QUADS; ++j) {
-        const int i = first + j * 4096;
-        if (vec && i + 3 < V) {
-            if (p.f32) {
-                const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(logits) + i);
-                e[4 * j] = x.x; e[4 * j + 1] = x.y; e[4 * j + 2] = x.z; e[4 * j + 3] = x.w;
-            } else {
-                const uint2 x = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(logits) + i);
-                e[4 * j] = __uint_as_float(x.x << 16); e[4 * j + 1] = __uint_as_float(x.x & 0xffff0000u);
-                e[4 * j + 2] = __uint_as_float(x.y << 16); e[4 * j + 3] = __uint_as_float(x.y & 0xffff0000u);
-            }
-        } else {
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                e[4 * j + q] = i + q >= V ? -INFINITY
-                               : p.f32   ? static_cast<const float*>(logits)[i + q]
-                                         : __uint_as_float((uint32_t)static_cast<const uint16_t*>(logits)[i + q] << 16);
-        }
-    }
+    // The slice, and the largest logit with its first index.
     float mx = -INFINITY;
     int mi = 0;
-#pragma unroll
-    for (int j = 0; j < QUADS * 4; ++j) {
-        e[j] = usable(e[j]);
-        if (e[j] > mx) {
-            mx = e[j];
-            mi = first + (j / 4) * 4096 + j % 4;
+    const int quads = (reinterpret_cast<uintptr_t>(logits) & (p.f32 ? 15 : 7)) == 0 ? n / 4 : 0;
+#pragma unroll 4
+    for (int q = tid; q < quads; q += SA_THREADS) {
+        float4 v;
+        if (p.f32) {
+            v = reinterpret_cast<const float4*>(static_cast<const float*>(logits) + first)[q];
+        } else {
+            const uint2 b = reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(logits) + first)[q];
+            v = make_float4(__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xffff0000u), __uint_as_float(b.y << 16),
+                            __uint_as_float(b.y & 0xffff0000u));
+        }
+        v = make_float4(usable(v.x), usable(v.y), usable(v.z), usable(v.w));
+        reinterpret_cast<float4*>(x)[q] = v;
+        const float m = fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w));
+        if (m > mx) {
+            mx = m;
+            mi = 4 * q + (v.x == m ? 0 : v.y == m ? 1 : v.z == m ? 2 : 3);
         }
     }
-    u64 best = mx > -INFINITY ? order_of(mx, mi) : 0;
+    for (int i = 4 * quads + tid; i < n; i += SA_THREADS) {
+        const float v = logit_at(p, logits, first + i);
+        x[i] = v;
+        if (v > mx) { mx = v; mi = i; }
+    }
+    u64 best = mx > -INFINITY ? order_of(mx, first + mi) : 0;
 #pragma unroll
     for (int o = 16; o; o >>= 1) best = max(best, __shfl_xor_sync(ALL, best, o));
     if (lane == 0) sh.part[warp] = best;
     __syncthreads();
     if constexpr (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");   // all have: their memory may be written
     if (warp == 0) {
-        best = sh.part[lane];
+        best = sh.part[lane & (SA_WARPS - 1)];
 #pragma unroll
-        for (int o = 16; o; o >>= 1) best = max(best, __shfl_xor_sync(ALL, best, o));
+        for (int o = SA_WARPS / 2; o; o >>= 1) best = max(best, __shfl_xor_sync(ALL, best, o));
         if (lane < C) *in_block<C>(&sh.top[rank], lane) = best;
     }
     cluster_sync<C>();
@@ -227,200 +261,183 @@ __global__ void __launch_bounds__(SA_THREADS, 1) sample_kernel(Sample p) {
         return;
     }
     const float top = value_of((uint32_t)(best >> 32));
-#pragma unroll
-    for (int j = 0; j < QUADS * 4; ++j) e[j] = e[j] == -INFINITY ? -1.f : chance(e[j], top, T);   // -1: not a token
+    const float per_bin = fminf(__fdiv_rn(64.f * 1.44269504f, T), 1e30f);
+    const auto logit_bin = [&](float l) {                  // not below the bin of a lower logit
+        return l == top ? BINS - 1 : BINS - 1 - (int)fminf(__fmul_rn(__fsub_rn(top, l), per_bin), (float)(BINS - 1));
+    };
 
-    const auto index_of = [&](int j) { return first + (j / 4) * 4096 + j % 4; };
-    Cut cut = {-1, 0};
-    const auto is_in = [&](int j) {                        // of the kept set
-        if (e[j] < 0.f) return false;
-        if (cut.bin < 0) return true;
-        const int b = bin_of(e[j]);
-        if (b != cut.bin) return b > cut.bin;
-        return order_of(logit_at(p, logits, index_of(j)), index_of(j)) >= cut.order;
+    // What is kept so far. After top-k x still holds logits, and bins are logit_bin; top-p replaces them by e (-1: not
+    // kept by top-k) and bins are bin_of. bin -1: everything.
+    bool held = false, used = false;                       // x holds e; the histogram has been filled
+    int cut_bin = -1;
+    u64 cut_order = 0;
+    const auto k_keeps = [&](float l, int i) {             // top-k's cut, on logits
+        if (l == -INFINITY) return false;
+        if (cut_bin < 0) return true;
+        const int b = logit_bin(l);
+        return b != cut_bin ? b > cut_bin : order_of(l, first + i) >= cut_order;
     };
 
     for (int which = 0; which < 2; ++which) {              // 0: top-k by count, 1: top-p by weight
         if (which == 0 ? top_k <= 0 || top_k >= V : top_p >= 1.f) continue;
-        __syncthreads();
-        for (int i = tid; i < BINS; i += SA_THREADS) sh.hist.n[i] = sh.hist.lo[i] = sh.hist.hi[i] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < QUADS * 4; ++j) {
-            if (!is_in(j)) continue;
-            const int b = bin_of(e[j]);
-            atomicAdd(&sh.hist.n[b], 1u);
-            if (which == 1 && b > 0) {
-                const u64 w = weight(e[j]);
-                atomicAdd(&sh.hist.lo[b], (uint32_t)w & 0xffffu);
-                atomicAdd(&sh.hist.hi[b], (uint32_t)(w >> 16));
+        const bool by_weight = which == 1;
+        if (by_weight) {
+            if (used) {
+                __syncthreads();
+                clear_hist();
+                __syncthreads();
+            }
+#pragma unroll 2
+            for (int i = tid; i < n; i += SA_THREADS) {
+                const float l = x[i];
+                float e = -1.f;
+                if (k_keeps(l, i)) {
+                    e = chance(l, top, T);
+                    const int b = bin_of(e);
+                    const u64 w = weight(e);
+                    atomicAdd(&sh.hist.n[b], 1u);
+                    if (w) {
+                        atomicAdd(&sh.hist.lo[b], (uint32_t)w & 0xffffu);
+                        atomicAdd(&sh.hist.hi[b], (uint32_t)(w >> 16));
+                    }
+                }
+                x[i] = e;
+            }
+            held = true;
+            cut_bin = -1;
+        } else {
+            used = true;
+#pragma unroll 4
+            for (int i = tid; i < n; i += SA_THREADS) {
+                const float l = x[i];
+                if (l > -INFINITY) atomicAdd(&sh.hist.n[logit_bin(l)], 1u);
             }
         }
         __syncthreads();
-        {                                                  // octave sums, to every block
-            Sum s;
-            const int b = 64 * warp + lane;
-            s.n = __reduce_add_sync(ALL, sh.hist.n[b] + sh.hist.n[b + 32]);
-            s.w = which == 0 ? 0
-                             : warp_sum((u64)sh.hist.lo[b] + sh.hist.lo[b + 32] + ((u64)sh.hist.hi[b] + sh.hist.hi[b + 32] << 16));
-            s.pad = 0;
-            if (lane < C) *in_block<C>(&sh.coarse[rank][warp], lane) = s;
+        for (int c = warp; c < 32; c += SA_WARPS) {        // sums of 64 bins, to every block
+            const int b = 64 * c + lane;
+            Sum s = {0, __reduce_add_sync(ALL, sh.hist.n[b] + sh.hist.n[b + 32]), 0};
+            if (by_weight) s.w = warp_sum((u64)sh.hist.lo[b] + sh.hist.lo[b + 32] + ((u64)sh.hist.hi[b] + sh.hist.hi[b + 32] << 16));
+            if (lane < C) *in_block<C>(&sh.coarse[rank][c], lane) = s;
         }
         cluster_sync<C>();
-        // The octave that holds the cut (every warp finds it by itself), from the top down: lane i is octave 31 - i.
-        Sum s = {0, 0, 0};
+        if (warp == 0) {
+            u64 mass = 0;
+            if (by_weight) {
 #pragma unroll
-        for (int r = 0; r < C; ++r) {
-            const Sum x = sh.coarse[r][31 - lane];
-            s.n += x.n;
-            s.w += x.w;
+                for (int r = 0; r < C; ++r) mass += sh.coarse[r][lane].w;
+                mass = warp_sum(mass);
+            }
+            if (lane == 0) {
+                sh.mass = mass;
+                sh.found = Found{0, 0, 0, 0};
+            }
+            __syncwarp();
+            find_cut<C, 1>(&sh.coarse[0][0], 32, by_weight,
+                           !by_weight ? (double)top_k : top_p > 0.f ? (double)top_p * (double)mass : 0., &sh.found);
         }
-        const u64 mass = which == 0 ? 0 : warp_sum(s.w);
-        const double enough = which == 0 ? (double)top_k : top_p > 0.f ? (double)top_p * (double)mass : 0.;
-        u64 own = which == 0 ? s.n : s.w, upto = warp_scan(own);
-        uint32_t above_n;
-        u64 above;
-        const uint32_t found = __ballot_sync(ALL, (double)upto >= enough && s.n > 0);
-        if (found == 0) continue;                          // fewer tokens than top_k: all are kept
-        const int at = __ffs(found) - 1, oct = 31 - at;
-        above = __shfl_sync(ALL, upto - own, at);
-        {
-            const u64 n = warp_scan((u64)s.n);
-            above_n = (uint32_t)__shfl_sync(ALL, n - s.n, at);
+        __syncthreads();
+        const double enough = !by_weight ? (double)top_k : top_p > 0.f ? (double)top_p * (double)sh.mass : 0.;
+        const int oct = sh.found.at;
+        if (oct < 0) {                                     // fewer tokens than top_k: all are kept
+            cluster_sync<C>();                             // every block has read coarse
+            continue;
         }
-        if (tid < 64 * C) {                                // the octave's bins, to every block
+        if (tid < 64 * C) {                                // its bins, to every block
             const int b = 64 * oct + (tid & 63);
-            *in_block<C>(&sh.fine[rank][tid & 63], tid >> 6) =
-                Sum{(u64)sh.hist.lo[b] + ((u64)sh.hist.hi[b] << 16), sh.hist.n[b], 0};
+            *in_block<C>(&sh.fine[rank][tid & 63], tid >> 6) = Sum{(u64)sh.hist.lo[b] + ((u64)sh.hist.hi[b] << 16), sh.hist.n[b], 0};
         }
         cluster_sync<C>();
-        // The bin: lane i holds bins 63 - 2 i and 62 - 2 i.
-        Sum a = {0, 0, 0}, z = {0, 0, 0};
-#pragma unroll
-        for (int r = 0; r < C; ++r) {
-            const Sum x = sh.fine[r][63 - 2 * lane], y = sh.fine[r][62 - 2 * lane];
-            a.n += x.n; a.w += x.w;
-            z.n += y.n; z.w += y.w;
+        if (warp == 0) find_cut<C, 2>(&sh.fine[0][0], 64, by_weight, enough, &sh.found);
+        if (tid == 0) sh.next = 0;
+        __syncthreads();
+        const int in_oct = sh.found.at, bin = 64 * oct + in_oct;
+        const bool finish = sh.found.above_n + sh.found.in <= LIST;      // one block takes it from here
+        if (warp < C) {                                    // how many tokens block `warp` will gather
+            uint32_t c = 0;
+            if (finish) {
+                c = lane > oct ? sh.coarse[warp][lane].n : 0;
+                if (lane >= in_oct) c += sh.fine[warp][lane].n;
+                if (lane + 32 >= in_oct) c += sh.fine[warp][lane + 32].n;
+            } else if (lane == 0) {
+                c = sh.fine[warp][in_oct].n;
+            }
+            c = __reduce_add_sync(ALL, c);
+            if (lane == 0) sh.count[warp] = c;
         }
-        const u64 ownA = which == 0 ? a.n : a.w, ownZ = which == 0 ? z.n : z.w;
-        upto = above + warp_scan(ownA + ownZ);
-        const bool hitA = (double)(upto - ownZ) >= enough && a.n > 0, hitZ = (double)upto >= enough && z.n > 0;
-        const uint32_t hits = __ballot_sync(ALL, hitA || hitZ);
-        const int hl = __ffs(hits) - 1;                    // there is one: the octave holds the cut
-        const bool second = !__shfl_sync(ALL, (int)hitA, hl);
-        const int bin = 64 * oct + 63 - 2 * hl - second;
-        above = __shfl_sync(ALL, second ? upto - ownZ : upto - ownZ - ownA, hl);
-        {
-            const u64 n = warp_scan((u64)(a.n + z.n));
-            above_n += (uint32_t)__shfl_sync(ALL, n - z.n - (second ? 0 : a.n), hl);
-        }
-        uint32_t in_bin = __shfl_sync(ALL, second ? z.n : a.n, hl);
-        const bool finish = above_n + in_bin <= LIST;      // one block takes it from here
+        __syncthreads();
 
-        // Narrow a bin that holds too many: digits of (logit, index), 5 bits a round.
-        u64 prefix = 0;
-        int known = 0;                                     // leading bits of the order that are fixed
-        const auto in_range = [&](int j, u64* o) {         // a token of the bin whose order has the prefix
-            if (e[j] < 0.f || bin_of(e[j]) != bin || !is_in(j)) return false;
-            *o = order_of(logit_at(p, logits, index_of(j)), index_of(j));
-            return known == 0 || *o >> (64 - known) == prefix;
+        // A token of the bin (or, to finish, from it up), and its order.
+        const auto here = [&](int i, bool from) {
+            const float v = x[i];
+            if (held ? v < 0.f : v == -INFINITY) return false;
+            const int b = held ? bin_of(v) : logit_bin(v);
+            return from ? b >= bin : b == bin;
         };
+        const auto order_at = [&](int i) { return order_of(held ? logit_at(p, logits, first + i) : x[i], first + i); };
+        u64 prefix = 0;                                    // of the orders in a narrowed bin
+        int known = 0;
         if (!finish) {
-            for (int round = 0; in_bin > LIST; ++round) {
+            for (int round = 0; sh.found.in > LIST; ++round) {           // 5 bits a round
                 const int bits = min(5, 64 - known);
                 __syncthreads();
                 if (tid < 32) sh.hist.n[tid] = sh.hist.lo[tid] = sh.hist.hi[tid] = 0;
                 __syncthreads();
-#pragma unroll
-                for (int j = 0; j < QUADS * 4; ++j) {
-                    u64 o;
-                    if (!in_range(j, &o)) continue;
+                for (int i = tid; i < n; i += SA_THREADS) {
+                    if (!here(i, false)) continue;
+                    const u64 o = order_at(i);
+                    if (known && o >> (64 - known) != prefix) continue;
                     const int d = (int)(o >> (64 - known - bits)) & ((1 << bits) - 1);
                     atomicAdd(&sh.hist.n[d], 1u);
-                    const u64 w = weight(e[j]);
-                    atomicAdd(&sh.hist.lo[d], (uint32_t)w & 0xffffu);
-                    atomicAdd(&sh.hist.hi[d], (uint32_t)(w >> 16));
+                    if (by_weight) {
+                        const u64 w = weight(x[i]);
+                        atomicAdd(&sh.hist.lo[d], (uint32_t)w & 0xffffu);
+                        atomicAdd(&sh.hist.hi[d], (uint32_t)(w >> 16));
+                    }
                 }
                 __syncthreads();
-                Sum* mine = round & 1 ? sh.fine[rank] : sh.coarse[rank];
-                if (tid < 32 * C)
-                    *in_block<C>(mine + lane, warp) = Sum{(u64)sh.hist.lo[lane] + ((u64)sh.hist.hi[lane] << 16), sh.hist.n[lane], 0};
+                Sum* tab = round & 1 ? &sh.fine[0][0] : &sh.coarse[0][0];
+                const int width = round & 1 ? 64 : 32;
+                for (int r = warp; r < C; r += SA_WARPS)
+                    *in_block<C>(tab + rank * width + lane, r) =
+                        Sum{(u64)sh.hist.lo[lane] + ((u64)sh.hist.hi[lane] << 16), sh.hist.n[lane], 0};
                 cluster_sync<C>();
-                Sum x = {0, 0, 0};
-#pragma unroll
-                for (int r = 0; r < C; ++r) {
-                    const Sum y = (round & 1 ? sh.fine[r] : sh.coarse[r])[31 - lane];
-                    x.n += y.n; x.w += y.w;
+                if (warp == 0) {
+                    find_cut<C, 1>(tab, width, by_weight, enough, &sh.found);
+                    __syncwarp();
+                    if (lane < C) sh.count[lane] = tab[lane * width + sh.found.at].n;
                 }
-                const u64 o = which == 0 ? x.n : x.w, to = above + warp_scan(o);
-                const uint32_t hit = __ballot_sync(ALL, (double)to >= enough && x.n > 0);
-                const int l = __ffs(hit) - 1;              // there is one: the bin holds the cut
-                above = __shfl_sync(ALL, to - o, l);
-                {
-                    const u64 n = warp_scan((u64)x.n);
-                    above_n += (uint32_t)__shfl_sync(ALL, n - x.n, l);
-                }
-                in_bin = __shfl_sync(ALL, x.n, l);
-                prefix = prefix << bits | (u64)(31 - l);
+                __syncthreads();
+                prefix = prefix << bits | (u64)sh.found.at;
                 known += bits;
             }
         }
 
-        // Gather, in index order: all of the kept set from the bin up (to block 0), or the narrowed bin (to all).
-        const auto taken = [&](int j, u64* o) {
-            if (!finish) return in_range(j, o);
-            if (e[j] < 0.f || bin_of(e[j]) < bin || !is_in(j)) return false;
-            *o = order_of(logit_at(p, logits, index_of(j)), index_of(j));
-            return true;
-        };
-        uint32_t flags = 0;
-        u64 order[1];
-#pragma unroll
-        for (int j = 0; j < QUADS * 4; ++j) flags |= (uint32_t)taken(j, order) << j;
-#pragma unroll
-        for (int j = 0; j < QUADS; ++j) {
-            const uint32_t n = __reduce_add_sync(ALL, (uint32_t)__popc(flags >> 4 * j & 15u));
-            if (lane == 0) sh.table[j][warp] = n;
-        }
-        u64 local;
-        __syncthreads();
-        {
-            const u64 n = tid < QUADS * SA_WARPS ? sh.table[tid >> 5][lane] : 0;
-            const u64 x = block_scan(n, sh.part, &local);
-            if (tid < QUADS * SA_WARPS) sh.table[tid >> 5][lane] = x - n;
-        }
-        if (tid < C) *in_block<C>(&sh.total[rank], tid) = Sum{0, (uint32_t)local, 0};
-        cluster_sync<C>();
-        uint32_t base = 0, n_list = 0;
+        // Gather: everything from the bin up (to block 0), or the narrowed bin (to every block).
+        uint32_t base = 0, listed = 0;
 #pragma unroll
         for (int r = 0; r < C; ++r) {
-            if (r < rank) base += sh.total[r].n;
-            n_list += sh.total[r].n;
+            if (r < rank) base += sh.count[r];
+            listed += sh.count[r];
         }
-#pragma unroll
-        for (int j = 0; j < QUADS; ++j) {
-            const uint32_t mine = flags >> 4 * j & 15u, c = __popc(mine);
-            if (__any_sync(ALL, c != 0)) {
-                uint32_t x = c;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const uint32_t y = __shfl_up_sync(ALL, x, o);
-                    if (lane >= o) x += y;
-                }
-                uint32_t to = base + (uint32_t)sh.table[j][warp] + x - c;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    if (!(mine >> q & 1u)) continue;
-                    const int i = first + j * 4096 + q;
-                    const u64 o = order_of(logit_at(p, logits, i), i);
-                    if (to < LIST) {
-                        if (finish) {
-                            *in_block<C>(&sh.list[to], 0) = o;
-                        } else {
-                            for (int r = 0; r < C; ++r) *in_block<C>(&sh.list[to], r) = o;
-                        }
-                    }
-                    ++to;
+        for (int i0 = warp * 32; i0 < n; i0 += SA_THREADS) {
+            const int i = i0 + lane;
+            bool take = i < n && here(i, finish);
+            u64 o = 0;
+            if (take) {
+                o = order_at(i);
+                take = known == 0 || o >> (64 - known) == prefix;
+            }
+            const uint32_t all = __ballot_sync(ALL, take);
+            if (all == 0) continue;
+            uint32_t to = 0;
+            if (lane == 0) to = atomicAdd(&sh.next, (uint32_t)__popc(all));
+            to = base + __shfl_sync(ALL, to, 0) + __popc(all & ((1u << lane) - 1));
+            if (take && to < LIST) {
+                if (finish) {
+                    *in_block<C>(&sh.list[to], 0) = o;
+                } else {
+                    for (int r = 0; r < C; ++r) *in_block<C>(&sh.list[to], r) = o;
                 }
             }
         }
@@ -428,79 +445,94 @@ __global__ void __launch_bounds__(SA_THREADS, 1) sample_kernel(Sample p) {
         if (finish && rank != 0) return;                   // block 0 has all it needs
 
         // Sorted, a thread's token is the tid-th: the filters are conditions on a prefix.
+        const int count = (int)listed;
         int size = 32;
-        while (size < (int)n_list) size <<= 1;
-        const u64 o = sort_down(tid < (int)n_list ? sh.list[tid] : 0, size, sh.sorted);
-        const bool real = tid < (int)n_list;
+        while (size < count) size <<= 1;
+        const bool real = tid < count;
+        const u64 o = sort_down(real ? sh.list[tid] : 0, size, sh.sorted);
         const float ce = real ? chance(value_of((uint32_t)(o >> 32)), top, T) : 0.f;
         const u64 cw = real ? weight(ce) : 0;
         u64 all;
         const u64 cum = block_scan(cw, sh.part, &all);
+        const u64 above = finish ? 0 : sh.found.above;
+        const uint32_t above_n = finish ? 0 : sh.found.above_n;
         bool keep;
-        if (which == 0) {
-            const bool counted = real && (u64)tid < (u64)top_k - (finish ? 0 : above);
-            keep = counted;
+        if (!by_weight) {
+            keep = real && (u64)tid + above < (u64)top_k;
             if (finish) {
-                if (tid == min(top_k, (int)n_list) - 1) sh.pick[0] = cum;
+                if (tid == top_k - 1) sh.pick[0] = cum;    // there is one: the cut lies in the list
                 __syncthreads();
                 const double want = top_p > 0.f ? (double)top_p * (double)sh.pick[0] : 0.;
-                keep = counted && (top_p >= 1.f || tid == 0 || (double)(cum - cw) < want);
+                keep = keep && (top_p >= 1.f || tid == 0 || (double)(cum - cw) < want);
             }
         } else {
-            // in the list from the bin up, the weights before a token are all listed
-            const u64 before = (finish ? 0 : above) + cum - cw;
-            keep = real && ((double)before < enough || (tid == 0 && (finish ? true : above_n == 0)));
+            keep = real && ((double)(above + cum - cw) < enough || (tid == 0 && above_n == 0));
         }
         if (finish) keep = keep && !(ce < min_p);
         const int n_keep = __syncthreads_count(keep);      // at least one
-        if (tid == n_keep - 1) sh.pick[1] = o;
-        __syncthreads();
-        const u64 last = sh.pick[1];
         if (!finish) {
-            cut.bin = bin;
-            cut.order = last;
+            if (tid == n_keep - 1) sh.pick[1] = o;
+            __syncthreads();
+            cut_bin = bin;
+            cut_order = sh.pick[1];
             continue;
         }
         // The draw, in index order.
-        const u64 lo = real ? sh.list[tid] : 0;
-        const bool in = real && lo >= last;
-        const float le = in ? chance(value_of((uint32_t)(lo >> 32)), top, T) : 0.f;
-        const u64 lw = in ? weight(le) : 0;
+        int small = 32;
+        while (small < n_keep) small <<= 1;
+        const u64 by_index = sort_down(tid < n_keep ? o << 32 | o >> 32 : 0, small, sh.sorted);
+        const float le = tid < n_keep ? chance(value_of((uint32_t)by_index), top, T) : 0.f;
+        const u64 lw = tid < n_keep ? weight(le) : 0;
         const u64 to = block_scan(lw, sh.part, &all);
         const double target = u > 0.f ? (double)u * (double)all : 0.;
-        const auto past = [&](u64 x) { return u >= 1.f ? x >= all : (double)x > target; };
+        const auto past = [&](u64 v) { return u >= 1.f ? v >= all : (double)v > target; };
         if (lw && past(to) && !past(to - lw)) {
-            p.tokens[row] = (int)~(uint32_t)lo;
+            p.tokens[row] = (int)~(uint32_t)(by_index >> 32);
             if (p.probs) p.probs[row] = __fdiv_rn(le, (float)((double)all * 0x1p-32));
             if (p.kept) p.kept[row] = n_keep;
         }
         return;
     }
 
-    // The draw over the whole row, in index order.
-    u64 sum = 0, kept = 0;
-    uint32_t flags = 0;
-    u64 quad[QUADS];
-#pragma unroll
-    for (int j = 0; j < QUADS; ++j) {
-        quad[j] = 0;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (!is_in(4 * j + q) || e[4 * j + q] < min_p) continue;
-            flags |= 1u << (4 * j + q);
-            quad[j] += weight(e[4 * j + q]);
+    // The draw over the whole row, in index order: a warp has neighbouring tokens.
+    const int run = ((n + SA_WARPS - 1) / SA_WARPS + 31) / 32 * 32, w0 = warp * run, w1 = min(n, w0 + run);
+    const auto chosen = [&](int i) -> float {              // e of a kept token, -1 otherwise
+        const float v = x[i];
+        if (!held) {
+            if (!k_keeps(v, i)) return -1.f;
+            const float e = chance(v, top, T);
+            return e < min_p ? -1.f : e;
         }
-        const u64 x = warp_sum(quad[j]);
-        if (lane == 0) sh.table[j][warp] = x;
+        if (v < min_p) return -1.f;                        // min_p >= 0
+        if (cut_bin >= 0) {
+            const int b = bin_of(v);
+            if (b < cut_bin || (b == cut_bin && order_of(logit_at(p, logits, first + i), first + i) < cut_order)) return -1.f;
+        }
+        return v;
+    };
+    u64 sum = 0;
+    uint32_t kept = 0;
+#pragma unroll 2
+    for (int i = w0 + lane; i < w1; i += 32) {
+        const float e = chosen(i);
+        if (e >= 0.f) {
+            sum += weight(e);
+            ++kept;
+        }
+        if (!held) x[i] = e;                               // the search below reads it
     }
-    kept = __popc(flags);
-    u64 nk;
+    sum = warp_sum(sum);
+    kept = __reduce_add_sync(ALL, kept);
+    if (lane == 0) {
+        sh.warp_w[warp] = sum;
+        sh.part[warp] = kept;
+    }
     __syncthreads();
-    block_scan(kept, sh.part, &nk);
-    const u64 mine = tid < QUADS * SA_WARPS ? sh.table[tid >> 5][lane] : 0;
-    const u64 upto = block_scan(mine, sh.part, &sum);
-    if (tid < QUADS * SA_WARPS) sh.table[tid >> 5][lane] = upto - mine;
-    if (tid < C) *in_block<C>(&sh.total[rank], tid) = Sum{sum, (uint32_t)nk, 0};
+    if (warp == 0) {
+        const u64 w = warp_sum(lane < SA_WARPS ? sh.warp_w[lane] : 0);
+        const uint32_t k = __reduce_add_sync(ALL, lane < SA_WARPS ? (uint32_t)sh.part[lane] : 0);
+        if (lane < C) *in_block<C>(&sh.total[rank], lane) = Sum{w, k, 0};
+    }
     cluster_sync<C>();
     u64 before = 0, all = 0;
     uint32_t n_all = 0;
@@ -511,32 +543,35 @@ __global__ void __launch_bounds__(SA_THREADS, 1) sample_kernel(Sample p) {
         n_all += sh.total[r].n;
     }
     if (rank == 0 && tid == 0 && p.kept) p.kept[row] = (int)n_all;
+    for (int w = 0; w < warp; ++w) before += sh.warp_w[w];
     const double target = u > 0.f ? (double)u * (double)all : 0.;
-    const auto past = [&](u64 x) { return u >= 1.f ? x >= all : (double)x > target; };
-    if (past(before) || !past(before + sum)) return;       // another block's
-#pragma unroll
-    for (int j = 0; j < QUADS; ++j) {
-        const u64 start = before + sh.table[j][warp], x = warp_scan(quad[j]);
-        u64 to = start + x - quad[j];
-        if (quad[j] == 0 || past(to) || !past(to + quad[j])) continue;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (!(flags >> (4 * j + q) & 1u)) continue;
-            const u64 w = weight(e[4 * j + q]);
-            if (!past(to) && past(to + w)) {
-                p.tokens[row] = first + j * 4096 + q;
-                if (p.probs) p.probs[row] = __fdiv_rn(e[4 * j + q], (float)((double)all * 0x1p-32));
-            }
-            to += w;
+    const auto past = [&](u64 v) { return u >= 1.f ? v >= all : (double)v > target; };
+    if (past(before) || !past(before + sum)) return;       // another warp's
+    for (int i0 = w0; i0 < w1; i0 += 32) {
+        const int i = i0 + lane;
+        const float e = i < w1 ? (held ? chosen(i) : x[i]) : -1.f;
+        const u64 w = e >= 0.f ? weight(e) : 0;
+        const u64 to = before + warp_scan(w);
+        if (w && past(to) && !past(to - w)) {
+            p.tokens[row] = first + i;
+            if (p.probs) p.probs[row] = __fdiv_rn(e, (float)((double)all * 0x1p-32));
         }
+        before = __shfl_sync(ALL, to, 31);
+        if (past(before)) return;
     }
 }
 
-template <int C, int QUADS>
+template <int C>
 cudaError_t launch(const Sample& p, cudaStream_t s) {
+    static LaunchPrep prep;
+    const int slice = ((p.vocab + C - 1) / C + 3) / 4 * 4, most = C == SA_BLOCKS ? SAMPLE_MAX_VOCAB / SA_BLOCKS : 4096;
+    int sms = 0;
+    cudaError_t e = prep.get(sample_kernel<C>, SHARED_BYTES + 4 * (size_t)most, &sms);
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.batch * C);
     cfg.blockDim = dim3(SA_THREADS);
+    cfg.dynamicSmemBytes = SHARED_BYTES + 4 * (size_t)slice;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -545,20 +580,16 @@ cudaError_t launch(const Sample& p, cudaStream_t s) {
     attr[1].val.clusterDim = {C, 1, 1};
     cfg.attrs = attr;
     cfg.numAttrs = C > 1 ? 2 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, sample_kernel<C, QUADS>, p);
+    e = cudaLaunchKernelEx(&cfg, sample_kernel<C>, p, slice);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
 
-// As many blocks as 16 tokens a thread need, up to a portable cluster.
 cudaError_t launch_sample(const Sample& p, cudaStream_t s) {
-    if (p.vocab <= 4096) return launch<1, 1>(p, s);
-    if (p.vocab <= 16384) return launch<1, 4>(p, s);
-    if (p.vocab <= 32768) return launch<2, 4>(p, s);
-    if (p.vocab <= 65536) return launch<4, 4>(p, s);
-    if (p.vocab <= 131072) return launch<8, 4>(p, s);
-    return launch<8, 8>(p, s);
+    if (p.vocab <= 4096) return launch<1>(p, s);
+    if (p.vocab <= 16384) return launch<4>(p, s);
+    return launch<SA_BLOCKS>(p, s);
 }
 
 }  // namespace vbq
