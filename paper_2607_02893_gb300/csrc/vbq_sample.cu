@@ -77,11 +77,38 @@ __device__ __forceinline__ float usable(float v) { return v == v ? v + 0.f : -IN
 __device__ __forceinline__ float chance(float v, float top, float t) {
     return v == top ? 1.f : v == -INFINITY ? 0.f : expf(__fdiv_rn(__fsub_rn(v, top), t));
 }
-__device__ __forceinline__ u64 weight(float e) { return (u64)rintf(__fmul_rn(e, 0x1p32f)); }
+// e in whole multiples of 2^-32, ties to even: e 2^32 is whole from 2^23 on; below, adding 2^23 rounds it there.
+// (Conversions to 64-bit integers and fp64 comparisons are slow on this GPU.)
+__device__ __forceinline__ u64 weight(float e) {
+    const float f = __fmul_rn(e, 0x1p32f);
+    const uint32_t bits = __float_as_uint(f);
+    const u64 large = (u64)((bits & 0x7fffffu) | 0x800000u) << ((bits >> 23) - 150u & 31u);
+    return f >= 0x1p23f ? large : (u64)(__float_as_uint(__fadd_rn(f, 0x1p23f)) - 0x4b000000u);
+}
+// The least whole number that is at least (or, `over`, more than) f * m, for 0 < f < 1 and m below 2^51.
+__device__ __forceinline__ u64 at_least(float f, u64 m, bool over) {
+    const uint32_t bits = __float_as_uint(f), ex = max(bits >> 23, 1u);
+    const u64 man = (bits & 0x7fffffu) | (bits >> 23 ? 0x800000u : 0u);
+    const int s = 150 - (int)ex;                           // f = man 2^-s, s of 24..149
+    const u64 lo = man * m, hi = __umul64hi(man, m);
+    u64 whole, rest;
+    if (s < 64) {
+        whole = hi << (64 - s) | lo >> s;
+        rest = lo << (64 - s);
+    } else {
+        whole = s < 128 ? hi >> (s - 64) : 0;
+        rest = s == 64 ? lo : lo | (s < 128 ? hi << (128 - s) : hi);
+    }
+    return over ? whole + 1 : whole + (rest != 0);
+}
 // Bin of a weight: its factor of 2 (2^-32 and below: the first) and 6 bits; no weight: bin 0.
 __device__ __forceinline__ int bin_of(float e) {
     const int b = (int)(__float_as_uint(e) >> 17) - 95 * 64;
     return e <= 0x1p-33f ? 0 : min(max(b, 1), BINS - 1);
+}
+// The least e of a bin (of bin BINS: past the last).
+__device__ __forceinline__ float bin_from(int b) {
+    return b == 0 ? 0.f : b == 1 ? 0x1.000002p-33f : b == BINS ? INFINITY : __uint_as_float((uint32_t)(b + 95 * 64) << 17);
 }
 
 __device__ __forceinline__ float logit_at(const Sample& p, const void* row, int i) {
@@ -116,6 +143,11 @@ __device__ __forceinline__ u64 block_scan(u64 v, u64* part, u64* all) {
     return x + (warp ? before : 0);
 }
 
+// The weight that a top-p prefix reaches at least.
+__device__ __forceinline__ u64 share_of(float top_p, u64 mass) { return top_p > 0.f ? at_least(top_p, mass, false) : 0; }
+// The least running weight that is past the random number's share.
+__device__ __forceinline__ u64 drawn_at(float u, u64 mass) { return u >= 1.f ? mass : u > 0.f ? at_least(u, mass, true) : 1; }
+
 template <int C>
 __device__ __forceinline__ void cluster_sync() {
     if constexpr (C == 1) {
@@ -135,7 +167,7 @@ __device__ __forceinline__ T* in_block(T* p, int rank) {
 // One warp: the cut's place among PER * 32 bins, from the highest down, whose
 // sums are the C blocks' added up; above counts what lies above all of them.
 template <int C, int PER>
-__device__ __forceinline__ void find_cut(const Sum* tab, int width, bool by_weight, double enough, Found* f) {
+__device__ __forceinline__ void find_cut(const Sum* tab, int width, bool by_weight, u64 enough, Found* f) {
     const int lane = threadIdx.x & 31, hi = PER * (32 - lane) - 1;       // this lane's bins: hi, hi - 1
     Sum a = {0, 0, 0}, z = {0, 0, 0};
 #pragma unroll
@@ -150,8 +182,8 @@ __device__ __forceinline__ void find_cut(const Sum* tab, int width, bool by_weig
     const u64 own_a = by_weight ? a.w : a.n, own_z = by_weight ? z.w : z.n;
     const u64 upto = f->above + warp_scan(own_a + own_z);
     const uint32_t n = f->above_n + (uint32_t)warp_scan((u64)(a.n + z.n));
-    const bool hit_a = (double)(upto - own_z) >= enough && a.n > 0;
-    const bool hit_z = PER == 2 && (double)upto >= enough && z.n > 0;
+    const bool hit_a = upto - own_z >= enough && a.n > 0;
+    const bool hit_z = PER == 2 && upto >= enough && z.n > 0;
     const uint32_t hits = __ballot_sync(ALL, hit_a || hit_z);
     __syncwarp();                         // every lane has read *f
     if (hits == 0) {
@@ -231,8 +263,10 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
             mi = 4 * q + (v.x == m ? 0 : v.y == m ? 1 : v.z == m ? 2 : 3);
         }
     }
-    for (int i = 4 * quads + tid; i < n; i += SA_THREADS) {
-        const float v = logit_at(p, logits, first + i);
+    const int quads4 = (n + 3) / 4;                        // the last is filled up with what no row keeps
+    float4* x4 = reinterpret_cast<float4*>(x);
+    for (int i = 4 * quads + tid; i < 4 * quads4; i += SA_THREADS) {
+        const float v = i < n ? logit_at(p, logits, first + i) : -INFINITY;
         x[i] = v;
         if (v > mx) { mx = v; mi = i; }
     }
@@ -287,30 +321,43 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
                 clear_hist();
                 __syncthreads();
             }
-#pragma unroll 2
-            for (int i = tid; i < n; i += SA_THREADS) {
-                const float l = x[i];
-                float e = -1.f;
-                if (k_keeps(l, i)) {
-                    e = chance(l, top, T);
-                    const int b = bin_of(e);
+            // Tokens too light to be in the shortest prefix even if all V weighed as much, next to the largest alone
+            // (2^32): they count towards the whole weight only.
+            // Whole bins, so that a bin's tokens are all counted or all not.
+            const float light = bin_from(bin_of(fmaxf(0.f, __fmul_rn(__fdiv_rn(1.f - top_p, (float)V), 0.999f))));
+            u64 rest = 0;
+            for (int q = tid; q < quads4; q += SA_THREADS) {
+                float4 v = x4[q];
+                float* l = &v.x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float e = k_keeps(l[j], 4 * q + j) ? chance(l[j], top, T) : -1.f;
+                    l[j] = e;
+                    if (e < 0.f) continue;
                     const u64 w = weight(e);
-                    atomicAdd(&sh.hist.n[b], 1u);
-                    if (w) {
-                        atomicAdd(&sh.hist.lo[b], (uint32_t)w & 0xffffu);
-                        atomicAdd(&sh.hist.hi[b], (uint32_t)(w >> 16));
+                    if (e < light) {
+                        rest += w;
+                        continue;
                     }
+                    const int b = bin_of(e);
+                    atomicAdd(&sh.hist.n[b], 1u);
+                    atomicAdd(&sh.hist.lo[b], (uint32_t)w & 0xffffu);
+                    atomicAdd(&sh.hist.hi[b], (uint32_t)(w >> 16));
                 }
-                x[i] = e;
+                x4[q] = v;
             }
+            rest = warp_sum(rest);
+            if (lane == 0) sh.warp_w[warp] = rest;
             held = true;
             cut_bin = -1;
         } else {
             used = true;
-#pragma unroll 4
-            for (int i = tid; i < n; i += SA_THREADS) {
-                const float l = x[i];
-                if (l > -INFINITY) atomicAdd(&sh.hist.n[logit_bin(l)], 1u);
+            for (int q = tid; q < quads4; q += SA_THREADS) {
+                const float4 v = x4[q];
+                const float* l = &v.x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (l[j] > -INFINITY) atomicAdd(&sh.hist.n[logit_bin(l[j])], 1u);
             }
         }
         __syncthreads();
@@ -318,6 +365,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
             const int b = 64 * c + lane;
             Sum s = {0, __reduce_add_sync(ALL, sh.hist.n[b] + sh.hist.n[b + 32]), 0};
             if (by_weight) s.w = warp_sum((u64)sh.hist.lo[b] + sh.hist.lo[b + 32] + ((u64)sh.hist.hi[b] + sh.hist.hi[b + 32] << 16));
+            if (by_weight && c == 0) s.w += warp_sum(lane < SA_WARPS ? sh.warp_w[lane] : 0);   // below every possible cut
             if (lane < C) *in_block<C>(&sh.coarse[rank][c], lane) = s;
         }
         cluster_sync<C>();
@@ -333,11 +381,10 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
                 sh.found = Found{0, 0, 0, 0};
             }
             __syncwarp();
-            find_cut<C, 1>(&sh.coarse[0][0], 32, by_weight,
-                           !by_weight ? (double)top_k : top_p > 0.f ? (double)top_p * (double)mass : 0., &sh.found);
+            find_cut<C, 1>(&sh.coarse[0][0], 32, by_weight, !by_weight ? (u64)top_k : share_of(top_p, mass), &sh.found);
         }
         __syncthreads();
-        const double enough = !by_weight ? (double)top_k : top_p > 0.f ? (double)top_p * (double)sh.mass : 0.;
+        const u64 enough = !by_weight ? (u64)top_k : share_of(top_p, sh.mass);
         const int oct = sh.found.at;
         if (oct < 0) {                                     // fewer tokens than top_k: all are kept
             cluster_sync<C>();                             // every block has read coarse
@@ -367,12 +414,15 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         }
         __syncthreads();
 
-        // A token of the bin (or, to finish, from it up), and its order.
-        const auto here = [&](int i, bool from) {
-            const float v = x[i];
-            if (held ? v < 0.f : v == -INFINITY) return false;
-            const int b = held ? bin_of(v) : logit_bin(v);
-            return from ? b >= bin : b == bin;
+        // A token of the bin (or, to finish, from it up), and its order. On e the bin is an interval; on logits the
+        // distance to the largest is compared as logit_bin computes it.
+        const float e_from = bin_from(bin), e_to = finish ? INFINITY : bin_from(bin + 1);
+        const float z_to = bin == 0 ? INFINITY : (float)(BINS - bin), z_from = finish ? 0.f : (float)(BINS - 1 - bin);
+        const auto here = [&](float v) {
+            if (held) return v >= e_from && v < e_to;
+            if (v == -INFINITY) return false;
+            const float z = v == top ? 0.f : __fmul_rn(__fsub_rn(top, v), per_bin);
+            return z >= z_from && (z < z_to || bin == 0);
         };
         const auto order_at = [&](int i) { return order_of(held ? logit_at(p, logits, first + i) : x[i], first + i); };
         u64 prefix = 0;                                    // of the orders in a narrowed bin
@@ -384,7 +434,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
                 if (tid < 32) sh.hist.n[tid] = sh.hist.lo[tid] = sh.hist.hi[tid] = 0;
                 __syncthreads();
                 for (int i = tid; i < n; i += SA_THREADS) {
-                    if (!here(i, false)) continue;
+                    if (!here(x[i])) continue;
                     const u64 o = order_at(i);
                     if (known && o >> (64 - known) != prefix) continue;
                     const int d = (int)(o >> (64 - known - bits)) & ((1 << bits) - 1);
@@ -420,24 +470,29 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
             if (r < rank) base += sh.count[r];
             listed += sh.count[r];
         }
-        for (int i0 = warp * 32; i0 < n; i0 += SA_THREADS) {
-            const int i = i0 + lane;
-            bool take = i < n && here(i, finish);
-            u64 o = 0;
-            if (take) {
-                o = order_at(i);
-                take = known == 0 || o >> (64 - known) == prefix;
+        uint32_t* found = reinterpret_cast<uint32_t*>(&sh.hist);         // this block's, in any order
+        const uint32_t mine = sh.count[rank];
+        __syncthreads();                                   // the histogram is done with
+        for (int q = tid; q < quads4; q += SA_THREADS) {
+            const float4 v = x4[q];
+            const float* l = &v.x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (!here(l[j])) continue;
+                if (known && order_at(4 * q + j) >> (64 - known) != prefix) continue;
+                const uint32_t to = atomicAdd(&sh.next, 1u);
+                if (to < LIST) found[to] = 4 * q + j;
             }
-            const uint32_t all = __ballot_sync(ALL, take);
-            if (all == 0) continue;
-            uint32_t to = 0;
-            if (lane == 0) to = atomicAdd(&sh.next, (uint32_t)__popc(all));
-            to = base + __shfl_sync(ALL, to, 0) + __popc(all & ((1u << lane) - 1));
-            if (take && to < LIST) {
+        }
+        __syncthreads();
+        if (tid < (int)mine) {
+            const u64 o = order_at((int)found[tid]);
+            if (base + tid < LIST) {
                 if (finish) {
-                    *in_block<C>(&sh.list[to], 0) = o;
+                    *in_block<C>(&sh.list[base + tid], 0) = o;
                 } else {
-                    for (int r = 0; r < C; ++r) *in_block<C>(&sh.list[to], r) = o;
+#pragma unroll
+                    for (int r = 0; r < C; ++r) *in_block<C>(&sh.list[base + tid], r) = o;
                 }
             }
         }
@@ -462,11 +517,10 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
             if (finish) {
                 if (tid == top_k - 1) sh.pick[0] = cum;    // there is one: the cut lies in the list
                 __syncthreads();
-                const double want = top_p > 0.f ? (double)top_p * (double)sh.pick[0] : 0.;
-                keep = keep && (top_p >= 1.f || tid == 0 || (double)(cum - cw) < want);
+                keep = keep && (top_p >= 1.f || tid == 0 || cum - cw < share_of(top_p, sh.pick[0]));
             }
         } else {
-            keep = real && ((double)(above + cum - cw) < enough || (tid == 0 && above_n == 0));
+            keep = real && (above + cum - cw < enough || (tid == 0 && above_n == 0));
         }
         if (finish) keep = keep && !(ce < min_p);
         const int n_keep = __syncthreads_count(keep);      // at least one
@@ -484,42 +538,38 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         const float le = tid < n_keep ? chance(value_of((uint32_t)by_index), top, T) : 0.f;
         const u64 lw = tid < n_keep ? weight(le) : 0;
         const u64 to = block_scan(lw, sh.part, &all);
-        const double target = u > 0.f ? (double)u * (double)all : 0.;
-        const auto past = [&](u64 v) { return u >= 1.f ? v >= all : (double)v > target; };
-        if (lw && past(to) && !past(to - lw)) {
+        const u64 target = drawn_at(u, all);
+        if (to >= target && to - lw < target) {
             p.tokens[row] = (int)~(uint32_t)(by_index >> 32);
-            if (p.probs) p.probs[row] = __fdiv_rn(le, (float)((double)all * 0x1p-32));
+            if (p.probs) p.probs[row] = __fdiv_rn(le, __ull2float_rn(all) * 0x1p-32f);
             if (p.kept) p.kept[row] = n_keep;
         }
         return;
     }
 
-    // The draw over the whole row, in index order: a warp has neighbouring tokens.
-    const int run = ((n + SA_WARPS - 1) / SA_WARPS + 31) / 32 * 32, w0 = warp * run, w1 = min(n, w0 + run);
-    const auto chosen = [&](int i) -> float {              // e of a kept token, -1 otherwise
-        const float v = x[i];
-        if (!held) {
-            if (!k_keeps(v, i)) return -1.f;
-            const float e = chance(v, top, T);
-            return e < min_p ? -1.f : e;
-        }
-        if (v < min_p) return -1.f;                        // min_p >= 0
-        if (cut_bin >= 0) {
-            const int b = bin_of(v);
-            if (b < cut_bin || (b == cut_bin && order_of(logit_at(p, logits, first + i), first + i) < cut_order)) return -1.f;
-        }
-        return v;
-    };
+    // The draw over the whole row, in index order: a warp has neighbouring tokens. x becomes e, -1 where not kept.
+    const int run = (quads4 + SA_WARPS - 1) / SA_WARPS, q0 = warp * run, q1 = min(quads4, q0 + run);
+    const float e_cut = bin_from(max(cut_bin, 0)), e_tie = bin_from(max(cut_bin, 0) + 1);
     u64 sum = 0;
     uint32_t kept = 0;
-#pragma unroll 2
-    for (int i = w0 + lane; i < w1; i += 32) {
-        const float e = chosen(i);
-        if (e >= 0.f) {
-            sum += weight(e);
-            ++kept;
+    for (int q = q0 + lane; q < q1; q += 32) {
+        float4 v = x4[q];
+        float* e = &v.x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (!held) {
+                e[j] = k_keeps(e[j], 4 * q + j) ? chance(e[j], top, T) : -1.f;
+            } else if (cut_bin >= 0 && e[j] < e_tie) {
+                const int i = first + 4 * q + j;
+                if (e[j] < e_cut || order_of(logit_at(p, logits, i), i) < cut_order) e[j] = -1.f;
+            }
+            if (e[j] < min_p) e[j] = -1.f;                 // min_p >= 0
+            if (e[j] >= 0.f) {
+                sum += weight(e[j]);
+                ++kept;
+            }
         }
-        if (!held) x[i] = e;                               // the search below reads it
+        x4[q] = v;
     }
     sum = warp_sum(sum);
     kept = __reduce_add_sync(ALL, kept);
@@ -544,20 +594,32 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
     }
     if (rank == 0 && tid == 0 && p.kept) p.kept[row] = (int)n_all;
     for (int w = 0; w < warp; ++w) before += sh.warp_w[w];
-    const double target = u > 0.f ? (double)u * (double)all : 0.;
-    const auto past = [&](u64 v) { return u >= 1.f ? v >= all : (double)v > target; };
-    if (past(before) || !past(before + sum)) return;       // another warp's
-    for (int i0 = w0; i0 < w1; i0 += 32) {
-        const int i = i0 + lane;
-        const float e = i < w1 ? (held ? chosen(i) : x[i]) : -1.f;
-        const u64 w = e >= 0.f ? weight(e) : 0;
-        const u64 to = before + warp_scan(w);
-        if (w && past(to) && !past(to - w)) {
-            p.tokens[row] = first + i;
-            if (p.probs) p.probs[row] = __fdiv_rn(e, (float)((double)all * 0x1p-32));
+    const u64 target = drawn_at(u, all);
+    if (before >= target || before + sum < target) return; // another warp's
+    for (int s0 = q0; s0 < q1; s0 += 32) {
+        const int q = s0 + lane;
+        const float4 v = q < q1 ? x4[q] : make_float4(-1.f, -1.f, -1.f, -1.f);
+        const float* e = &v.x;
+        u64 w[4], own = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            w[j] = e[j] >= 0.f ? weight(e[j]) : 0;
+            own += w[j];
         }
+        u64 to = before + warp_scan(own);
         before = __shfl_sync(ALL, to, 31);
-        if (past(before)) return;
+        if (to >= target && to - own < target) {
+            to -= own;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (to < target && to + w[j] >= target) {
+                    p.tokens[row] = first + 4 * q + j;
+                    if (p.probs) p.probs[row] = __fdiv_rn(e[j], __ull2float_rn(all) * 0x1p-32f);
+                }
+                to += w[j];
+            }
+        }
+        if (before >= target) return;
     }
 }
 
