@@ -47,7 +47,7 @@ struct Found {                            // where a cut lies
 
 struct Shared {
     union {
-        struct { uint32_t n[BINS], lo[BINS], hi[BINS]; } hist;   // counts; weights' low 16 and high bits
+        struct { uint32_t n[BINS], hi[BINS]; int lo[BINS]; } hist;   // counts; weights' parts
         u64 sorted[LIST];
     };
     u64 list[LIST];                       // gathered tokens
@@ -74,16 +74,44 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 __device__ __forceinline__ u64 order_of(float v, int i) { return (u64)key_of(v) << 32 | (uint32_t)~i; }
 __device__ __forceinline__ float usable(float v) { return v == v ? v + 0.f : -INFINITY; }   // NaN is never drawn; -0 ties with 0
 
-__device__ __forceinline__ float chance(float v, float top, float t) {
-    return v == top ? 1.f : v == -INFINITY ? 0.f : expf(__fdiv_rn(__fsub_rn(v, top), t));
-}
-// e in whole multiples of 2^-32, ties to even: e 2^32 is whole from 2^23 on; below, adding 2^23 rounds it there.
-// (Conversions to 64-bit integers and fp64 comparisons are slow on this GPU.)
+// e = 2^t for t = (l - max) log2(e) / T, with log2(e) / T as the sum of two floats: t = n + f with n whole and |f| <= 1/2,
+// f to 2^-25, then the hardware's 2^f (2 ulps) and n added to the exponent.
+struct Scale {
+    float top, hi, lo;                                     // the maximum; log2(e) / T
+    __device__ Scale(float top_, float T) : top(top_) {
+        hi = fminf(__fdiv_rn(1.44269502f, T), 1e30f);
+        lo = __fdiv_rn(__fmaf_rn(-hi, T, 1.44269502f) + 1.92596303e-8f, T);
+        if (!(hi < 1e30f) || !(fabsf(lo) < 1e20f)) lo = 0.f;             // T below 1.5e-30 or infinite
+    }
+    __device__ __forceinline__ float chance(float l) const {
+        const float x = __fsub_rn(l, top), t = __fmul_rn(x, hi);
+        const float r = __fadd_rn(fmaxf(t, -126.f), 0x1.8p23f), n = __fsub_rn(r, 0x1.8p23f);
+        const float f = __fmaf_rn(x, lo, __fmaf_rn(x, hi, -n));
+        float y;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(f));
+        return t < -126.f ? 0.f : __int_as_float(__float_as_int(y) + (__float_as_int(r) << 23));
+    }
+    // Bin of a logit: 64 to a factor of 2 below the largest, 0: 2^-32 and less. Never above a larger logit's bin.
+    __device__ __forceinline__ int bin(float l) const {
+        const float t = fmaxf(__fmul_rn(__fsub_rn(l, top), hi), -(BINS - 1) / 64.f);
+        return (int)(__float_as_uint(__fmaf_rn(t, 64.f, 0x1.8p23f)) - 0x4b400000u) + BINS - 1;
+    }
+};
+// w = 65536 hi + lo: e in whole multiples of 2^-32, ties to even, lo within +-2^15. Both parts by adding 1.5 2^23, which
+// rounds to a whole number there. (Conversions to 64-bit integers and fp64 comparisons are slow on this GPU.)
+struct Parts {
+    int hi, lo;
+    __device__ explicit Parts(float e) {
+        const float a = __fmaf_rn(e, 0x1p16f, 0x1.8p23f), h = __fsub_rn(a, 0x1.8p23f);
+        const float b = __fadd_rn(__fmaf_rn(h, -0x1p16f, __fmul_rn(e, 0x1p32f)), 0x1.8p23f);
+        hi = (int)(__float_as_uint(a) - 0x4b400000u);
+        lo = (int)(__float_as_uint(b) - 0x4b400000u);
+    }
+};
+__device__ __forceinline__ u64 whole(long long hi, long long lo) { return (u64)(hi * 65536 + lo); }
 __device__ __forceinline__ u64 weight(float e) {
-    const float f = __fmul_rn(e, 0x1p32f);
-    const uint32_t bits = __float_as_uint(f);
-    const u64 large = (u64)((bits & 0x7fffffu) | 0x800000u) << ((bits >> 23) - 150u & 31u);
-    return f >= 0x1p23f ? large : (u64)(__float_as_uint(__fadd_rn(f, 0x1p23f)) - 0x4b000000u);
+    const Parts w(e);
+    return whole(w.hi, w.lo);
 }
 // The least whole number that is at least (or, `over`, more than) f * m, for 0 < f < 1 and m below 2^51.
 __device__ __forceinline__ u64 at_least(float f, u64 m, bool over) {
@@ -101,16 +129,6 @@ __device__ __forceinline__ u64 at_least(float f, u64 m, bool over) {
     }
     return over ? whole + 1 : whole + (rest != 0);
 }
-// Bin of a weight: its factor of 2 (2^-32 and below: the first) and 6 bits; no weight: bin 0.
-__device__ __forceinline__ int bin_of(float e) {
-    const int b = (int)(__float_as_uint(e) >> 17) - 95 * 64;
-    return e <= 0x1p-33f ? 0 : min(max(b, 1), BINS - 1);
-}
-// The least e of a bin (of bin BINS: past the last).
-__device__ __forceinline__ float bin_from(int b) {
-    return b == 0 ? 0.f : b == 1 ? 0x1.000002p-33f : b == BINS ? INFINITY : __uint_as_float((uint32_t)(b + 95 * 64) << 17);
-}
-
 __device__ __forceinline__ float logit_at(const Sample& p, const void* row, int i) {
     return usable(p.f32 ? static_cast<const float*>(row)[i]
                         : __uint_as_float((uint32_t)static_cast<const uint16_t*>(row)[i] << 16));
@@ -294,22 +312,21 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         }
         return;
     }
-    const float top = value_of((uint32_t)(best >> 32));
-    const float per_bin = fminf(__fdiv_rn(64.f * 1.44269504f, T), 1e30f);
-    const auto logit_bin = [&](float l) {                  // not below the bin of a lower logit
-        return l == top ? BINS - 1 : BINS - 1 - (int)fminf(__fmul_rn(__fsub_rn(top, l), per_bin), (float)(BINS - 1));
-    };
+    float top = value_of((uint32_t)(best >> 32));
+    if (top == INFINITY) {                                 // infinite logits share the draw; the others weigh nothing
+        __syncthreads();
+        for (int i = tid; i < 4 * quads4; i += SA_THREADS) x[i] = x[i] == INFINITY ? 0.f : x[i] == -INFINITY ? x[i] : -3e38f;
+        __syncthreads();
+        top = 0.f;
+    }
+    const Scale scale(top, T);
 
-    // What is kept so far. After top-k x still holds logits, and bins are logit_bin; top-p replaces them by e (-1: not
-    // kept by top-k) and bins are bin_of. bin -1: everything.
-    bool held = false, used = false;                       // x holds e; the histogram has been filled
+    // What is kept so far: the tokens above a bin, and those of the bin from an order up (bin -1: all).
     int cut_bin = -1;
     u64 cut_order = 0;
-    const auto k_keeps = [&](float l, int i) {             // top-k's cut, on logits
-        if (l == -INFINITY) return false;
-        if (cut_bin < 0) return true;
-        const int b = logit_bin(l);
-        return b != cut_bin ? b > cut_bin : order_of(l, first + i) >= cut_order;
+    bool used = false;                                     // the histogram has been filled
+    const auto keeps = [&](float l, int b, int i) {
+        return l != -INFINITY && b >= cut_bin && (b > cut_bin || order_of(l, first + i) >= cut_order);
     };
 
     for (int which = 0; which < 2; ++which) {              // 0: top-k by count, 1: top-p by weight
@@ -322,49 +339,48 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
                 __syncthreads();
             }
             // Tokens too light to be in the shortest prefix even if all V weighed as much, next to the largest alone
-            // (2^32): they count towards the whole weight only.
-            // Whole bins, so that a bin's tokens are all counted or all not.
-            const float light = bin_from(bin_of(fmaxf(0.f, __fmul_rn(__fdiv_rn(1.f - top_p, (float)V), 0.999f))));
-            u64 rest = 0;
+            // (2^32; light is 64 of its multiples or more): they count towards the whole weight only. By whole bins, so that a bin's tokens are all in the
+            // histogram or all not.
+            const float light = __fdiv_rn(1.f - top_p, (float)V);
+            const int light_bin = light >= 0x1p-26f ? BINS - 3 + (int)floorf(64.f * __log2f(light)) : 0;
+            int rest_hi = 0;
+            long long rest_lo = 0;
             for (int q = tid; q < quads4; q += SA_THREADS) {
-                float4 v = x4[q];
-                float* l = &v.x;
+                const float4 v = x4[q];
+                const float* l = &v.x;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float e = k_keeps(l[j], 4 * q + j) ? chance(l[j], top, T) : -1.f;
-                    l[j] = e;
-                    if (e < 0.f) continue;
-                    const u64 w = weight(e);
-                    if (e < light) {
-                        rest += w;
+                    const int b = scale.bin(l[j]);
+                    if (!keeps(l[j], b, 4 * q + j)) continue;
+                    const Parts w(scale.chance(l[j]));
+                    if (b < light_bin) {
+                        rest_hi += w.hi;
+                        rest_lo += w.lo;
                         continue;
                     }
-                    const int b = bin_of(e);
                     atomicAdd(&sh.hist.n[b], 1u);
-                    atomicAdd(&sh.hist.lo[b], (uint32_t)w & 0xffffu);
-                    atomicAdd(&sh.hist.hi[b], (uint32_t)(w >> 16));
+                    atomicAdd(&sh.hist.lo[b], w.lo);
+                    atomicAdd(&sh.hist.hi[b], (uint32_t)w.hi);
                 }
-                x4[q] = v;
             }
-            rest = warp_sum(rest);
+            const u64 rest = warp_sum(whole(rest_hi, rest_lo));
             if (lane == 0) sh.warp_w[warp] = rest;
-            held = true;
-            cut_bin = -1;
         } else {
-            used = true;
             for (int q = tid; q < quads4; q += SA_THREADS) {
                 const float4 v = x4[q];
                 const float* l = &v.x;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (l[j] > -INFINITY) atomicAdd(&sh.hist.n[logit_bin(l[j])], 1u);
+                    if (l[j] > -INFINITY) atomicAdd(&sh.hist.n[scale.bin(l[j])], 1u);
             }
         }
+        used = true;
         __syncthreads();
         for (int c = warp; c < 32; c += SA_WARPS) {        // sums of 64 bins, to every block
             const int b = 64 * c + lane;
             Sum s = {0, __reduce_add_sync(ALL, sh.hist.n[b] + sh.hist.n[b + 32]), 0};
-            if (by_weight) s.w = warp_sum((u64)sh.hist.lo[b] + sh.hist.lo[b + 32] + ((u64)sh.hist.hi[b] + sh.hist.hi[b + 32] << 16));
+            if (by_weight)
+                s.w = warp_sum(whole((long long)sh.hist.hi[b] + sh.hist.hi[b + 32], (long long)sh.hist.lo[b] + sh.hist.lo[b + 32]));
             if (by_weight && c == 0) s.w += warp_sum(lane < SA_WARPS ? sh.warp_w[lane] : 0);   // below every possible cut
             if (lane < C) *in_block<C>(&sh.coarse[rank][c], lane) = s;
         }
@@ -392,7 +408,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         }
         if (tid < 64 * C) {                                // its bins, to every block
             const int b = 64 * oct + (tid & 63);
-            *in_block<C>(&sh.fine[rank][tid & 63], tid >> 6) = Sum{(u64)sh.hist.lo[b] + ((u64)sh.hist.hi[b] << 16), sh.hist.n[b], 0};
+            *in_block<C>(&sh.fine[rank][tid & 63], tid >> 6) = Sum{whole(sh.hist.hi[b], sh.hist.lo[b]), sh.hist.n[b], 0};
         }
         cluster_sync<C>();
         if (warp == 0) find_cut<C, 2>(&sh.fine[0][0], 64, by_weight, enough, &sh.found);
@@ -414,17 +430,12 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         }
         __syncthreads();
 
-        // A token of the bin (or, to finish, from it up), and its order. On e the bin is an interval; on logits the
-        // distance to the largest is compared as logit_bin computes it.
-        const float e_from = bin_from(bin), e_to = finish ? INFINITY : bin_from(bin + 1);
-        const float z_to = bin == 0 ? INFINITY : (float)(BINS - bin), z_from = finish ? 0.f : (float)(BINS - 1 - bin);
-        const auto here = [&](float v) {
-            if (held) return v >= e_from && v < e_to;
-            if (v == -INFINITY) return false;
-            const float z = v == top ? 0.f : __fmul_rn(__fsub_rn(top, v), per_bin);
-            return z >= z_from && (z < z_to || bin == 0);
+        // A kept token of the bin (or, to finish, from it up), and its order.
+        const auto here = [&](float l, int i) {
+            const int b = scale.bin(l);
+            return (finish ? b >= bin : b == bin) && keeps(l, b, i);
         };
-        const auto order_at = [&](int i) { return order_of(held ? logit_at(p, logits, first + i) : x[i], first + i); };
+        const auto order_at = [&](int i) { return order_of(x[i], first + i); };
         u64 prefix = 0;                                    // of the orders in a narrowed bin
         int known = 0;
         if (!finish) {
@@ -434,15 +445,15 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
                 if (tid < 32) sh.hist.n[tid] = sh.hist.lo[tid] = sh.hist.hi[tid] = 0;
                 __syncthreads();
                 for (int i = tid; i < n; i += SA_THREADS) {
-                    if (!here(x[i])) continue;
+                    if (!here(x[i], i)) continue;
                     const u64 o = order_at(i);
                     if (known && o >> (64 - known) != prefix) continue;
                     const int d = (int)(o >> (64 - known - bits)) & ((1 << bits) - 1);
                     atomicAdd(&sh.hist.n[d], 1u);
                     if (by_weight) {
-                        const u64 w = weight(x[i]);
-                        atomicAdd(&sh.hist.lo[d], (uint32_t)w & 0xffffu);
-                        atomicAdd(&sh.hist.hi[d], (uint32_t)(w >> 16));
+                        const Parts w(scale.chance(x[i]));
+                        atomicAdd(&sh.hist.lo[d], w.lo);
+                        atomicAdd(&sh.hist.hi[d], (uint32_t)w.hi);
                     }
                 }
                 __syncthreads();
@@ -450,7 +461,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
                 const int width = round & 1 ? 64 : 32;
                 for (int r = warp; r < C; r += SA_WARPS)
                     *in_block<C>(tab + rank * width + lane, r) =
-                        Sum{(u64)sh.hist.lo[lane] + ((u64)sh.hist.hi[lane] << 16), sh.hist.n[lane], 0};
+                        Sum{whole(sh.hist.hi[lane], sh.hist.lo[lane]), sh.hist.n[lane], 0};
                 cluster_sync<C>();
                 if (warp == 0) {
                     find_cut<C, 1>(tab, width, by_weight, enough, &sh.found);
@@ -478,7 +489,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
             const float* l = &v.x;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (!here(l[j])) continue;
+                if (!here(l[j], 4 * q + j)) continue;
                 if (known && order_at(4 * q + j) >> (64 - known) != prefix) continue;
                 const uint32_t to = atomicAdd(&sh.next, 1u);
                 if (to < LIST) found[to] = 4 * q + j;
@@ -505,7 +516,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         while (size < count) size <<= 1;
         const bool real = tid < count;
         const u64 o = sort_down(real ? sh.list[tid] : 0, size, sh.sorted);
-        const float ce = real ? chance(value_of((uint32_t)(o >> 32)), top, T) : 0.f;
+        const float ce = real ? scale.chance(value_of((uint32_t)(o >> 32))) : 0.f;
         const u64 cw = real ? weight(ce) : 0;
         u64 all;
         const u64 cum = block_scan(cw, sh.part, &all);
@@ -535,7 +546,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         int small = 32;
         while (small < n_keep) small <<= 1;
         const u64 by_index = sort_down(tid < n_keep ? o << 32 | o >> 32 : 0, small, sh.sorted);
-        const float le = tid < n_keep ? chance(value_of((uint32_t)by_index), top, T) : 0.f;
+        const float le = tid < n_keep ? scale.chance(value_of((uint32_t)by_index)) : 0.f;
         const u64 lw = tid < n_keep ? weight(le) : 0;
         const u64 to = block_scan(lw, sh.part, &all);
         const u64 target = drawn_at(u, all);
@@ -547,30 +558,27 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         return;
     }
 
-    // The draw over the whole row, in index order: a warp has neighbouring tokens. x becomes e, -1 where not kept.
+    // The draw over the whole row, in index order: a warp has neighbouring tokens. x becomes e, 0 where not kept.
     const int run = (quads4 + SA_WARPS - 1) / SA_WARPS, q0 = warp * run, q1 = min(quads4, q0 + run);
-    const float e_cut = bin_from(max(cut_bin, 0)), e_tie = bin_from(max(cut_bin, 0) + 1);
-    u64 sum = 0;
+    int sum_hi = 0;
+    long long sum_lo = 0;
     uint32_t kept = 0;
     for (int q = q0 + lane; q < q1; q += 32) {
         float4 v = x4[q];
         float* e = &v.x;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if (!held) {
-                e[j] = k_keeps(e[j], 4 * q + j) ? chance(e[j], top, T) : -1.f;
-            } else if (cut_bin >= 0 && e[j] < e_tie) {
-                const int i = first + 4 * q + j;
-                if (e[j] < e_cut || order_of(logit_at(p, logits, i), i) < cut_order) e[j] = -1.f;
-            }
-            if (e[j] < min_p) e[j] = -1.f;                 // min_p >= 0
-            if (e[j] >= 0.f) {
-                sum += weight(e[j]);
-                ++kept;
-            }
+            const float c = scale.chance(e[j]);
+            const bool in = c >= min_p && keeps(e[j], scale.bin(e[j]), 4 * q + j);
+            e[j] = in ? c : 0.f;
+            kept += in;
+            const Parts w(e[j]);
+            sum_hi += w.hi;
+            sum_lo += w.lo;
         }
         x4[q] = v;
     }
+    u64 sum = whole(sum_hi, sum_lo);
     sum = warp_sum(sum);
     kept = __reduce_add_sync(ALL, kept);
     if (lane == 0) {
@@ -598,12 +606,12 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
     if (before >= target || before + sum < target) return; // another warp's
     for (int s0 = q0; s0 < q1; s0 += 32) {
         const int q = s0 + lane;
-        const float4 v = q < q1 ? x4[q] : make_float4(-1.f, -1.f, -1.f, -1.f);
+        const float4 v = q < q1 ? x4[q] : make_float4(0.f, 0.f, 0.f, 0.f);
         const float* e = &v.x;
         u64 w[4], own = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            w[j] = e[j] >= 0.f ? weight(e[j]) : 0;
+            w[j] = weight(e[j]);
             own += w[j];
         }
         u64 to = before + warp_scan(own);
