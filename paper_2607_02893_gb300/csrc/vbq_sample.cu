@@ -62,6 +62,9 @@ struct Shared {
     uint32_t next;
 };
 constexpr int SHARED_BYTES = (sizeof(Shared) + 15) / 16 * 16;    // the row's slice follows
+constexpr size_t SMEM_ALONE = 120 * 1024; // more than half an SM's
+constexpr size_t SMEM_MOST = SHARED_BYTES + 4 * (SAMPLE_MAX_VOCAB / 6 + 4);
+static_assert(SMEM_MOST <= 227 * 1024, "the largest slice fits");
 
 __device__ __forceinline__ uint32_t key_of(float v) {
     const uint32_t u = __float_as_uint(v);
@@ -321,13 +324,11 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
     }
     const Scale scale(top, T);
 
-    // What is kept so far: the tokens above a bin, and those of the bin from an order up (bin -1: all).
-    int cut_bin = -1;
-    u64 cut_order = 0;
+    // What is kept so far: the logits above cut, and those equal to it up to an index.
+    float cut = -INFINITY;
+    int cut_i = -1;
     bool used = false;                                     // the histogram has been filled
-    const auto keeps = [&](float l, int b, int i) {
-        return l != -INFINITY && b >= cut_bin && (b > cut_bin || order_of(l, first + i) >= cut_order);
-    };
+    const auto keeps = [&](float l, int i) { return l > cut || (l == cut && first + i <= cut_i); };
 
     for (int which = 0; which < 2; ++which) {              // 0: top-k by count, 1: top-p by weight
         if (which == 0 ? top_k <= 0 || top_k >= V : top_p >= 1.f) continue;
@@ -350,8 +351,8 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
                 const float* l = &v.x;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
+                    if (!keeps(l[j], 4 * q + j)) continue;
                     const int b = scale.bin(l[j]);
-                    if (!keeps(l[j], b, 4 * q + j)) continue;
                     const Parts w(scale.chance(l[j]));
                     if (b < light_bin) {
                         rest_hi += w.hi;
@@ -433,7 +434,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         // A kept token of the bin (or, to finish, from it up), and its order.
         const auto here = [&](float l, int i) {
             const int b = scale.bin(l);
-            return (finish ? b >= bin : b == bin) && keeps(l, b, i);
+            return (finish ? b >= bin : b == bin) && keeps(l, i);
         };
         const auto order_at = [&](int i) { return order_of(x[i], first + i); };
         u64 prefix = 0;                                    // of the orders in a narrowed bin
@@ -538,8 +539,8 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         if (!finish) {
             if (tid == n_keep - 1) sh.pick[1] = o;
             __syncthreads();
-            cut_bin = bin;
-            cut_order = sh.pick[1];
+            cut = value_of((uint32_t)(sh.pick[1] >> 32));
+            cut_i = (int)~(uint32_t)sh.pick[1];
             continue;
         }
         // The draw, in index order.
@@ -569,7 +570,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float c = scale.chance(e[j]);
-            const bool in = c >= min_p && keeps(e[j], scale.bin(e[j]), 4 * q + j);
+            const bool in = c >= min_p && keeps(e[j], 4 * q + j);
             e[j] = in ? c : 0.f;
             kept += in;
             const Parts w(e[j]);
@@ -631,17 +632,19 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
     }
 }
 
+// least: shared memory to ask for at least.
 template <int C>
-cudaError_t launch(const Sample& p, cudaStream_t s) {
+cudaError_t launch(const Sample& p, size_t least, cudaStream_t s) {
     static LaunchPrep prep;
-    const int slice = ((p.vocab + C - 1) / C + 3) / 4 * 4, most = C == SA_BLOCKS ? SAMPLE_MAX_VOCAB / SA_BLOCKS : 4096;
+    const int slice = ((p.vocab + C - 1) / C + 3) / 4 * 4;
+    const size_t need = SHARED_BYTES + 4 * (size_t)slice;
     int sms = 0;
-    cudaError_t e = prep.get(sample_kernel<C>, SHARED_BYTES + 4 * (size_t)most, &sms);
+    cudaError_t e = prep.get(sample_kernel<C>, SMEM_MOST, &sms);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.batch * C);
     cfg.blockDim = dim3(SA_THREADS);
-    cfg.dynamicSmemBytes = SHARED_BYTES + 4 * (size_t)slice;
+    cfg.dynamicSmemBytes = need > least ? need : least;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -656,10 +659,15 @@ cudaError_t launch(const Sample& p, cudaStream_t s) {
 
 }  // namespace
 
+// Blocks per row: few tokens are not worth an exchange; up to 8 rows spread over clusters of 8. Clusters of 8 no
+// longer get an SM per block at 16 rows (two blocks on some SMs: 33 us for 16 x 128256 under top-p 0.9; two waves
+// where shared memory allows one: 45 us), clusters of 6 do (29 us; 5: 31 us, 4: 34 us). Beyond an SM per block the
+// rows queue either way.
 cudaError_t launch_sample(const Sample& p, cudaStream_t s) {
-    if (p.vocab <= 4096) return launch<1>(p, s);
-    if (p.vocab <= 16384) return launch<4>(p, s);
-    return launch<SA_BLOCKS>(p, s);
+    if (p.vocab <= 4096) return launch<1>(p, 0, s);
+    if (p.vocab <= 16384) return launch<4>(p, 0, s);
+    if (p.batch > 8 && p.batch <= 24) return launch<6>(p, SMEM_ALONE, s);
+    return launch<8>(p, 0, s);
 }
 
 }  // namespace vbq
