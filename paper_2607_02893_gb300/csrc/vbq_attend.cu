@@ -36,10 +36,14 @@
 //
 // A warp takes whole pages (64 keys of one head, one contiguous blob) through
 // its own ring of shared-memory stages filled by bulk copies: no barrier in the
-// steady state. The pages of all (sequence, head) segments form one list that
-// is cut evenly over the blocks, one per SM, whatever the lengths; a segment
-// that crosses blocks is joined through the workspace by the block that
-// finishes last, in block order, so results do not depend on timing.
+// steady state. The (sequence, row tile, head) segments are cut into parts of at
+// most `quantum` pages, one part per block and one block per SM, if that leaves
+// no block with much more than an even share; otherwise the pages of all
+// segments form one list that is cut evenly, and a block may finish one segment
+// and start another. Parts are joined through the workspace by the block that
+// finishes a segment last, in block order, so results do not depend on timing.
+#include <type_traits>
+
 #include <cuda_bf16.h>
 
 #include "vbq_decode.h"
@@ -49,8 +53,9 @@ namespace vbq {
 namespace {
 
 constexpr uint32_t FULL = 0xffffffffu;
-constexpr int JOIN = 8;
+constexpr int JOIN = 10;
 constexpr int CUT = 6;                           // pages a block takes at least of a segment that is cut
+constexpr int STRADDLE = 16;                     // pages whose time a block's second segment costs
 constexpr uint32_t LOW = 0x003c003cu, HIGH = 0x03c003c0u;    // codes at bits 2..5 and 6..9 of each half
 
 // D: head dimension, NT: 8-row tiles of query rows per pass, W: warps, S: stages per warp.
@@ -63,20 +68,21 @@ struct Shape {
     static constexpr int TILES = D / 16;         // output tiles of 16 dimensions
     static constexpr int BLOB = 68 * D;
     static constexpr int THREADS = 32 * W;
-    static constexpr int UNITS = ROWS * D / 8;   // 8 outputs each
+    static constexpr int UNITS = ROWS * D / 4;   // 4 outputs each
     // shared memory
     static constexpr int BARS = W * S * BLOB;                    // full barriers
     static constexpr int ML = BARS + W * S * 8;                  // (maximum, sum) per warp and row
     static constexpr int CUM = ML + W * ROWS * 8;                // pages before each sequence
-    static constexpr int LO = CUM + (KV_MAX_BATCH + 2) * 8;      // first page of each sequence
-    static constexpr int MISC = LO + KV_MAX_BATCH * 4;
+    static constexpr int SPAN = CUM + (KV_MAX_BATCH + 2) * 8;    // first page and last key of each sequence
+    static constexpr int MISC = SPAN + KV_MAX_BATCH * 8;
     static constexpr int SMEM = MISC + 64 + 4 * W;
     static constexpr int PART = ROWS * D + 2 * ROWS;             // floats of a partial result
 };
 
-struct __align__(16) Misc {
+struct Misc {
     int64_t quantum;
     int abort, last;
+    int aligned;                                 // a block has one part of one segment
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -126,25 +132,31 @@ struct Segment {
 
 struct List {
     const int64_t* cum;                          // shared: pages of one head before each sequence
-    const int* lo;
     int batch, kv_heads, per_seq;                // segments per sequence
-    __device__ Segment at(int64_t p) const {
+    __device__ Segment segment(int b, int64_t k) const {
+        Segment s;
+        s.b = b;
+        s.pages = cum[b + 1] - cum[b];
+        s.start = cum[b] * per_seq + k * s.pages;
+        s.rt = (int)k / kv_heads;
+        s.h = (int)k - s.rt * kv_heads;
+        s.index = (int64_t)b * per_seq + k;
+        return s;
+    }
+    __device__ Segment at(int64_t p) const {     // of a page of the list
         int b = 0, e = batch;                    // the last b with cum[b] * per_seq <= p (it has pages: p is in the list)
         while (e - b > 1) {
             const int m = (b + e) >> 1;
             if (cum[m] * per_seq <= p) b = m; else e = m;
         }
-        Segment s;
-        s.b = b;
-        s.pages = cum[b + 1] - cum[b];
-        const int64_t in = p - cum[b] * per_seq, k = in / s.pages;
-        s.start = cum[b] * per_seq + k * s.pages;
-        s.rt = (int)(k / kv_heads);
-        s.h = (int)(k - (int64_t)s.rt * kv_heads);
-        s.index = (int64_t)b * per_seq + k;
-        return s;
+        const int64_t in = p - cum[b] * per_seq;
+        return segment(b, in / (cum[b + 1] - cum[b]));
     }
 };
+
+__device__ __forceinline__ int parts_of(int64_t pages, int64_t quantum) {
+    return (int)(((uint32_t)pages + (uint32_t)quantum - 1) / (uint32_t)quantum);     // a sequence has below 2^26 pages
+}
 
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAttend a, int row_tiles, uint32_t* counts,
@@ -154,9 +166,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     const uint32_t sbase = smem_u32(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, t4 = lane & 3;
+    // The lane's place in a blob: its key's words, the key's scales, its value words.
+    const uint32_t klane = g * (D / 2) + t4 * (D / 8), slane = kv_scales_at(D) + g * (D / 16);
+    const uint32_t vlane = kv_values_at(D) + t4 * (D / 2) + (D == 64 ? g : D == 128 ? g ^ ((t4 >> 1) << 2) : g ^ (t4 << 1)) * (D / 16);
     float2* ml = reinterpret_cast<float2*>(smem + C::ML);
     int64_t* cum = reinterpret_cast<int64_t*>(smem + C::CUM);
-    int* lo_page = reinterpret_cast<int*>(smem + C::LO);
+    int2* span = reinterpret_cast<int2*>(smem + C::SPAN);
     Misc* misc = reinterpret_cast<Misc*>(smem + C::MISC);
     int* kept_in = reinterpret_cast<int*>(smem + C::MISC + 64);          // the stage a warp's partial result is in
     const uint32_t abort_addr = sbase + C::MISC + 8;
@@ -186,17 +201,19 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             mn = min(mn, hi);
         }
         const int lo = hi >= 0 && a.window > 0 && mn >= a.window ? mn - a.window + 1 : 0;
-        lo_page[b] = lo / KV_PAGE;
+        span[b] = make_int2(lo / KV_PAGE, hi);
         cum[b + 1] = hi < 0 ? 0 : hi / KV_PAGE - lo / KV_PAGE + 1;
     }
     if (tid == 0) cum[0] = 0;
     __syncthreads();
     if (warp == 0) {
-        int64_t before = 0, most = 0;
+        int64_t before = 0;
+        int most = 0, used = 0;                   // sequences with pages
         for (int b0 = 0; b0 < a.batch; b0 += 32) {
             const int b = b0 + lane;
             int64_t x = b < a.batch ? cum[b + 1] : 0;
-            most = max(most, x);
+            most = max(most, (int)x);
+            used += __popc(__ballot_sync(FULL, x > 0));
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int64_t y = __shfl_up_sync(FULL, x, o);
@@ -206,21 +223,66 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             before = __shfl_sync(FULL, x, 31);
             if (b < a.batch) cum[b + 1] = x;
         }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) most = max(most, (int64_t)__shfl_xor_sync(FULL, most, o));
+        most = __reduce_max_sync(FULL, most);
+        __syncwarp();
+        // An even share of the pages; segments that a block's warps take at once are not cut, and none into parts
+        // that cost more to join than to read.
+        const int blocks = (int)gridDim.x, least = most <= W ? most : CUT;
+        const int64_t even = max((before * per_seq + blocks - 1) / blocks, (int64_t)max(least, 1));
+        // One part per block: parts of at most q pages, the least of a few q that fit.
+        const int64_t segments = (int64_t)used * per_seq;
+        int aligned = 0;
+        int64_t quantum = even;
+        if (segments <= blocks && used > 0) {
+            const int share = blocks / (int)segments;      // parts each: always fits
+            int fit = max((most + share - 1) / share, least), low = (int)even;
+            for (int i = 0; i < 5 && low < fit; ++i) {
+                const int q = (low + fit) / 2;
+                uint32_t n = 0;
+                for (int b = lane; b < a.batch; b += 32) n += parts_of(cum[b + 1] - cum[b], q);
+                n = __reduce_add_sync(FULL, n);
+                if ((int64_t)n * per_seq <= blocks) fit = q; else low = q + 1;
+            }
+            if (fit <= even + STRADDLE) {
+                aligned = 1;
+                quantum = fit;
+            }
+        }
         if (lane == 0) {
-            // an even share of the pages; segments that a block's warps take at once are not cut, and no
-            // segment into parts that cost more to join than to read
-            int64_t q = (before * per_seq + gridDim.x - 1) / gridDim.x;
-            const int64_t least = most <= W ? most : CUT;
-            if (q < least) q = least;
-            misc->quantum = q > 0 ? q : 1;
+            misc->quantum = quantum;
+            misc->aligned = aligned;
         }
     }
     __syncthreads();
-    const List list{cum, lo_page, a.batch, c.kv_heads, per_seq};
-    const int64_t total = cum[a.batch] * per_seq, quantum = misc->quantum;
-    const int64_t p0 = min(total, (int64_t)blockIdx.x * quantum), p1 = min(total, p0 + quantum);
+    const List list{cum, a.batch, c.kv_heads, per_seq};
+    const int64_t quantum = misc->quantum;
+    const bool aligned = misc->aligned;
+    int64_t p0 = 0, p1 = 0;                       // the block's pages of the list
+    int first_part = 0, parts_here = 0;           // aligned: the segment's blocks
+    Segment s = {};
+    if (aligned) {
+        int left = blockIdx.x;
+        for (int b = 0; b < a.batch; ++b) {
+            const int64_t pages = cum[b + 1] - cum[b];
+            const int n = parts_of(pages, quantum);
+            if (left < n * per_seq) {
+                const int k = left / n, i = left - k * n;
+                s = list.segment(b, k);
+                const int each = (int)pages / n, more = (int)pages - each * n;
+                p0 = s.start + i * each + min(i, more);
+                p1 = p0 + each + (i < more);
+                first_part = (int)blockIdx.x - i;
+                parts_here = n;
+                break;
+            }
+            left -= n * per_seq;
+        }
+    } else {
+        const int64_t total = cum[a.batch] * per_seq;
+        p0 = min(total, (int64_t)blockIdx.x * quantum);
+        p1 = min(total, p0 + quantum);
+        if (p0 < p1) s = list.at(p0);
+    }
 
     // Sequences without keys: zeros.
     for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
@@ -231,22 +293,22 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
 
     // The warp's own pages: p0 + warp, + W, ...; the k-th uses stage k % S.
     const uint8_t* src = nullptr;                 // lane i: of the page 32 * n + i
-    int64_t issued = 0, used = 0, landed = 0;     // landed: copies waited for
+    uint32_t issued = 0, used = 0, landed = 0;    // landed: copies waited for
     bool ok = true;
-    const int64_t mine = p1 - p0 > warp ? (p1 - p0 - warp + W - 1) / W : 0;
+    const uint32_t mine = p1 - p0 > warp ? (uint32_t)((uint64_t)(p1 - p0 - warp + W - 1) / W) : 0;
     auto issue = [&]() {                          // the next page's copy
         if (issued >= mine || !ok) return;
         if ((issued & 31) == 0) {
-            const int64_t k = issued + lane;
+            const uint32_t k = issued + lane;
             if (k < mine) {
-                const int64_t p = p0 + warp + k * W;
-                const Segment s = list.at(p);
-                int64_t page = c.table[s.b * c.table_stride + lo_page[s.b] + (p - s.start)];
+                const int64_t p = p0 + warp + (int64_t)k * W;
+                const Segment t = p < s.start + s.pages ? s : list.at(p);
+                int64_t page = c.table[t.b * c.table_stride + span[t.b].x + (p - t.start)];
                 if (page < 0 || page >= c.n_pages) {
                     atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
                     page = 0;
                 }
-                src = c.pages + (page * c.kv_heads + s.h) * C::BLOB;
+                src = c.pages + (page * c.kv_heads + t.h) * C::BLOB;
             }
         }
         const int st = (int)(issued % S);
@@ -257,13 +319,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     for (int i = 0; i < S; ++i) issue();
 
     for (int64_t cur = p0; cur < p1;) {
-        const Segment s = list.at(cur);
+        if (cur != p0) s = list.at(cur);
         const int64_t end = min(p1, s.start + s.pages);
-        const int hi_key = [&] {                  // the sequence's last key
-            int hi = -1;
-            for (int t = 0; t < a.rows; ++t) hi = max(hi, a.pos[s.b * a.rows + t]);
-            return (int)min((int64_t)hi, table_keys - 1);
-        }();
+        const int hi_key = span[s.b].y, page0 = span[s.b].x;             // the sequence's last key and first page
 
         // Query fragments of the tile's rows, and the rows' parameters per accumulator column.
         uint32_t qb[NT][KW][4];
@@ -287,8 +345,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             top = max(top, __shfl_xor_sync(FULL, top, 1));
             top = max(top, __shfl_xor_sync(FULL, top, 2));
             const int e = max((int)(top >> 23), 13);                     // biased exponent of the row's largest value
-            const float up = pow2(139 - e);                              // to [2^12, 2^13)
-            const float fr = a.scale * 1.44269504f * 0x1p22f * pow2(e - 139);
+            // to [2^12, 2^13), with the scale's sign, so that the scores' factor is positive (scale 0: all scores 0)
+            const float up = a.scale > 0.f ? pow2(139 - e) : a.scale < 0.f ? -pow2(139 - e) : 0.f;
+            const float fr = fmaxf(fabsf(a.scale) * 1.44269504f * 0x1p22f * pow2(e - 139), 1e-37f);
             float sum[GR];
 #pragma unroll
             for (int i = 0; i < GR; ++i) sum[i] = 0.f;
@@ -353,7 +412,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
         int vexp = -13;                           // value scales are taken in units of 2^(vexp - 14)
         bool any = false;
 
-        for (int64_t p = p0 + warp + used * W; p < end; p += W) {
+        // The warp's pages of the segment, from the segment's first.
+        const int in_end = (int)(end - s.start);
+        for (int in = (int)(p0 + warp + (int64_t)used * W - s.start); in < in_end; in += W) {
             if (any) { __syncwarp(); issue(); }   // into the stage of the page before
             any = true;
             const int st = (int)(used % S);
@@ -365,28 +426,29 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             ++used;
             if (!ok) continue;
             landed = used;
-            const int key0 = (int)((lo_page[s.b] + (p - s.start)) * KV_PAGE);
-            const int subs = min(4, (hi_key - key0) / 16 + 1);
-            const bool edge = key0 + KV_PAGE - 1 > close || key0 <= open;
-
-            float sc[4][NT][4];
-            __half2 vtop = __float2half2_rn(0.f);
+            const int key0 = (page0 + in) * KV_PAGE;
+            const auto page = [&](auto is_edge) {                        // is_edge: some row does not attend to all of it
+                constexpr bool EDGE = decltype(is_edge)::value;
+                const int subs = EDGE ? min(4, (hi_key - key0) / 16 + 1) : 4;
+                float sc[4][NT][4];
+                __half2 vtop = __float2half2_rn(0.f);
 #pragma unroll
-            for (int sub = 0; sub < 4; ++sub) {
-                if (sub < subs) {
+                for (int sub = 0; sub < 4; ++sub) {
+                    if (EDGE && sub >= subs) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) sc[sub][n][i] = -INFINITY;
+                        continue;
+                    }
                     uint32_t k0[KW], k1[KW], sw0[GR], sw1[GR];           // keys g and g + 8 (in row order), their scales
-                    const uint32_t krow = stage + (sub * 16 + g) * (D / 2) + t4 * (D / 8);
-                    const uint32_t srow = stage + kv_scales_at(D) + (sub * 16 + g) * (D / 16);
+                    const uint32_t krow = stage + sub * 8 * D + klane, srow = stage + sub * D + slane;
                     lds_words<KW>(k0, krow);
-                    lds_words<KW>(k1, krow + 8 * (D / 2));
+                    lds_words<KW>(k1, krow + 4 * D);
                     lds_words<GR>(sw0, srow);
-                    lds_words<GR>(sw1, srow + 8 * (D / 16));
+                    lds_words<GR>(sw1, srow + D / 2);
                     const __half* s0 = reinterpret_cast<const __half*>(sw0);
                     const __half* s1 = reinterpret_cast<const __half*>(sw1);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) sc[sub][n][i] = 0.f;
 #pragma unroll
                     for (int q = 0; q < GR; ++q) {
                         float d[NT][4];
@@ -400,140 +462,138 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
                             const uint32_t x0 = k0[j], x1 = k1[j], y0 = prmt(x0, 0, 0x2301), y1 = prmt(x1, 0, 0x2301);
 #pragma unroll
                             for (int n = 0; n < NT; ++n) {
-                                mma(d[n], x0 & LOW, x1 & LOW, x0 & HIGH, x1 & HIGH,
-                                    qb[n][j][0], qb[n][j][1]);
-                                mma(d[n], y0 & LOW, y1 & LOW, y0 & HIGH, y1 & HIGH,
-                                    qb[n][j][2], qb[n][j][3]);
+                                mma(d[n], x0 & LOW, x1 & LOW, x0 & HIGH, x1 & HIGH, qb[n][j][0], qb[n][j][1]);
+                                mma(d[n], y0 & LOW, y1 & LOW, y0 & HIGH, y1 & HIGH, qb[n][j][2], qb[n][j][3]);
                             }
                         }
                         const float e0 = __half2float(s0[q]), e1 = __half2float(s1[q]);
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            sc[sub][n][0] = fmaf(d[n][0], e0, sc[sub][n][0]);
-                            sc[sub][n][1] = fmaf(d[n][1], e0, sc[sub][n][1]);
-                            sc[sub][n][2] = fmaf(d[n][2], e1, sc[sub][n][2]);
-                            sc[sub][n][3] = fmaf(d[n][3], e1, sc[sub][n][3]);
-                        }
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                sc[sub][n][i] = q == 0 ? d[n][i] * (i < 2 ? e0 : e1) : fmaf(d[n][i], i < 2 ? e0 : e1, sc[sub][n][i]);
                     }
                     const int key = key0 + sub * 16 + (g >> 1) + (g & 1) * 4;
+                    if (EDGE) {
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
+                        for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            sc[sub][n][i] *= f[n][i & 1];
-                            if (edge) {
+                            for (int i = 0; i < 4; ++i) {
                                 const int k = key + (i >> 1) * 8, p_ = pos[n][i & 1];
                                 if (k > p_ || k > hi_key || (a.window > 0 && k <= p_ - a.window)) sc[sub][n][i] = -INFINITY;
                             }
-                        }
+                    }
                     // the largest value scale among keys that exist
 #pragma unroll
                     for (int q = 0; q < GR; ++q) {
                         const __half z = __float2half(0.f);
-                        vtop = __hmax2(vtop, __halves2half2(edge && key > hi_key ? z : s0[GR + q],
-                                                            edge && key + 8 > hi_key ? z : s1[GR + q]));
+                        vtop = __hmax2(vtop, __halves2half2(EDGE && key > hi_key ? z : s0[GR + q],
+                                                            EDGE && key + 8 > hi_key ? z : s1[GR + q]));
                     }
-                } else {
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) sc[sub][n][i] = -INFINITY;
                 }
-            }
 
-            // Running maximum per row, running power of two of the value scales.
-            const uint32_t vb = __reduce_max_sync(
-                FULL, max((uint32_t)__half_as_ushort(__low2half(vtop)), (uint32_t)__half_as_ushort(__high2half(vtop))));
-            const int vnew = max(vexp, max((int)(vb >> 10), 1) - 14);    // scales below 2^vnew
-            const float shrink = pow2(vexp - vnew);
-            bool moved = vnew != vexp;
-            vexp = vnew;
-            float mu[NT][2], fac[NT][2];
+                // Running maximum per row, running power of two of the value scales.
+                const uint32_t vb = __reduce_max_sync(
+                    FULL, max((uint32_t)__half_as_ushort(__low2half(vtop)), (uint32_t)__half_as_ushort(__high2half(vtop))));
+                const int vnew = max(vexp, max((int)(vb >> 10), 1) - 14);            // scales below 2^vnew
+                bool moved = vnew != vexp;
+                float mnew[NT][2], mu[NT][2];
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float x = m[n][i];
+                    for (int i = 0; i < 2; ++i) {
+                        float x = fmaxf(sc[0][n][i], sc[0][n][i + 2]);
 #pragma unroll
-                    for (int sub = 0; sub < 4; ++sub) x = fmaxf(x, fmaxf(sc[sub][n][i], sc[sub][n][i + 2]));
-                    x = fmaxf(x, __shfl_xor_sync(FULL, x, 4));
-                    x = fmaxf(x, __shfl_xor_sync(FULL, x, 8));
-                    x = fmaxf(x, __shfl_xor_sync(FULL, x, 16));
-                    mu[n][i] = x == -INFINITY ? 0.f : x;
-                    fac[n][i] = ex2(m[n][i] - mu[n][i]);
-                    moved |= x != m[n][i];
-                    m[n][i] = x;
-                    l[n][i] *= fac[n][i];
-                    fac[n][i] *= shrink;
-                }
-            if (__any_sync(FULL, moved)) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-#pragma unroll
-                    for (int k = 0; k < C::TILES; ++k)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[k][n][i] *= fac[n][i & 1];
-#pragma unroll
-                    for (int k = 0; k < GR; ++k)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) ones[k][n][i] *= fac[n][i & 1];
-                }
-            }
-            const float vup = pow2(14 - vexp);
-
-#pragma unroll
-            for (int sub = 0; sub < 4; ++sub) {
-                if (sub >= subs) break;
-                uint32_t sw0[GR], sw1[GR], vw[4][GR];
-                const uint32_t srow = stage + kv_scales_at(D) + (sub * 16 + g) * (D / 16);
-                lds_words<GR>(sw0, srow);
-                lds_words<GR>(sw1, srow + 8 * (D / 16));
-                const uint32_t turn = D == 64 ? g : D == 128 ? g ^ ((t4 >> 1) << 2) : g ^ (t4 << 1);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    lds_words<GR>(vw[j], stage + kv_values_at(D) + (sub * 16 + 4 * j + t4) * (D / 2) + turn * (D / 16));
-                const __half* s0 = reinterpret_cast<const __half*>(sw0);
-                const __half* s1 = reinterpret_cast<const __half*>(sw1);
-                const int key = key0 + sub * 16 + (g >> 1) + (g & 1) * 4;
-                float pr[NT][4];
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) pr[n][i] = ex2(sc[sub][n][i] - mu[n][i & 1]);
-                    l[n][0] += pr[n][0] + pr[n][2];
-                    l[n][1] += pr[n][1] + pr[n][3];
-                }
-#pragma unroll
-                for (int q = 0; q < GR; ++q) {
-                    float e0 = __half2float(s0[GR + q]) * vup, e1 = __half2float(s1[GR + q]) * vup;
-                    if (edge) {                   // what was never written may be anything
-                        if (key > hi_key) e0 = 0.f;
-                        if (key + 8 > hi_key) e1 = 0.f;
+                        for (int sub = 1; sub < 4; ++sub) x = fmaxf(x, fmaxf(sc[sub][n][i], sc[sub][n][i + 2]));
+                        x = fmaxf(x, __shfl_xor_sync(FULL, x, 4));
+                        x = fmaxf(x, __shfl_xor_sync(FULL, x, 8));
+                        x = fmaxf(x, __shfl_xor_sync(FULL, x, 16));
+                        x = fmaxf(x * f[n][i], m[n][i]);
+                        mnew[n][i] = x;
+                        mu[n][i] = x == -INFINITY ? 0.f : x;
+                        moved |= x != m[n][i];
                     }
-                    uint32_t b0[NT], b1[NT];
+                if (__any_sync(FULL, moved)) {
+                    const float shrink = pow2(vexp - vnew);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        b0[n] = transposed(half2_bits(pr[n][0] * e0, pr[n][1] * e0));
-                        b1[n] = transposed(half2_bits(pr[n][2] * e1, pr[n][3] * e1));
+                        float fac[2];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            fac[i] = ex2(m[n][i] - mu[n][i]);
+                            l[n][i] *= fac[i];
+                            fac[i] *= shrink;
+                            m[n][i] = mnew[n][i];
+                        }
+#pragma unroll
+                        for (int k = 0; k < C::TILES; ++k)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) acc[k][n][i] *= fac[i & 1];
+#pragma unroll
+                        for (int k = 0; k < GR; ++k)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) ones[k][n][i] *= fac[i & 1];
+                    }
+                    vexp = vnew;
+                }
+                const float vup = pow2(14 - vexp);
+
+#pragma unroll
+                for (int sub = 0; sub < 4; ++sub) {
+                    if (EDGE && sub >= subs) break;
+                    uint32_t sw0[GR], sw1[GR], vw[4][GR];
+                    const uint32_t srow = stage + sub * D + slane, vrow = stage + sub * 8 * D + vlane;
+                    lds_words<GR>(sw0, srow);
+                    lds_words<GR>(sw1, srow + D / 2);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) lds_words<GR>(vw[j], vrow + j * 2 * D);
+                    const __half* s0 = reinterpret_cast<const __half*>(sw0);
+                    const __half* s1 = reinterpret_cast<const __half*>(sw1);
+                    const int key = key0 + sub * 16 + (g >> 1) + (g & 1) * 4;
+                    float pr[NT][4];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) pr[n][i] = ex2(fmaf(sc[sub][n][i], f[n][i & 1], -mu[n][i & 1]));
+                        l[n][0] += pr[n][0] + pr[n][2];
+                        l[n][1] += pr[n][1] + pr[n][3];
                     }
 #pragma unroll
-                    for (int hf = 0; hf < 2; ++hf) {                     // dimensions 0..3 and 4..7 of the words
-                        // codes 0, 1 and (bytes swapped) 2, 3 of the half: two keys' side by side
-                        const uint32_t sel = hf ? 0x7632u : 0x5410u, swp = hf ? 0x6723u : 0x4501u;
-                        const uint32_t x0 = prmt(vw[0][q], vw[1][q], sel), x2 = prmt(vw[2][q], vw[3][q], sel);
-                        const uint32_t y0 = prmt(vw[0][q], vw[1][q], swp), y2 = prmt(vw[2][q], vw[3][q], swp);
+                    for (int q = 0; q < GR; ++q) {
+                        float e0 = __half2float(s0[GR + q]) * vup, e1 = __half2float(s1[GR + q]) * vup;
+                        if (EDGE) {               // what was never written may be anything
+                            if (key > hi_key) e0 = 0.f;
+                            if (key + 8 > hi_key) e1 = 0.f;
+                        }
+                        uint32_t b0[NT], b1[NT];
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            mma(acc[4 * q + 2 * hf][n], x0 << 4 & HIGH, y0 << 4 & HIGH, x2 << 4 & HIGH, y2 << 4 & HIGH, b0[n],
-                                b1[n]);
-                            mma(acc[4 * q + 2 * hf + 1][n], x0 & HIGH, y0 & HIGH, x2 & HIGH, y2 & HIGH, b0[n], b1[n]);
+                            b0[n] = transposed(half2_bits(pr[n][0] * e0, pr[n][1] * e0));
+                            b1[n] = transposed(half2_bits(pr[n][2] * e1, pr[n][3] * e1));
                         }
-                    }
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        mma(ones[q][n], 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, b0[n], b1[n]);
+                        for (int hf = 0; hf < 2; ++hf) {                 // dimensions 0..3 and 4..7 of the words
+                            // codes 0, 1 and (bytes swapped) 2, 3 of the half: two keys' side by side
+                            const uint32_t sel = hf ? 0x7632u : 0x5410u, swp = hf ? 0x6723u : 0x4501u;
+                            const uint32_t x0 = prmt(vw[0][q], vw[1][q], sel), x2 = prmt(vw[2][q], vw[3][q], sel);
+                            const uint32_t y0 = prmt(vw[0][q], vw[1][q], swp), y2 = prmt(vw[2][q], vw[3][q], swp);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) {
+                                mma(acc[4 * q + 2 * hf][n], x0 << 4 & HIGH, y0 << 4 & HIGH, x2 << 4 & HIGH, y2 << 4 & HIGH,
+                                    b0[n], b1[n]);
+                                mma(acc[4 * q + 2 * hf + 1][n], x0 & HIGH, y0 & HIGH, x2 & HIGH, y2 & HIGH, b0[n], b1[n]);
+                            }
+                        }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            mma(ones[q][n], 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, b0[n], b1[n]);
+                    }
                 }
-            }
+            };
+            if (key0 + KV_PAGE - 1 > close || key0 <= open)
+                page(std::true_type{});
+            else
+                page(std::false_type{});
         }
 
         // The warp's part of the segment, into the stage it has just read.
@@ -564,98 +624,92 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             }
         __syncthreads();
 
-        // Join the warps: a unit is 8 neighbouring dimensions of a row.
+        // Join the warps: a unit is 4 neighbouring dimensions of a row.
         const bool whole = s.start >= cur && s.start + s.pages <= end;
-        const int64_t slot = 2 * (int64_t)blockIdx.x + (s.start <= p0 ? 0 : 1);
+        const int64_t slot = aligned ? (int64_t)blockIdx.x : 2 * (int64_t)blockIdx.x + (s.start <= p0 ? 0 : 1);
+        const auto store = [&](int r, int dim, float4 v, float sum) {
+            const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;        // no keys: zeros; NaN stays
+            const __nv_bfloat162 x = __floats2bfloat162_rn(v.x * inv, v.y * inv), y = __floats2bfloat162_rn(v.z * inv, v.w * inv);
+            *reinterpret_cast<uint2*>(a.out + (((int64_t)s.b * a.rows + r / group) * a.heads + s.h * group + r % group) * D + dim) =
+                make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+        };
         for (int u = tid; u < C::UNITS; u += C::THREADS) {
-            const int par = u >> 5 & 1, n = (u >> 6) % NT, q = (u >> 6) / NT, ln = u & 31;
-            const int row = 8 * n + 2 * (ln & 3) + par;
-            float mx = -INFINITY, sum = 0.f, v[8] = {};
+            const int ln = u & 31, par = u >> 5 & 1, hf = u >> 6 & 1, n = (u >> 7) % NT, q = (u >> 7) / NT;
+            const int row = 8 * n + 2 * (ln & 3) + par, dim = 64 * q + 8 * (ln >> 2) + 4 * hf;
+            float mx = -INFINITY, sum = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < W; ++w) mx = fmaxf(mx, ml[w * C::ROWS + row].x);
-#pragma unroll
+#pragma unroll 4
             for (int w = 0; w < W; ++w) {
                 const float2 x = ml[w * C::ROWS + row];
                 if (x.y == 0.f) continue;
                 const float fw = ex2(x.x - mx);
                 sum = fmaf(x.y, fw, sum);
-                const float* buf = reinterpret_cast<const float*>(smem + (w * S + kept_in[w]) * C::BLOB);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int tile = 4 * q + (i >> 2) * 2 + (i & 1), hf = i >> 1 & 1;
-                    v[i] = fmaf(buf[((tile * NT + n) * 4 + 2 * hf + par) * 32 + ln], fw, v[i]);
-                }
+                // code i of a half-word is in row half i >> 1 of output tile i & 1
+                const float* buf = reinterpret_cast<const float*>(smem + (w * S + kept_in[w]) * C::BLOB) +
+                                   (((4 * q + 2 * hf) * NT + n) * 4 + par) * 32 + ln;
+                v.x = fmaf(buf[0], fw, v.x);
+                v.y = fmaf(buf[NT * 128], fw, v.y);
+                v.z = fmaf(buf[64], fw, v.z);
+                v.w = fmaf(buf[NT * 128 + 64], fw, v.w);
             }
             if (!whole) {
-                float4* o = reinterpret_cast<float4*>(parts + slot * C::PART) + 2 * u;
-                o[0] = make_float4(v[0], v[1], v[2], v[3]);
-                o[1] = make_float4(v[4], v[5], v[6], v[7]);
-                if (q == 0 && ln < 4) reinterpret_cast<float2*>(parts + slot * C::PART + C::ROWS * D)[row] = make_float2(mx, sum);
+                reinterpret_cast<float4*>(parts + slot * C::PART)[u] = v;
+                if (q == 0 && hf == 0 && ln < 4) reinterpret_cast<float2*>(parts + slot * C::PART + C::ROWS * D)[row] = make_float2(mx, sum);
                 continue;
             }
             const int r = s.rt * C::ROWS + row;
-            if (r >= rows_all) continue;
-            const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;     // no keys: zeros; NaN stays
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i] * inv, v[2 * i + 1] * inv);
-                w[i] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            *reinterpret_cast<uint4*>(a.out + (((int64_t)s.b * a.rows + r / group) * a.heads + s.h * group + r % group) * D +
-                                      64 * q + 8 * (ln >> 2)) = make_uint4(w[0], w[1], w[2], w[3]);
+            if (r < rows_all) store(r, dim, v, sum);
         }
         if (!whole) {
             // The last of the segment's blocks joins their parts, in order.
-            const int64_t b0 = s.start / quantum, b1 = (s.start + s.pages - 1) / quantum;
+            const int64_t b0 = aligned ? first_part : s.start / quantum;
+            const int n_parts = aligned ? parts_here : (int)((s.start + s.pages - 1) / quantum - b0) + 1;
             __threadfence();
             __syncthreads();
-            if (tid == 0) misc->last = atomicAdd(&counts[s.index], 1u) == (uint32_t)(b1 - b0);
+            if (tid == 0) misc->last = atomicAdd(&counts[s.index], 1u) == (uint32_t)(n_parts - 1);
             __syncthreads();
             if (misc->last) {
                 __threadfence();
                 if (tid == 0) counts[s.index] = 0;
-                // half a unit per thread, JOIN parts' loads in flight
-                for (int v = tid; v < 2 * C::UNITS; v += C::THREADS) {
-                    const int u = v >> 1, par = u >> 5 & 1, n = (u >> 6) % NT, q = (u >> 6) / NT, ln = u & 31;
-                    const int row = 8 * n + 2 * (ln & 3) + par;
+                for (int u = tid; u < C::UNITS; u += C::THREADS) {
+                    const int ln = u & 31, par = u >> 5 & 1, hf = u >> 6 & 1, n = (u >> 7) % NT, q = (u >> 7) / NT;
+                    const int row = 8 * n + 2 * (ln & 3) + par, dim = 64 * q + 8 * (ln >> 2) + 4 * hf;
                     const int r = s.rt * C::ROWS + row;
                     if (r >= rows_all) continue;
                     float mx = -INFINITY, sum = 0.f;
                     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int64_t k0 = b0; k0 <= b1; k0 += JOIN) {
+                    for (int k0 = 0; k0 < n_parts; k0 += JOIN) {         // JOIN parts' loads in flight
                         float2 x[JOIN];
                         float4 y[JOIN];
 #pragma unroll
                         for (int j = 0; j < JOIN; ++j) {
-                            const int64_t k = min(k0 + j, b1);
-                            const float* part = parts + (2 * k + (s.start <= k * quantum ? 0 : 1)) * C::PART;
+                            const int64_t k = b0 + min(k0 + j, n_parts - 1);
+                            const float* part = parts + (aligned ? k : 2 * k + (s.start <= k * quantum ? 0 : 1)) * C::PART;
                             x[j] = __ldcg(reinterpret_cast<const float2*>(part + C::ROWS * D) + row);
-                            y[j] = __ldcg(reinterpret_cast<const float4*>(part) + v);
-                            if (k0 + j > b1) x[j] = make_float2(-INFINITY, 0.f);
+                            y[j] = __ldcg(reinterpret_cast<const float4*>(part) + u);
                         }
                         float mn = mx;
 #pragma unroll
-                        for (int j = 0; j < JOIN; ++j) mn = fmaxf(mn, x[j].x);
+                        for (int j = 0; j < JOIN; ++j) {
+                            if (k0 + j >= n_parts) x[j] = make_float2(-INFINITY, 0.f);
+                            mn = fmaxf(mn, x[j].x);
+                        }
                         const float f0 = sum == 0.f ? 0.f : ex2(mx - mn);
                         mx = mn;
                         sum *= f0;
                         o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
 #pragma unroll
                         for (int j = 0; j < JOIN; ++j) {
-                            const float fj = x[j].y == 0.f ? 0.f : ex2(x[j].x - mn);
-                            if (x[j].y == 0.f) y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (x[j].y == 0.f) continue;                 // no keys: its vector may be anything
+                            const float fj = ex2(x[j].x - mn);
                             sum = fmaf(x[j].y, fj, sum);
                             o.x = fmaf(y[j].x, fj, o.x); o.y = fmaf(y[j].y, fj, o.y);
                             o.z = fmaf(y[j].z, fj, o.z); o.w = fmaf(y[j].w, fj, o.w);
                         }
                     }
-                    const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
-                    const __nv_bfloat162 h0 = __floats2bfloat162_rn(o.x * inv, o.y * inv),
-                                         h1 = __floats2bfloat162_rn(o.z * inv, o.w * inv);
-                    *reinterpret_cast<uint2*>(a.out + (((int64_t)s.b * a.rows + r / group) * a.heads + s.h * group + r % group) * D +
-                                              64 * q + 8 * (ln >> 2) + 4 * (v & 1)) =
-                        make_uint2(*reinterpret_cast<const uint32_t*>(&h0), *reinterpret_cast<const uint32_t*>(&h1));
+                    store(r, dim, o, sum);
                 }
             }
         }
