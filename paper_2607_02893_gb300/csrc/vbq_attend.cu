@@ -42,8 +42,6 @@
 // segments form one list that is cut evenly, and a block may finish one segment
 // and start another. Parts are joined through the workspace by the block that
 // finishes a segment last, in block order, so results do not depend on timing.
-#include <type_traits>
-
 #include <cuda_bf16.h>
 
 #include "vbq_decode.h"
@@ -53,7 +51,7 @@ namespace vbq {
 namespace {
 
 constexpr uint32_t FULL = 0xffffffffu;
-constexpr int JOIN = 10;
+constexpr int JOIN = 8;                         // parts whose loads are in flight at once
 constexpr int CUT = 6;                           // pages a block takes at least of a segment that is cut
 constexpr int STRADDLE = 16;                     // pages whose time a block's second segment costs
 constexpr uint32_t LOW = 0x003c003cu, HIGH = 0x03c003c0u;    // codes at bits 2..5 and 6..9 of each half
@@ -72,7 +70,9 @@ struct Shape {
     // shared memory
     static constexpr int BARS = W * S * BLOB;                    // full barriers
     static constexpr int ML = BARS + W * S * 8;                  // (maximum, sum) per warp and row
-    static constexpr int CUM = ML + W * ROWS * 8;                // pages before each sequence
+    static constexpr int FACTOR = ML + W * ROWS * 8;             // a warp's factor per row, then (maximum, sum) per row
+    static constexpr int CUM = FACTOR + W * ROWS * 4 + ROWS * 8; // pages before each sequence
+    static_assert(W <= 16 && ROWS * 16 <= THREADS, "the join's first step");
     static constexpr int SPAN = CUM + (KV_MAX_BATCH + 2) * 8;    // first page and last key of each sequence
     static constexpr int MISC = SPAN + KV_MAX_BATCH * 8;
     static constexpr int SMEM = MISC + 64 + 4 * W;
@@ -143,7 +143,7 @@ struct List {
         s.index = (int64_t)b * per_seq + k;
         return s;
     }
-    __device__ Segment at(int64_t p) const {     // of a page of the list
+    __device__ __noinline__ Segment at(int64_t p) const {     // of a page of the list
         int b = 0, e = batch;                    // the last b with cum[b] * per_seq <= p (it has pages: p is in the list)
         while (e - b > 1) {
             const int m = (b + e) >> 1;
@@ -170,10 +170,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     const uint32_t klane = g * (D / 2) + t4 * (D / 8), slane = kv_scales_at(D) + g * (D / 16);
     const uint32_t vlane = kv_values_at(D) + t4 * (D / 2) + (D == 64 ? g : D == 128 ? g ^ ((t4 >> 1) << 2) : g ^ (t4 << 1)) * (D / 16);
     float2* ml = reinterpret_cast<float2*>(smem + C::ML);
+    float* factor = reinterpret_cast<float*>(smem + C::FACTOR);
+    float2* joined = reinterpret_cast<float2*>(smem + C::FACTOR + W * C::ROWS * 4);
     int64_t* cum = reinterpret_cast<int64_t*>(smem + C::CUM);
     int2* span = reinterpret_cast<int2*>(smem + C::SPAN);
     Misc* misc = reinterpret_cast<Misc*>(smem + C::MISC);
-    int* kept_in = reinterpret_cast<int*>(smem + C::MISC + 64);          // the stage a warp's partial result is in
+    int* kept_in = reinterpret_cast<int*>(smem + C::MISC + 64);          // where a warp's partial result is
     const uint32_t abort_addr = sbase + C::MISC + 8;
     const int group = a.heads / c.kv_heads, rows_all = group * a.rows, per_seq = row_tiles * c.kv_heads;
 
@@ -188,8 +190,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
 
     // Every sequence's range of pages.
     const int64_t table_keys = (int64_t)c.table_pages * KV_PAGE;
+#pragma unroll 1
     for (int b = tid; b < a.batch; b += C::THREADS) {
         int hi = -1, mn = 0x7fffffff;
+#pragma unroll 1
         for (int t = 0; t < a.rows; ++t) {
             const int p = a.pos[b * a.rows + t];
             hi = max(hi, p);
@@ -209,6 +213,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     if (warp == 0) {
         int64_t before = 0;
         int most = 0, used = 0;                   // sequences with pages
+#pragma unroll 1
         for (int b0 = 0; b0 < a.batch; b0 += 32) {
             const int b = b0 + lane;
             int64_t x = b < a.batch ? cum[b + 1] : 0;
@@ -228,7 +233,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
         // An even share of the pages; segments that a block's warps take at once are not cut, and none into parts
         // that cost more to join than to read.
         const int blocks = (int)gridDim.x, least = most <= W ? most : CUT;
-        const int64_t even = max((before * per_seq + blocks - 1) / blocks, (int64_t)max(least, 1));
+        const int64_t total = before * per_seq;
+        const int64_t share_up = total < (1 << 30) ? (int64_t)(((uint32_t)total + blocks - 1) / (uint32_t)blocks)
+                                                   : (total + blocks - 1) / blocks;
+        const int64_t even = max(share_up, (int64_t)max(least, 1));
         // One part per block: parts of at most q pages, the least of a few q that fit.
         const int64_t segments = (int64_t)used * per_seq;
         int aligned = 0;
@@ -236,9 +244,11 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
         if (segments <= blocks && used > 0) {
             const int share = blocks / (int)segments;      // parts each: always fits
             int fit = max((most + share - 1) / share, least), low = (int)even;
+#pragma unroll 1
             for (int i = 0; i < 5 && low < fit; ++i) {
                 const int q = (low + fit) / 2;
                 uint32_t n = 0;
+#pragma unroll 1
                 for (int b = lane; b < a.batch; b += 32) n += parts_of(cum[b + 1] - cum[b], q);
                 n = __reduce_add_sync(FULL, n);
                 if ((int64_t)n * per_seq <= blocks) fit = q; else low = q + 1;
@@ -262,6 +272,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     Segment s = {};
     if (aligned) {
         int left = blockIdx.x;
+#pragma unroll 1
         for (int b = 0; b < a.batch; ++b) {
             const int64_t pages = cum[b + 1] - cum[b];
             const int n = parts_of(pages, quantum);
@@ -285,17 +296,19 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     }
 
     // Sequences without keys: zeros.
+#pragma unroll 1
     for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
         if (cum[b + 1] != cum[b]) continue;
         uint4* o = reinterpret_cast<uint4*>(a.out + (int64_t)b * a.rows * a.heads * D);
+#pragma unroll 1
         for (int64_t i = tid; i < (int64_t)a.rows * a.heads * (D / 8); i += C::THREADS) o[i] = make_uint4(0, 0, 0, 0);
     }
 
-    // The warp's own pages: p0 + warp, + W, ...; the k-th uses stage k % S.
+    // The block's pages go round the warps: p0 + warp, + W, ...; the k-th of a warp uses stage k % S.
+    const uint32_t n_pages = (uint32_t)(p1 - p0), mine = n_pages / W + ((uint32_t)warp < n_pages % W);
     const uint8_t* src = nullptr;                 // lane i: of the page 32 * n + i
     uint32_t issued = 0, used = 0, landed = 0;    // landed: copies waited for
     bool ok = true;
-    const uint32_t mine = p1 - p0 > warp ? (uint32_t)((uint64_t)(p1 - p0 - warp + W - 1) / W) : 0;
     auto issue = [&]() {                          // the next page's copy
         if (issued >= mine || !ok) return;
         if ((issued & 31) == 0) {
@@ -316,29 +329,52 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             bulk_load(sbase + (warp * S + st) * C::BLOB, src, C::BLOB, sbase + C::BARS + 8 * (warp * S + st));
         ++issued;
     };
+    // A segment's queries (16 bytes of each word of the lane's row) and, per accumulator column, its rows' positions.
+    uint4 qw[NT][KW];
+    int pos[NT][2];
+    const auto load_rows = [&] {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int r = s.rt * C::ROWS + 8 * n + g;
+            const bool live = r < rows_all;
+            const int t = live ? r / group : 0, hq = live ? s.h * group + r - t * group : 0;
+            const uint16_t* q = a.q + (((int64_t)s.b * a.rows + t) * a.heads + hq) * D + 8 * t4;
+#pragma unroll
+            for (int j = 0; j < KW; ++j)
+                qw[n][j] = live ? *reinterpret_cast<const uint4*>(q + 64 * (j / 2) + 32 * (j & 1)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int rc = s.rt * C::ROWS + 8 * n + 2 * t4 + i;
+                pos[n][i] = rc < rows_all ? a.pos[s.b * a.rows + rc / group] : 0x7fffffff;
+            }
+        }
+    };
+    if (p0 < p1 && warp == 0) {                   // the first queries, before the copies: behind them they would wait
+        const int r = s.rt * C::ROWS + lane % C::ROWS;
+        if (r < rows_all) {
+            const uint16_t* q = a.q + (((int64_t)s.b * a.rows + r / group) * a.heads + s.h * group + r % group) * D;
+            for (int i = lane / C::ROWS; i < D / 64; i += 32 / C::ROWS) asm volatile("prefetch.global.L1 [%0];" :: "l"(q + 64 * i));
+        }
+    }
+#pragma unroll 1
     for (int i = 0; i < S; ++i) issue();
 
+#pragma unroll 1
     for (int64_t cur = p0; cur < p1;) {
         if (cur != p0) s = list.at(cur);
+        load_rows();
         const int64_t end = min(p1, s.start + s.pages);
         const int hi_key = span[s.b].y, page0 = span[s.b].x;             // the sequence's last key and first page
 
         // Query fragments of the tile's rows, and the rows' parameters per accumulator column.
         uint32_t qb[NT][KW][4];
         float corr[NT][GR][2], f[NT][2];
-        int pos[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int r = s.rt * C::ROWS + 8 * n + g;
-            const bool live = r < rows_all;
-            const int t = live ? r / group : 0, hq = live ? s.h * group + r % group : 0;
-            const uint16_t* q = a.q + (((int64_t)s.b * a.rows + t) * a.heads + hq) * D;
-            uint4 w[KW];
             uint32_t top = 0;
 #pragma unroll
             for (int j = 0; j < KW; ++j) {
-                w[j] = live ? *reinterpret_cast<const uint4*>(q + 64 * (j / 2) + 32 * (j & 1) + 8 * t4) : make_uint4(0, 0, 0, 0);
-                const uint32_t v[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+                const uint32_t v[4] = {qw[n][j].x, qw[n][j].y, qw[n][j].z, qw[n][j].w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = max(top, max(v[i] << 16 & 0x7fff0000u, v[i] & 0x7fff0000u));
             }
@@ -353,7 +389,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             for (int i = 0; i < GR; ++i) sum[i] = 0.f;
 #pragma unroll
             for (int j = 0; j < KW; ++j) {
-                const uint32_t v[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+                const uint32_t v[4] = {qw[n][j].x, qw[n][j].y, qw[n][j].z, qw[n][j].w};
                 float x[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -377,11 +413,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             }
             f[n][0] = __shfl_sync(FULL, fr, 8 * t4);
             f[n][1] = __shfl_sync(FULL, fr, 8 * t4 + 4);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int rc = s.rt * C::ROWS + 8 * n + 2 * t4 + i;
-                pos[n][i] = rc < rows_all ? a.pos[s.b * a.rows + rc / group] : 0x7fffffff;
-            }
         }
         // Keys that every row of the tile attends to: (open, close].
         int close = 0x7fffffff, open = -1;
@@ -412,10 +443,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
         int vexp = -13;                           // value scales are taken in units of 2^(vexp - 14)
         bool any = false;
 
-        // The warp's pages of the segment, from the segment's first.
-        const int in_end = (int)(end - s.start);
+        const int in_end = (int)(end - s.start);                         // pages from the segment's first
+#pragma unroll 1
         for (int in = (int)(p0 + warp + (int64_t)used * W - s.start); in < in_end; in += W) {
-            if (any) { __syncwarp(); issue(); }   // into the stage of the page before
             any = true;
             const int st = (int)(used % S);
             const uint32_t stage = sbase + (warp * S + st) * C::BLOB;
@@ -424,193 +454,195 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
                 ok = false;
             }
             ++used;
-            if (!ok) continue;
+            if (!ok) break;
             landed = used;
             const int key0 = (page0 + in) * KV_PAGE;
-            const auto page = [&](auto is_edge) {                        // is_edge: some row does not attend to all of it
-                constexpr bool EDGE = decltype(is_edge)::value;
-                const int subs = EDGE ? min(4, (hi_key - key0) / 16 + 1) : 4;
-                float sc[4][NT][4];
-                __half2 vtop = __float2half2_rn(0.f);
+            float sc[4][NT][4];
+            uint32_t vs[4][2][(GR + 1) / 2];      // the value scales of the lane's two keys, in pairs of groups
 #pragma unroll
-                for (int sub = 0; sub < 4; ++sub) {
-                    if (EDGE && sub >= subs) {
+            for (int sub = 0; sub < 4; ++sub) {
+                uint32_t k0[KW], k1[KW], sw0[GR], sw1[GR];               // keys g and g + 8 (in row order), their scales
+                const uint32_t krow = stage + sub * 8 * D + klane, srow = stage + sub * D + slane;
+                lds_words<KW>(k0, krow);
+                lds_words<KW>(k1, krow + 4 * D);
+                lds_words<GR>(sw0, srow);
+                lds_words<GR>(sw1, srow + D / 2);
+                const __half* s0 = reinterpret_cast<const __half*>(sw0);
+                const __half* s1 = reinterpret_cast<const __half*>(sw1);
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
+                for (int q = 0; q < GR; ++q) {
+                    float d[NT][4];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) sc[sub][n][i] = -INFINITY;
-                        continue;
+                    for (int n = 0; n < NT; ++n) {
+                        d[n][0] = d[n][2] = corr[n][q][0];
+                        d[n][1] = d[n][3] = corr[n][q][1];
                     }
-                    uint32_t k0[KW], k1[KW], sw0[GR], sw1[GR];           // keys g and g + 8 (in row order), their scales
-                    const uint32_t krow = stage + sub * 8 * D + klane, srow = stage + sub * D + slane;
-                    lds_words<KW>(k0, krow);
-                    lds_words<KW>(k1, krow + 4 * D);
-                    lds_words<GR>(sw0, srow);
-                    lds_words<GR>(sw1, srow + D / 2);
-                    const __half* s0 = reinterpret_cast<const __half*>(sw0);
-                    const __half* s1 = reinterpret_cast<const __half*>(sw1);
 #pragma unroll
-                    for (int q = 0; q < GR; ++q) {
-                        float d[NT][4];
+                    for (int j = 2 * q; j < 2 * q + 2; ++j) {
+                        const uint32_t x0 = k0[j], x1 = k1[j], y0 = prmt(x0, 0, 0x2301), y1 = prmt(x1, 0, 0x2301);
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            d[n][0] = d[n][2] = corr[n][q][0];
-                            d[n][1] = d[n][3] = corr[n][q][1];
+                            mma(d[n], x0 & LOW, x1 & LOW, x0 & HIGH, x1 & HIGH, qb[n][j][0], qb[n][j][1]);
+                            mma(d[n], y0 & LOW, y1 & LOW, y0 & HIGH, y1 & HIGH, qb[n][j][2], qb[n][j][3]);
                         }
-#pragma unroll
-                        for (int j = 2 * q; j < 2 * q + 2; ++j) {
-                            const uint32_t x0 = k0[j], x1 = k1[j], y0 = prmt(x0, 0, 0x2301), y1 = prmt(x1, 0, 0x2301);
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) {
-                                mma(d[n], x0 & LOW, x1 & LOW, x0 & HIGH, x1 & HIGH, qb[n][j][0], qb[n][j][1]);
-                                mma(d[n], y0 & LOW, y1 & LOW, y0 & HIGH, y1 & HIGH, qb[n][j][2], qb[n][j][3]);
-                            }
-                        }
-                        const float e0 = __half2float(s0[q]), e1 = __half2float(s1[q]);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                sc[sub][n][i] = q == 0 ? d[n][i] * (i < 2 ? e0 : e1) : fmaf(d[n][i], i < 2 ? e0 : e1, sc[sub][n][i]);
                     }
-                    const int key = key0 + sub * 16 + (g >> 1) + (g & 1) * 4;
-                    if (EDGE) {
+                    const float e0 = __half2float(s0[q]), e1 = __half2float(s1[q]);
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int k = key + (i >> 1) * 8, p_ = pos[n][i & 1];
-                                if (k > p_ || k > hi_key || (a.window > 0 && k <= p_ - a.window)) sc[sub][n][i] = -INFINITY;
-                            }
-                    }
-                    // the largest value scale among keys that exist
+                        for (int i = 0; i < 4; ++i)
+                            sc[sub][n][i] = q == 0 ? d[n][i] * (i < 2 ? e0 : e1) : fmaf(d[n][i], i < 2 ? e0 : e1, sc[sub][n][i]);
+                }
+                if constexpr (GR == 1) {          // key scale, value scale
+                    vs[sub][0][0] = sw0[0] >> 16;
+                    vs[sub][1][0] = sw1[0] >> 16;
+                } else {
 #pragma unroll
-                    for (int q = 0; q < GR; ++q) {
-                        const __half z = __float2half(0.f);
-                        vtop = __hmax2(vtop, __halves2half2(EDGE && key > hi_key ? z : s0[GR + q],
-                                                            EDGE && key + 8 > hi_key ? z : s1[GR + q]));
+                    for (int q = 0; q < GR / 2; ++q) {
+                        vs[sub][0][q] = sw0[GR / 2 + q];
+                        vs[sub][1][q] = sw1[GR / 2 + q];
                     }
                 }
-
-                // Running maximum per row, running power of two of the value scales.
-                const uint32_t vb = __reduce_max_sync(
-                    FULL, max((uint32_t)__half_as_ushort(__low2half(vtop)), (uint32_t)__half_as_ushort(__high2half(vtop))));
-                const int vnew = max(vexp, max((int)(vb >> 10), 1) - 14);            // scales below 2^vnew
-                bool moved = vnew != vexp;
-                float mnew[NT][2], mu[NT][2];
+            }
+            if (key0 + KV_PAGE - 1 > close || key0 <= open) {            // some row does not attend to all of the page
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int sub = 0; sub < 4; ++sub)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int key = key0 + sub * 16 + (g >> 1) + (g & 1) * 4 + 8 * x;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+                                if (key > min(pos[n][i], hi_key) || (a.window > 0 && key <= pos[n][i] - a.window))
+                                    sc[sub][n][2 * x + i] = -INFINITY;
+                        if (key > hi_key)         // what was never written may be anything
+#pragma unroll
+                            for (int q = 0; q < (GR + 1) / 2; ++q) vs[sub][x][q] = 0;
+                    }
+            }
+
+            // Running maximum per row, running power of two of the value scales.
+            __half2 vtop = *reinterpret_cast<const __half2*>(&vs[0][0][0]);
+#pragma unroll
+            for (int sub = 0; sub < 4; ++sub)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int q = 0; q < (GR + 1) / 2; ++q) vtop = __hmax2(vtop, *reinterpret_cast<const __half2*>(&vs[sub][x][q]));
+            const uint32_t vb = __reduce_max_sync(
+                FULL, max((uint32_t)__half_as_ushort(__low2half(vtop)), (uint32_t)__half_as_ushort(__high2half(vtop))));
+            const int vnew = max(vexp, max((int)(vb >> 10), 1) - 14);    // scales below 2^vnew
+            bool moved = vnew != vexp;
+            float mnew[NT][2], mu[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float x = fmaxf(sc[0][n][i], sc[0][n][i + 2]);
+#pragma unroll
+                    for (int sub = 1; sub < 4; ++sub) x = fmaxf(x, fmaxf(sc[sub][n][i], sc[sub][n][i + 2]));
+                    x = fmaxf(x, __shfl_xor_sync(FULL, x, 4));
+                    x = fmaxf(x, __shfl_xor_sync(FULL, x, 8));
+                    x = fmaxf(x, __shfl_xor_sync(FULL, x, 16));
+                    x = fmaxf(x * f[n][i], m[n][i]);
+                    mnew[n][i] = x;
+                    mu[n][i] = x == -INFINITY ? 0.f : x;
+                    moved |= x != m[n][i];
+                }
+            if (__any_sync(FULL, moved)) {
+                const float shrink = pow2(vexp - vnew);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float fac[2];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        float x = fmaxf(sc[0][n][i], sc[0][n][i + 2]);
-#pragma unroll
-                        for (int sub = 1; sub < 4; ++sub) x = fmaxf(x, fmaxf(sc[sub][n][i], sc[sub][n][i + 2]));
-                        x = fmaxf(x, __shfl_xor_sync(FULL, x, 4));
-                        x = fmaxf(x, __shfl_xor_sync(FULL, x, 8));
-                        x = fmaxf(x, __shfl_xor_sync(FULL, x, 16));
-                        x = fmaxf(x * f[n][i], m[n][i]);
-                        mnew[n][i] = x;
-                        mu[n][i] = x == -INFINITY ? 0.f : x;
-                        moved |= x != m[n][i];
+                        fac[i] = ex2(m[n][i] - mu[n][i]);
+                        l[n][i] *= fac[i];
+                        fac[i] *= shrink;
+                        m[n][i] = mnew[n][i];
                     }
-                if (__any_sync(FULL, moved)) {
-                    const float shrink = pow2(vexp - vnew);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        float fac[2];
+                    for (int k = 0; k < C::TILES; ++k)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            fac[i] = ex2(m[n][i] - mu[n][i]);
-                            l[n][i] *= fac[i];
-                            fac[i] *= shrink;
-                            m[n][i] = mnew[n][i];
-                        }
+                        for (int i = 0; i < 4; ++i) acc[k][n][i] *= fac[i & 1];
 #pragma unroll
-                        for (int k = 0; k < C::TILES; ++k)
+                    for (int k = 0; k < GR; ++k)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) acc[k][n][i] *= fac[i & 1];
-#pragma unroll
-                        for (int k = 0; k < GR; ++k)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) ones[k][n][i] *= fac[i & 1];
-                    }
-                    vexp = vnew;
+                        for (int i = 0; i < 4; ++i) ones[k][n][i] *= fac[i & 1];
                 }
-                const float vup = pow2(14 - vexp);
+                vexp = vnew;
+            }
+            const float vup = pow2(14 - vexp);
 
 #pragma unroll
-                for (int sub = 0; sub < 4; ++sub) {
-                    if (EDGE && sub >= subs) break;
-                    uint32_t sw0[GR], sw1[GR], vw[4][GR];
-                    const uint32_t srow = stage + sub * D + slane, vrow = stage + sub * 8 * D + vlane;
-                    lds_words<GR>(sw0, srow);
-                    lds_words<GR>(sw1, srow + D / 2);
+            for (int sub = 0; sub < 4; ++sub) {
+                uint32_t vw[4][GR];
+                const uint32_t vrow = stage + sub * 8 * D + vlane;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) lds_words<GR>(vw[j], vrow + j * 2 * D);
-                    const __half* s0 = reinterpret_cast<const __half*>(sw0);
-                    const __half* s1 = reinterpret_cast<const __half*>(sw1);
-                    const int key = key0 + sub * 16 + (g >> 1) + (g & 1) * 4;
-                    float pr[NT][4];
+                for (int j = 0; j < 4; ++j) lds_words<GR>(vw[j], vrow + j * 2 * D);
+                float pr[NT][4];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pr[n][i] = ex2(fmaf(sc[sub][n][i], f[n][i & 1], -mu[n][i & 1]));
+                    l[n][0] += pr[n][0] + pr[n][2];
+                    l[n][1] += pr[n][1] + pr[n][3];
+                }
+#pragma unroll
+                for (int q = 0; q < GR; ++q) {
+                    const float e0 = __half2float(reinterpret_cast<const __half*>(vs[sub][0])[q]) * vup,
+                                e1 = __half2float(reinterpret_cast<const __half*>(vs[sub][1])[q]) * vup;
+                    uint32_t b0[NT], b1[NT];
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) pr[n][i] = ex2(fmaf(sc[sub][n][i], f[n][i & 1], -mu[n][i & 1]));
-                        l[n][0] += pr[n][0] + pr[n][2];
-                        l[n][1] += pr[n][1] + pr[n][3];
+                        b0[n] = transposed(half2_bits(pr[n][0] * e0, pr[n][1] * e0));
+                        b1[n] = transposed(half2_bits(pr[n][2] * e1, pr[n][3] * e1));
                     }
 #pragma unroll
-                    for (int q = 0; q < GR; ++q) {
-                        float e0 = __half2float(s0[GR + q]) * vup, e1 = __half2float(s1[GR + q]) * vup;
-                        if (EDGE) {               // what was never written may be anything
-                            if (key > hi_key) e0 = 0.f;
-                            if (key + 8 > hi_key) e1 = 0.f;
-                        }
-                        uint32_t b0[NT], b1[NT];
+                    for (int hf = 0; hf < 2; ++hf) {                     // dimensions 0..3 and 4..7 of the words
+                        // codes 0, 1 and (bytes swapped) 2, 3 of the half: two keys' side by side
+                        const uint32_t sel = hf ? 0x7632u : 0x5410u, swp = hf ? 0x6723u : 0x4501u;
+                        const uint32_t x0 = prmt(vw[0][q], vw[1][q], sel), x2 = prmt(vw[2][q], vw[3][q], sel);
+                        const uint32_t y0 = prmt(vw[0][q], vw[1][q], swp), y2 = prmt(vw[2][q], vw[3][q], swp);
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            b0[n] = transposed(half2_bits(pr[n][0] * e0, pr[n][1] * e0));
-                            b1[n] = transposed(half2_bits(pr[n][2] * e1, pr[n][3] * e1));
+                            mma(acc[4 * q + 2 * hf][n], x0 << 4 & HIGH, y0 << 4 & HIGH, x2 << 4 & HIGH, y2 << 4 & HIGH,
+                                b0[n], b1[n]);
+                            mma(acc[4 * q + 2 * hf + 1][n], x0 & HIGH, y0 & HIGH, x2 & HIGH, y2 & HIGH, b0[n], b1[n]);
                         }
-#pragma unroll
-                        for (int hf = 0; hf < 2; ++hf) {                 // dimensions 0..3 and 4..7 of the words
-                            // codes 0, 1 and (bytes swapped) 2, 3 of the half: two keys' side by side
-                            const uint32_t sel = hf ? 0x7632u : 0x5410u, swp = hf ? 0x6723u : 0x4501u;
-                            const uint32_t x0 = prmt(vw[0][q], vw[1][q], sel), x2 = prmt(vw[2][q], vw[3][q], sel);
-                            const uint32_t y0 = prmt(vw[0][q], vw[1][q], swp), y2 = prmt(vw[2][q], vw[3][q], swp);
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) {
-                                mma(acc[4 * q + 2 * hf][n], x0 << 4 & HIGH, y0 << 4 & HIGH, x2 << 4 & HIGH, y2 << 4 & HIGH,
-                                    b0[n], b1[n]);
-                                mma(acc[4 * q + 2 * hf + 1][n], x0 & HIGH, y0 & HIGH, x2 & HIGH, y2 & HIGH, b0[n], b1[n]);
-                            }
-                        }
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            mma(ones[q][n], 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, b0[n], b1[n]);
                     }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        mma(ones[q][n], 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, b0[n], b1[n]);
                 }
-            };
-            if (key0 + KV_PAGE - 1 > close || key0 <= open)
-                page(std::true_type{});
-            else
-                page(std::false_type{});
+            }
+            if (in + W < in_end) {                // refill the stage; the last of the segment is still needed
+                __syncwarp();
+                issue();
+            }
         }
 
         // The warp's part of the segment, into the stage it has just read.
+        if (!any && lane == 0) kept_in[warp] = -1;
         if (any) {
             const int st = (int)((used - 1) % S);
-            float* buf = reinterpret_cast<float*>(smem + (warp * S + st) * C::BLOB);
+            float4* buf = reinterpret_cast<float4*>(smem + (warp * S + st) * C::BLOB);
             const float down = pow2(vexp - 14);
             __syncwarp();
 #pragma unroll
-            for (int k = 0; k < C::TILES; ++k)
+            for (int k = 0; k < C::TILES; k += 2)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        buf[((k * NT + n) * 4 + i) * 32 + lane] =
-                            (acc[k][n][i] * 0x1p18f - 8.f * ones[k / 4][n][i]) * down;
-            if (lane == 0) kept_in[warp] = st;
+                    for (int par = 0; par < 2; ++par) {
+                        // dimensions 8 g + 0..3 of a group from tiles 4 q and 4 q + 1, 4..7 from the next two
+                        const float z = 8.f * ones[k / 4][n][par];
+                        buf[((k / 2 * NT + n) * 2 + par) * 32 + lane] =
+                            make_float4((acc[k][n][par] * 0x1p18f - z) * down, (acc[k + 1][n][par] * 0x1p18f - z) * down,
+                                        (acc[k][n][2 + par] * 0x1p18f - z) * down, (acc[k + 1][n][2 + par] * 0x1p18f - z) * down);
+                    }
+            if (lane == 0) kept_in[warp] = (warp * S + st) * C::BLOB;
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -624,7 +656,27 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             }
         __syncthreads();
 
-        // Join the warps: a unit is 4 neighbouring dimensions of a row.
+        // Join the warps: first each warp's factor per row (16 lanes a row), then the rows, by units of 4 neighbouring
+        // dimensions.
+        {
+            const int row = (tid >> 4) % C::ROWS, w = tid & 15;
+            float2 x = ml[min(w, W - 1) * C::ROWS + row];
+            if (w >= W) x = make_float2(-INFINITY, 0.f);
+            float mx = x.x;
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, o));
+            const float fw = x.y == 0.f ? 0.f : ex2(x.x - mx);
+            float sum = x.y == 0.f ? 0.f : x.y * fw;
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor_sync(FULL, sum, o);
+            if (tid < 16 * C::ROWS && w < W) factor[w * C::ROWS + row] = fw;
+            if (tid < 16 * C::ROWS && w == 0) joined[row] = make_float2(mx, sum);
+            // a warp without pages: another's values, times 0
+            const int at = w < W ? kept_in[w] : -1, some = __reduce_max_sync(FULL, at);
+            __syncthreads();
+            if (tid < W && at < 0) kept_in[w] = some;
+        }
+        __syncthreads();
         const bool whole = s.start >= cur && s.start + s.pages <= end;
         const int64_t slot = aligned ? (int64_t)blockIdx.x : 2 * (int64_t)blockIdx.x + (s.start <= p0 ? 0 : 1);
         const auto store = [&](int r, int dim, float4 v, float sum) {
@@ -633,34 +685,27 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             *reinterpret_cast<uint2*>(a.out + (((int64_t)s.b * a.rows + r / group) * a.heads + s.h * group + r % group) * D + dim) =
                 make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
         };
+#pragma unroll 1
         for (int u = tid; u < C::UNITS; u += C::THREADS) {
-            const int ln = u & 31, par = u >> 5 & 1, hf = u >> 6 & 1, n = (u >> 7) % NT, q = (u >> 7) / NT;
-            const int row = 8 * n + 2 * (ln & 3) + par, dim = 64 * q + 8 * (ln >> 2) + 4 * hf;
-            float mx = -INFINITY, sum = 0.f;
+            const int ln = u & 31, par = u >> 5 & 1, n = (u >> 6) % NT, qh = (u >> 6) / NT;
+            const int row = 8 * n + 2 * (ln & 3) + par, dim = 64 * (qh >> 1) + 8 * (ln >> 2) + 4 * (qh & 1);
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int w = 0; w < W; ++w) mx = fmaxf(mx, ml[w * C::ROWS + row].x);
-#pragma unroll 4
             for (int w = 0; w < W; ++w) {
-                const float2 x = ml[w * C::ROWS + row];
-                if (x.y == 0.f) continue;
-                const float fw = ex2(x.x - mx);
-                sum = fmaf(x.y, fw, sum);
-                // code i of a half-word is in row half i >> 1 of output tile i & 1
-                const float* buf = reinterpret_cast<const float*>(smem + (w * S + kept_in[w]) * C::BLOB) +
-                                   (((4 * q + 2 * hf) * NT + n) * 4 + par) * 32 + ln;
-                v.x = fmaf(buf[0], fw, v.x);
-                v.y = fmaf(buf[NT * 128], fw, v.y);
-                v.z = fmaf(buf[64], fw, v.z);
-                v.w = fmaf(buf[NT * 128 + 64], fw, v.w);
+                const float fw = factor[w * C::ROWS + row];
+                const float4 y = reinterpret_cast<const float4*>(smem + kept_in[w])[u];
+                v.x = fmaf(y.x, fw, v.x);
+                v.y = fmaf(y.y, fw, v.y);
+                v.z = fmaf(y.z, fw, v.z);
+                v.w = fmaf(y.w, fw, v.w);
             }
             if (!whole) {
                 reinterpret_cast<float4*>(parts + slot * C::PART)[u] = v;
-                if (q == 0 && hf == 0 && ln < 4) reinterpret_cast<float2*>(parts + slot * C::PART + C::ROWS * D)[row] = make_float2(mx, sum);
+                if (qh == 0 && ln < 4) reinterpret_cast<float2*>(parts + slot * C::PART + C::ROWS * D)[row] = joined[row];
                 continue;
             }
             const int r = s.rt * C::ROWS + row;
-            if (r < rows_all) store(r, dim, v, sum);
+            if (r < rows_all) store(r, dim, v, joined[row].y);
         }
         if (!whole) {
             // The last of the segment's blocks joins their parts, in order.
@@ -673,13 +718,15 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             if (misc->last) {
                 __threadfence();
                 if (tid == 0) counts[s.index] = 0;
-                for (int u = tid; u < C::UNITS; u += C::THREADS) {
-                    const int ln = u & 31, par = u >> 5 & 1, hf = u >> 6 & 1, n = (u >> 7) % NT, q = (u >> 7) / NT;
-                    const int row = 8 * n + 2 * (ln & 3) + par, dim = 64 * q + 8 * (ln >> 2) + 4 * hf;
+#pragma unroll 1
+        for (int u = tid; u < C::UNITS; u += C::THREADS) {
+                    const int ln = u & 31, par = u >> 5 & 1, n = (u >> 6) % NT, qh = (u >> 6) / NT;
+                    const int row = 8 * n + 2 * (ln & 3) + par, dim = 64 * (qh >> 1) + 8 * (ln >> 2) + 4 * (qh & 1);
                     const int r = s.rt * C::ROWS + row;
                     if (r >= rows_all) continue;
                     float mx = -INFINITY, sum = 0.f;
                     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
                     for (int k0 = 0; k0 < n_parts; k0 += JOIN) {         // JOIN parts' loads in flight
                         float2 x[JOIN];
                         float4 y[JOIN];
@@ -689,11 +736,11 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
                             const float* part = parts + (aligned ? k : 2 * k + (s.start <= k * quantum ? 0 : 1)) * C::PART;
                             x[j] = __ldcg(reinterpret_cast<const float2*>(part + C::ROWS * D) + row);
                             y[j] = __ldcg(reinterpret_cast<const float4*>(part) + u);
+                            if (k0 + j >= n_parts) x[j] = make_float2(-INFINITY, 0.f);
                         }
                         float mn = mx;
 #pragma unroll
                         for (int j = 0; j < JOIN; ++j) {
-                            if (k0 + j >= n_parts) x[j] = make_float2(-INFINITY, 0.f);
                             mn = fmaxf(mn, x[j].x);
                         }
                         const float f0 = sum == 0.f ? 0.f : ex2(mx - mn);
@@ -723,6 +770,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     }
     // A wait that ran out: let every copy land before the block's memory goes.
     if (!ok)
+#pragma unroll 1
         for (; landed < issued; ++landed)
             mbar_wait_bounded(sbase + C::BARS + 8 * (warp * S + (int)(landed % S)), (uint32_t)(landed / S) & 1u);
 }
