@@ -164,7 +164,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     constexpr int D = C::D, NT = C::NT, W = C::W, S = C::S, GR = C::GR, KW = C::KW;
     extern __shared__ __align__(128) uint8_t smem[];
     const uint32_t sbase = smem_u32(smem);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // (the shuffle tells the compiler that its index is one for the whole warp)
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);
     const int g = lane >> 2, t4 = lane & 3;
     // The lane's place in a blob: its key's words, the key's scales, its value words.
     const uint32_t klane = g * (D / 2) + t4 * (D / 8), slane = kv_scales_at(D) + g * (D / 16);

@@ -10,15 +10,15 @@
 // exchange through distributed shared memory, decide", and those rounds are
 // what bounds it (a row of 128256 is 0.5 MB: 0.08 us of HBM bandwidth). A cut
 // (top-k by count, top-p by weight) is found in two rounds from one histogram
-// of 2048 bins, 64 to a factor of 2 in weight: 32 sums of 64 bins, then the 64
+// of 4096 bins, 128 to a factor of 2 in weight: 64 sums of 64 bins, then the 64
 // bins that hold the cut. For top-k the bins are of the logits themselves and no
 // exponential is taken but of the tokens that remain. If no more than LIST
-// tokens lie in or above the cut's bin, one block gathers them, sorts them by
-// (logit, lowest index first), applies the filters as a prefix, sorts what is
-// left by index and draws. Otherwise only the bin's own tokens are gathered and
-// sorted, by every block, for the exact cut; a bin that holds more than LIST
-// (equal logits by the thousand) is narrowed 5 bits of (logit, index) a round
-// first. The draw then adds up in index order over the whole row.
+// tokens lie in or above the cut's bin, one block gathers them, ranks each
+// against the others by (logit, lowest index first), applies the filters, and
+// adds up what is left in index order. Otherwise only the bin's own tokens are
+// gathered and ranked, by every block, for the exact cut; a bin that holds more
+// than LIST (equal logits by the thousand) is narrowed 5 bits of (logit, index)
+// a round first. The draw then adds up in index order over the whole row.
 #include <cooperative_groups.h>
 
 #include "vbq_decode.h"
@@ -34,8 +34,9 @@ constexpr uint32_t ALL = 0xffffffffu;
 constexpr int SA_THREADS = 512;
 constexpr int SA_WARPS = SA_THREADS / 32;
 constexpr int SA_BLOCKS = 8;              // most blocks of a cluster
-constexpr int BINS = 2048;
-constexpr int LIST = SA_THREADS;          // tokens a block sorts, one per thread
+constexpr int BINS = 4096;                // 64 groups of 64
+constexpr int PER_OCTAVE = 128;           // bins to a factor of 2 in weight
+constexpr int LIST = 256;                 // tokens a block ranks
 
 struct Sum { u64 w; uint32_t n, pad; };   // weight and count
 
@@ -48,23 +49,24 @@ struct Found {                            // where a cut lies
 struct Shared {
     union {
         struct { uint32_t n[BINS], hi[BINS]; int lo[BINS]; } hist;   // counts; weights' parts
-        u64 sorted[LIST];
+        uint32_t found[LIST];             // a block's tokens to gather
+        Sum beside[SA_THREADS + 16];       // ranking: what a thread has counted, and the whole weight's parts
     };
-    u64 list[LIST];                       // gathered tokens
-    Sum coarse[SA_BLOCKS][32];            // written by the blocks of the cluster; the rounds that narrow a
+    u64 list[LIST], weights[LIST];        // gathered tokens
+    Sum coarse[SA_BLOCKS][64];            // written by the blocks of the cluster; the rounds that narrow a
     Sum fine[SA_BLOCKS][64];              // bin take the two in turn, each free since the exchange before
     u64 top[SA_BLOCKS];
     Sum total[SA_BLOCKS];
     uint32_t count[SA_BLOCKS];            // tokens each block gathers
     u64 part[SA_WARPS], warp_w[SA_WARPS];
     u64 mass, pick[2];
-    Found found;
+    Found found_cut;
     uint32_t next;
 };
 constexpr int SHARED_BYTES = (sizeof(Shared) + 15) / 16 * 16;    // the row's slice follows
-constexpr size_t SMEM_ALONE = 120 * 1024; // more than half an SM's
-constexpr size_t SMEM_MOST = SHARED_BYTES + 4 * (SAMPLE_MAX_VOCAB / 6 + 4);
-static_assert(SMEM_MOST <= 227 * 1024, "the largest slice fits");
+constexpr size_t SMEM_MOST = 227 * 1024, SMEM_ALONE = 120 * 1024;        // a block's most; more than half an SM's
+constexpr int SLICE_MOST = (SMEM_MOST - SHARED_BYTES) / 4;
+static_assert(SLICE_MOST >= SAMPLE_MAX_VOCAB / SA_BLOCKS, "the largest slice fits");
 
 __device__ __forceinline__ uint32_t key_of(float v) {
     const uint32_t u = __float_as_uint(v);
@@ -94,10 +96,10 @@ struct Scale {
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(f));
         return t < -126.f ? 0.f : __int_as_float(__float_as_int(y) + (__float_as_int(r) << 23));
     }
-    // Bin of a logit: 64 to a factor of 2 below the largest, 0: 2^-32 and less. Never above a larger logit's bin.
+    // Bin of a logit, from the largest down; 0: 2^-32 and less. Never above a larger logit's bin.
     __device__ __forceinline__ int bin(float l) const {
-        const float t = fmaxf(__fmul_rn(__fsub_rn(l, top), hi), -(BINS - 1) / 64.f);
-        return (int)(__float_as_uint(__fmaf_rn(t, 64.f, 0x1.8p23f)) - 0x4b400000u) + BINS - 1;
+        const float t = fmaxf(__fmul_rn(__fsub_rn(l, top), hi), -(BINS - 1) / (float)PER_OCTAVE);
+        return (int)(__float_as_uint(__fmaf_rn(t, (float)PER_OCTAVE, 0x1.8p23f)) - 0x4b400000u) + BINS - 1;
     }
 };
 // w = 65536 hi + lo: e in whole multiples of 2^-32, ties to even, lo within +-2^15. Both parts by adding 1.5 2^23, which
@@ -137,6 +139,9 @@ __device__ __forceinline__ float logit_at(const Sample& p, const void* row, int 
                         : __uint_as_float((uint32_t)static_cast<const uint16_t*>(row)[i] << 16));
 }
 
+// The warp's index, known to the compiler to be one for the whole warp.
+__device__ __forceinline__ int uniform_warp() { return __shfl_sync(ALL, (int)threadIdx.x >> 5, 0); }
+
 __device__ __forceinline__ u64 warp_sum(u64 v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(ALL, v, o);
@@ -151,19 +156,6 @@ __device__ __forceinline__ u64 warp_scan(u64 v) {          // inclusive
     }
     return v;
 }
-// Inclusive scan over the block; the block's sum in all.
-__device__ __forceinline__ u64 block_scan(u64 v, u64* part, u64* all) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const u64 x = warp_scan(v);
-    __syncthreads();
-    if (lane == 31) part[warp] = x;
-    __syncthreads();
-    const u64 y = warp_scan(lane < SA_WARPS ? part[lane] : 0);
-    *all = __shfl_sync(ALL, y, 31);
-    const u64 before = __shfl_sync(ALL, y, max(warp, 1) - 1);
-    return x + (warp ? before : 0);
-}
-
 // The weight that a top-p prefix reaches at least.
 __device__ __forceinline__ u64 share_of(float top_p, u64 mass) { return top_p > 0.f ? at_least(top_p, mass, false) : 0; }
 // The least running weight that is past the random number's share.
@@ -217,26 +209,40 @@ __device__ __forceinline__ void find_cut(const Sum* tab, int width, bool by_weig
     }
 }
 
-// Descending bitonic sort of one value per thread below size (a power of two,
-// 32..LIST); the others pass through.
-__device__ u64 sort_down(u64 v, int size, u64* buf) {
-    const int t = threadIdx.x;
-    for (int k = 2; k <= size; k <<= 1) {
-        for (int j = k >> 1; j; j >>= 1) {
-            u64 y;
-            if (j >= 32) {
-                __syncthreads();
-                buf[t] = v;
-                __syncthreads();
-                y = buf[t ^ j];
-            } else {
-                y = __shfl_xor_sync(ALL, v, j);
+// Over the list's tokens j that come before this thread's in `first`'s sense: how many and their weight, with the
+// list split over the threads that share a token (size: the list's length rounded up to a power of two, 32..LIST).
+// Every thread calls it; threads below count get their token's sums, and the whole weight in all.
+template <class Before>
+__device__ __forceinline__ Sum rank_in(const Shared& sh, Sum* beside, int count, int size, Before before, u64* all) {
+    const int tid = threadIdx.x, c = tid & (size - 1), step = SA_THREADS / size;
+    Sum s = {0, 0, 0};
+    u64 mine = 0;
+    if (c < count) {
+        const u64 o = sh.list[c];
+        for (int j = tid / size; j < count; j += step) {   // one j for the whole warp
+            const u64 w = sh.weights[j];
+            if (before(sh.list[j], o)) {
+                s.w += w;
+                ++s.n;
             }
-            const bool larger = ((t & j) == 0) == ((t & k) == 0);      // this side keeps the larger
-            if (t < size) v = larger ? max(v, y) : min(v, y);
+            mine += w;
         }
     }
-    return v;
+    // Every token's threads have seen the same list: the first token's weights are the whole.
+    __syncthreads();
+    beside[tid] = s;
+    u64* totals = reinterpret_cast<u64*>(beside + SA_THREADS);
+    if (c == 0) totals[tid / size] = mine;
+    __syncthreads();
+    *all = 0;
+    s = Sum{0, 0, 0};
+    for (int i = 0; i < step; ++i) {
+        const Sum x = beside[i * size + c];
+        s.w += x.w;
+        s.n += x.n;
+        *all += totals[i];
+    }
+    return s;
 }
 
 // C blocks per row, each with `slice` neighbouring tokens (a multiple of 4).
@@ -245,7 +251,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
     extern __shared__ __align__(16) uint8_t smem[];
     Shared& sh = *reinterpret_cast<Shared*>(smem);
     float* x = reinterpret_cast<float*>(smem + SHARED_BYTES);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp();
     const int rank = C == 1 ? 0 : (int)(blockIdx.x % C);
     const int64_t row = blockIdx.x / C;
     if constexpr (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // this block has started
@@ -343,7 +349,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
             // (2^32; light is 64 of its multiples or more): they count towards the whole weight only. By whole bins, so that a bin's tokens are all in the
             // histogram or all not.
             const float light = __fdiv_rn(1.f - top_p, (float)V);
-            const int light_bin = light >= 0x1p-26f ? BINS - 3 + (int)floorf(64.f * __log2f(light)) : 0;
+            const int light_bin = light >= 0x1p-26f ? BINS - 4 + (int)floorf((float)PER_OCTAVE * __log2f(light)) : 0;
             int rest_hi = 0;
             long long rest_lo = 0;
             for (int q = tid; q < quads4; q += SA_THREADS) {
@@ -361,7 +367,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
                     }
                     atomicAdd(&sh.hist.n[b], 1u);
                     atomicAdd(&sh.hist.lo[b], w.lo);
-                    atomicAdd(&sh.hist.hi[b], (uint32_t)w.hi);
+                    if (w.hi) atomicAdd(&sh.hist.hi[b], (uint32_t)w.hi);
                 }
             }
             const u64 rest = warp_sum(whole(rest_hi, rest_lo));
@@ -377,7 +383,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         }
         used = true;
         __syncthreads();
-        for (int c = warp; c < 32; c += SA_WARPS) {        // sums of 64 bins, to every block
+        for (int c = warp; c < 64; c += SA_WARPS) {        // sums of 64 bins, to every block
             const int b = 64 * c + lane;
             Sum s = {0, __reduce_add_sync(ALL, sh.hist.n[b] + sh.hist.n[b + 32]), 0};
             if (by_weight)
@@ -390,19 +396,19 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
             u64 mass = 0;
             if (by_weight) {
 #pragma unroll
-                for (int r = 0; r < C; ++r) mass += sh.coarse[r][lane].w;
+                for (int r = 0; r < C; ++r) mass += sh.coarse[r][lane].w + sh.coarse[r][lane + 32].w;
                 mass = warp_sum(mass);
             }
             if (lane == 0) {
                 sh.mass = mass;
-                sh.found = Found{0, 0, 0, 0};
+                sh.found_cut = Found{0, 0, 0, 0};
             }
             __syncwarp();
-            find_cut<C, 1>(&sh.coarse[0][0], 32, by_weight, !by_weight ? (u64)top_k : share_of(top_p, mass), &sh.found);
+            find_cut<C, 2>(&sh.coarse[0][0], 64, by_weight, !by_weight ? (u64)top_k : share_of(top_p, mass), &sh.found_cut);
         }
         __syncthreads();
         const u64 enough = !by_weight ? (u64)top_k : share_of(top_p, sh.mass);
-        const int oct = sh.found.at;
+        const int oct = sh.found_cut.at;
         if (oct < 0) {                                     // fewer tokens than top_k: all are kept
             cluster_sync<C>();                             // every block has read coarse
             continue;
@@ -412,15 +418,15 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
             *in_block<C>(&sh.fine[rank][tid & 63], tid >> 6) = Sum{whole(sh.hist.hi[b], sh.hist.lo[b]), sh.hist.n[b], 0};
         }
         cluster_sync<C>();
-        if (warp == 0) find_cut<C, 2>(&sh.fine[0][0], 64, by_weight, enough, &sh.found);
+        if (warp == 0) find_cut<C, 2>(&sh.fine[0][0], 64, by_weight, enough, &sh.found_cut);
         if (tid == 0) sh.next = 0;
         __syncthreads();
-        const int in_oct = sh.found.at, bin = 64 * oct + in_oct;
-        const bool finish = sh.found.above_n + sh.found.in <= LIST;      // one block takes it from here
+        const int in_oct = sh.found_cut.at, bin = 64 * oct + in_oct;
+        const bool finish = sh.found_cut.above_n + sh.found_cut.in <= LIST;      // one block takes it from here
         if (warp < C) {                                    // how many tokens block `warp` will gather
             uint32_t c = 0;
             if (finish) {
-                c = lane > oct ? sh.coarse[warp][lane].n : 0;
+                c = (lane > oct ? sh.coarse[warp][lane].n : 0) + (lane + 32 > oct ? sh.coarse[warp][lane + 32].n : 0);
                 if (lane >= in_oct) c += sh.fine[warp][lane].n;
                 if (lane + 32 >= in_oct) c += sh.fine[warp][lane + 32].n;
             } else if (lane == 0) {
@@ -437,17 +443,26 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
             return (finish ? b >= bin : b == bin) && keeps(l, i);
         };
         const auto order_at = [&](int i) { return order_of(x[i], first + i); };
+        // To narrow a bin, orders are taken from the lowest logit that it can hold, so that their leading bits say something.
+        const float down = __fdiv_rn(1.f / PER_OCTAVE, scale.hi), dist = (float)(BINS - 1 - bin);
+        const bool far = !(down < 1e30f);                  // temperatures past 1e32: any logit may be in any bin
+        const uint32_t key_hi = far ? 0xffffffffu : key_of(fmaf(-fmaxf(dist - 0.75f, 0.f), down, top)) + 8;
+        const uint32_t key_lo = far || bin == 0 ? 0 : key_of(fmaf(-(dist + 0.75f), down, top)) - 8;
+        const auto from_low = [&](int i) {
+            return (u64)(min(max(key_of(x[i]), key_lo), key_hi) - key_lo) << 32 | (uint32_t)~(first + i);
+        };
         u64 prefix = 0;                                    // of the orders in a narrowed bin
         int known = 0;
+        if (!finish && sh.found_cut.in > LIST) known = min(__clz(key_hi - key_lo), 31);
         if (!finish) {
-            for (int round = 0; sh.found.in > LIST; ++round) {           // 5 bits a round
+            for (int round = 0; sh.found_cut.in > LIST; ++round) {           // 5 bits a round
                 const int bits = min(5, 64 - known);
                 __syncthreads();
                 if (tid < 32) sh.hist.n[tid] = sh.hist.lo[tid] = sh.hist.hi[tid] = 0;
                 __syncthreads();
                 for (int i = tid; i < n; i += SA_THREADS) {
                     if (!here(x[i], i)) continue;
-                    const u64 o = order_at(i);
+                    const u64 o = from_low(i);
                     if (known && o >> (64 - known) != prefix) continue;
                     const int d = (int)(o >> (64 - known - bits)) & ((1 << bits) - 1);
                     atomicAdd(&sh.hist.n[d], 1u);
@@ -459,18 +474,18 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
                 }
                 __syncthreads();
                 Sum* tab = round & 1 ? &sh.fine[0][0] : &sh.coarse[0][0];
-                const int width = round & 1 ? 64 : 32;
+                const int width = 64;
                 for (int r = warp; r < C; r += SA_WARPS)
                     *in_block<C>(tab + rank * width + lane, r) =
                         Sum{whole(sh.hist.hi[lane], sh.hist.lo[lane]), sh.hist.n[lane], 0};
                 cluster_sync<C>();
                 if (warp == 0) {
-                    find_cut<C, 1>(tab, width, by_weight, enough, &sh.found);
+                    find_cut<C, 1>(tab, width, by_weight, enough, &sh.found_cut);
                     __syncwarp();
-                    if (lane < C) sh.count[lane] = tab[lane * width + sh.found.at].n;
+                    if (lane < C) sh.count[lane] = tab[lane * width + sh.found_cut.at].n;
                 }
                 __syncthreads();
-                prefix = prefix << bits | (u64)sh.found.at;
+                prefix = prefix << bits | (u64)sh.found_cut.at;
                 known += bits;
             }
         }
@@ -482,7 +497,6 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
             if (r < rank) base += sh.count[r];
             listed += sh.count[r];
         }
-        uint32_t* found = reinterpret_cast<uint32_t*>(&sh.hist);         // this block's, in any order
         const uint32_t mine = sh.count[rank];
         __syncthreads();                                   // the histogram is done with
         for (int q = tid; q < quads4; q += SA_THREADS) {
@@ -491,14 +505,14 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (!here(l[j], 4 * q + j)) continue;
-                if (known && order_at(4 * q + j) >> (64 - known) != prefix) continue;
+                if (known && from_low(4 * q + j) >> (64 - known) != prefix) continue;
                 const uint32_t to = atomicAdd(&sh.next, 1u);
-                if (to < LIST) found[to] = 4 * q + j;
+                if (to < LIST) sh.found[to] = 4 * q + j;          // in any order
             }
         }
         __syncthreads();
         if (tid < (int)mine) {
-            const u64 o = order_at((int)found[tid]);
+            const u64 o = order_at((int)sh.found[tid]);
             if (base + tid < LIST) {
                 if (finish) {
                     *in_block<C>(&sh.list[base + tid], 0) = o;
@@ -511,49 +525,49 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         cluster_sync<C>();
         if (finish && rank != 0) return;                   // block 0 has all it needs
 
-        // Sorted, a thread's token is the tid-th: the filters are conditions on a prefix.
+        // The filters: a thread's token has `ahead.n` tokens of the list before it, weighing ahead.w.
         const int count = (int)listed;
         int size = 32;
         while (size < count) size <<= 1;
         const bool real = tid < count;
-        const u64 o = sort_down(real ? sh.list[tid] : 0, size, sh.sorted);
+        const u64 o = real ? sh.list[tid] : 0;
         const float ce = real ? scale.chance(value_of((uint32_t)(o >> 32))) : 0.f;
         const u64 cw = real ? weight(ce) : 0;
+        if (real) sh.weights[tid] = cw;
+        __syncthreads();
         u64 all;
-        const u64 cum = block_scan(cw, sh.part, &all);
-        const u64 above = finish ? 0 : sh.found.above;
-        const uint32_t above_n = finish ? 0 : sh.found.above_n;
+        const Sum ahead = rank_in(sh, sh.beside, count, size, [](u64 j, u64 i) { return j > i; }, &all);
+        const u64 above = finish ? 0 : sh.found_cut.above;
+        const uint32_t above_n = finish ? 0 : sh.found_cut.above_n;
         bool keep;
         if (!by_weight) {
-            keep = real && (u64)tid + above < (u64)top_k;
+            keep = real && ahead.n + above < (u64)top_k;
             if (finish) {
-                if (tid == top_k - 1) sh.pick[0] = cum;    // there is one: the cut lies in the list
+                if (real && ahead.n == (uint32_t)top_k - 1) sh.pick[0] = ahead.w + cw;       // the cut lies in the list
                 __syncthreads();
-                keep = keep && (top_p >= 1.f || tid == 0 || cum - cw < share_of(top_p, sh.pick[0]));
+                keep = keep && (top_p >= 1.f || ahead.n == 0 || ahead.w < share_of(top_p, sh.pick[0]));
             }
         } else {
-            keep = real && (above + cum - cw < enough || (tid == 0 && above_n == 0));
+            keep = real && (above + ahead.w < enough || ahead.n + above_n == 0);
         }
         if (finish) keep = keep && !(ce < min_p);
         const int n_keep = __syncthreads_count(keep);      // at least one
         if (!finish) {
-            if (tid == n_keep - 1) sh.pick[1] = o;
+            if (keep && (int)ahead.n == n_keep - 1) sh.pick[1] = o;      // what is kept comes first
             __syncthreads();
             cut = value_of((uint32_t)(sh.pick[1] >> 32));
             cut_i = (int)~(uint32_t)sh.pick[1];
             continue;
         }
         // The draw, in index order.
-        int small = 32;
-        while (small < n_keep) small <<= 1;
-        const u64 by_index = sort_down(tid < n_keep ? o << 32 | o >> 32 : 0, small, sh.sorted);
-        const float le = tid < n_keep ? scale.chance(value_of((uint32_t)by_index)) : 0.f;
-        const u64 lw = tid < n_keep ? weight(le) : 0;
-        const u64 to = block_scan(lw, sh.part, &all);
+        const u64 lw = keep ? cw : 0;
+        if (real) sh.weights[tid] = lw;
+        __syncthreads();
+        const u64 to = rank_in(sh, sh.beside, count, size, [](u64 j, u64 i) { return (uint32_t)j > (uint32_t)i; }, &all).w + lw;
         const u64 target = drawn_at(u, all);
-        if (to >= target && to - lw < target) {
-            p.tokens[row] = (int)~(uint32_t)(by_index >> 32);
-            if (p.probs) p.probs[row] = __fdiv_rn(le, __ull2float_rn(all) * 0x1p-32f);
+        if (real && to >= target && to - lw < target) {
+            p.tokens[row] = (int)~(uint32_t)o;
+            if (p.probs) p.probs[row] = __fdiv_rn(ce, __ull2float_rn(all) * 0x1p-32f);
             if (p.kept) p.kept[row] = n_keep;
         }
         return;
@@ -661,12 +675,13 @@ cudaError_t launch(const Sample& p, size_t least, cudaStream_t s) {
 
 // Blocks per row: few tokens are not worth an exchange; up to 8 rows spread over clusters of 8. Clusters of 8 no
 // longer get an SM per block at 16 rows (two blocks on some SMs: 33 us for 16 x 128256 under top-p 0.9; two waves
-// where shared memory allows one: 45 us), clusters of 6 do (29 us; 5: 31 us, 4: 34 us). Beyond an SM per block the
+// where shared memory allows one: 45 us), clusters of 6 do (29 us; 5: 31 us, 4: 34 us). (Blocks of 1024 threads: 25 us
+// there, but 17 us instead of 15 under top-k 50 and 13 instead of 11 at 32000 logits.) Beyond an SM per block the
 // rows queue either way.
 cudaError_t launch_sample(const Sample& p, cudaStream_t s) {
     if (p.vocab <= 4096) return launch<1>(p, 0, s);
     if (p.vocab <= 16384) return launch<4>(p, 0, s);
-    if (p.batch > 8 && p.batch <= 24) return launch<6>(p, SMEM_ALONE, s);
+    if (p.batch > 8 && p.batch <= 24 && p.vocab <= 6 * (SLICE_MOST - 4)) return launch<6>(p, SMEM_ALONE, s);
     return launch<8>(p, 0, s);
 }
 

@@ -236,3 +236,32 @@ def test_sample_in_a_graph_repeats():
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(i, j) for i, j in zip(want, got))
+
+
+@pytest.mark.parametrize("vocab", [3000, 20000, 128256, 1 << 18])
+@pytest.mark.parametrize("spread", [0.0, 1e-7, 1e-3, 0.02])
+def test_sample_cuts_among_near_equal_logits(vocab, spread):
+    """Thousands of logits too near one another for a histogram to tell apart, either side of zero and about 7, with many exact ties."""
+    rng = np.random.default_rng(vocab)
+    b = 10
+    x = (rng.integers(-300, 300, (b, vocab)) * spread / 300).astype(np.float32)
+    x[5:] += 7.0
+    u = torch.from_numpy(rng.random(b).astype(np.float32))
+    k = [1, 255, 256, 257, 1500] * 2
+    tok, _, kept, _ = _check(torch.from_numpy(x), u=u, top_k=k)
+    assert kept.tolist() == k
+    order = np.argsort(-x, axis=1, kind="stable")
+    for i in range(b):                                            # all weigh nearly the same: the draw is by place
+        rank = np.flatnonzero(np.sort(order[i, :k[i]]) == tok[i])
+        assert rank.size == 1 and abs(int(rank[0]) - k[i] * float(u[i])) <= 1 + k[i] * 0.03
+    _check(torch.from_numpy(x), u=u, top_p=[0.1, 0.3, 0.5, 0.7, 0.9] * 2)
+    _check(torch.from_numpy(x), u=u, top_k=2000, top_p=0.5, min_p=0.5)
+
+
+@pytest.mark.parametrize("temperature", [1e-30, 1e-6, 1e-3, 50.0, 1e6, 1e30, float("inf")])
+def test_sample_temperatures_far_out(temperature):
+    rng = np.random.default_rng(9)
+    x = torch.from_numpy((rng.standard_normal((9, 40000)) * 3).astype(np.float32))
+    u = torch.from_numpy(rng.random(9).astype(np.float32))
+    for over in ({}, {"top_k": 700}, {"top_p": 0.6}, {"top_k": 300, "top_p": 0.9}):
+        _check(x, u=u, temperature=temperature, **over)
