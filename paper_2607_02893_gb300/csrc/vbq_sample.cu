@@ -455,7 +455,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         int known = 0;
         if (!finish && sh.found_cut.in > LIST) known = min(__clz(key_hi - key_lo), 31);
         if (!finish) {
-            for (int round = 0; sh.found_cut.in > LIST; ++round) {           // 5 bits a round
+            for (int round = 0; sh.found_cut.in > LIST && known < 64; ++round) {   // 5 bits a round
                 const int bits = min(5, 64 - known);
                 __syncthreads();
                 if (tid < 32) sh.hist.n[tid] = sh.hist.lo[tid] = sh.hist.hi[tid] = 0;
