@@ -51,7 +51,7 @@ namespace vbq {
 namespace {
 
 constexpr uint32_t FULL = 0xffffffffu;
-constexpr int JOIN = 8;                         // parts whose loads are in flight at once
+constexpr int JOIN = 4;                         // parts whose loads are in flight at once
 constexpr int CUT = 6;                           // pages a block takes at least of a segment that is cut
 constexpr int STRADDLE = 16;                     // pages whose time a block's second segment costs
 constexpr uint32_t LOW = 0x003c003cu, HIGH = 0x03c003c0u;    // codes at bits 2..5 and 6..9 of each half
@@ -73,6 +73,7 @@ struct Shape {
     static constexpr int FACTOR = ML + W * ROWS * 8;             // a warp's factor per row, then (maximum, sum) per row
     static constexpr int CUM = FACTOR + W * ROWS * 4 + ROWS * 8; // pages before each sequence
     static_assert(W <= 16 && ROWS * 16 <= THREADS, "the join's first step");
+    static_assert(KV_MAX_ROWS == 16, "16 lanes to a sequence");
     static constexpr int SPAN = CUM + (KV_MAX_BATCH + 2) * 8;    // first page and last key of each sequence
     static constexpr int MISC = SPAN + KV_MAX_BATCH * 8;
     static constexpr int SMEM = MISC + 64 + 4 * W;
@@ -192,14 +193,15 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     // Every sequence's range of pages.
     const int64_t table_keys = (int64_t)c.table_pages * KV_PAGE;
 #pragma unroll 1
-    for (int b = tid; b < a.batch; b += C::THREADS) {
-        int hi = -1, mn = 0x7fffffff;
-#pragma unroll 1
-        for (int t = 0; t < a.rows; ++t) {
-            const int p = a.pos[b * a.rows + t];
-            hi = max(hi, p);
-            if (p >= 0) mn = min(mn, p);
+    for (int b0 = 0; b0 < a.batch; b0 += C::THREADS / KV_MAX_ROWS) {     // a lane per row, 16 to a sequence
+        const int b = b0 + tid / KV_MAX_ROWS, t = tid % KV_MAX_ROWS;
+        int hi = b < a.batch && t < a.rows ? a.pos[b * a.rows + t] : -1, mn = hi >= 0 ? hi : 0x7fffffff;
+#pragma unroll
+        for (int o = 1; o < KV_MAX_ROWS; o <<= 1) {
+            hi = max(hi, __shfl_xor_sync(FULL, hi, o));
+            mn = min(mn, __shfl_xor_sync(FULL, mn, o));
         }
+        if (t != 0 || b >= a.batch) continue;
         if (hi >= table_keys) {
             if (blockIdx.x == 0) atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
             hi = (int)(table_keys - 1);
@@ -712,12 +714,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             // The last of the segment's blocks joins their parts, in order.
             const int64_t b0 = aligned ? first_part : s.start / quantum;
             const int n_parts = aligned ? parts_here : (int)((s.start + s.pages - 1) / quantum - b0) + 1;
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) misc->last = atomicAdd(&counts[s.index], 1u) == (uint32_t)(n_parts - 1);
+            __syncthreads();                      // the part is written: released by the count, acquired by its last adder
+            if (tid == 0) misc->last = atom_add_acq_rel_gpu(&counts[s.index], 1u) == (uint32_t)(n_parts - 1);
             __syncthreads();
             if (misc->last) {
-                __threadfence();
                 if (tid == 0) counts[s.index] = 0;
 #pragma unroll 1
         for (int u = tid; u < C::UNITS; u += C::THREADS) {
