@@ -373,3 +373,32 @@ def test_positions_and_pages_outside_the_cache_are_reported():
     vbq.vbq_kv_append(cache, table, torch.tensor([[4], [3]], dtype=I32, device=DEV), x, x, cos=cos, sin=cos)
     with pytest.raises(vbq.VbqError):
         vbq.vbq_device_status()
+
+
+@pytest.mark.parametrize("batch,hk,heads,rows,most", [(1024, 1, 2, 1, 200), (300, 2, 6, 3, 150), (1024, 3, 3, 2, 40)])
+def test_attend_many_sequences(batch, hk, heads, rows, most):
+    """More segments than blocks, short and uneven, some empty; every output checked on a sample of sequences."""
+    rng = np.random.default_rng(batch + rows)
+    lens = [int(n) for n in rng.integers(0, most, batch)]
+    table, pages = _table(lens, rng)
+    cache = vbq.KvCache(pages, hk, 64)
+    cache.pages.fill_(0xff)
+    n = max(lens)
+    k, v = (rng.standard_normal((batch, n, hk, 64)).astype(np.float32) for _ in "kv")
+    pos = np.where(np.arange(n)[None] < np.array(lens)[:, None], np.arange(n)[None], -1).astype(np.int32)
+    vbq.vbq_kv_append(cache, table, torch.from_numpy(pos).to(DEV), torch.from_numpy(k).to(DEV), torch.from_numpy(v).to(DEV))
+    q = torch.randn(batch, rows, heads, 64, device=DEV).to(torch.bfloat16)
+    at = np.array([[m - rows + t if m else -1 for t in range(rows)] for m in lens], np.int32)
+    at = np.maximum(at, -1)
+    out = vbq.vbq_kv_attend(cache, table, torch.from_numpy(at).to(DEV), q).float().cpu().numpy()
+    qd = q.float().cpu().numpy()
+    for i in list(range(8)) + [int(x) for x in rng.integers(8, batch, 60)] + [batch - 1]:
+        m = lens[i]
+        if m == 0:
+            assert not out[i].any()
+            continue
+        kd, ks = _held(k[i, :m])
+        vd, vs = _held(v[i, :m])
+        ref, spread, reach = o.attend(qd[i], kd, vd, at[i], 0.125, 0, ks)
+        assert o.attend_within_bound(out[i], ref, spread, reach, 8 * float(vs.max()), m).all(), i
+    assert vbq.vbq_device_status() is None
