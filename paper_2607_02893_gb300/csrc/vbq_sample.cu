@@ -52,7 +52,8 @@ struct Shared {
         uint32_t found[LIST];             // a block's tokens to gather
         Sum beside[SA_THREADS + 16];       // ranking: what a thread has counted, and the whole weight's parts
     };
-    u64 list[LIST], weights[LIST];        // gathered tokens
+    u64 list[LIST];                       // gathered tokens
+    ulonglong2 ranked[LIST];              // and their weights beside them
     Sum coarse[SA_BLOCKS][64];            // written by the blocks of the cluster; the rounds that narrow a
     Sum fine[SA_BLOCKS][64];              // bin take the two in turn, each free since the exchange before
     u64 top[SA_BLOCKS];
@@ -219,13 +220,13 @@ __device__ __forceinline__ Sum rank_in(const Shared& sh, Sum* beside, int count,
     u64 mine = 0;
     if (c < count) {
         const u64 o = sh.list[c];
+#pragma unroll 4
         for (int j = tid / size; j < count; j += step) {   // one j for the whole warp
-            const u64 w = sh.weights[j];
-            if (before(sh.list[j], o)) {
-                s.w += w;
-                ++s.n;
-            }
-            mine += w;
+            const ulonglong2 y = sh.ranked[j];
+            const bool first = before(y.x, o);
+            s.w += first ? y.y : 0;
+            s.n += first;
+            mine += y.y;
         }
     }
     // Every token's threads have seen the same list: the first token's weights are the whole.
@@ -533,7 +534,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         const u64 o = real ? sh.list[tid] : 0;
         const float ce = real ? scale.chance(value_of((uint32_t)(o >> 32))) : 0.f;
         const u64 cw = real ? weight(ce) : 0;
-        if (real) sh.weights[tid] = cw;
+        if (real) sh.ranked[tid] = make_ulonglong2(o, cw);
         __syncthreads();
         u64 all;
         const Sum ahead = rank_in(sh, sh.beside, count, size, [](u64 j, u64 i) { return j > i; }, &all);
@@ -561,7 +562,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         }
         // The draw, in index order.
         const u64 lw = keep ? cw : 0;
-        if (real) sh.weights[tid] = lw;
+        if (real) sh.ranked[tid].y = lw;
         __syncthreads();
         const u64 to = rank_in(sh, sh.beside, count, size, [](u64 j, u64 i) { return (uint32_t)j > (uint32_t)i; }, &all).w + lw;
         const u64 target = drawn_at(u, all);
