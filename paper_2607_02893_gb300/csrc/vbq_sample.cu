@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
     float cut = -INFINITY;
     int cut_i = -1;
     bool used = false;                                     // the histogram has been filled
-    const auto keeps = [&](float l, int i) { return l > cut || (l == cut && first + i <= cut_i); };
+    const auto keeps = [&](float l, int i) { return (l > cut) | ((l == cut) & (first + i <= cut_i)); };
 
     for (int which = 0; which < 2; ++which) {              // 0: top-k by count, 1: top-p by weight
         if (which == 0 ? top_k <= 0 || top_k >= V : top_p >= 1.f) continue;
@@ -352,23 +352,22 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
             const float light = __fdiv_rn(1.f - top_p, (float)V);
             const int light_bin = light >= 0x1p-26f ? BINS - 4 + (int)floorf((float)PER_OCTAVE * __log2f(light)) : 0;
             int rest_hi = 0;
-            long long rest_lo = 0;
+            int rest_lo = 0;
             for (int q = tid; q < quads4; q += SA_THREADS) {
                 const float4 v = x4[q];
                 const float* l = &v.x;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (!keeps(l[j], 4 * q + j)) continue;
+                    const bool in = keeps(l[j], 4 * q + j);
                     const int b = scale.bin(l[j]);
                     const Parts w(scale.chance(l[j]));
-                    if (b < light_bin) {
-                        rest_hi += w.hi;
-                        rest_lo += w.lo;
-                        continue;
+                    if (in & (b >= light_bin)) {
+                        atomicAdd(&sh.hist.n[b], 1u);
+                        atomicAdd(&sh.hist.lo[b], w.lo);
+                        if (w.hi) atomicAdd(&sh.hist.hi[b], (uint32_t)w.hi);
                     }
-                    atomicAdd(&sh.hist.n[b], 1u);
-                    atomicAdd(&sh.hist.lo[b], w.lo);
-                    if (w.hi) atomicAdd(&sh.hist.hi[b], (uint32_t)w.hi);
+                    rest_hi += in & (b < light_bin) ? w.hi : 0;
+                    rest_lo += in & (b < light_bin) ? w.lo : 0;
                 }
             }
             const u64 rest = warp_sum(whole(rest_hi, rest_lo));
@@ -441,7 +440,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         // A kept token of the bin (or, to finish, from it up), and its order.
         const auto here = [&](float l, int i) {
             const int b = scale.bin(l);
-            return (finish ? b >= bin : b == bin) && keeps(l, i);
+            return (finish ? b >= bin : b == bin) & keeps(l, i);
         };
         const auto order_at = [&](int i) { return order_of(x[i], first + i); };
         // To narrow a bin, orders are taken from the lowest logit that it can hold, so that their leading bits say something.
@@ -577,7 +576,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
     // The draw over the whole row, in index order: a warp has neighbouring tokens. x becomes e, 0 where not kept.
     const int run = (quads4 + SA_WARPS - 1) / SA_WARPS, q0 = warp * run, q1 = min(quads4, q0 + run);
     int sum_hi = 0;
-    long long sum_lo = 0;
+    int sum_lo = 0;
     uint32_t kept = 0;
     for (int q = q0 + lane; q < q1; q += 32) {
         float4 v = x4[q];
@@ -585,7 +584,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float c = scale.chance(e[j]);
-            const bool in = c >= min_p && keeps(e[j], 4 * q + j);
+            const bool in = (c >= min_p) & keeps(e[j], 4 * q + j);
             e[j] = in ? c : 0.f;
             kept += in;
             const Parts w(e[j]);
