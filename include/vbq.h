@@ -451,8 +451,7 @@ vbq_status_t vbq_kv_read(const vbq_kv_cache* cache, const int32_t* table, int64_
  *   workspace  device, vbq_kv_workspace_bytes of these sizes, 16-byte aligned,
  *              zero before its first use; every call leaves it ready for the
  *              next. Calls that share one must not overlap on the GPU. It
- *              serves every call of at most these sizes (each of batch, rows,
- *              heads) on a cache of the same shape.
+ *              serves every call that needs no more bytes, on any cache.
  * Scores, softmax statistics and sums are fp32; queries and probabilities
  * enter the tensor cores in FP16, scaled by powers of two (11 significant
  * bits: finer than the BF16 of q and out). Results do not vary between calls.

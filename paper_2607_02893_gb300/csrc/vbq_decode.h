@@ -99,7 +99,7 @@ struct KvAttend {
 };
 constexpr int KV_MAX_BATCH = 1024;
 constexpr int KV_MAX_ROWS = 16;
-size_t kv_workspace_bytes(int batch, int rows, int heads, int kv_heads, int head_dim, int sms);
+size_t kv_workspace_bytes(int batch, int rows, int heads, int kv_heads, int sms);
 cudaError_t launch_kv_attend(const KvView& c, const KvAttend& a, cudaStream_t s);
 
 struct Norm {

@@ -155,7 +155,7 @@ vbq_status_t vbq_kv_workspace_bytes(const vbq_kv_cache* cache, int batch, int ro
     int dev = 0, sms = 0;
     VBQ_CUDA(cudaGetDevice(&dev));
     VBQ_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    *bytes = vbq::kv_workspace_bytes(batch, rows, heads, cache->kv_heads, cache->head_dim, sms);
+    *bytes = vbq::kv_workspace_bytes(batch, rows, heads, cache->kv_heads, sms);
     return VBQ_OK;
 }
 
@@ -180,7 +180,7 @@ vbq_status_t vbq_kv_attend(const vbq_kv_cache* cache, const int32_t* table, int6
     int dev = 0, sms = 0;
     VBQ_CUDA(cudaGetDevice(&dev));
     VBQ_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    const size_t need = vbq::kv_workspace_bytes(batch, rows, heads, cache->kv_heads, cache->head_dim, sms);
+    const size_t need = vbq::kv_workspace_bytes(batch, rows, heads, cache->kv_heads, sms);
     if (workspace_bytes < need)
         return fail(VBQ_ERR_ARG, "the workspace has %zu bytes, this call needs %zu", workspace_bytes, need);
     VBQ_CUDA(vbq::launch_kv_attend(view_of(cache, table, table_stride, table_pages), a, static_cast<cudaStream_t>(stream)));

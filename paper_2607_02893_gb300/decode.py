@@ -176,7 +176,7 @@ def vbq_kv_workspace_bytes(cache: KvCache, batch: int, rows: int, heads: int) ->
 
 
 def vbq_kv_workspace(cache: KvCache, batch: int, rows: int, heads: int):
-    """A zeroed workspace for vbq_kv_attend calls of at most these sizes."""
+    """A zeroed workspace for vbq_kv_attend calls that need no more than these sizes do."""
     n = vbq_kv_workspace_bytes(cache, batch, rows, heads)
     return torch.zeros(n, dtype=torch.uint8, device=cache.pages.device)
 

@@ -402,3 +402,18 @@ def test_attend_many_sequences(batch, hk, heads, rows, most):
         ref, spread, reach = o.attend(qd[i], kd, vd, at[i], 0.125, 0, ks)
         assert o.attend_within_bound(out[i], ref, spread, reach, 8 * float(vs.max()), m).all(), i
     assert vbq.vbq_device_status() is None
+
+
+def test_one_workspace_serves_every_shape():
+    """Head dimensions, head counts and tiles in turn on one workspace, each as with its own."""
+    rng = np.random.default_rng(31)
+    made = [_fill([5000, 300], hk, d, rng)[:2] for hk, d in ((2, 128), (1, 64), (2, 256), (4, 64))]
+    ws = torch.zeros(max(vbq.vbq_kv_workspace_bytes(c, 2, 16, 8) for c, _ in made), dtype=torch.uint8, device=DEV)
+    pos = torch.tensor([[4999], [299]], dtype=I32, device=DEV)
+    for _ in range(2):
+        for cache, table in made:
+            for rows in (1, 16):
+                q = torch.randn(2, rows, 8, cache.head_dim, device=DEV).to(torch.bfloat16)
+                p = (pos - torch.arange(rows, dtype=I32, device=DEV)).contiguous()
+                x, y = vbq.vbq_kv_attend(cache, table, p, q, workspace=ws), vbq.vbq_kv_attend(cache, table, p, q)
+                assert torch.equal(x.view(torch.int16), y.view(torch.int16))
