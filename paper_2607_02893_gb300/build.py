@@ -1,7 +1,9 @@
 """Build the CUDA library libvbq.so in-tree for GB300 (sm_103a).
 
 Each .cu file under csrc/ is compiled in parallel with nvcc, then linked into
-paper_2607_02893_gb300/libvbq.so (CUDA runtime linked statically).
+paper_2607_02893_gb300/libvbq.so (CUDA runtime linked statically). The CPython
+module native/_decode.c (argument marshalling of decode.py) is compiled beside
+them into paper_2607_02893_gb300/_decode.so.
 """
 
 from __future__ import annotations
@@ -10,6 +12,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -17,6 +20,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build", "vbq")
 LIB = os.path.join(PKG, "libvbq.so")
+MODULE_SRC = os.path.join(PKG, "native", "_decode.c")
+MODULE = os.path.join(PKG, "_decode.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC,-O2",
@@ -47,8 +52,21 @@ def _compile(src: str, verbose_ptxas: bool) -> str:
     return obj
 
 
+def _compile_module() -> None:
+    deps = (MODULE_SRC, os.path.join(ROOT, "include", "vbq.h"))
+    if os.path.exists(MODULE) and all(os.path.getmtime(d) <= os.path.getmtime(MODULE) for d in deps):
+        return
+    tmp = MODULE + ".tmp"
+    r = subprocess.run([shutil.which("gcc") or "cc", "-O2", "-std=gnu11", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"],
+                        "-I", os.path.join(ROOT, "include"), MODULE_SRC, "-o", tmp], capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compiling {MODULE_SRC} failed:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, MODULE)
+
+
 def build(verbose_ptxas: bool = False, force: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
+    _compile_module()
     srcs = sources()
     deps = srcs + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]
     deps.append(os.path.join(ROOT, "include", "vbq.h"))

@@ -1,69 +1,50 @@
 """Binding of the decode step's other operators (include/vbq.h): the 4-bit
 key-value cache and its attention, the residual norm, the sampler.
 
-Argument marshalling only, as in vbq.py. Tensors are checked for what the C
-call cannot see (type, shape, strides, device); everything else is checked there.
+Argument marshalling only, as in vbq.py. A decode step makes these calls every
+few microseconds, so their checks (of what the C call cannot see: a tensor's
+type, size, strides and device) and the calls themselves are in the CPython
+module native/_decode.c, built beside libvbq.so; the ones that are not in a
+step's way go through ctypes.
 """
 
 from __future__ import annotations
 
 import ctypes
+import os
 
 import torch
 
 from . import vbq as _b
 from .vbq import _check
 
-_bf16, _i16, _f32, _i32 = torch.bfloat16, torch.int16, torch.float32, torch.int32
-_BF16 = (_bf16, _i16)
+_native = None
 
 
-class _CacheStruct(ctypes.Structure):
-    _fields_ = [("pages", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("kv_heads", ctypes.c_int),
-                ("head_dim", ctypes.c_int)]
+def _load():
+    """The marshalling module, given the library's entry points. Fails loudly if absent."""
+    global _native
+    lib = _b.load()
+    try:
+        from . import _decode
+    except ImportError as e:
+        raise RuntimeError(f"VBQ decode binding not built: {os.path.join(os.path.dirname(__file__), '_decode.so')} ({e}); "
+                           "run `python -c 'import __graft_entry__ as g; g.build()'`") from e
+    raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+    address = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
+    _decode.setup(torch.float32, torch.bfloat16, torch.int16, torch.int32, raw_stream, address(lib.vbq_kv_append),
+                  address(lib.vbq_kv_read), address(lib.vbq_kv_attend), address(lib.vbq_residual_norm), address(lib.vbq_sample))
+    _native = _decode
+    return _decode
 
 
 def _lib():
     return _b._lib or _b.load()
 
 
-# A decode step makes these calls every few microseconds, so the checks below
-# are the few cheapest ones that keep a wrong tensor away from the kernels, and
-# the stream is asked for without building a torch.cuda.Stream.
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
-    (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
-
-
-def _stream(stream, dev):
-    if stream is None:
-        return _raw_stream(dev)
-    return stream if isinstance(stream, int) else stream.cuda_stream
-
-
-def _device(t) -> int:
-    dev = t.get_device()
-    if dev < 0:
-        raise ValueError("tensors must be on a GPU")
-    return dev
-
-
-def _type(t) -> int:
-    d = t.dtype
-    if d is _f32:
-        return 1
-    if d in _BF16:
-        return 0
-    raise ValueError(f"expected float32 or bfloat16, got {d}")
-
-
-def _dense(t, dtype, n, dev, name):
-    """Address of a contiguous tensor of n elements of that type on that device."""
-    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
-        if dtype is _bf16 and t.dtype is _i16:                  # BF16 bit patterns
-            return _dense(t, _i16, n, dev, name)
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on cuda:{dev}, got {t.dtype} "
-                         f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
-    return t.data_ptr()
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int)]
 
 
 def vbq_kv_page_bytes(kv_heads: int, head_dim: int) -> int:
@@ -87,31 +68,8 @@ class KvCache:
         self.n_pages, self.kv_heads, self.head_dim = int(n_pages), int(kv_heads), int(head_dim)
         self.device = pages.get_device()
         self._struct = _CacheStruct(pages.data_ptr(), self.n_pages, self.kv_heads, self.head_dim)
-        self._as_parameter_ = ctypes.c_void_p(ctypes.addressof(self._struct))
-
-
-def _rows(cache, table, pos):
-    """(device, table, stride, pages, pos, batch, rows) of a cache call."""
-    shape, stride = table.shape, table.stride()
-    if table.dtype is not _i32 or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
-        raise ValueError("table must be an int32 tensor (batch, pages) with dense rows")
-    pshape = pos.shape
-    if pos.dtype is not _i32 or len(pshape) != 2 or not pos.is_contiguous() or pshape[0] != shape[0]:
-        raise ValueError("pos must be a contiguous int32 tensor (batch, rows)")
-    dev = _device(table)
-    if pos.get_device() != dev or cache.device != dev:
-        raise ValueError("table, pos and the cache must be on one GPU")
-    return dev, table.data_ptr(), stride[0], shape[1], pos.data_ptr(), pshape[0], pshape[1]
-
-
-def _row_stride(t, b, r, heads, d, dev, name):
-    """Elements between rows of a (batch, rows, heads, d) tensor whose rows are dense and evenly spaced."""
-    if t.shape != (b, r, heads, d) or t.get_device() != dev:
-        raise ValueError(f"{name} must have shape {(b, r, heads, d)} on cuda:{dev}, got {tuple(t.shape)} on {t.device}")
-    s0, s1, s2, s3 = t.stride()
-    if s3 != 1 or (heads > 1 and s2 != d) or (r > 1 and b > 1 and s0 != r * s1):
-        raise ValueError(f"{name}'s rows must be dense and evenly spaced, got strides {t.stride()}")
-    return s1 if r > 1 else s0
+        self._address = ctypes.addressof(self._struct)
+        self._as_parameter_ = ctypes.c_void_p(self._address)
 
 
 def vbq_kv_append(cache: KvCache, table, pos, k, v, q=None, cos=None, sin=None, q_out=None, stream=None):
@@ -120,29 +78,9 @@ def vbq_kv_append(cache: KvCache, table, pos, k, v, q=None, cos=None, sin=None, 
     bfloat16; rows may be slices of a fused product's output) of the tokens at
     pos (batch, rows; negative: unused). With q (batch, rows, heads, head_dim)
     the rotated q is returned as bfloat16 (q_out, allocated when not given)."""
-    dev, tp, ts, tn, pp, b, r = _rows(cache, table, pos)
-    hk, d = cache.kv_heads, cache.head_dim
-    ty = _type(k)
-    if v.dtype is not k.dtype or (q is not None and q.dtype is not k.dtype):
-        raise ValueError("q, k and v must have one type")
-    ks, vs = _row_stride(k, b, r, hk, d, dev, "k"), _row_stride(v, b, r, hk, d, dev, "v")
-    qp = op = None
-    qs = heads = 0
-    if q is not None:
-        heads = q.shape[2]
-        qs = _row_stride(q, b, r, heads, d, dev, "q")
-        if q_out is None:
-            q_out = torch.empty((b, r, heads, d), dtype=_bf16, device=q.device)
-        qp, op = q.data_ptr(), _dense(q_out, _bf16, b * r * heads * d, dev, "q_out")
-    cp = sp = None
-    rot = rot_rows = 0
-    if cos is not None:
-        rot_rows, half = cos.shape
-        rot = 2 * half
-        cp = _dense(cos, _f32, rot_rows * half, dev, "cos")
-        sp = _dense(sin, _f32, rot_rows * half, dev, "sin")
-    st = _lib().vbq_kv_append(cache._as_parameter_, tp, ts, tn, pp, b, r, qp, qs, heads, k.data_ptr(), ks, v.data_ptr(), vs,
-                              ty, cp, sp, rot, rot_rows, op, _stream(stream, dev))
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    st = (_native or _load()).append(cache._address, cache.device, table, pos, k, v, q, cos, sin, q_out, stream)
     if st:
         _check(st)
     return q_out
@@ -152,18 +90,11 @@ def vbq_kv_read(cache: KvCache, table, pos, k_out=None, v_out=None, stream=None)
     """What the cache holds for the rows at pos, as float32 (batch, rows,
     kv_heads, head_dim); returns (k_out, v_out), allocating those not given
     (pass False to skip one)."""
-    dev, tp, ts, tn, pp, b, r = _rows(cache, table, pos)
-    n = b * r * cache.kv_heads * cache.head_dim
-    kp = vp = None
-    if k_out is None:
-        k_out = torch.empty((b, r, cache.kv_heads, cache.head_dim), dtype=_f32, device=pos.device)
-    if v_out is None:
-        v_out = torch.empty((b, r, cache.kv_heads, cache.head_dim), dtype=_f32, device=pos.device)
-    if k_out is not False:
-        kp = _dense(k_out, _f32, n, dev, "k_out")
-    if v_out is not False:
-        vp = _dense(v_out, _f32, n, dev, "v_out")
-    st = _lib().vbq_kv_read(cache._as_parameter_, tp, ts, tn, pp, b, r, kp, vp, _stream(stream, dev))
+    if k_out is None or v_out is None:
+        shape = (*pos.shape, cache.kv_heads, cache.head_dim)
+        k_out = torch.empty(shape, dtype=torch.float32, device=pos.device) if k_out is None else k_out
+        v_out = torch.empty(shape, dtype=torch.float32, device=pos.device) if v_out is None else v_out
+    st = (_native or _load()).read(cache._address, cache.device, table, pos, k_out, v_out, stream)
     if st:
         _check(st)
     return None if k_out is False else k_out, None if v_out is False else v_out
@@ -187,20 +118,11 @@ def vbq_kv_attend(cache: KvCache, table, pos, q, scale=None, window: int = 0, ou
     scale defaults to head_dim ** -0.5. Returns out (bfloat16, as q). Give the
     workspace of vbq_kv_workspace to keep it between calls; one is made (and
     zeroed) for this call otherwise."""
-    dev, tp, ts, tn, pp, b, r = _rows(cache, table, pos)
-    heads, d = q.shape[2], cache.head_dim
-    n = b * r * heads * d
-    if q.dim() != 4 or q.shape[3] != d:
-        raise ValueError(f"q must have shape {(b, r, 'heads', d)}, got {tuple(q.shape)}")
     if out is None:
         out = torch.empty_like(q)
     if workspace is None:
-        workspace = vbq_kv_workspace(cache, b, r, heads)
-    elif workspace.get_device() != dev or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous tensor on the cache's GPU")
-    st = _lib().vbq_kv_attend(cache._as_parameter_, tp, ts, tn, pp, b, r, _dense(q, _bf16, n, dev, "q"), heads,
-                              d ** -0.5 if scale is None else scale, window, _dense(out, _bf16, n, dev, "out"),
-                              workspace.data_ptr(), workspace.nbytes, _stream(stream, dev))
+        workspace = vbq_kv_workspace(cache, q.shape[0], q.shape[1], q.shape[2])
+    st = (_native or _load()).attend(cache._address, cache.device, table, pos, q, scale, window, out, workspace, stream)
     if st:
         _check(st)
     return out
@@ -211,21 +133,11 @@ def vbq_residual_norm(x, residual, weight, eps: float, out=None, residual_out=No
     and out = r' * rsqrt(mean(r'^2) + eps) * weight as bfloat16, per row of the
     last dimension. Returns (out, residual_out), allocating those not given;
     residual_out may be residual itself."""
-    dev, n, xt = _device(x), x.numel(), _type(x)
-    width = x.shape[-1]
     if out is None:
-        out = torch.empty(x.shape, dtype=_bf16, device=x.device)
-    rp = ro = None
-    rt = 0
-    if residual is not None:
-        rt, rd = _type(residual), residual.dtype
-        if residual_out is None:
-            residual_out = torch.empty_like(residual)
-        rp = _dense(residual, rd, n, dev, "residual")
-        ro = rp if residual_out is residual else _dense(residual_out, rd, n, dev, "residual_out")
-    st = _lib().vbq_residual_norm(_dense(x, x.dtype, n, dev, "x"), xt, rp, rt, _dense(weight, _f32, width, dev, "weight"),
-                                  eps, n // width if width else 0, width, _dense(out, _bf16, n, dev, "out"), ro,
-                                  _stream(stream, dev))
+        out = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
+    if residual is not None and residual_out is None:
+        residual_out = torch.empty_like(residual)
+    st = (_native or _load()).norm(x, residual, weight, eps, out, residual_out, stream)
     if st:
         _check(st)
     return out, residual_out
@@ -236,23 +148,14 @@ def vbq_sample(logits, temperature, top_k, top_p, min_p, u, tokens=None, probs=N
     per-row temperature, top_p, min_p, u (float32) and top_k (int32), all of
     shape (batch,). Returns (tokens, probs, kept), allocating those not given
     (pass False to skip probs or kept)."""
-    dev = _device(logits)
-    b, vocab = logits.shape
-    stride, unit = logits.stride()
-    if unit != 1 and vocab > 1:
-        raise ValueError("logits' rows must be dense")
+    b, dev = logits.shape[0], logits.device
     if tokens is None:
-        tokens = torch.empty(b, dtype=_i32, device=logits.device)
+        tokens = torch.empty(b, dtype=torch.int32, device=dev)
     if probs is None:
-        probs = torch.empty(b, dtype=_f32, device=logits.device)
+        probs = torch.empty(b, dtype=torch.float32, device=dev)
     if kept is None:
-        kept = torch.empty(b, dtype=_i32, device=logits.device)
-    st = _lib().vbq_sample(logits.data_ptr(), stride, _type(logits), b, vocab,
-                           _dense(temperature, _f32, b, dev, "temperature"), _dense(top_k, _i32, b, dev, "top_k"),
-                           _dense(top_p, _f32, b, dev, "top_p"), _dense(min_p, _f32, b, dev, "min_p"),
-                           _dense(u, _f32, b, dev, "u"), _dense(tokens, _i32, b, dev, "tokens"),
-                           None if probs is False else _dense(probs, _f32, b, dev, "probs"),
-                           None if kept is False else _dense(kept, _i32, b, dev, "kept"), _stream(stream, dev))
+        kept = torch.empty(b, dtype=torch.int32, device=dev)
+    st = (_native or _load()).sample(logits, temperature, top_k, top_p, min_p, u, tokens, probs, kept, stream)
     if st:
         _check(st)
     return tokens, None if probs is False else probs, None if kept is False else kept
