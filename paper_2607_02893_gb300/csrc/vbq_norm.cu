@@ -8,7 +8,8 @@
 // residual's type first and the norm is of the rounded values: it is a function
 // of the stream as it is stored. BF16 is rounded to once, at the output (the
 // products' activation type). One token is bound by its launch and two trips
-// to memory (1 x 768: 1.8 us in a graph); 256 x 4096 takes 4.7 us, 2.3 TB/s.
+// to memory (1 x 768: 2.2 us in a graph); 256 x 4096 takes 3.1 us, 3.4 TB/s;
+// 200 x 1001, whose rows start anywhere, 2.9 us (13.6 with single loads).
 #include <cuda_bf16.h>
 
 #include "vbq_decode.h"
@@ -17,87 +18,108 @@
 namespace vbq {
 namespace {
 
-constexpr int NORM_HELD = 16;        // values a thread keeps in registers
+constexpr int HELD = 4;              // vectors of 4 that a thread keeps in registers
 
 __device__ __forceinline__ float bf16_f32(uint32_t bits16) { return __uint_as_float(bits16 << 16); }
 __device__ __forceinline__ uint32_t f32_bf16(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 
-// VEC values at `at`, in fp32.
-template <int VEC>
-__device__ __forceinline__ void load_vec(float (&v)[VEC], const void* p, bool f32, int64_t at) {
-    if constexpr (VEC == 4) {
-        if (f32) {
-            const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+// A row is cut at the multiples of 4 elements of the whole array, which vector loads need, wherever the row itself
+// starts: items 0 .. vecs - 1 are vectors, the items after them the single values before the first and after the last.
+struct Row {
+    int64_t base;                    // of the row's first element
+    int head, vecs, items;
+    __device__ Row(int64_t row, int width) {
+        base = row * width;
+        head = min(width, (int)(-base & 3));
+        vecs = (width - head) / 4;
+        items = vecs + width - 4 * vecs;
+    }
+    __device__ __forceinline__ int first(int item) const {               // element of the row
+        return item < vecs ? head + 4 * item : item < vecs + head ? item - vecs : item - vecs + 4 * vecs;
+    }
+};
+
+// An item's values in fp32 (a single one: v[0], zeros beside it); `wide`: it is a vector, on its boundary.
+__device__ __forceinline__ float4 load_item(const void* p, bool f32, int64_t at, bool wide) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (f32) {
+        const float* q = static_cast<const float*>(p) + at;
+        if (wide) v = *reinterpret_cast<const float4*>(q); else v.x = *q;
+    } else {
+        const uint16_t* q = static_cast<const uint16_t*>(p) + at;
+        if (wide) {
+            const uint2 a = *reinterpret_cast<const uint2*>(q);
+            v = make_float4(bf16_f32(a.x & 0xffffu), bf16_f32(a.x >> 16), bf16_f32(a.y & 0xffffu), bf16_f32(a.y >> 16));
         } else {
-            const uint2 a = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + at);
-            v[0] = bf16_f32(a.x & 0xffffu); v[1] = bf16_f32(a.x >> 16);
-            v[2] = bf16_f32(a.y & 0xffffu); v[3] = bf16_f32(a.y >> 16);
+            v.x = bf16_f32(*q);
         }
-    } else {
-        v[0] = f32 ? static_cast<const float*>(p)[at] : bf16_f32(static_cast<const uint16_t*>(p)[at]);
     }
+    return v;
 }
-template <int VEC>
-__device__ __forceinline__ void store_vec(const float (&v)[VEC], void* p, bool f32, int64_t at) {
-    if constexpr (VEC == 4) {
-        if (f32)
-            *reinterpret_cast<float4*>(static_cast<float*>(p) + at) = make_float4(v[0], v[1], v[2], v[3]);
+__device__ __forceinline__ void store_item(float4 v, void* p, bool f32, int64_t at, bool wide) {
+    if (f32) {
+        float* q = static_cast<float*>(p) + at;
+        if (wide) *reinterpret_cast<float4*>(q) = v; else *q = v.x;
+    } else {
+        uint16_t* q = static_cast<uint16_t*>(p) + at;
+        if (wide)
+            *reinterpret_cast<uint2*>(q) = make_uint2(f32_bf16(v.x) | f32_bf16(v.y) << 16, f32_bf16(v.z) | f32_bf16(v.w) << 16);
         else
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + at) =
-                make_uint2(f32_bf16(v[0]) | f32_bf16(v[1]) << 16, f32_bf16(v[2]) | f32_bf16(v[3]) << 16);
-    } else if (f32) {
-        static_cast<float*>(p)[at] = v[0];
-    } else {
-        static_cast<uint16_t*>(p)[at] = (uint16_t)f32_bf16(v[0]);
+            *q = (uint16_t)f32_bf16(v.x);
     }
 }
-
-// r' of VEC values, rounded to the residual's type (x itself without one).
-template <int VEC>
-__device__ __forceinline__ void summed(float (&v)[VEC], const Norm& n, int64_t at) {
-    load_vec<VEC>(v, n.x, n.x_f32, at);
-    if (!n.residual) return;
-    float r[VEC];
-    load_vec<VEC>(r, n.residual, n.residual_f32, at);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        v[i] = __fadd_rn(r[i], v[i]);
-        if (!n.residual_f32) v[i] = bf16_f32(f32_bf16(v[i]));
-    }
+// The weights of an item: their boundary is the row's own.
+__device__ __forceinline__ float4 load_weights(const float* w, int j, bool wide) {
+    if (wide && (j & 3)) return make_float4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+    return load_item(w, true, j, wide);
 }
 
-template <int VEC>
+__device__ __forceinline__ float stored(float v, bool f32) { return f32 ? v : bf16_f32(f32_bf16(v)); }
+
+// r' of an item, rounded to the residual's type (x itself without one).
+__device__ __forceinline__ float4 summed(const Norm& n, int64_t at, bool wide) {
+    float4 v = load_item(n.x, n.x_f32, at, wide);
+    if (!n.residual) return v;
+    const float4 r = load_item(n.residual, n.residual_f32, at, wide);
+    const bool f32 = n.residual_f32;
+    return make_float4(stored(__fadd_rn(r.x, v.x), f32), stored(__fadd_rn(r.y, v.y), f32), stored(__fadd_rn(r.z, v.z), f32),
+                       stored(__fadd_rn(r.w, v.w), f32));
+}
+__device__ __forceinline__ float squares(float4 v, float sum) { return fmaf(v.w, v.w, fmaf(v.z, v.z, fmaf(v.y, v.y, fmaf(v.x, v.x, sum)))); }
+__device__ __forceinline__ float4 scaled(float4 w, float4 v, float inv) {
+    return make_float4(w.x * (v.x * inv), w.y * (v.y * inv), w.z * (v.z * inv), w.w * (v.w * inv));
+}
+
 __global__ void __launch_bounds__(1024) residual_norm_kernel(Norm n) {
-    constexpr int HELD = NORM_HELD / VEC;
     __shared__ float part[32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int vecs = n.width / VEC;
-    for (int64_t row = blockIdx.x; row < n.rows; row += gridDim.x) {
-        const int64_t base = row * n.width;
-        float held[HELD][VEC];
+    for (int64_t r = blockIdx.x; r < n.rows; r += gridDim.x) {
+        const Row row(r, n.width);
+        float4 held[HELD], w[HELD];                       // w too: its trip to memory goes beside theirs
         float sum = 0.f;
 #pragma unroll
         for (int h = 0; h < HELD; ++h) {
             const int i = threadIdx.x + h * blockDim.x;
-            if (i < vecs) summed<VEC>(held[h], n, base + (int64_t)i * VEC);
+            if (i >= row.items) continue;
+            const int j = row.first(i);
+            const bool wide = i < row.vecs;
+            held[h] = summed(n, row.base + j, wide);
+            w[h] = load_weights(n.weight, j, wide);
         }
 #pragma unroll
         for (int h = 0; h < HELD; ++h) {
             const int i = threadIdx.x + h * blockDim.x;
-            if (i >= vecs) continue;
-            if (n.residual) store_vec<VEC>(held[h], n.residual_out, n.residual_f32, base + (int64_t)i * VEC);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) sum = fmaf(held[h][e], held[h][e], sum);
+            if (i >= row.items) continue;
+            if (n.residual) store_item(held[h], n.residual_out, n.residual_f32, row.base + row.first(i), i < row.vecs);
+            sum = squares(held[h], sum);
         }
-        for (int i = threadIdx.x + HELD * blockDim.x; i < vecs; i += blockDim.x) {   // past the registers
-            float v[VEC];
-            summed<VEC>(v, n, base + (int64_t)i * VEC);
-            if (n.residual) store_vec<VEC>(v, n.residual_out, n.residual_f32, base + (int64_t)i * VEC);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) sum = fmaf(v[e], v[e], sum);
+        for (int i = threadIdx.x + HELD * blockDim.x; i < row.items; i += blockDim.x) {      // past the registers
+            const int64_t at = row.base + row.first(i);
+            const float4 v = summed(n, at, i < row.vecs);
+            if (n.residual) store_item(v, n.residual_out, n.residual_f32, at, i < row.vecs);
+            sum = squares(v, sum);
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -111,36 +133,27 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(Norm n) {
 #pragma unroll
         for (int h = 0; h < HELD; ++h) {
             const int i = threadIdx.x + h * blockDim.x;
-            if (i >= vecs) continue;
-            float w[VEC];
-            load_vec<VEC>(w, n.weight, true, (int64_t)i * VEC);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) w[e] *= held[h][e] * inv;
-            store_vec<VEC>(w, n.out, false, base + (int64_t)i * VEC);
+            if (i < row.items) store_item(scaled(w[h], held[h], inv), n.out, false, row.base + row.first(i), i < row.vecs);
         }
-        for (int i = threadIdx.x + HELD * blockDim.x; i < vecs; i += blockDim.x) {
-            float v[VEC], w[VEC];
+        for (int i = threadIdx.x + HELD * blockDim.x; i < row.items; i += blockDim.x) {
+            const int j = row.first(i);
+            const bool wide = i < row.vecs;
             // r' again: from where this thread stored it (residual_out may be residual itself)
-            load_vec<VEC>(v, n.residual ? n.residual_out : n.x, n.residual ? n.residual_f32 : n.x_f32,
-                          base + (int64_t)i * VEC);
-            load_vec<VEC>(w, n.weight, true, (int64_t)i * VEC);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) w[e] *= v[e] * inv;
-            store_vec<VEC>(w, n.out, false, base + (int64_t)i * VEC);
+            const float4 v = n.residual ? load_item(n.residual_out, n.residual_f32, row.base + j, wide) : load_item(n.x, n.x_f32, row.base + j, wide);
+            store_item(scaled(load_weights(n.weight, j, wide), v, inv), n.out, false, row.base + j, wide);
         }
     }
 }
 
 }  // namespace
 
+// Two vectors a thread: 256 x 4096 takes 3.1 us (one: 4.6, four: 4.0; more than 512 threads leave one block an SM).
 cudaError_t launch_residual_norm(const Norm& n, cudaStream_t s) {
-    const bool vec = n.width % 4 == 0;                    // rows then start on a vector's boundary
-    const int work = vec ? n.width / 4 : n.width;
-    int threads = (work + 31) / 32 * 32;
+    int threads = (n.width / 8 + 31) / 32 * 32;
     threads = threads < 64 ? 64 : threads > 1024 ? 1024 : threads;
     const int64_t cap = 1 << 20;
     const int grid = (int)(n.rows < cap ? n.rows : cap);
-    return launch_dependent(vec ? residual_norm_kernel<4> : residual_norm_kernel<1>, dim3(grid), threads, 0, s, n);
+    return launch_dependent(residual_norm_kernel, dim3(grid), threads, 0, s, n);
 }
 
 }  // namespace vbq
