@@ -42,6 +42,12 @@
 // segments form one list that is cut evenly, and a block may finish one segment
 // and start another. Parts are joined through the workspace by the block that
 // finishes a segment last, in block order, so results do not depend on timing.
+// With more segments than blocks, teams of a block's warps (1, 2, ... all of
+// them) may take whole segments instead, each team by itself: a segment's start
+// and join cost a block 5 us, and a list of short ones is a run of those. A
+// small cost model picks the team's size or the list, the same in every block.
+// Only calls that can have that many segments run the variant with teams: its
+// list is 4% slower (32 sequences of 16384: 106 us, 102 without).
 //
 // Measured (one GB300, in a graph): 8 sequences of 65536 tokens, 32 heads of 128
 // over 8: 99 us, 5.75 TB/s of cache. One of 32768: 17 us, of which 7 are the
@@ -49,10 +55,16 @@
 // sequences, 4096 keys a row: 20 us, bound by instruction issue. 100 keys, 12
 // heads of 64: 4.9 us, a chain of loads. 1022 warp instructions a page (d = 128,
 // 8 rows); 12 warps take 103 us where 8 take 108 and 16 take 118 (8 x 65536).
+// 64 sequences of up to 100 tokens, 32 heads over 8: 11 us (teams of 3; 14 by
+// single warps, 27 by blocks, 21 as a list); of up to 1000: 25 us (48, 35, 75);
+// 24 of up to 659, 5 rows, 24 heads over 12: 18 us (teams of 4; 41 as a list).
 #include <cuda_bf16.h>
+
+#include <algorithm>
 
 #include "vbq_decode.h"
 #include "vbq_device.cuh"
+#include "vbq_kernels.h"
 
 namespace vbq {
 namespace {
@@ -63,10 +75,12 @@ constexpr int CUT = 6;                           // pages a block takes at least
 constexpr int STRADDLE = 16;                     // pages whose time a block's second segment costs
 constexpr uint32_t LOW = 0x003c003cu, HIGH = 0x03c003c0u;    // codes at bits 2..5 and 6..9 of each half
 
-// D: head dimension, NT: 8-row tiles of query rows per pass, W: warps, S: stages per warp.
-template <int D_, int NT_, int W_, int S_>
+// D: head dimension, NT: 8-row tiles of query rows per pass, W: warps, S: stages per warp,
+// MANY: there may be more segments than blocks.
+template <int D_, int NT_, int W_, int S_, bool MANY_>
 struct Shape {
     static constexpr int D = D_, NT = NT_, W = W_, S = S_;
+    static constexpr bool MANY = MANY_;
     static constexpr int ROWS = 8 * NT;
     static constexpr int GR = D / 64;            // scale groups
     static constexpr int KW = D / 32;            // words of a key per lane
@@ -82,7 +96,8 @@ struct Shape {
     static_assert(W <= 16 && ROWS * 16 <= THREADS, "the join's first step");
     static_assert(KV_MAX_ROWS == 16, "16 lanes to a sequence");
     static constexpr int SPAN = CUM + (KV_MAX_BATCH + 2) * 8;    // first page and last key of each sequence
-    static constexpr int MISC = SPAN + KV_MAX_BATCH * 8;
+    static constexpr int FILLED = SPAN + KV_MAX_BATCH * 8;       // sequences with pages before each
+    static constexpr int MISC = FILLED + (MANY ? (KV_MAX_BATCH + 4) * 4 : 0);
     static constexpr int SMEM = MISC + 64 + 4 * W;
     static constexpr int PART = ROWS * D + 2 * ROWS;             // floats of a partial result
 };
@@ -91,6 +106,7 @@ struct Misc {
     int64_t quantum;
     int abort, last;
     int aligned;                                 // a block has one part of one segment
+    int team;                                    // warps that take a segment together, 0: none does
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -182,6 +198,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     float* factor = reinterpret_cast<float*>(smem + C::FACTOR);
     float2* joined = reinterpret_cast<float2*>(smem + C::FACTOR + W * C::ROWS * 4);
     int64_t* cum = reinterpret_cast<int64_t*>(smem + C::CUM);
+    int* filled = reinterpret_cast<int*>(smem + C::FILLED);
     int2* span = reinterpret_cast<int2*>(smem + C::SPAN);
     Misc* misc = reinterpret_cast<Misc*>(smem + C::MISC);
     int* kept_in = reinterpret_cast<int*>(smem + C::MISC + 64);          // where a warp's partial result is
@@ -218,7 +235,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
         span[b] = make_int2(lo / KV_PAGE, hi);
         cum[b + 1] = hi < 0 ? 0 : hi / KV_PAGE - lo / KV_PAGE + 1;
     }
-    if (tid == 0) cum[0] = 0;
+    if (tid == 0) {
+        cum[0] = 0;
+        if constexpr (C::MANY) filled[0] = 0;
+    }
     __syncthreads();
     if (warp == 0) {
         int64_t before = 0;
@@ -228,7 +248,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             const int b = b0 + lane;
             int64_t x = b < a.batch ? cum[b + 1] : 0;
             most = max(most, (int)x);
-            used += __popc(__ballot_sync(FULL, x > 0));
+            const uint32_t has = __ballot_sync(FULL, x > 0);
+            if constexpr (C::MANY)
+                if (b < a.batch) filled[b + 1] = used + __popc(has << (31 - lane));
+            used += __popc(has);
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int64_t y = __shfl_up_sync(FULL, x, o);
@@ -268,15 +291,38 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
                 quantum = fit;
             }
         }
+        int team = 0;
+        if constexpr (C::MANY) {
+            if (segments > blocks) {
+                // The cost in pages of a warp (2.8 us, mostly latency): of teams of t warps (lane t - 1) that take their
+                // segments one after another, each with its start and join (3.5 us, less for a warp alone); and of the
+                // list (lane W), where a block may have a run of the shortest segments (5 us each). Fitted to every team's
+                // time over eight sets of sequences; it picks the fastest or one within a tenth of it.
+                const uint32_t n = (uint32_t)segments, avg = (uint32_t)((float)total / (float)n + 0.999f), t = lane + 1;
+                float cost = INFINITY;
+                if (t <= W && W % t == 0) {
+                    const uint32_t teams = (uint32_t)blocks * (W / t), rounds = (n + teams - 1) / teams;
+                    cost = (float)((most + t - 1) / t) + (float)(rounds - 1) * ((avg + t - 1) / t) +
+                           (float)rounds * (t == 1 ? 0.5f : 1.25f + 0.04f * t);
+                }
+                if (lane == W)
+                    cost = (float)even / W + 2.f + 2.f * fminf((float)n / blocks * most / avg, (float)even);
+                const uint32_t least_cost = __reduce_min_sync(FULL, __float_as_uint(cost));
+                const int pick = __ffs(__ballot_sync(FULL, __float_as_uint(cost) == least_cost));
+                team = pick <= W ? pick : 0;
+            }
+        }
         if (lane == 0) {
             misc->quantum = quantum;
             misc->aligned = aligned;
+            misc->team = team;
         }
     }
     __syncthreads();
     const List list{cum, a.batch, c.kv_heads, per_seq};
     const int64_t quantum = misc->quantum;
     const bool aligned = misc->aligned;
+    const int team = C::MANY ? misc->team : 0;
     int64_t p0 = 0, p1 = 0;                       // the block's pages of the list
     int first_part = 0, parts_here = 0;           // aligned: the segment's blocks
     Segment s = {};
@@ -298,12 +344,32 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             }
             left -= n * per_seq;
         }
-    } else {
+    } else if (!C::MANY || team == 0) {
         const int64_t total = cum[a.batch] * per_seq;
         p0 = min(total, (int64_t)blockIdx.x * quantum);
         p1 = min(total, p0 + quantum);
         if (p0 < p1) s = list.at(p0);
     }
+
+    // Teams: the warp's place in its own, the team's segments (every so many of those with pages).
+    int member = 0;
+    int next = 0, every = 0, n_segments = 0;     // (below 2^31 segments)
+    if constexpr (C::MANY)
+        if (team != 0) {
+            n_segments = filled[a.batch] * per_seq;
+            member = warp % team;
+            next = (int)blockIdx.x * (W / team) + warp / team;
+            every = (int)gridDim.x * (W / team);
+        }
+    const auto nth = [&](int r) {
+        int b = 0, e = a.batch;                   // the last b with filled[b] * per_seq <= r
+#pragma unroll 1
+        while (e - b > 1) {
+            const int m = (b + e) >> 1;
+            if (filled[m] * per_seq <= r) b = m; else e = m;
+        }
+        return list.segment(b, r - filled[b] * per_seq);
+    };
 
     // Sequences without keys: zeros.
 #pragma unroll 1
@@ -319,23 +385,42 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     const uint8_t* src = nullptr;                 // lane i: of the page 32 * n + i
     uint32_t issued = 0, used = 0, landed = 0;    // landed: copies waited for
     bool ok = true;
+    int ahead_next = next;                        // teams: the next segment to copy, and the one being copied
+    int ahead = 0, ahead_end = 0;                 // (its next page and its pages)
+    const auto page_at = [&](const Segment& t, int64_t in) {             // the blob of a segment's page
+        int64_t page = c.table[t.b * c.table_stride + span[t.b].x + in];
+        if (page < 0 || page >= c.n_pages) {
+            atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
+            page = 0;
+        }
+        return c.pages + (page * c.kv_heads + t.h) * C::BLOB;
+    };
     auto issue = [&]() {                          // the next page's copy
-        if (issued >= mine || !ok) return;
-        if ((issued & 31) == 0) {
-            const uint32_t k = issued + lane;
-            if (k < mine) {
-                const int64_t p = p0 + warp + (int64_t)k * W;
-                const Segment t = p < s.start + s.pages ? s : list.at(p);
-                int64_t page = c.table[t.b * c.table_stride + span[t.b].x + (p - t.start)];
-                if (page < 0 || page >= c.n_pages) {
-                    atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
-                    page = 0;
+        if (!ok) return;
+        uint32_t from = issued;                   // the lane that knows the page
+        if (C::MANY && team != 0) {
+            while (ahead >= ahead_end) {          // (a short segment has no page for some of the team)
+                if (ahead_next >= n_segments) return;
+                ahead_end = (int)nth(ahead_next).pages;
+                ahead_next += every;
+                ahead = member;
+            }
+            from = (uint32_t)(ahead / team);
+            if ((from & 31) == 0 && ahead + lane * team < ahead_end) src = page_at(nth(ahead_next - every), ahead + lane * team);
+            ahead += team;
+        } else {
+            if (issued >= mine) return;
+            if ((issued & 31) == 0) {
+                const uint32_t k = issued + lane;
+                if (k < mine) {
+                    const int64_t p = p0 + warp + (int64_t)k * W;
+                    const Segment t = p < s.start + s.pages ? s : list.at(p);
+                    src = page_at(t, p - t.start);
                 }
-                src = c.pages + (page * c.kv_heads + t.h) * C::BLOB;
             }
         }
         const int st = (int)(issued % S);
-        if (lane == (int)(issued & 31))
+        if (lane == (int)(from & 31))
             bulk_load(sbase + (warp * S + st) * C::BLOB, src, C::BLOB, sbase + C::BARS + 8 * (warp * S + st));
         ++issued;
     };
@@ -369,11 +454,17 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
 #pragma unroll 1
     for (int i = 0; i < S; ++i) issue();
 
+    int64_t cur = p0;
 #pragma unroll 1
-    for (int64_t cur = p0; cur < p1;) {
-        if (cur != p0) s = list.at(cur);
+    while (C::MANY && team != 0 ? next < n_segments : cur < p1) {
+        if (C::MANY && team != 0) {
+            s = nth(next);
+            next += every;
+        } else if (cur != p0) {
+            s = list.at(cur);
+        }
         load_rows();
-        const int64_t end = min(p1, s.start + s.pages);
+        const int64_t end = C::MANY && team != 0 ? s.start + s.pages : min(p1, s.start + s.pages);
         const int hi_key = span[s.b].y, page0 = span[s.b].x;             // the sequence's last key and first page
 
         // Query fragments of the tile's rows, and the rows' parameters per accumulator column.
@@ -453,9 +544,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
         int vexp = -13;                           // value scales are taken in units of 2^(vexp - 14)
         bool any = false;
 
-        const int in_end = (int)(end - s.start);                         // pages from the segment's first
+        // The warp's pages of the segment, counted from the segment's first.
+        const int in_end = (int)(end - s.start), step = C::MANY && team != 0 ? team : W;
 #pragma unroll 1
-        for (int in = (int)(p0 + warp + (int64_t)used * W - s.start); in < in_end; in += W) {
+        for (int in = C::MANY && team != 0 ? member : (int)(p0 + warp + (int64_t)used * W - s.start); in < in_end; in += step) {
             any = true;
             const int st = (int)(used % S);
             const uint32_t stage = sbase + (warp * S + st) * C::BLOB;
@@ -627,7 +719,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
                         mma(ones[q][n], 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, b0[n], b1[n]);
                 }
             }
-            if (in + W < in_end) {                // refill the stage; the last of the segment is still needed
+            if (in + step < in_end) {             // refill the stage; the last of the segment is still needed
                 __syncwarp();
                 issue();
             }
@@ -664,6 +756,52 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
                 x += __shfl_xor_sync(FULL, x, 16);
                 if (g == 0) ml[warp * C::ROWS + 8 * n + 2 * t4 + i] = make_float2(m[n][i], x);
             }
+        const auto store = [&](int r, int dim, float4 v, float sum) {
+            const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;        // no keys: zeros; NaN stays
+            const __nv_bfloat162 x = __floats2bfloat162_rn(v.x * inv, v.y * inv), y = __floats2bfloat162_rn(v.z * inv, v.w * inv);
+            *reinterpret_cast<uint2*>(a.out + (((int64_t)s.b * a.rows + r / group) * a.heads + s.h * group + r % group) * D + dim) =
+                make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+        };
+        if constexpr (C::MANY)
+            if (team != 0) {
+                // Join the team: each thread the whole sum of a unit of 4 neighbouring dimensions.
+                const auto meet = [&] {
+                    if (team == 1) __syncwarp();
+                    else asm volatile("bar.sync %0, %1;" :: "r"(1 + warp / team), "r"(32 * team) : "memory");
+                };
+                meet();
+                const int w0 = warp - member;
+#pragma unroll 1
+                for (int u = 32 * member + lane; u < C::UNITS; u += 32 * team) {
+                    const int par = u >> 5 & 1, n = (u >> 6) % NT, qh = (u >> 6) / NT;
+                    const int row = 8 * n + 2 * (lane & 3) + par, r = s.rt * C::ROWS + row;
+                    if (r >= rows_all) continue;
+                    float mx = -INFINITY, sum = 0.f;
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+                    for (int w = w0; w < w0 + team; ++w) mx = fmaxf(mx, ml[w * C::ROWS + row].x);
+#pragma unroll 1
+                    for (int w = w0; w < w0 + team; ++w) {
+                        const float2 x = ml[w * C::ROWS + row];
+                        if (x.y == 0.f) continue;                        // no keys: its vector may be anything
+                        const float fw = ex2(x.x - mx);
+                        const float4 y = reinterpret_cast<const float4*>(smem + kept_in[w])[u];
+                        sum = fmaf(x.y, fw, sum);
+                        v.x = fmaf(y.x, fw, v.x);
+                        v.y = fmaf(y.y, fw, v.y);
+                        v.z = fmaf(y.z, fw, v.z);
+                        v.w = fmaf(y.w, fw, v.w);
+                    }
+                    store(r, 64 * (qh >> 1) + 8 * (lane >> 2) + 4 * (qh & 1), v, sum);
+                }
+                meet();
+                if (any) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    issue();
+                }
+                continue;
+            }
         __syncthreads();
 
         // Join the warps: first each warp's factor per row (16 lanes a row), then the rows, by units of 4 neighbouring
@@ -689,12 +827,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
         __syncthreads();
         const bool whole = s.start >= cur && s.start + s.pages <= end;
         const int64_t slot = aligned ? (int64_t)blockIdx.x : 2 * (int64_t)blockIdx.x + (s.start <= p0 ? 0 : 1);
-        const auto store = [&](int r, int dim, float4 v, float sum) {
-            const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;        // no keys: zeros; NaN stays
-            const __nv_bfloat162 x = __floats2bfloat162_rn(v.x * inv, v.y * inv), y = __floats2bfloat162_rn(v.z * inv, v.w * inv);
-            *reinterpret_cast<uint2*>(a.out + (((int64_t)s.b * a.rows + r / group) * a.heads + s.h * group + r % group) * D + dim) =
-                make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-        };
 #pragma unroll 1
         for (int u = tid; u < C::UNITS; u += C::THREADS) {
             const int ln = u & 31, par = u >> 5 & 1, n = (u >> 6) % NT, qh = (u >> 6) / NT;
@@ -783,11 +915,11 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             mbar_wait_bounded(sbase + C::BARS + 8 * (warp * S + (int)(landed % S)), (uint32_t)(landed / S) & 1u);
 }
 
-using Shape64a = Shape<64, 1, 12, 4>;
-using Shape64b = Shape<64, 2, 12, 4>;
-using Shape128a = Shape<128, 1, 12, 2>;
-using Shape128b = Shape<128, 2, 8, 3>;
-using Shape256a = Shape<256, 1, 6, 2>;
+template <bool MANY> using Shape64a = Shape<64, 1, 12, 4, MANY>;
+template <bool MANY> using Shape64b = Shape<64, 2, 12, 4, MANY>;
+template <bool MANY> using Shape128a = Shape<128, 1, 12, 2, MANY>;
+template <bool MANY> using Shape128b = Shape<128, 2, 8, 3, MANY>;
+template <bool MANY> using Shape256a = Shape<256, 1, 6, 2, MANY>;
 
 // Query rows per pass: 16 where there are more than 8 (the registers for 16
 // rows of 256 dimensions are not there).
@@ -795,12 +927,12 @@ int tile_rows(int rows, int head_dim) { return rows > 8 && head_dim <= 128 ? 16 
 
 // The same for every shape, so that a workspace's counts do not move between calls.
 size_t parts_bytes(int sms) {
-    constexpr size_t most = Shape128b::PART > Shape256a::PART ? Shape128b::PART : Shape256a::PART;
+    constexpr size_t most = std::max(Shape128b<false>::PART, Shape256a<false>::PART);
     return (2 * (size_t)sms * most * sizeof(float) + 255) / 256 * 256;
 }
 
 template <class C>
-cudaError_t launch(const KvView& c, const KvAttend& a, int row_tiles, cudaStream_t s) {
+cudaError_t launch_shape(const KvView& c, const KvAttend& a, int row_tiles, cudaStream_t s) {
     static LaunchPrep prep;
     int sms = 0;
     const cudaError_t e = prep.get(kv_attend_kernel<C>, C::SMEM, &sms);
@@ -808,6 +940,15 @@ cudaError_t launch(const KvView& c, const KvAttend& a, int row_tiles, cudaStream
     uint32_t* counts = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.workspace) + parts_bytes(sms));
     return launch_dependent(kv_attend_kernel<C>, dim3(sms), C::THREADS, C::SMEM, s, c, a, row_tiles, counts,
                             static_cast<float*>(a.workspace));
+}
+
+template <template <bool> class C>
+cudaError_t launch(const KvView& c, const KvAttend& a, int row_tiles, cudaStream_t s) {
+    int sms = 0;
+    const int e = device_sms(&sms);
+    if (e != 0) return (cudaError_t)e;
+    return (int64_t)a.batch * c.kv_heads * row_tiles > sms ? launch_shape<C<true>>(c, a, row_tiles, s)
+                                                          : launch_shape<C<false>>(c, a, row_tiles, s);
 }
 
 }  // namespace

@@ -417,3 +417,44 @@ def test_one_workspace_serves_every_shape():
                 p = (pos - torch.arange(rows, dtype=I32, device=DEV)).contiguous()
                 x, y = vbq.vbq_kv_attend(cache, table, p, q, workspace=ws), vbq.vbq_kv_attend(cache, table, p, q)
                 assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+
+
+@pytest.mark.parametrize("d,rows,heads,hk", [(64, 1, 6, 6), (64, 3, 12, 3), (128, 1, 16, 8), (128, 5, 9, 3), (256, 1, 8, 4),
+                                             (256, 3, 8, 2)], ids=str)
+@pytest.mark.parametrize("lens", ["short", "equal", "uneven", "one_long"])
+@pytest.mark.parametrize("window", [0, 90])
+def test_attend_segments_by_teams(d, rows, heads, hk, lens, window):
+    """More segments than blocks: by one warp, by a few, by all of a block's, and as a list that is cut."""
+    rng = np.random.default_rng(d + rows + len(lens) + window)
+    n = 460 // hk                                                 # sequences
+    if lens == "short":
+        lens = [int(x) for x in rng.integers(0, 70, n)]
+    elif lens == "equal":
+        lens = [330] * n
+    elif lens == "uneven":
+        lens = [int(x) for x in np.exp(rng.uniform(0, np.log(1500), n))]
+    else:
+        lens = [int(x) for x in rng.integers(1, 130, n)]
+        lens[n // 2] = 9000
+    cache, table, ks, vs = _fill(lens, hk, d, rng)
+    pos = np.array([[max(m - rows + t, -1) if m else -1 for t in range(rows)] for m in lens], np.int32)
+    pos[n // 3, 0] = -1
+    _check_attend(cache, table, ks, vs, pos, heads, rng, window=window)
+
+
+def test_attend_teams_report_pages_outside_the_cache():
+    """One sequence's page is outside: reported, and every other sequence has what it has without."""
+    rng = np.random.default_rng(33)
+    cache, table, ks, vs = _fill([200] * 100, 3, 128, rng)
+    pos = torch.full((100, 1), 199, dtype=I32, device=DEV)
+    q = torch.randn(100, 1, 6, 128, device=DEV).to(torch.bfloat16)
+    want = vbq.vbq_kv_attend(cache, table, pos, q)
+    assert vbq.vbq_device_status() is None
+    table[41, 2] = -3
+    got = vbq.vbq_kv_attend(cache, table, pos, q)
+    with pytest.raises(vbq.VbqError) as e:
+        vbq.vbq_device_status()
+    assert e.value.name == "VBQ_ERR_RANGE"
+    same = (got == want).flatten(1).all(1).cpu()
+    same[41] = True
+    assert bool(same.all())
