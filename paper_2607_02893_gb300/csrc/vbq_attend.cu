@@ -36,7 +36,9 @@
 //
 // A warp takes whole pages (64 keys of one head, one contiguous blob) through
 // its own ring of shared-memory stages filled by bulk copies: no barrier in the
-// steady state. The (sequence, row tile, head) segments are cut into parts of at
+// steady state. At 256 dimensions (17 KB a page) the keys' and the values'
+// halves of one stage are filled apart, each as soon as it is read, which makes
+// room for 8 warps: a page is a chain of 5 us that only more warps hide. The (sequence, row tile, head) segments are cut into parts of at
 // most `quantum` pages, one part per block and one block per SM, if that leaves
 // no block with much more than an even share; otherwise the pages of all
 // segments form one list that is cut evenly, and a block may finish one segment
@@ -58,6 +60,8 @@
 // 64 sequences of up to 100 tokens, 32 heads over 8: 11 us (teams of 3; 14 by
 // single warps, 27 by blocks, 21 as a list); of up to 1000: 25 us (48, 35, 75);
 // 24 of up to 659, 5 rows, 24 heads over 12: 18 us (teams of 4; 41 as a list).
+// 8 of 9000, 8 heads of 256 over 4: 26 us (30 by 6 warps with two whole stages
+// each; 6 warps with two stages in halves take 31).
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -76,10 +80,12 @@ constexpr int STRADDLE = 16;                     // pages whose time a block's s
 constexpr uint32_t LOW = 0x003c003cu, HIGH = 0x03c003c0u;    // codes at bits 2..5 and 6..9 of each half
 
 // D: head dimension, NT: 8-row tiles of query rows per pass, W: warps, S: stages per warp,
+// HALVES: a page's keys and its values are copied apart, each as soon as its half of the stage is read,
 // MANY: there may be more segments than blocks.
-template <int D_, int NT_, int W_, int S_, bool MANY_>
+template <int D_, int NT_, int W_, int S_, bool HALVES_, bool MANY_>
 struct Shape {
     static constexpr int D = D_, NT = NT_, W = W_, S = S_;
+    static constexpr bool HALVES = HALVES_;
     static constexpr bool MANY = MANY_;
     static constexpr int ROWS = 8 * NT;
     static constexpr int GR = D / 64;            // scale groups
@@ -90,10 +96,13 @@ struct Shape {
     static constexpr int UNITS = ROWS * D / 4;   // 4 outputs each
     // shared memory
     static constexpr int BARS = W * S * BLOB;                    // full barriers
-    static constexpr int ML = BARS + W * S * 8;                  // (maximum, sum) per warp and row
+    static constexpr int VBARS = BARS + (HALVES ? W * S * 8 : 0);   // of the values
+    static constexpr int ML = VBARS + W * S * 8;                 // (maximum, sum) per warp and row
     static constexpr int FACTOR = ML + W * ROWS * 8;             // a warp's factor per row, then (maximum, sum) per row
     static constexpr int CUM = FACTOR + W * ROWS * 4 + ROWS * 8; // pages before each sequence
     static_assert(W <= 16 && ROWS * 16 <= THREADS, "the join's first step");
+    static constexpr int KEPT = HALVES ? kv_values_at(D) : 0;    // a stage's place for a partial result
+    static_assert(KEPT + UNITS * 16 <= BLOB, "a partial result has room in a stage");
     static_assert(KV_MAX_ROWS == 16, "16 lanes to a sequence");
     static constexpr int SPAN = CUM + (KV_MAX_BATCH + 2) * 8;    // first page and last key of each sequence
     static constexpr int FILLED = SPAN + KV_MAX_BATCH * 8;       // sequences with pages before each
@@ -205,7 +214,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     const uint32_t abort_addr = sbase + C::MISC + 8;
     const int group = a.heads / c.kv_heads, rows_all = group * a.rows, per_seq = row_tiles * c.kv_heads;
 
-    if (tid < W * S) mbar_init(sbase + C::BARS + 8 * tid, 1);
+    if (tid < W * S) {
+        mbar_init(sbase + C::BARS + 8 * tid, C::HALVES ? 2 : 1);         // keys and scales
+        if constexpr (C::HALVES) mbar_init(sbase + C::VBARS + 8 * tid, 1);
+    }
     if (tid == 0) {
         misc->abort = 0;
         misc->last = 0;
@@ -384,6 +396,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     const uint32_t n_pages = (uint32_t)(p1 - p0), mine = n_pages / W + ((uint32_t)warp < n_pages % W);
     const uint8_t* src = nullptr;                 // lane i: of the page 32 * n + i
     uint32_t issued = 0, used = 0, landed = 0;    // landed: copies waited for
+    uint32_t v_issued = 0, v_landed = 0, last = 0;   // HALVES: the values' (one page behind at most); lane of the last page
     bool ok = true;
     int ahead_next = next;                        // teams: the next segment to copy, and the one being copied
     int ahead = 0, ahead_end = 0;                 // (its next page and its pages)
@@ -398,17 +411,22 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     auto issue = [&]() {                          // the next page's copy
         if (!ok) return;
         uint32_t from = issued;                   // the lane that knows the page
-        if (C::MANY && team != 0) {
-            while (ahead >= ahead_end) {          // (a short segment has no page for some of the team)
-                if (ahead_next >= n_segments) return;
-                ahead_end = (int)nth(ahead_next).pages;
-                ahead_next += every;
-                ahead = member;
+        bool listed = true;
+        if constexpr (C::MANY)
+            if (team != 0) {
+                while (ahead >= ahead_end) {      // (a short segment has no page for some of the team)
+                    if (ahead_next >= n_segments) return;
+                    ahead_end = (int)nth(ahead_next).pages;
+                    ahead_next += every;
+                    ahead = member;
+                }
+                from = (uint32_t)(ahead / team);
+                if ((from & 31) == 0 && ahead + lane * team < ahead_end)
+                    src = page_at(nth(ahead_next - every), ahead + lane * team);
+                ahead += team;
+                listed = false;
             }
-            from = (uint32_t)(ahead / team);
-            if ((from & 31) == 0 && ahead + lane * team < ahead_end) src = page_at(nth(ahead_next - every), ahead + lane * team);
-            ahead += team;
-        } else {
+        if (listed) {
             if (issued >= mine) return;
             if ((issued & 31) == 0) {
                 const uint32_t k = issued + lane;
@@ -420,9 +438,28 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             }
         }
         const int st = (int)(issued % S);
-        if (lane == (int)(from & 31))
+        if constexpr (C::HALVES) {
+            const uint32_t stage = sbase + (warp * S + st) * C::BLOB, bar = sbase + C::BARS + 8 * (warp * S + st);
+            if (lane == (int)(from & 31)) {
+                bulk_load(stage, src, kv_values_at(D), bar);
+                bulk_load(stage + kv_scales_at(D), src + kv_scales_at(D), C::BLOB - kv_scales_at(D), bar);
+            }
+            last = from & 31;
+        } else if (lane == (int)(from & 31)) {
             bulk_load(sbase + (warp * S + st) * C::BLOB, src, C::BLOB, sbase + C::BARS + 8 * (warp * S + st));
+        }
         ++issued;
+    };
+    auto issue_values = [&]() {                   // HALVES: of the page whose keys were copied last
+        if (!ok || v_issued == issued) return;
+        const int st = (int)(v_issued % S);
+        if (lane == (int)last)
+            bulk_load(sbase + (warp * S + st) * C::BLOB + kv_values_at(D), src + kv_values_at(D),
+                      kv_scales_at(D) - kv_values_at(D), sbase + C::VBARS + 8 * (warp * S + st));
+        ++v_issued;
+    };
+    auto refill = [&]() {                         // a stage whose last reads were a partial result's
+        if constexpr (C::HALVES) issue_values(); else issue();
     };
     // A segment's queries (16 bytes of each word of the lane's row) and, per accumulator column, its rows' positions.
     uint4 qw[NT][KW];
@@ -452,7 +489,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
         }
     }
 #pragma unroll 1
-    for (int i = 0; i < S; ++i) issue();
+    for (int i = 0; i < S; ++i) {
+        issue();
+        if constexpr (C::HALVES) issue_values();
+    }
 
     int64_t cur = p0;
 #pragma unroll 1
@@ -606,6 +646,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
                     }
                 }
             }
+            if constexpr (C::HALVES) {            // the keys' half is read
+                __syncwarp();
+                issue();
+            }
             if (key0 + KV_PAGE - 1 > close || key0 <= open) {            // some row does not attend to all of the page
 #pragma unroll
                 for (int sub = 0; sub < 4; ++sub)
@@ -677,6 +721,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             }
             const float vup = pow2(14 - vexp);
 
+            if constexpr (C::HALVES) {
+                if (!warp_wait(sbase + C::VBARS + 8 * (warp * S + st), (uint32_t)((used - 1) / S) & 1u, abort_addr)) {
+                    if (lane == 0) raise_abort(&misc->abort);
+                    ok = false;
+                    break;
+                }
+                v_landed = used;
+            }
 #pragma unroll
             for (int sub = 0; sub < 4; ++sub) {
                 uint32_t vw[4][GR];
@@ -721,7 +773,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             }
             if (in + step < in_end) {             // refill the stage; the last of the segment is still needed
                 __syncwarp();
-                issue();
+                refill();
             }
         }
 
@@ -729,7 +781,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
         if (!any && lane == 0) kept_in[warp] = -1;
         if (any) {
             const int st = (int)((used - 1) % S);
-            float4* buf = reinterpret_cast<float4*>(smem + (warp * S + st) * C::BLOB);
+            float4* buf = reinterpret_cast<float4*>(smem + (warp * S + st) * C::BLOB + C::KEPT);
             const float down = pow2(vexp - 14);
             __syncwarp();
 #pragma unroll
@@ -744,7 +796,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
                             make_float4((acc[k][n][par] * 0x1p18f - z) * down, (acc[k + 1][n][par] * 0x1p18f - z) * down,
                                         (acc[k][n][2 + par] * 0x1p18f - z) * down, (acc[k + 1][n][2 + par] * 0x1p18f - z) * down);
                     }
-            if (lane == 0) kept_in[warp] = (warp * S + st) * C::BLOB;
+            if (lane == 0) kept_in[warp] = (warp * S + st) * C::BLOB + C::KEPT;
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -798,7 +850,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
                 if (any) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                    issue();
+                    refill();
                 }
                 continue;
             }
@@ -904,22 +956,27 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
         if (any) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            issue();
+            refill();
         }
         cur = end;
     }
     // A wait that ran out: let every copy land before the block's memory goes.
-    if (!ok)
+    if (!ok) {
 #pragma unroll 1
         for (; landed < issued; ++landed)
             mbar_wait_bounded(sbase + C::BARS + 8 * (warp * S + (int)(landed % S)), (uint32_t)(landed / S) & 1u);
+        if constexpr (C::HALVES)
+#pragma unroll 1
+            for (; v_landed < v_issued; ++v_landed)
+                mbar_wait_bounded(sbase + C::VBARS + 8 * (warp * S + (int)(v_landed % S)), (uint32_t)(v_landed / S) & 1u);
+    }
 }
 
-template <bool MANY> using Shape64a = Shape<64, 1, 12, 4, MANY>;
-template <bool MANY> using Shape64b = Shape<64, 2, 12, 4, MANY>;
-template <bool MANY> using Shape128a = Shape<128, 1, 12, 2, MANY>;
-template <bool MANY> using Shape128b = Shape<128, 2, 8, 3, MANY>;
-template <bool MANY> using Shape256a = Shape<256, 1, 6, 2, MANY>;
+template <bool MANY> using Shape64a = Shape<64, 1, 12, 4, false, MANY>;
+template <bool MANY> using Shape64b = Shape<64, 2, 12, 4, false, MANY>;
+template <bool MANY> using Shape128a = Shape<128, 1, 12, 2, false, MANY>;
+template <bool MANY> using Shape128b = Shape<128, 2, 8, 3, false, MANY>;
+template <bool MANY> using Shape256a = Shape<256, 1, 8, 1, true, MANY>;
 
 // Query rows per pass: 16 where there are more than 8 (the registers for 16
 // rows of 256 dimensions are not there).
