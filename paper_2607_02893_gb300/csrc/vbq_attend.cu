@@ -81,12 +81,14 @@ constexpr uint32_t LOW = 0x003c003cu, HIGH = 0x03c003c0u;    // codes at bits 2.
 
 // D: head dimension, NT: 8-row tiles of query rows per pass, W: warps, S: stages per warp,
 // HALVES: a page's keys and its values are copied apart, each as soon as its half of the stage is read,
-// MANY: there may be more segments than blocks.
-template <int D_, int NT_, int W_, int S_, bool HALVES_, bool MANY_>
+// KIND: what the kernel is made for (see launch).
+enum Kind { PLAIN, TEAMS, SHARES };
+
+template <int D_, int NT_, int W_, int S_, bool HALVES_, Kind KIND_>
 struct Shape {
     static constexpr int D = D_, NT = NT_, W = W_, S = S_;
     static constexpr bool HALVES = HALVES_;
-    static constexpr bool MANY = MANY_;
+    static constexpr bool MANY = KIND_ == TEAMS, SHARED = KIND_ == SHARES;
     static constexpr int ROWS = 8 * NT;
     static constexpr int GR = D / 64;            // scale groups
     static constexpr int KW = D / 32;            // words of a key per lane
@@ -910,8 +912,25 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             __syncthreads();
             if (misc->last) {
                 if (tid == 0) counts[s.index] = 0;
+                // By units of 4 dimensions. Where the rows that there are leave threads over, and no copy is in flight (a
+                // block's one part), several threads to a unit share the parts: the loads are a chain of JOIN at a time.
+                const int live = min(C::ROWS, rows_all - s.rt * C::ROWS), units = live * (D / 4);
+                int shares = 1, each = n_parts;
+                if (C::SHARED && aligned && 2 * units <= C::THREADS && n_parts > JOIN) {
+                    shares = min(C::THREADS / units, (n_parts + JOIN - 1) / JOIN);
+                    each = (n_parts + shares - 1) / shares;
+                }
+                float4* ov = reinterpret_cast<float4*>(smem);
+                float2* om = reinterpret_cast<float2*>(smem + C::THREADS * 16);
 #pragma unroll 1
-        for (int u = tid; u < C::UNITS; u += C::THREADS) {
+                for (int i = tid; i < (C::SHARED && shares > 1 ? units * shares : C::UNITS); i += C::THREADS) {
+                    int u = i, ka = 0;
+                    if (C::SHARED && shares > 1) {
+                        const int share = i / units, at = i - share * units, d4 = at / live, row = at - d4 * live;
+                        u = (((2 * (d4 >> 4) + (d4 & 1)) * NT + (row >> 3)) * 2 + (row & 1)) * 32 + 4 * (d4 >> 1 & 7) + (row >> 1 & 3);
+                        ka = share * each;
+                    }
+                    const int kb = C::SHARED ? min(ka + each, n_parts) : n_parts;
                     const int ln = u & 31, par = u >> 5 & 1, n = (u >> 6) % NT, qh = (u >> 6) / NT;
                     const int row = 8 * n + 2 * (ln & 3) + par, dim = 64 * (qh >> 1) + 8 * (ln >> 2) + 4 * (qh & 1);
                     const int r = s.rt * C::ROWS + row;
@@ -919,16 +938,16 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
                     float mx = -INFINITY, sum = 0.f;
                     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-                    for (int k0 = 0; k0 < n_parts; k0 += JOIN) {         // JOIN parts' loads in flight
+                    for (int k0 = ka; k0 < kb; k0 += JOIN) {             // JOIN parts' loads in flight
                         float2 x[JOIN];
                         float4 y[JOIN];
 #pragma unroll
                         for (int j = 0; j < JOIN; ++j) {
-                            const int64_t k = b0 + min(k0 + j, n_parts - 1);
+                            const int64_t k = b0 + min(k0 + j, kb - 1);
                             const float* part = parts + (aligned ? k : 2 * k + (s.start <= k * quantum ? 0 : 1)) * C::PART;
                             x[j] = __ldcg(reinterpret_cast<const float2*>(part + C::ROWS * D) + row);
                             y[j] = __ldcg(reinterpret_cast<const float4*>(part) + u);
-                            if (k0 + j >= n_parts) x[j] = make_float2(-INFINITY, 0.f);
+                            if (k0 + j >= kb) x[j] = make_float2(-INFINITY, 0.f);
                         }
                         float mn = mx;
 #pragma unroll
@@ -948,7 +967,33 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
                             o.z = fmaf(y[j].z, fj, o.z); o.w = fmaf(y[j].w, fj, o.w);
                         }
                     }
-                    store(r, dim, o, sum);
+                    if (!C::SHARED || shares == 1) {
+                        store(r, dim, o, sum);
+                    } else {
+                        ov[i] = o;
+                        om[i] = make_float2(mx, sum);
+                    }
+                }
+                if (C::SHARED && shares > 1) {
+                    __syncthreads();
+#pragma unroll 1
+                    for (int at = tid; at < units; at += C::THREADS) {
+                        float mx = -INFINITY, sum = 0.f;
+                        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+                        for (int k = 0; k < shares; ++k) mx = fmaxf(mx, om[k * units + at].x);
+#pragma unroll 1
+                        for (int k = 0; k < shares; ++k) {
+                            const float2 x = om[k * units + at];
+                            if (x.y == 0.f) continue;
+                            const float4 y = ov[k * units + at];
+                            const float fk = ex2(x.x - mx);
+                            sum = fmaf(x.y, fk, sum);
+                            o.x = fmaf(y.x, fk, o.x); o.y = fmaf(y.y, fk, o.y);
+                            o.z = fmaf(y.z, fk, o.z); o.w = fmaf(y.w, fk, o.w);
+                        }
+                        store(s.rt * C::ROWS + at % live, 4 * (at / live), o, sum);
+                    }
                 }
             }
         }
@@ -972,11 +1017,11 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     }
 }
 
-template <bool MANY> using Shape64a = Shape<64, 1, 12, 4, false, MANY>;
-template <bool MANY> using Shape64b = Shape<64, 2, 12, 4, false, MANY>;
-template <bool MANY> using Shape128a = Shape<128, 1, 12, 2, false, MANY>;
-template <bool MANY> using Shape128b = Shape<128, 2, 8, 3, false, MANY>;
-template <bool MANY> using Shape256a = Shape<256, 1, 8, 1, true, MANY>;
+template <Kind KIND> using Shape64a = Shape<64, 1, 12, 4, false, KIND>;
+template <Kind KIND> using Shape64b = Shape<64, 2, 12, 4, false, KIND>;
+template <Kind KIND> using Shape128a = Shape<128, 1, 12, 2, false, KIND>;
+template <Kind KIND> using Shape128b = Shape<128, 2, 8, 3, false, KIND>;
+template <Kind KIND> using Shape256a = Shape<256, 1, 8, 1, true, KIND>;
 
 // Query rows per pass: 16 where there are more than 8 (the registers for 16
 // rows of 256 dimensions are not there).
@@ -984,7 +1029,7 @@ int tile_rows(int rows, int head_dim) { return rows > 8 && head_dim <= 128 ? 16 
 
 // The same for every shape, so that a workspace's counts do not move between calls.
 size_t parts_bytes(int sms) {
-    constexpr size_t most = std::max(Shape128b<false>::PART, Shape256a<false>::PART);
+    constexpr size_t most = std::max(Shape128b<PLAIN>::PART, Shape256a<PLAIN>::PART);
     return (2 * (size_t)sms * most * sizeof(float) + 255) / 256 * 256;
 }
 
@@ -999,13 +1044,23 @@ cudaError_t launch_shape(const KvView& c, const KvAttend& a, int row_tiles, cuda
                             static_cast<float*>(a.workspace));
 }
 
-template <template <bool> class C>
+// TEAMS where there may be more segments than blocks. SHARES where a segment may be cut into more than 2 JOIN parts and
+// its rows leave half of the threads over that join them. The code of either costs the others' loop over the pages 2 to 4%
+// (registers), so each is a kernel of its own. 32768 keys, 4 heads of 128 over 1: 13.0 us (17.6 without SHARES), 1 over
+// 1: 11.1 (17.5), 8 of 64 over 1: 11.7 (14.8); 54384 keys of 2 sequences, 6 heads of 256 over 3: 28.5 (32.2).
+template <template <Kind> class C>
 cudaError_t launch(const KvView& c, const KvAttend& a, int row_tiles, cudaStream_t s) {
     int sms = 0;
     const int e = device_sms(&sms);
     if (e != 0) return (cudaError_t)e;
-    return (int64_t)a.batch * c.kv_heads * row_tiles > sms ? launch_shape<C<true>>(c, a, row_tiles, s)
-                                                          : launch_shape<C<false>>(c, a, row_tiles, s);
+    const int64_t segments = (int64_t)a.batch * c.kv_heads * row_tiles;
+    const int rows = std::min(a.heads / c.kv_heads * a.rows, +C<PLAIN>::ROWS);
+    if (segments > sms) return launch_shape<C<TEAMS>>(c, a, row_tiles, s);
+    using P = C<PLAIN>;
+    if constexpr (2 * (P::ROWS - 7) * (P::D / 4) <= P::THREADS)          // for the fewest rows that take this shape
+        if (segments * 2 * JOIN < sms && 2 * rows * (P::D / 4) <= P::THREADS)
+            return launch_shape<C<SHARES>>(c, a, row_tiles, s);
+    return launch_shape<C<PLAIN>>(c, a, row_tiles, s);
 }
 
 }  // namespace

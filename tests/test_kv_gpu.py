@@ -458,3 +458,18 @@ def test_attend_teams_report_pages_outside_the_cache():
     same = (got == want).flatten(1).all(1).cpu()
     same[41] = True
     assert bool(same.all())
+
+
+@pytest.mark.parametrize("d,rows,heads,hk", [(64, 1, 1, 1), (64, 3, 4, 1), (64, 1, 5, 1), (128, 1, 4, 1), (128, 5, 2, 2), (128, 1, 3, 3),
+                                             (256, 1, 2, 1), (256, 2, 2, 2)], ids=str)
+@pytest.mark.parametrize("window", [0, 4000])
+def test_attend_many_parts_few_rows(d, rows, heads, hk, window):
+    """Few segments of few rows, cut into many parts; rows far apart, so that parts hold keys of some rows only; an unused row."""
+    rng = np.random.default_rng(d + 10 * rows + heads + window)
+    lens = [9000, 2500]
+    cache, table, ks, vs = _fill(lens, hk, d, rng)
+    pos = np.array([[n - 1 - 1500 * t for t in range(rows)] for n in lens], np.int32)
+    pos[1, rows // 2:] = -1 if rows > 1 else pos[1, rows // 2:]
+    pos = np.maximum(pos, -1)
+    _check_attend(cache, table, ks, vs, pos, heads, rng, window=window)
+    _check_attend(cache, table[:1], ks[:1], vs[:1], pos[:1], heads, rng, window=window)
