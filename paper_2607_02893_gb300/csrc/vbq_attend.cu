@@ -38,12 +38,15 @@
 // its own ring of shared-memory stages filled by bulk copies: no barrier in the
 // steady state. At 256 dimensions (17 KB a page) the keys' and the values'
 // halves of one stage are filled apart, each as soon as it is read, which makes
-// room for 8 warps: a page is a chain of 5 us that only more warps hide. The (sequence, row tile, head) segments are cut into parts of at
-// most `quantum` pages, one part per block and one block per SM, if that leaves
-// no block with much more than an even share; otherwise the pages of all
-// segments form one list that is cut evenly, and a block may finish one segment
-// and start another. Parts are joined through the workspace by the block that
-// finishes a segment last, in block order, so results do not depend on timing.
+// room for 8 warps: a page is a chain of 5 us that only more warps hide.
+//
+// The (sequence, row tile, head) segments are cut into parts of at most `quantum`
+// pages, one part per block and one block per SM, if that leaves no block with
+// much more than an even share (long segments by whole rounds of a block's warps:
+// fewer parts to join); otherwise the pages of all segments form one list that is
+// cut evenly, and a block may finish one segment and start another. Parts are
+// joined through the workspace by the block that finishes a segment last, in an
+// order of their own, so results do not depend on timing.
 // With more segments than blocks, teams of a block's warps (1, 2, ... all of
 // them) may take whole segments instead, each team by itself: a segment's start
 // and join cost a block 5 us, and a list of short ones is a run of those. A
@@ -57,7 +60,8 @@
 // sequences, 4096 keys a row: 20 us, bound by instruction issue. 100 keys, 12
 // heads of 64: 4.9 us, a chain of loads. 1022 warp instructions a page (d = 128,
 // 8 rows); 12 warps take 103 us where 8 take 108 and 16 take 118 (8 x 65536).
-// 64 sequences of up to 100 tokens, 32 heads over 8: 11 us (teams of 3; 14 by
+// One sequence of 32768, 16 heads over 2: 13.9 us (16.7 in parts of 7 pages
+// instead of 12). 64 sequences of up to 100 tokens, 32 heads over 8: 11 us (teams of 3; 14 by
 // single warps, 27 by blocks, 21 as a list); of up to 1000: 25 us (48, 35, 75);
 // 24 of up to 659, 5 rows, 24 heads over 12: 18 us (teams of 4; 41 as a list).
 // 8 of 9000, 8 heads of 256 over 4: 26 us (30 by 6 warps with two whole stages
@@ -303,6 +307,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             if (fit <= even + STRADDLE) {
                 aligned = 1;
                 quantum = fit;
+                if (most > 2 * JOIN * fit) {
+                    // Up to a whole round of the warps: a page more costs 0.13 us, a step of the join 0.44.
+                    const int round = (fit + W - 1) / W * W;
+                    const int steps = (parts_of(most, fit) + JOIN - 1) / JOIN - (parts_of(most, round) + JOIN - 1) / JOIN;
+                    if (10 * steps > 3 * (round - fit)) quantum = round;
+                }
             }
         }
         int team = 0;
