@@ -1034,8 +1034,16 @@ template <Kind KIND> using Shape128b = Shape<128, 2, 8, 3, false, KIND>;
 template <Kind KIND> using Shape256a = Shape<256, 1, 8, 1, true, KIND>;
 
 // Query rows per pass: 16 where there are more than 8 (the registers for 16
-// rows of 256 dimensions are not there).
-int tile_rows(int rows, int head_dim) { return rows > 8 && head_dim <= 128 ? 16 : 8; }
+// rows of 256 dimensions are not there). At 128 dimensions 5 passes of 8 cost
+// what 3 of 16 do, and start and join sooner: 24 rows in 3 passes of 8 take 52.8
+// us where 2 of 16 take 52.5 (8 x 8000 keys, 8 key heads) and 8.6 where they take
+// 11.0 (2000 keys, 4 key heads); 40 rows 77.1 and 76.9, 8.8 and 11.2; but 16 rows
+// in 2 of 8 take 37.4 where one of 16 takes 30.9. At 64 dimensions a pass of 16
+// is always cheaper (24 rows: 35.1 against 37.3).
+int tile_rows(int rows, int head_dim) {
+    const int by8 = (rows + 7) / 8, by16 = (rows + 15) / 16;
+    return by8 == 1 || head_dim > 128 || (head_dim == 128 && 3 * by8 <= 5 * by16) ? 8 : 16;
+}
 
 // The same for every shape, so that a workspace's counts do not move between calls.
 size_t parts_bytes(int sms) {
