@@ -197,6 +197,15 @@ __device__ __forceinline__ int parts_of(int64_t pages, int64_t quantum) {
     return (int)(((uint32_t)pages + (uint32_t)quantum - 1) / (uint32_t)quantum);     // a sequence has below 2^26 pages
 }
 
+// A part's pages, up to a whole round of the block's W warps if the join gains by it: a page more costs 0.13 us, a step of
+// the join 0.44. (Out of line: few calls come here, and the code in between is time at every start.)
+template <int W>
+__device__ __noinline__ int whole_rounds(int most, int pages) {
+    const int round = (pages + W - 1) / W * W;
+    const int steps = (parts_of(most, pages) + JOIN - 1) / JOIN - (parts_of(most, round) + JOIN - 1) / JOIN;
+    return 10 * steps > 3 * (round - pages) ? round : pages;
+}
+
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAttend a, int row_tiles, uint32_t* counts,
                                                                  float* parts) {
@@ -307,12 +316,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             if (fit <= even + STRADDLE) {
                 aligned = 1;
                 quantum = fit;
-                if (most > 2 * JOIN * fit) {
-                    // Up to a whole round of the warps: a page more costs 0.13 us, a step of the join 0.44.
-                    const int round = (fit + W - 1) / W * W;
-                    const int steps = (parts_of(most, fit) + JOIN - 1) / JOIN - (parts_of(most, round) + JOIN - 1) / JOIN;
-                    if (10 * steps > 3 * (round - fit)) quantum = round;
-                }
+                if (most > 2 * JOIN * fit) quantum = whole_rounds<W>(most, fit);
             }
         }
         int team = 0;
@@ -1076,7 +1080,7 @@ cudaError_t launch(const KvView& c, const KvAttend& a, int row_tiles, cudaStream
     if (segments > sms) return launch_shape<C<TEAMS>>(c, a, row_tiles, s);
     using P = C<PLAIN>;
     if constexpr (2 * (P::ROWS - 7) * (P::D / 4) <= P::THREADS)          // for the fewest rows that take this shape
-        if (segments * 2 * JOIN < sms && 2 * rows * (P::D / 4) <= P::THREADS)
+        if (segments * 2 * JOIN < sms && c.table_pages > 2 * JOIN * CUT && 2 * rows * (P::D / 4) <= P::THREADS)
             return launch_shape<C<SHARES>>(c, a, row_tiles, s);
     return launch_shape<C<PLAIN>>(c, a, row_tiles, s);
 }

@@ -14,28 +14,30 @@
 
 #include "vbq_decode.h"
 #include "vbq_device.cuh"
+#include "vbq_kernels.h"
 
 namespace vbq {
 namespace {
-
-constexpr int HELD = 4;              // vectors of 4 that a thread keeps in registers
 
 __device__ __forceinline__ float bf16_f32(uint32_t bits16) { return __uint_as_float(bits16 << 16); }
 __device__ __forceinline__ uint32_t f32_bf16(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 
 // A row is cut at the multiples of 4 elements of the whole array, which vector loads need, wherever the row itself
 // starts: items 0 .. vecs - 1 are vectors, the items after them the single values before the first and after the last.
+// EVEN: the width is a multiple of 4, so every row is vectors only.
+template <bool EVEN>
 struct Row {
     int64_t base;                    // of the row's first element
     int head, vecs, items;
     __device__ Row(int64_t row, int width) {
         base = row * width;
-        head = min(width, (int)(-base & 3));
+        head = EVEN ? 0 : min(width, (int)(-base & 3));
         vecs = (width - head) / 4;
-        items = vecs + width - 4 * vecs;
+        items = EVEN ? vecs : vecs + width - 4 * vecs;
     }
+    __device__ __forceinline__ bool wide(int item) const { return EVEN || item < vecs; }
     __device__ __forceinline__ int first(int item) const {               // element of the row
-        return item < vecs ? head + 4 * item : item < vecs + head ? item - vecs : item - vecs + 4 * vecs;
+        return EVEN ? 4 * item : item < vecs ? head + 4 * item : item < vecs + head ? item - vecs : item - vecs + 4 * vecs;
     }
 };
 
@@ -90,13 +92,15 @@ __device__ __forceinline__ float4 scaled(float4 w, float4 v, float inv) {
     return make_float4(w.x * (v.x * inv), w.y * (v.y * inv), w.z * (v.z * inv), w.w * (v.w * inv));
 }
 
+// HELD: the vectors of 4 that a thread keeps in registers. WHOLE: they are the whole row.
+template <bool EVEN, int HELD, bool WHOLE>
 __global__ void __launch_bounds__(1024) residual_norm_kernel(Norm n) {
     __shared__ float part[32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     for (int64_t r = blockIdx.x; r < n.rows; r += gridDim.x) {
-        const Row row(r, n.width);
+        const Row<EVEN> row(r, n.width);
         float4 held[HELD], w[HELD];                       // w too: its trip to memory goes beside theirs
         float sum = 0.f;
 #pragma unroll
@@ -104,7 +108,7 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(Norm n) {
             const int i = threadIdx.x + h * blockDim.x;
             if (i >= row.items) continue;
             const int j = row.first(i);
-            const bool wide = i < row.vecs;
+            const bool wide = row.wide(i);
             held[h] = summed(n, row.base + j, wide);
             w[h] = load_weights(n.weight, j, wide);
         }
@@ -112,13 +116,13 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(Norm n) {
         for (int h = 0; h < HELD; ++h) {
             const int i = threadIdx.x + h * blockDim.x;
             if (i >= row.items) continue;
-            if (n.residual) store_item(held[h], n.residual_out, n.residual_f32, row.base + row.first(i), i < row.vecs);
+            if (n.residual) store_item(held[h], n.residual_out, n.residual_f32, row.base + row.first(i), row.wide(i));
             sum = squares(held[h], sum);
         }
-        for (int i = threadIdx.x + HELD * blockDim.x; i < row.items; i += blockDim.x) {      // past the registers
+        for (int i = threadIdx.x + HELD * blockDim.x; !WHOLE && i < row.items; i += blockDim.x) {    // past the registers
             const int64_t at = row.base + row.first(i);
-            const float4 v = summed(n, at, i < row.vecs);
-            if (n.residual) store_item(v, n.residual_out, n.residual_f32, at, i < row.vecs);
+            const float4 v = summed(n, at, row.wide(i));
+            if (n.residual) store_item(v, n.residual_out, n.residual_f32, at, row.wide(i));
             sum = squares(v, sum);
         }
 #pragma unroll
@@ -133,11 +137,11 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(Norm n) {
 #pragma unroll
         for (int h = 0; h < HELD; ++h) {
             const int i = threadIdx.x + h * blockDim.x;
-            if (i < row.items) store_item(scaled(w[h], held[h], inv), n.out, false, row.base + row.first(i), i < row.vecs);
+            if (i < row.items) store_item(scaled(w[h], held[h], inv), n.out, false, row.base + row.first(i), row.wide(i));
         }
-        for (int i = threadIdx.x + HELD * blockDim.x; i < row.items; i += blockDim.x) {
+        for (int i = threadIdx.x + HELD * blockDim.x; !WHOLE && i < row.items; i += blockDim.x) {
             const int j = row.first(i);
-            const bool wide = i < row.vecs;
+            const bool wide = row.wide(i);
             // r' again: from where this thread stored it (residual_out may be residual itself)
             const float4 v = n.residual ? load_item(n.residual_out, n.residual_f32, row.base + j, wide) : load_item(n.x, n.x_f32, row.base + j, wide);
             store_item(scaled(load_weights(n.weight, j, wide), v, inv), n.out, false, row.base + j, wide);
@@ -147,13 +151,20 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(Norm n) {
 
 }  // namespace
 
-// Two vectors a thread: 256 x 4096 takes 3.1 us (one: 4.6, four: 4.0; more than 512 threads leave one block an SM).
 cudaError_t launch_residual_norm(const Norm& n, cudaStream_t s) {
+    int sms = 0;
+    const int err = device_sms(&sms);
+    if (err != 0) return (cudaError_t)err;
+    const int64_t cap = 1 << 20;
+    const dim3 grid((unsigned)(n.rows < cap ? n.rows : cap));
+    const bool even = n.width % 4 == 0;
+    if (even && n.rows <= sms && n.width <= 4096)
+        return launch_dependent(residual_norm_kernel<true, 1, true>, grid, (n.width / 4 + 31) / 32 * 32, 0, s, n);
     int threads = (n.width / 8 + 31) / 32 * 32;
     threads = threads < 64 ? 64 : threads > 1024 ? 1024 : threads;
-    const int64_t cap = 1 << 20;
-    const int grid = (int)(n.rows < cap ? n.rows : cap);
-    return launch_dependent(residual_norm_kernel, dim3(grid), threads, 0, s, n);
+    if (even && n.width <= 8 * threads) return launch_dependent(residual_norm_kernel<true, 2, true>, grid, threads, 0, s, n);
+    if (even) return launch_dependent(residual_norm_kernel<true, 4, false>, grid, threads, 0, s, n);
+    return launch_dependent(residual_norm_kernel<false, 4, false>, grid, threads, 0, s, n);
 }
 
 }  // namespace vbq
