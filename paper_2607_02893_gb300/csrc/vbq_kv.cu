@@ -13,7 +13,8 @@
 // neighbours in a warp: 16- or 32-byte loads, three shuffles for the maximum,
 // one 4-byte store. A decoded token is a few blocks of work (48 heads of 128:
 // 768 threads) and takes as long as a launch: 4.5 us in a graph with its read;
-// a prompt of 256 tokens moves 8 MB, 8.8 us with its read.
+// a prompt of 256 tokens moves 8 MB, 7.1 us with its read (8.8 with 64-bit
+// divisions and the partners of the rotation loaded after the position).
 #include <cuda_bf16.h>
 
 #include "vbq_decode.h"
@@ -77,40 +78,43 @@ __device__ __forceinline__ uint32_t code4(float x, float s, float inv) {
     return (uint32_t)(8 + (int)copysignf(k, x));
 }
 
-template <bool F32>
+// Index: an integer that holds the words of the call (64-bit divisions are long).
+template <bool F32, class Index>
 __global__ void __launch_bounds__(KA_THREADS) kv_append_kernel(KvView c, KvAppend a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int d = c.head_dim, chunks = d / 8;
+    const int d = c.head_dim, shift = __ffs(d) - 4, chunks = 1 << shift;   // d / 8, a power of two
     const int heads = a.q ? a.heads : 0;
     const int per_row = (heads + 2 * c.kv_heads) * chunks;                 // a multiple of 8
-    const int64_t total = (int64_t)a.batch * a.rows * per_row;
-    const int64_t step = (int64_t)gridDim.x * KA_THREADS;
-    for (int64_t i0 = (int64_t)blockIdx.x * KA_THREADS; i0 < total; i0 += step) {
-        int64_t i = i0 + threadIdx.x;
+    const Index total = (Index)((int64_t)a.batch * a.rows * per_row), step = (Index)gridDim.x * KA_THREADS;
+    for (Index i0 = (Index)blockIdx.x * KA_THREADS; i0 < total; i0 += step) {
+        Index i = i0 + (Index)threadIdx.x;
         const bool live = i < total;                                       // whole groups: total is a multiple of 8
         if (!live) i = total - 1;
-        const int64_t row = i / per_row;
+        const Index row = i / per_row;
         const int in_row = (int)(i - row * per_row);
-        const int vec = in_row / chunks, ch = in_row - vec * chunks;
+        const int vec = in_row >> shift, ch = in_row & (chunks - 1);
         const bool is_q = vec < heads, is_k = !is_q && vec < heads + c.kv_heads;
         const int h = is_q ? vec : is_k ? vec - heads : vec - heads - c.kv_heads;
         const void* src = is_q ? a.q : is_k ? a.k : a.v;
-        const int64_t at = row * (is_q ? a.q_stride : is_k ? a.k_stride : a.v_stride) + (int64_t)h * d;
+        const int64_t at = (int64_t)row * (is_q ? a.q_stride : is_k ? a.k_stride : a.v_stride) + (int64_t)h * d;
+        // The values and their partners in the rotation, then what depends on the position: two trips to memory.
         const int64_t p = a.pos[row];
+        const int half = a.rot_dim / 2;                                    // a multiple of 8
+        const bool rotated = a.cos && (is_q || is_k) && ch * 8 < a.rot_dim, first = ch * 8 < half;
+        const int j = first ? ch * 8 : ch * 8 - half;
+        float x[8], y[8];
+        load8<F32>(x, src, at + ch * 8);
+        if (rotated) load8<F32>(y, src, at + (first ? ch * 8 + half : j));
         bool ok = p >= 0;
         if (ok && ((a.cos && p >= a.rot_rows) || p >= (int64_t)c.table_pages * KV_PAGE)) {
             if (live) atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
             ok = false;
         }
-        float x[8];
-        load8<F32>(x, src, at + ch * 8);
-        if (ok && a.cos && (is_q || is_k) && ch * 8 < a.rot_dim) {
-            const int half = a.rot_dim / 2;                                // a multiple of 8
-            const bool first = ch * 8 < half;
-            const int j = first ? ch * 8 : ch * 8 - half;
-            float y[8], cs[8], sn[8];
-            load8<F32>(y, src, at + (first ? ch * 8 + half : j));
+        int64_t page = 0;
+        if (ok && !is_q) page = c.table[(int64_t)(row / a.rows) * c.table_stride + p / KV_PAGE];
+        if (ok && rotated) {
+            float cs[8], sn[8];
             load8<true>(cs, a.cos, p * half + j);
             load8<true>(sn, a.sin, p * half + j);
 #pragma unroll
@@ -121,7 +125,7 @@ __global__ void __launch_bounds__(KA_THREADS) kv_append_kernel(KvView c, KvAppen
         }
         if (is_q) {
             if (live)
-                *reinterpret_cast<uint4*>(a.q_out + (row * a.heads + h) * d + ch * 8) =
+                *reinterpret_cast<uint4*>(a.q_out + ((int64_t)row * a.heads + h) * d + ch * 8) =
                     ok ? make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]),
                                     bf16_pair(x[6], x[7]))
                        : make_uint4(0, 0, 0, 0);
@@ -132,7 +136,6 @@ __global__ void __launch_bounds__(KA_THREADS) kv_append_kernel(KvView c, KvAppen
 #pragma unroll
         for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         if (is_q || !ok || !live) continue;
-        int64_t page = c.table[(row / a.rows) * c.table_stride + p / KV_PAGE];
         if (page < 0 || page >= c.n_pages) {
             atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
             continue;
@@ -159,17 +162,18 @@ __global__ void __launch_bounds__(KA_THREADS) kv_append_kernel(KvView c, KvAppen
 
 // The inverse: what the cache holds for (sequence, position) rows, in fp32.
 // Rows with a negative position, or one outside the cache, give zeros.
+template <class Index>
 __global__ void __launch_bounds__(KA_THREADS) kv_read_kernel(KvView c, const int32_t* pos, int batch, int rows,
                                                              float* k_out, float* v_out) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int d = c.head_dim, chunks = d / 8;
+    const int d = c.head_dim, shift = __ffs(d) - 4, chunks = 1 << shift;
     const int per_row = 2 * c.kv_heads * chunks;
-    const int64_t total = (int64_t)batch * rows * per_row;
-    for (int64_t i = (int64_t)blockIdx.x * KA_THREADS + threadIdx.x; i < total; i += (int64_t)gridDim.x * KA_THREADS) {
-        const int64_t row = i / per_row;
+    const Index total = (Index)((int64_t)batch * rows * per_row), step = (Index)gridDim.x * KA_THREADS;
+    for (Index i = (Index)blockIdx.x * KA_THREADS + (Index)threadIdx.x; i < total; i += step) {
+        const Index row = i / per_row;
         const int in_row = (int)(i - row * per_row);
-        const int vec = in_row / chunks, ch = in_row - vec * chunks;
+        const int vec = in_row >> shift, ch = in_row & (chunks - 1);
         const bool is_k = vec < c.kv_heads;
         const int h = is_k ? vec : vec - c.kv_heads;
         float* out = is_k ? k_out : v_out;
@@ -179,7 +183,7 @@ __global__ void __launch_bounds__(KA_THREADS) kv_read_kernel(KvView c, const int
         uint32_t w = 0;
         if (p >= 0) {
             int64_t page = -1;
-            if (p < (int64_t)c.table_pages * KV_PAGE) page = c.table[(row / rows) * c.table_stride + p / KV_PAGE];
+            if (p < (int64_t)c.table_pages * KV_PAGE) page = c.table[(int64_t)(row / rows) * c.table_stride + p / KV_PAGE];
             if (page < 0 || page >= c.n_pages) {
                 atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
             } else {
@@ -198,11 +202,13 @@ __global__ void __launch_bounds__(KA_THREADS) kv_read_kernel(KvView c, const int
         if (s == 0.f)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = 0.f;                        // no -0
-        float4* o = reinterpret_cast<float4*>(out + (row * c.kv_heads + h) * d + ch * 8);
+        float4* o = reinterpret_cast<float4*>(out + ((int64_t)row * c.kv_heads + h) * d + ch * 8);
         o[0] = make_float4(x[0], x[1], x[2], x[3]);
         o[1] = make_float4(x[4], x[5], x[6], x[7]);
     }
 }
+
+constexpr int64_t SHORT = 1 << 30;           // below it an int holds a call's words and a step past them
 
 int grid_for(int64_t threads, int sms) {
     const int64_t want = (threads + KA_THREADS - 1) / KA_THREADS, cap = (int64_t)sms * 16;
@@ -222,8 +228,10 @@ cudaError_t launch_kv_append(const KvView& c, const KvAppend& a, cudaStream_t s)
     const cudaError_t e = sm_count(&sms);
     if (e != cudaSuccess) return e;
     const int64_t total = (int64_t)a.batch * a.rows * ((a.q ? a.heads : 0) + 2 * c.kv_heads) * (c.head_dim / 8);
-    return launch_dependent(a.f32 ? kv_append_kernel<true> : kv_append_kernel<false>, dim3(grid_for(total, sms)),
-                            KA_THREADS, 0, s, c, a);
+    const dim3 grid(grid_for(total, sms));
+    const auto go = [&](auto kernel) { return launch_dependent(kernel, grid, KA_THREADS, 0, s, c, a); };
+    if (total < SHORT) return a.f32 ? go(kv_append_kernel<true, int>) : go(kv_append_kernel<false, int>);
+    return a.f32 ? go(kv_append_kernel<true, int64_t>) : go(kv_append_kernel<false, int64_t>);
 }
 
 cudaError_t launch_kv_read(const KvView& c, const int32_t* pos, int batch, int rows, float* k_out, float* v_out,
@@ -232,8 +240,9 @@ cudaError_t launch_kv_read(const KvView& c, const int32_t* pos, int batch, int r
     const cudaError_t e = sm_count(&sms);
     if (e != cudaSuccess) return e;
     const int64_t total = (int64_t)batch * rows * 2 * c.kv_heads * (c.head_dim / 8);
-    return launch_dependent(kv_read_kernel, dim3(grid_for(total, sms)), KA_THREADS, 0, s, c, pos, batch, rows, k_out,
-                            v_out);
+    const dim3 grid(grid_for(total, sms));
+    const auto go = [&](auto kernel) { return launch_dependent(kernel, grid, KA_THREADS, 0, s, c, pos, batch, rows, k_out, v_out); };
+    return total < SHORT ? go(kv_read_kernel<int>) : go(kv_read_kernel<int64_t>);
 }
 
 cudaError_t read_device_status_kv(uint32_t* status) {

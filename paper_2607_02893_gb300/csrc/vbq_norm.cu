@@ -7,9 +7,15 @@
 // and the warps, so results do not vary between calls. r' is rounded to the
 // residual's type first and the norm is of the rounded values: it is a function
 // of the stream as it is stored. BF16 is rounded to once, at the output (the
-// products' activation type). One token is bound by its launch and two trips
-// to memory (1 x 768: 2.2 us in a graph); 256 x 4096 takes 3.1 us, 3.4 TB/s;
-// 200 x 1001, whose rows start anywhere, 2.9 us (13.6 with single loads).
+// products' activation type).
+//
+// One token is bound by its launch, two trips to memory and, between the other
+// kernels of a decode step, by fetching its instructions: kernels that know the
+// types, and that every row is whole vectors and fits the registers, have few of
+// them (1 x 768: 1.2 us in a graph, 2.2 by one kernel for everything; a step of
+// 22 layers of width 2048, 45 norms: 712 us against 784). 256 x 4096 takes 2.7
+// us, 3.9 TB/s; 200 x 1001, whose rows start anywhere, 2.9 us (13.6 with single
+// loads).
 #include <cuda_bf16.h>
 
 #include "vbq_decode.h"
@@ -18,6 +24,8 @@
 
 namespace vbq {
 namespace {
+
+enum Type { ANY, NONE, F32, BF16 };
 
 __device__ __forceinline__ float bf16_f32(uint32_t bits16) { return __uint_as_float(bits16 << 16); }
 __device__ __forceinline__ uint32_t f32_bf16(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
@@ -79,9 +87,9 @@ __device__ __forceinline__ float4 load_weights(const float* w, int j, bool wide)
 __device__ __forceinline__ float stored(float v, bool f32) { return f32 ? v : bf16_f32(f32_bf16(v)); }
 
 // r' of an item, rounded to the residual's type (x itself without one).
-__device__ __forceinline__ float4 summed(const Norm& n, int64_t at, bool wide) {
+__device__ __forceinline__ float4 summed(const Norm& n, bool adds, int64_t at, bool wide) {
     float4 v = load_item(n.x, n.x_f32, at, wide);
-    if (!n.residual) return v;
+    if (!adds) return v;
     const float4 r = load_item(n.residual, n.residual_f32, at, wide);
     const bool f32 = n.residual_f32;
     return make_float4(stored(__fadd_rn(r.x, v.x), f32), stored(__fadd_rn(r.y, v.y), f32), stored(__fadd_rn(r.z, v.z), f32),
@@ -93,8 +101,13 @@ __device__ __forceinline__ float4 scaled(float4 w, float4 v, float inv) {
 }
 
 // HELD: the vectors of 4 that a thread keeps in registers. WHOLE: they are the whole row.
-template <bool EVEN, int HELD, bool WHOLE>
+// X, R: the types of x and of the residual, if known.
+template <bool EVEN, int HELD, bool WHOLE, Type X = ANY, Type R = ANY>
 __global__ void __launch_bounds__(1024) residual_norm_kernel(Norm n) {
+    if constexpr (X != ANY) n.x_f32 = X == F32;
+    if constexpr (R != ANY) n.residual_f32 = R == F32;
+    if constexpr (R == NONE) n.residual = nullptr;
+    const bool adds = R == ANY ? n.residual != nullptr : R != NONE;
     __shared__ float part[32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -109,20 +122,20 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(Norm n) {
             if (i >= row.items) continue;
             const int j = row.first(i);
             const bool wide = row.wide(i);
-            held[h] = summed(n, row.base + j, wide);
+            held[h] = summed(n, adds, row.base + j, wide);
             w[h] = load_weights(n.weight, j, wide);
         }
 #pragma unroll
         for (int h = 0; h < HELD; ++h) {
             const int i = threadIdx.x + h * blockDim.x;
             if (i >= row.items) continue;
-            if (n.residual) store_item(held[h], n.residual_out, n.residual_f32, row.base + row.first(i), row.wide(i));
+            if (adds) store_item(held[h], n.residual_out, n.residual_f32, row.base + row.first(i), row.wide(i));
             sum = squares(held[h], sum);
         }
         for (int i = threadIdx.x + HELD * blockDim.x; !WHOLE && i < row.items; i += blockDim.x) {    // past the registers
             const int64_t at = row.base + row.first(i);
-            const float4 v = summed(n, at, row.wide(i));
-            if (n.residual) store_item(v, n.residual_out, n.residual_f32, at, row.wide(i));
+            const float4 v = summed(n, adds, at, row.wide(i));
+            if (adds) store_item(v, n.residual_out, n.residual_f32, at, row.wide(i));
             sum = squares(v, sum);
         }
 #pragma unroll
@@ -143,14 +156,23 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(Norm n) {
             const int j = row.first(i);
             const bool wide = row.wide(i);
             // r' again: from where this thread stored it (residual_out may be residual itself)
-            const float4 v = n.residual ? load_item(n.residual_out, n.residual_f32, row.base + j, wide) : load_item(n.x, n.x_f32, row.base + j, wide);
+            const float4 v = adds ? load_item(n.residual_out, n.residual_f32, row.base + j, wide) : load_item(n.x, n.x_f32, row.base + j, wide);
             store_item(scaled(load_weights(n.weight, j, wide), v, inv), n.out, false, row.base + j, wide);
         }
     }
 }
 
+template <int HELD, Type X>
+cudaError_t launch_known(const Norm& n, dim3 grid, int threads, cudaStream_t s) {
+    if (!n.residual) return launch_dependent(residual_norm_kernel<true, HELD, true, X, NONE>, grid, threads, 0, s, n);
+    return n.residual_f32 ? launch_dependent(residual_norm_kernel<true, HELD, true, X, F32>, grid, threads, 0, s, n)
+                          : launch_dependent(residual_norm_kernel<true, HELD, true, X, BF16>, grid, threads, 0, s, n);
+}
+
 }  // namespace
 
+// One vector a thread where every row has an SM, else two (256 x 4096: 2.7 us; one 4.6, four 4.0; more than 512 threads
+// leave one block an SM).
 cudaError_t launch_residual_norm(const Norm& n, cudaStream_t s) {
     int sms = 0;
     const int err = device_sms(&sms);
@@ -158,11 +180,14 @@ cudaError_t launch_residual_norm(const Norm& n, cudaStream_t s) {
     const int64_t cap = 1 << 20;
     const dim3 grid((unsigned)(n.rows < cap ? n.rows : cap));
     const bool even = n.width % 4 == 0;
-    if (even && n.rows <= sms && n.width <= 4096)
-        return launch_dependent(residual_norm_kernel<true, 1, true>, grid, (n.width / 4 + 31) / 32 * 32, 0, s, n);
+    if (even && n.rows <= sms && n.width <= 4096) {
+        const int threads = (n.width / 4 + 31) / 32 * 32;
+        return n.x_f32 ? launch_known<1, F32>(n, grid, threads, s) : launch_known<1, BF16>(n, grid, threads, s);
+    }
     int threads = (n.width / 8 + 31) / 32 * 32;
     threads = threads < 64 ? 64 : threads > 1024 ? 1024 : threads;
-    if (even && n.width <= 8 * threads) return launch_dependent(residual_norm_kernel<true, 2, true>, grid, threads, 0, s, n);
+    if (even && n.width <= 8 * threads)
+        return n.x_f32 ? launch_known<2, F32>(n, grid, threads, s) : launch_known<2, BF16>(n, grid, threads, s);
     if (even) return launch_dependent(residual_norm_kernel<true, 4, false>, grid, threads, 0, s, n);
     return launch_dependent(residual_norm_kernel<false, 4, false>, grid, threads, 0, s, n);
 }
