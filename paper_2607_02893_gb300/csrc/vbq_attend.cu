@@ -83,11 +83,11 @@ constexpr int CUT = 6;                           // pages a block takes at least
 constexpr int STRADDLE = 16;                     // pages whose time a block's second segment costs
 constexpr uint32_t LOW = 0x003c003cu, HIGH = 0x03c003c0u;    // codes at bits 2..5 and 6..9 of each half
 
+enum Kind { PLAIN, TEAMS, SHARES };              // when which: at launch
+
 // D: head dimension, NT: 8-row tiles of query rows per pass, W: warps, S: stages per warp,
 // HALVES: a page's keys and its values are copied apart, each as soon as its half of the stage is read,
-// KIND: what the kernel is made for (see launch).
-enum Kind { PLAIN, TEAMS, SHARES };
-
+// KIND: what the kernel is made for.
 template <int D_, int NT_, int W_, int S_, bool HALVES_, Kind KIND_>
 struct Shape {
     static constexpr int D = D_, NT = NT_, W = W_, S = S_;
@@ -1068,7 +1068,8 @@ cudaError_t launch_shape(const KvView& c, const KvAttend& a, int row_tiles, cuda
 
 // TEAMS where there may be more segments than blocks. SHARES where a segment may be cut into more than 2 JOIN parts and
 // its rows leave half of the threads over that join them. The code of either costs the others' loop over the pages 2 to 4%
-// (registers), so each is a kernel of its own. 32768 keys, 4 heads of 128 over 1: 13.0 us (17.6 without SHARES), 1 over
+// (registers), and 0.5 us of instructions that come cold between the other kernels of a decode step (12 layers: 387
+// against 378 us a step), so each is a kernel of its own. 32768 keys, 4 heads of 128 over 1: 13.0 us (17.6 without SHARES), 1 over
 // 1: 11.1 (17.5), 8 of 64 over 1: 11.7 (14.8); 54384 keys of 2 sequences, 6 heads of 256 over 3: 28.5 (32.2).
 template <template <Kind> class C>
 cudaError_t launch(const KvView& c, const KvAttend& a, int row_tiles, cudaStream_t s) {
