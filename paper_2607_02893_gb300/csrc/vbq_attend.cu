@@ -667,6 +667,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
                 issue();
             }
             if (key0 + KV_PAGE - 1 > close || key0 <= open) {            // some row does not attend to all of the page
+                uint32_t seen = 0;                // bit 2 sub + x: a row attends to the lane's key
 #pragma unroll
                 for (int sub = 0; sub < 4; ++sub)
 #pragma unroll
@@ -675,13 +676,24 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
-                            for (int i = 0; i < 2; ++i)
+                            for (int i = 0; i < 2; ++i) {
                                 if (key > min(pos[n][i], hi_key) || (a.window > 0 && key <= pos[n][i] - a.window))
                                     sc[sub][n][2 * x + i] = -INFINITY;
-                        if (key > hi_key)         // what was never written may be anything
+                                else if (s.rt * C::ROWS + 8 * n + 2 * t4 + i < rows_all)
+                                    seen |= 1u << (2 * sub + x);
+                            }
+                    }
+                // A key that no row attends to (after the last, before a window, between two) may never have been
+                // written: a probability of 0 times a scale that is NaN would be NaN, and a large one would raise vexp.
+                seen |= __shfl_xor_sync(FULL, seen, 1);
+                seen |= __shfl_xor_sync(FULL, seen, 2);
+#pragma unroll
+                for (int sub = 0; sub < 4; ++sub)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+                        if (!(seen >> (2 * sub + x) & 1))
 #pragma unroll
                             for (int q = 0; q < (GR + 1) / 2; ++q) vs[sub][x][q] = 0;
-                    }
             }
 
             // Running maximum per row, running power of two of the value scales.
