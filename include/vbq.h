@@ -388,8 +388,8 @@ enum { VBQ_BF16 = 0, VBQ_F32 = 1 };
  * given as batch x rows positions `pos` (row (b, t) is a token of sequence b);
  * a negative position marks an unused row. A position or page outside the
  * cache is not touched: such a row is skipped (append), reads as zeros (read)
- * or gives an undefined output (attend), and vbq_device_status reports
- * VBQ_ERR_RANGE.
+ * or gives an undefined output (attend; other rows, of the same sequence too,
+ * are not affected), and vbq_device_status reports VBQ_ERR_RANGE.
  */
 typedef struct vbq_kv_cache {
     void*   pages;       /* device, n_pages * page bytes */

@@ -246,18 +246,18 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
 #pragma unroll 1
     for (int b0 = 0; b0 < a.batch; b0 += C::THREADS / KV_MAX_ROWS) {     // a lane per row, 16 to a sequence
         const int b = b0 + tid / KV_MAX_ROWS, t = tid % KV_MAX_ROWS;
-        int hi = b < a.batch && t < a.rows ? a.pos[b * a.rows + t] : -1, mn = hi >= 0 ? hi : 0x7fffffff;
+        int hi = b < a.batch && t < a.rows ? a.pos[b * a.rows + t] : -1;
+        if (hi >= table_keys) {                   // outside the cache: as an unused row
+            if (blockIdx.x == 0) atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
+            hi = -1;
+        }
+        int mn = hi >= 0 ? hi : 0x7fffffff;
 #pragma unroll
         for (int o = 1; o < KV_MAX_ROWS; o <<= 1) {
             hi = max(hi, __shfl_xor_sync(FULL, hi, o));
             mn = min(mn, __shfl_xor_sync(FULL, mn, o));
         }
         if (t != 0 || b >= a.batch) continue;
-        if (hi >= table_keys) {
-            if (blockIdx.x == 0) atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
-            hi = (int)(table_keys - 1);
-            mn = min(mn, hi);
-        }
         const int lo = hi >= 0 && a.window > 0 && mn >= a.window ? mn - a.window + 1 : 0;
         span[b] = make_int2(lo / KV_PAGE, hi);
         cum[b + 1] = hi < 0 ? 0 : hi / KV_PAGE - lo / KV_PAGE + 1;
@@ -494,6 +494,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
             for (int i = 0; i < 2; ++i) {
                 const int rc = s.rt * C::ROWS + 8 * n + 2 * t4 + i;
                 pos[n][i] = rc < rows_all ? a.pos[s.b * a.rows + rc / group] : 0x7fffffff;
+                if (rc < rows_all && pos[n][i] > span[s.b].y) pos[n][i] = -1;      // outside the cache
             }
         }
     };

@@ -81,3 +81,33 @@ def test_only_the_window_of_many_short_sequences(junk):
     ends = [int(n) for n in rng.integers(90, 700, 230)]
     cache, table, ks, vs = _written([[(n - 80, n)] for n in ends], 2, 64, junk, rng)
     _check_attend(cache, table, ks, vs, np.array([[n - 1] for n in ends], np.int32), 4, rng, window=80)
+
+
+def _expect_range():
+    with pytest.raises(vbq.VbqError) as e:
+        vbq.vbq_device_status()
+    assert e.value.name == "VBQ_ERR_RANGE"
+
+
+def _row_ok(out, q, row, k, v, p, scale, window=0):
+    """Row `row` of the first sequence within the bound of the oracle's, at position p."""
+    kd, ksc = _held(k)
+    vd, vsc = _held(v)
+    ref, spread, reach = o.attend(q[0, row:row + 1].float().cpu().numpy(), kd, vd, [p], scale, window, ksc)
+    got = out[0, row:row + 1].float().cpu().numpy().astype(np.float64)
+    return bool(o.attend_within_bound(got, ref, spread, reach, 8 * float(vsc.max()), len(k)).all())
+
+
+@pytest.mark.parametrize("junk", JUNK)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("window", [0, 40])
+def test_a_position_outside_leaves_the_sequence_s_other_rows_alone(junk, d, window):
+    """The table ends in pages that hold nothing; one row's position lies past them."""
+    rng = np.random.default_rng(junk + d + window)
+    cache, table, ks, vs = _written([[(0, 152)]], 2, d, junk, rng, spare=2)
+    q = torch.from_numpy(rng.standard_normal((1, 4, 4, d)).astype(np.float32)).to(DEV).to(torch.bfloat16)
+    for far in (1 << 20, table.shape[1] * 64, 0x7fffffff):
+        pos = [150, far, 151, 20]
+        out = vbq.vbq_kv_attend(cache, table, torch.tensor([pos], dtype=I32, device=DEV), q, window=window)
+        _expect_range()
+        assert all(_row_ok(out, q, r, ks[0], vs[0], pos[r], d ** -0.5, window) for r in (0, 2, 3))
