@@ -206,6 +206,19 @@ __device__ __noinline__ int whole_rounds(int most, int pages) {
     return 10 * steps > 3 * (round - pages) ? round : pages;
 }
 
+// In place of a page that the table has outside the cache: keys and values of scale 0, which change nothing for the rows that
+// do not attend to them. Reported if some row (positions pos) does; between the windows of distant rows none need be there.
+__device__ uint4 nothing[kv_blob_bytes(256) / 16];
+__device__ __noinline__ const uint8_t* no_page(const int32_t* pos, int rows, int window, int64_t page, int64_t table_keys) {
+    const int64_t key0 = page * KV_PAGE;
+#pragma unroll 1
+    for (int t = 0; t < rows; ++t) {
+        const int64_t p = pos[t];
+        if (p < table_keys && p >= key0 && (window <= 0 || key0 + KV_PAGE - 1 > p - window)) atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
+    }
+    return reinterpret_cast<const uint8_t*>(nothing);
+}
+
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAttend a, int row_tiles, uint32_t* counts,
                                                                  float* parts) {
@@ -416,12 +429,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
     bool ok = true;
     int ahead_next = next;                        // teams: the next segment to copy, and the one being copied
     int ahead = 0, ahead_end = 0;                 // (its next page and its pages)
-    const auto page_at = [&](const Segment& t, int64_t in) {             // the blob of a segment's page
-        int64_t page = c.table[t.b * c.table_stride + span[t.b].x + in];
-        if (page < 0 || page >= c.n_pages) {
-            atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
-            page = 0;
-        }
+    const auto page_at = [&](const Segment& t, int64_t in) -> const uint8_t* {       // the blob of a segment's page
+        const int64_t page = c.table[t.b * c.table_stride + span[t.b].x + in];
+        if (page < 0 || page >= c.n_pages) return no_page(a.pos + t.b * a.rows, a.rows, a.window, span[t.b].x + in, table_keys);
         return c.pages + (page * c.kv_heads + t.h) * C::BLOB;
     };
     auto issue = [&]() {                          // the next page's copy

@@ -32,14 +32,14 @@ def _written(spans, kv_heads, d, junk, rng, spare=1):
     """A cache of junk bytes in which sequence b holds only the tokens of spans[b], a list of (first, end). Returns
     (cache, table, keys, values), keys and values with zeros for what was not written."""
     need = [max(e for _, e in s) // 64 + 1 + spare for s in spans]
-    order = rng.permutation(sum(need)).astype(np.int32)
+    order = 1 + rng.permutation(sum(need)).astype(np.int32)      # page 0 is no sequence's
     table = np.zeros((len(spans), max(need)), np.int32)
     at = 0
     for b, n in enumerate(need):
         table[b, :n] = order[at:at + n]
         at += n
     table = torch.from_numpy(table).to(DEV)
-    cache = vbq.KvCache(sum(need), kv_heads, d)
+    cache = vbq.KvCache(1 + sum(need), kv_heads, d)
     cache.pages.fill_(junk)
     ks, vs = [], []
     for b, s in enumerate(spans):
@@ -111,3 +111,32 @@ def test_a_position_outside_leaves_the_sequence_s_other_rows_alone(junk, d, wind
         out = vbq.vbq_kv_attend(cache, table, torch.tensor([pos], dtype=I32, device=DEV), q, window=window)
         _expect_range()
         assert all(_row_ok(out, q, r, ks[0], vs[0], pos[r], d ** -0.5, window) for r in (0, 2, 3))
+
+
+@pytest.mark.parametrize("junk", JUNK)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("entry", [-1, 1 << 30])
+def test_a_page_outside_leaves_the_rows_before_it_alone(junk, d, entry):
+    """One page of a sequence is outside the cache; rows that end before it are served."""
+    rng = np.random.default_rng(junk + d)
+    cache, table, ks, vs = _written([[(0, 200)]], 2, d, junk, rng)
+    table[0, 1] = entry
+    q = torch.from_numpy(rng.standard_normal((1, 3, 4, d)).astype(np.float32)).to(DEV).to(torch.bfloat16)
+    pos = [10, 199, 63]
+    out = vbq.vbq_kv_attend(cache, table, torch.tensor([pos], dtype=I32, device=DEV), q)
+    _expect_range()
+    assert all(_row_ok(out, q, r, ks[0], vs[0], pos[r], d ** -0.5) for r in (0, 2))
+
+
+@pytest.mark.parametrize("junk", JUNK)
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_pages_between_the_windows_of_distant_rows_may_be_gone(junk, d):
+    """A table whose pages between two windows have been given back: nothing to report, nothing lost."""
+    rng = np.random.default_rng(junk + d)
+    cache, table, ks, vs = _written([[(31, 101), (4931, 5001)]], 2, d, junk, rng)
+    table[0, 2:77] = -1
+    _check_attend(cache, table, ks, vs, np.array([[100, 5000, -1]], np.int32), 8, rng, window=70)
+    table[0, 77] = -1                                             # tokens 4928 ..: needed
+    vbq.vbq_kv_attend(cache, table, torch.tensor([[100, 5000]], dtype=I32, device=DEV), torch.zeros(1, 2, 8, d, dtype=torch.bfloat16, device=DEV),
+                      window=70)
+    _expect_range()
