@@ -503,8 +503,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int rc = s.rt * C::ROWS + 8 * n + 2 * t4 + i;
-                pos[n][i] = rc < rows_all ? a.pos[s.b * a.rows + rc / group] : 0x7fffffff;
-                if (rc < rows_all && pos[n][i] > span[s.b].y) pos[n][i] = -1;      // outside the cache
+                pos[n][i] = rc < rows_all ? a.pos[s.b * a.rows + rc / group] : -1;
             }
         }
     };
@@ -588,8 +587,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                close = min(close, pos[n][i]);
-                if (a.window > 0 && pos[n][i] != 0x7fffffff) open = max(open, pos[n][i] - a.window);
+                if (pos[n][i] > hi_key) pos[n][i] = -1;                  // outside the cache: an unused row
+                if (s.rt * C::ROWS + 8 * n + 2 * t4 + i < rows_all) close = min(close, pos[n][i]);
+                if (a.window > 0 && pos[n][i] >= 0) open = max(open, pos[n][i] - a.window);
             }
         close = min(__reduce_min_sync(FULL, close), hi_key);
         open = __reduce_max_sync(FULL, open);
@@ -688,9 +688,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_attend_kernel(KvView c, KvAt
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
-                                if (key > min(pos[n][i], hi_key) || (a.window > 0 && key <= pos[n][i] - a.window))
+                                if (key > pos[n][i] || (a.window > 0 && key <= pos[n][i] - a.window))
                                     sc[sub][n][2 * x + i] = -INFINITY;
-                                else if (s.rt * C::ROWS + 8 * n + 2 * t4 + i < rows_all)
+                                else
                                     seen |= 1u << (2 * sub + x);
                             }
                     }

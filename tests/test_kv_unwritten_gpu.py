@@ -140,3 +140,11 @@ def test_pages_between_the_windows_of_distant_rows_may_be_gone(junk, d):
     vbq.vbq_kv_attend(cache, table, torch.tensor([[100, 5000]], dtype=I32, device=DEV), torch.zeros(1, 2, 8, d, dtype=torch.bfloat16, device=DEV),
                       window=70)
     _expect_range()
+
+
+def test_unused_rows_by_any_negative_position():
+    rng = np.random.default_rng(7)
+    cache, table, ks, vs = _written([[(0, 400)]], 2, 128, 0xff, rng)
+    for window in (0, 90):
+        got = _check_attend(cache, table, ks, vs, np.array([[399, -1, -2 ** 31, 398, -5]], np.int64), 4, rng, window=window)
+        assert not got[0, [1, 2, 4]].any() and got[0, [0, 3]].all(-1).all()
