@@ -6,10 +6,16 @@ few microseconds, so their checks (of what the C call cannot see: a tensor's
 type, size, strides and device) and the calls themselves are in the CPython
 module native/_decode.c, built beside libvbq.so; the ones that are not in a
 step's way go through ctypes.
+
+Outputs and a workspace that a call is not given are made on the stream that the
+call is enqueued on (`stream`, or PyTorch's current one), as by a caller under
+torch.cuda.stream(stream): the allocator then keeps their memory in that stream's
+order, and zeros are there before the kernel that needs them.
 """
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -40,6 +46,17 @@ def _load():
 
 def _lib():
     return _b._lib or _b.load()
+
+
+def _on(stream, device):
+    """The context in which to make a call's tensors."""
+    if stream is None or device.type != "cuda":
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = stream if isinstance(stream, int) else stream.cuda_stream
+        # 0 and 1 (cudaStreamLegacy) are the default stream
+        stream = torch.cuda.default_stream(device) if handle in (0, 1) else torch.cuda.ExternalStream(handle, device=device)
+    return torch.cuda.stream(stream)
 
 
 class _CacheStruct(ctypes.Structure):
@@ -79,7 +96,8 @@ def vbq_kv_append(cache: KvCache, table, pos, k, v, q=None, cos=None, sin=None, 
     pos (batch, rows; negative: unused). With q (batch, rows, heads, head_dim)
     the rotated q is returned as bfloat16 (q_out, allocated when not given)."""
     if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        with _on(stream, q.device):
+            q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
     st = (_native or _load()).append(cache._address, cache.device, table, pos, k, v, q, cos, sin, q_out, stream)
     if st:
         _check(st)
@@ -92,8 +110,9 @@ def vbq_kv_read(cache: KvCache, table, pos, k_out=None, v_out=None, stream=None)
     (pass False to skip one)."""
     if k_out is None or v_out is None:
         shape = (*pos.shape, cache.kv_heads, cache.head_dim)
-        k_out = torch.empty(shape, dtype=torch.float32, device=pos.device) if k_out is None else k_out
-        v_out = torch.empty(shape, dtype=torch.float32, device=pos.device) if v_out is None else v_out
+        with _on(stream, pos.device):
+            k_out = torch.empty(shape, dtype=torch.float32, device=pos.device) if k_out is None else k_out
+            v_out = torch.empty(shape, dtype=torch.float32, device=pos.device) if v_out is None else v_out
     st = (_native or _load()).read(cache._address, cache.device, table, pos, k_out, v_out, stream)
     if st:
         _check(st)
@@ -106,10 +125,12 @@ def vbq_kv_workspace_bytes(cache: KvCache, batch: int, rows: int, heads: int) ->
     return out.value
 
 
-def vbq_kv_workspace(cache: KvCache, batch: int, rows: int, heads: int):
-    """A zeroed workspace for vbq_kv_attend calls that need no more than these sizes do."""
+def vbq_kv_workspace(cache: KvCache, batch: int, rows: int, heads: int, stream=None):
+    """A workspace for vbq_kv_attend calls that need no more than these sizes do,
+    zeroed on `stream` (PyTorch's current one by default): calls on another wait for that first."""
     n = vbq_kv_workspace_bytes(cache, batch, rows, heads)
-    return torch.zeros(n, dtype=torch.uint8, device=cache.pages.device)
+    with _on(stream, cache.pages.device):
+        return torch.zeros(n, dtype=torch.uint8, device=cache.pages.device)
 
 
 def vbq_kv_attend(cache: KvCache, table, pos, q, scale=None, window: int = 0, out=None, workspace=None, stream=None):
@@ -119,9 +140,10 @@ def vbq_kv_attend(cache: KvCache, table, pos, q, scale=None, window: int = 0, ou
     workspace of vbq_kv_workspace to keep it between calls; one is made (and
     zeroed) for this call otherwise."""
     if out is None:
-        out = torch.empty_like(q)
+        with _on(stream, q.device):
+            out = torch.empty_like(q)
     if workspace is None:
-        workspace = vbq_kv_workspace(cache, q.shape[0], q.shape[1], q.shape[2])
+        workspace = vbq_kv_workspace(cache, q.shape[0], q.shape[1], q.shape[2], stream)
     st = (_native or _load()).attend(cache._address, cache.device, table, pos, q, scale, window, out, workspace, stream)
     if st:
         _check(st)
@@ -133,10 +155,10 @@ def vbq_residual_norm(x, residual, weight, eps: float, out=None, residual_out=No
     and out = r' * rsqrt(mean(r'^2) + eps) * weight as bfloat16, per row of the
     last dimension. Returns (out, residual_out), allocating those not given;
     residual_out may be residual itself."""
-    if out is None:
-        out = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
-    if residual is not None and residual_out is None:
-        residual_out = torch.empty_like(residual)
+    if out is None or (residual is not None and residual_out is None):
+        with _on(stream, x.device):
+            out = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device) if out is None else out
+            residual_out = torch.empty_like(residual) if residual is not None and residual_out is None else residual_out
     st = (_native or _load()).norm(x, residual, weight, eps, out, residual_out, stream)
     if st:
         _check(st)
@@ -149,12 +171,11 @@ def vbq_sample(logits, temperature, top_k, top_p, min_p, u, tokens=None, probs=N
     shape (batch,). Returns (tokens, probs, kept), allocating those not given
     (pass False to skip probs or kept)."""
     b, dev = logits.shape[0], logits.device
-    if tokens is None:
-        tokens = torch.empty(b, dtype=torch.int32, device=dev)
-    if probs is None:
-        probs = torch.empty(b, dtype=torch.float32, device=dev)
-    if kept is None:
-        kept = torch.empty(b, dtype=torch.int32, device=dev)
+    if tokens is None or probs is None or kept is None:
+        with _on(stream, dev):
+            tokens = torch.empty(b, dtype=torch.int32, device=dev) if tokens is None else tokens
+            probs = torch.empty(b, dtype=torch.float32, device=dev) if probs is None else probs
+            kept = torch.empty(b, dtype=torch.int32, device=dev) if kept is None else kept
     st = (_native or _load()).sample(logits, temperature, top_k, top_p, min_p, u, tokens, probs, kept, stream)
     if st:
         _check(st)
