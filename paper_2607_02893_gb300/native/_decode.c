@@ -123,6 +123,13 @@ static int stream_of(PyObject* s, long long dev, void** out) {
     return 0;
 }
 
+/* Two arguments that a call takes together or not at all. */
+static int together(PyObject* a, PyObject* b, const char* names) {
+    if ((a == Py_None) == (b == Py_None)) return 0;
+    PyErr_Format(PyExc_ValueError, "%s go together", names);
+    return -1;
+}
+
 /* ---- a cache call's table and rows ---- */
 
 typedef struct {
@@ -212,7 +219,7 @@ static PyObject* append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     Rows r;
     void *k, *v, *q = NULL, *q_out = NULL, *cos = NULL, *sin = NULL, *st;
     long long ks, vs, qs = 0, heads = 0, rot = 0, rot_rows = 0, shape[DIMS];
-    if (rows_of(a[0], a[1], a[2], a[3], &r) < 0) return NULL;
+    if (rows_of(a[0], a[1], a[2], a[3], &r) < 0 || together(a[6], a[9], "q and q_out") < 0 || together(a[7], a[8], "cos and sin") < 0) return NULL;
     const int type = type_of(a[4]), tv = type_of(a[5]);
     if (type < 0 || tv < 0) return NULL;
     int tq = type;
@@ -324,7 +331,7 @@ static PyObject* norm(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     NEED(7);
     long long dev, count, shape[DIMS], width;
     void *x, *w, *out, *r = NULL, *ro = NULL, *st;
-    if (device_of(a[0], &dev) < 0 || ask(a[0], s_numel, &count) < 0) return NULL;
+    if (device_of(a[0], &dev) < 0 || ask(a[0], s_numel, &count) < 0 || together(a[1], a[5], "residual and residual_out") < 0) return NULL;
     const int xt = type_of(a[0]), m = xt < 0 ? -1 : shape_of(a[0], shape);
     if (m < 0) return NULL;
     if (m == 0) {
