@@ -3,7 +3,7 @@ key-value cache and its attention, the residual norm, the sampler.
 
 Argument marshalling only, as in vbq.py. A decode step makes these calls every
 few microseconds, so their checks (of what the C call cannot see: a tensor's
-type, size, strides and device) and the calls themselves are in the CPython
+type, size, strides and device, which has to be the current one) and the calls themselves are in the CPython
 module native/_decode.c, built beside libvbq.so; the ones that are not in a
 step's way go through ctypes.
 
@@ -37,9 +37,11 @@ def _load():
         raise RuntimeError(f"VBQ decode binding not built: {os.path.join(os.path.dirname(__file__), '_decode.so')} ({e}); "
                            "run `python -c 'import __graft_entry__ as g; g.build()'`") from e
     raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+    current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     address = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
-    _decode.setup(torch.float32, torch.bfloat16, torch.int16, torch.int32, raw_stream, address(lib.vbq_kv_append),
-                  address(lib.vbq_kv_read), address(lib.vbq_kv_attend), address(lib.vbq_residual_norm), address(lib.vbq_sample))
+    _decode.setup(torch.float32, torch.bfloat16, torch.int16, torch.int32, raw_stream, current_device,
+                  address(lib.vbq_kv_append), address(lib.vbq_kv_read), address(lib.vbq_kv_attend),
+                  address(lib.vbq_residual_norm), address(lib.vbq_sample))
     _native = _decode
     return _decode
 

@@ -18,7 +18,7 @@ static __typeof__(&vbq_kv_attend) p_attend;
 static __typeof__(&vbq_residual_norm) p_norm;
 static __typeof__(&vbq_sample) p_sample;
 
-static PyObject *dt_f32, *dt_bf16, *dt_i16, *dt_i32, *raw_stream;
+static PyObject *dt_f32, *dt_bf16, *dt_i16, *dt_i32, *raw_stream, *current_device;
 static PyObject *s_dtype, *s_shape, *s_stride, *s_numel, *s_contiguous, *s_device, *s_ptr, *s_nbytes, *s_cuda_stream;
 
 enum { F32 = 1, BF16 = 2, I32 = 4 };            /* BF16: or its bit patterns in int16 */
@@ -42,10 +42,17 @@ static int kind_of(PyObject* t) {               /* 0: another type */
     return k;
 }
 
+/* The GPU of a call's first tensor. The library launches on the current device, whatever the addresses that it is given. */
 static int device_of(PyObject* t, long long* dev) {
+    long long current;
     if (ask(t, s_device, dev) < 0) return -1;
     if (*dev < 0) {
         PyErr_SetString(PyExc_ValueError, "tensors must be on a GPU");
+        return -1;
+    }
+    if (long_of(PyObject_CallNoArgs(current_device), &current) < 0) return -1;
+    if (*dev != current) {
+        PyErr_Format(PyExc_ValueError, "tensors are on cuda:%lld, but the current device is cuda:%lld", *dev, current);
         return -1;
     }
     return 0;
@@ -391,17 +398,17 @@ static PyObject* sample(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     return PyLong_FromLong(status);
 }
 
-/* setup(float32, bfloat16, int16, int32, raw_stream, addresses of the five functions) */
+/* setup(float32, bfloat16, int16, int32, raw_stream, current_device, addresses of the five functions) */
 static PyObject* setup(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     (void)self;
-    NEED(10);
+    NEED(11);
     long long f[5];
     for (int i = 0; i < 5; ++i) {
-        f[i] = PyLong_AsLongLong(a[5 + i]);
+        f[i] = PyLong_AsLongLong(a[6 + i]);
         if (f[i] == -1 && PyErr_Occurred()) return NULL;
     }
-    PyObject** keep[5] = {&dt_f32, &dt_bf16, &dt_i16, &dt_i32, &raw_stream};
-    for (int i = 0; i < 5; ++i) {
+    PyObject** keep[6] = {&dt_f32, &dt_bf16, &dt_i16, &dt_i32, &raw_stream, &current_device};
+    for (int i = 0; i < 6; ++i) {
         Py_INCREF(a[i]);
         Py_XSETREF(*keep[i], a[i]);
     }

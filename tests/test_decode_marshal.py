@@ -51,6 +51,7 @@ def calls(monkeypatch):
         kind = ctypes.CFUNCTYPE(*vbq.SIGNATURES[name][:1], *vbq.SIGNATURES[name][1])
         keep[name] = kind(lambda *a, name=name: log.append((name, a)) or 0)
     monkeypatch.setattr(decode._b, "load", lambda: SimpleNamespace(**keep))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
     decode._load()
     yield log
     monkeypatch.undo()
@@ -103,3 +104,20 @@ def test_arguments_arrive(calls):
     assert (a[2], a[3], a[5], a[6]) == (4, 4, 1, 2)               # table stride, its pages, batch, rows
     assert (a[7], a[8], a[9], a[10], a[11], a[14]) == (q.at, 256, 4, k.at, 128, 1)
     assert a[15:] == (cos.at, sin.at, 32, 100, q_out.at, STREAM)
+
+
+def test_tensors_of_another_device_than_the_current_one(calls):
+    """The library launches on the current device: tensors of another are refused, on its own default stream too."""
+    there = lambda *shape, dtype=F32: Fake(*shape, dtype=dtype, device=1)  # noqa: E731
+    table, pos, out = there(1, 4, dtype=I32), there(1, 2, dtype=I32), there(1, 2, 4, 64, dtype=BF16)
+    one = lambda dtype=F32: there(2, dtype=dtype)  # noqa: E731
+    for stream in (STREAM, 0):
+        for call in (lambda: vbq.vbq_kv_append(cache(1), table, pos, there(1, 2, 2, 64), there(1, 2, 2, 64), stream=stream),
+                     lambda: vbq.vbq_kv_read(cache(1), table, pos, k_out=there(1, 2, 2, 64), v_out=False, stream=stream),
+                     lambda: vbq.vbq_kv_attend(cache(1), table, pos, there(1, 2, 4, 64, dtype=BF16), out=out, workspace=there(4096), stream=stream),
+                     lambda: vbq.vbq_residual_norm(there(3, 64), None, there(64), 1e-5, out=there(3, 64, dtype=BF16), stream=stream),
+                     lambda: vbq.vbq_sample(there(2, 100), one(), one(I32), one(), one(), one(), tokens=one(I32), probs=False, kept=False,
+                                            stream=stream)):
+            with pytest.raises(ValueError, match="cuda:1.*cuda:0"):
+                call()
+    assert calls == []
