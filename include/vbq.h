@@ -488,7 +488,7 @@ vbq_status_t vbq_residual_norm(const void* x, int x_type, const void* residual, 
  *   multiple of 2^-32 (so sums are exact and do not depend on their order);
  *   top_k   keeps the k largest logits (0 or less: all);
  *   top_p   of those, the shortest run from the largest down whose weight is at
- *           least top_p times theirs, at least one (1 or more: all);
+ *           least top_p times theirs, at least one (1 or more: all; negative or NaN: one);
  *   min_p   of those, the ones with e_i >= min_p (at most 1 counts);
  *   the draw takes the least index i for which the kept weights of tokens
  *   0..i sum to more than u times the kept weights.

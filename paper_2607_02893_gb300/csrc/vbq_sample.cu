@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
     const void* logits = static_cast<const uint8_t*>(p.logits) + row * p.stride * (p.f32 ? 4 : 2);
     const float T = p.temperature[row];
     const int top_k = p.top_k[row];
-    const float top_p = p.top_p[row], mp = p.min_p[row], min_p = mp > 0.f ? fminf(mp, 1.f) : 0.f, u = p.u[row];
+    const float top_p = fmaxf(p.top_p[row], 0.f), mp = p.min_p[row], min_p = mp > 0.f ? fminf(mp, 1.f) : 0.f, u = p.u[row];
 
     // The slice, and the largest logit with its first index.
     float mx = -INFINITY;
