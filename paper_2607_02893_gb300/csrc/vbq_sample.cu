@@ -328,13 +328,14 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
         return;
     }
     float top = value_of((uint32_t)(best >> 32));
-    if (top == INFINITY) {                                 // infinite logits share the draw; the others weigh nothing
+    const bool infinite = top == INFINITY;
+    if (infinite) {                                        // infinite logits share the draw; the others weigh nothing, at any T
         __syncthreads();
         for (int i = tid; i < 4 * quads4; i += SA_THREADS) x[i] = x[i] == INFINITY ? 0.f : x[i] == -INFINITY ? x[i] : -3e38f;
         __syncthreads();
         top = 0.f;
     }
-    const Scale scale(top, T);
+    const Scale scale(top, infinite ? 1.f : T);
 
     // What is kept so far: the logits above cut, and those equal to it up to an index.
     float cut = -INFINITY;
