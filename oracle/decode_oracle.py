@@ -123,3 +123,53 @@ def sample_filters(logits, temperature, top_k, top_p, min_p):
     mask = np.zeros(l.shape, bool)
     mask[order] = True
     return np.where(mask, e, 0.0), mask, edge
+
+
+def sample_weights(logits, temperature):
+    """One row, on the whole weights that the sampler's definition gives: (order, low, high), the tokens above -inf from
+    the largest logit down, equal ones by index, and the least and the largest whole number of 2^-32 that each may weigh.
+    e = exp((l - m) / T) is of fp32: l - m is rounded once, 2^-24 of the exponent; the rest of the exponent's arithmetic
+    (2^-24) and a base-2 exponential good to 2 ulps (2^-22) come on top. Twice that is allowed: 2^-23 (|exponent| + 8)."""
+    l = np.asarray(logits, np.float64).copy()
+    l[np.isnan(l)] = -np.inf
+    order = np.argsort(-l, kind="stable")
+    order = order[l[order] > -np.inf]
+    x = (l[order] - l[order[0]]) / np.float64(temperature)
+    e, slack = np.exp(x), np.minimum(2.0 ** -23 * (np.abs(x) + 8.0), 1.0)
+    return order, np.rint(e * (1 - slack) * 2.0 ** 32), np.rint(np.minimum(e * (1 + slack), 1.0) * 2.0 ** 32)
+
+
+def sample_kept(low, high, top_k, top_p, min_p):
+    """How many tokens of sample_weights' order the filters may leave, at least and at most (each filter leaves a run from
+    the first one on)."""
+    n = len(low)
+    k = min(top_k, n) if top_k > 0 else n
+    a = b = k
+    if not top_p >= 1:
+        p = max(float(top_p), 0.0) if top_p == top_p else 0.0
+        lows, highs = low[:k].cumsum(), high[:k].cumsum()
+        a = int((highs < p * lows[-1]).sum()) + 1
+        b = min(int((lows < p * highs[-1]).sum()) + 1, k)
+    m = min(float(min_p), 1.0) * 2.0 ** 32
+    if m > 0:
+        a = min(a, max(int((low[:k] >= m + 1).sum()), 1))
+        b = min(b, max(int((high[:k] + 1 >= m).sum()), 1))
+    return a, b
+
+
+def sample_drawn_ok(order, low, high, temperature, logits, u, token, prob, kept):
+    """Whether token and prob are the draw among the first `kept` tokens of order: the kept weights before the token, at
+    their least, are at most u times all of them at their most, those up to it, at their most, more than u times all at
+    their least; prob is its weight's share, one rounding of each of its terms and of the quotient (2^-22) aside."""
+    at = np.flatnonzero(order[:kept] == token)
+    if at.size != 1:
+        return False
+    at = at[0]
+    lo, hi = low[:kept], high[:kept]
+    before = order[:kept] < token
+    if not (lo[before].sum() <= u * hi.sum() and hi[before].sum() + hi[at] > u * lo.sum()):
+        return False
+    l = np.asarray(logits, np.float64)
+    x = (l[token] - l[order[0]]) / np.float64(temperature)
+    e, slack = np.exp(x) * 2.0 ** 32, 2.0 ** -23 * (abs(x) + 8.0)
+    return e * (1 - slack) / hi.sum() * (1 - 2.0 ** -22) <= prob <= e * (1 + slack) / lo.sum() * (1 + 2.0 ** -22)
