@@ -3,7 +3,7 @@
 Each .cu file under csrc/ is compiled in parallel with nvcc, then linked into
 paper_2607_02893_gb300/libvbq.so (CUDA runtime linked statically). The CPython
 module native/_decode.c (argument marshalling of decode.py) is compiled beside
-them into paper_2607_02893_gb300/_decode.so.
+them into paper_2607_02893_gb300/_decode.<interpreter's tag>.so.
 """
 
 from __future__ import annotations
@@ -21,7 +21,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build", "vbq")
 LIB = os.path.join(PKG, "libvbq.so")
 MODULE_SRC = os.path.join(PKG, "native", "_decode.c")
-MODULE = os.path.join(PKG, "_decode.so")
+MODULE = os.path.join(PKG, "_decode" + sysconfig.get_config_var("EXT_SUFFIX"))      # of the interpreter that builds it
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC,-O2",

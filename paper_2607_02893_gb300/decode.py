@@ -3,9 +3,9 @@ key-value cache and its attention, the residual norm, the sampler.
 
 Argument marshalling only, as in vbq.py. A decode step makes these calls every
 few microseconds, so their checks (of what the C call cannot see: a tensor's
-type, size, strides and device, which has to be the current one) and the calls themselves are in the CPython
-module native/_decode.c, built beside libvbq.so; the ones that are not in a
-step's way go through ctypes.
+type, size, strides and device, which has to be the current one) and the calls
+themselves are in the CPython module native/_decode.c, built beside libvbq.so;
+the ones that are not in a step's way go through ctypes.
 
 Outputs and a workspace that a call is not given are made on the stream that the
 call is enqueued on (`stream`, or PyTorch's current one), as by a caller under
@@ -17,7 +17,6 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
-import os
 
 import torch
 
@@ -34,7 +33,8 @@ def _load():
     try:
         from . import _decode
     except ImportError as e:
-        raise RuntimeError(f"VBQ decode binding not built: {os.path.join(os.path.dirname(__file__), '_decode.so')} ({e}); "
+        from .build import MODULE
+        raise RuntimeError(f"VBQ decode binding not built: {MODULE} ({e}); "
                            "run `python -c 'import __graft_entry__ as g; g.build()'`") from e
     raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
     current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device

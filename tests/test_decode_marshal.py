@@ -121,3 +121,11 @@ def test_tensors_of_another_device_than_the_current_one(calls):
             with pytest.raises(ValueError, match="cuda:1.*cuda:0"):
                 call()
     assert calls == []
+
+
+def test_the_module_is_this_interpreter_s(calls):
+    """Its file carries the interpreter's tag, so another Python does not load it and builds its own."""
+    import sysconfig
+    from paper_2607_02893_gb300 import _decode, build
+    assert _decode.__file__ == build.MODULE and build.MODULE.endswith("_decode" + sysconfig.get_config_var("EXT_SUFFIX"))
+    assert sysconfig.get_config_var("SOABI") in build.MODULE
