@@ -19,6 +19,7 @@
 
 #include "vbq_decode.h"
 #include "vbq_device.cuh"
+#include "vbq_kernels.h"
 
 namespace vbq {
 namespace {
@@ -215,18 +216,12 @@ int grid_for(int64_t threads, int sms) {
     return (int)(want < cap ? want : cap);
 }
 
-cudaError_t sm_count(int* sms) {
-    int dev = 0;
-    const cudaError_t e = cudaGetDevice(&dev);
-    return e != cudaSuccess ? e : cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
-}
-
 }  // namespace
 
 cudaError_t launch_kv_append(const KvView& c, const KvAppend& a, cudaStream_t s) {
     int sms = 0;
-    const cudaError_t e = sm_count(&sms);
-    if (e != cudaSuccess) return e;
+    const int e = device_sms(&sms);
+    if (e != 0) return (cudaError_t)e;
     const int64_t total = (int64_t)a.batch * a.rows * ((a.q ? a.heads : 0) + 2 * c.kv_heads) * (c.head_dim / 8);
     const dim3 grid(grid_for(total, sms));
     const auto go = [&](auto kernel) { return launch_dependent(kernel, grid, KA_THREADS, 0, s, c, a); };
@@ -237,8 +232,8 @@ cudaError_t launch_kv_append(const KvView& c, const KvAppend& a, cudaStream_t s)
 cudaError_t launch_kv_read(const KvView& c, const int32_t* pos, int batch, int rows, float* k_out, float* v_out,
                            cudaStream_t s) {
     int sms = 0;
-    const cudaError_t e = sm_count(&sms);
-    if (e != cudaSuccess) return e;
+    const int e = device_sms(&sms);
+    if (e != 0) return (cudaError_t)e;
     const int64_t total = (int64_t)batch * rows * 2 * c.kv_heads * (c.head_dim / 8);
     const dim3 grid(grid_for(total, sms));
     const auto go = [&](auto kernel) { return launch_dependent(kernel, grid, KA_THREADS, 0, s, c, pos, batch, rows, k_out, v_out); };
