@@ -1129,7 +1129,7 @@ cudaError_t launch_kv_attend(const KvView& c, const KvAttend& a, cudaStream_t s)
 
 cudaError_t read_device_status_attend(uint32_t* status) {
     cudaError_t e = cudaMemcpyFromSymbol(status, g_device_status, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || *status == 0) return e;
     const uint32_t zero = 0;
     return cudaMemcpyToSymbol(g_device_status, &zero, sizeof(uint32_t));
 }

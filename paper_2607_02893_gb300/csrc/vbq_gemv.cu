@@ -1437,7 +1437,7 @@ cudaError_t read_device_status(uint32_t* status, cudaStream_t s) {
     uint32_t mine = 0, gemm = 0;
     if ((e = cudaMemcpyFromSymbol(&mine, g_device_status, sizeof(uint32_t))) != cudaSuccess) return e;
     const uint32_t zero = 0;
-    if ((e = cudaMemcpyToSymbol(g_device_status, &zero, sizeof(uint32_t))) != cudaSuccess) return e;
+    if (mine != 0 && (e = cudaMemcpyToSymbol(g_device_status, &zero, sizeof(uint32_t))) != cudaSuccess) return e;
     if ((e = read_device_status_gemm(&gemm)) != cudaSuccess) return e;
     *status = mine | gemm;
     return cudaSuccess;

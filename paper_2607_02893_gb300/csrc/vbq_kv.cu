@@ -242,7 +242,7 @@ cudaError_t launch_kv_read(const KvView& c, const int32_t* pos, int batch, int r
 
 cudaError_t read_device_status_kv(uint32_t* status) {
     cudaError_t e = cudaMemcpyFromSymbol(status, g_device_status, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || *status == 0) return e;
     const uint32_t zero = 0;
     return cudaMemcpyToSymbol(g_device_status, &zero, sizeof(uint32_t));
 }
