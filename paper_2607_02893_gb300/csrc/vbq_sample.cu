@@ -26,6 +26,8 @@
 // bound by instruction issue, and each exchange about 1.
 #include <cooperative_groups.h>
 
+#include <atomic>
+
 #include "vbq_decode.h"
 #include "vbq_device.cuh"
 
@@ -652,42 +654,75 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
     }
 }
 
+// A launch of C blocks a row, in clusters if C > 1.
+template <int C>
+struct Launch {
+    static inline LaunchPrep prep;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    Launch(int rows, size_t smem, cudaStream_t s) {
+        cfg.gridDim = dim3((unsigned)rows * C);
+        cfg.blockDim = dim3(SA_THREADS);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = s;
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim = {C, 1, 1};
+        cfg.attrs = attr;
+        cfg.numAttrs = C > 1 ? 2 : 1;
+    }
+};
+
 // least: shared memory to ask for at least.
 template <int C>
 cudaError_t launch(const Sample& p, size_t least, cudaStream_t s) {
-    static LaunchPrep prep;
     const int slice = ((p.vocab + C - 1) / C + 3) / 4 * 4;
     const size_t need = SHARED_BYTES + 4 * (size_t)slice;
     int sms = 0;
-    cudaError_t e = prep.get(sample_kernel<C>, SMEM_MOST, &sms);
+    cudaError_t e = Launch<C>::prep.get(sample_kernel<C>, SMEM_MOST, &sms);
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)p.batch * C);
-    cfg.blockDim = dim3(SA_THREADS);
-    cfg.dynamicSmemBytes = need > least ? need : least;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim = {C, 1, 1};
-    cfg.attrs = attr;
-    cfg.numAttrs = C > 1 ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, sample_kernel<C>, p, slice);
+    Launch<C> l(p.batch, need > least ? need : least, s);
+    e = cudaLaunchKernelEx(&l.cfg, sample_kernel<C>, p, slice);
     return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+// How many rows in clusters of C run at once with an SM to every block (clusters lie within a part of the GPU, so fewer
+// than its SMs hold). Asked for once per device.
+template <int C>
+cudaError_t rows_alone(int* rows) {
+    static std::atomic<int> known[LaunchPrep::MAX_DEVICES];              // and 1
+    int dev = 0, sms = 0, n = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = Launch<C>::prep.get(sample_kernel<C>, SMEM_MOST, &sms);      // (checks dev)
+    if (e != cudaSuccess) return e;
+    if ((n = known[dev].load(std::memory_order_relaxed)) == 0) {
+        Launch<C> l(1, SMEM_MOST, nullptr);
+        if ((e = cudaOccupancyMaxActiveClusters(&n, sample_kernel<C>, &l.cfg)) != cudaSuccess) return e;
+        known[dev].store(++n, std::memory_order_relaxed);
+    }
+    *rows = n - 1;
+    return cudaSuccess;
 }
 
 }  // namespace
 
-// Blocks per row: few tokens are not worth an exchange; up to 8 rows spread over clusters of 8. Clusters of 8 no
-// longer get an SM per block at 16 rows (two blocks on some SMs: 33 us for 16 x 128256 under top-p 0.9; two waves
-// where shared memory allows one: 45 us), clusters of 6 do (29 us; 5: 31 us, 4: 34 us). (Blocks of 1024 threads: 25 us
-// there, but 17 us instead of 15 under top-k 50 and 13 instead of 11 at 32000 logits.) Beyond an SM per block the
-// rows queue either way.
+// Blocks per row: few tokens are not worth an exchange. Above that clusters of 8 while every block gets an SM (15 rows on
+// the GPU measured), then of 6 while those do (23), then of 8, two to an SM where shared memory allows; beyond, the rows
+// queue either way. Under top-p 0.9, us for clusters of 8, of 6 (and of 8 without asking for an SM each):
+//   128256 logits   8 rows: 22.2, 25.4 (22.2)   15: 22.4, 25.7 (22.4)   16: 41.2, 25.7 (41.2)   23: 42.4, 25.6 (42.4)   24: 42.5, 46.6 (42.5)
+//   32000           8 rows: 13.6, 14.3 (17.6)   15: 14.5, 15.0 (19.1)   16: 25.1, 14.9 (18.9)   23: 26.5, 15.1 (20.4)   24: 26.6, 26.4 (20.3)
+// Of 16 x 128256, clusters of 5 take 27.9 and of 4 take 32.1.
 cudaError_t launch_sample(const Sample& p, cudaStream_t s) {
     if (p.vocab <= 4096) return launch<1>(p, 0, s);
     if (p.vocab <= 16384) return launch<4>(p, 0, s);
-    if (p.batch > 8 && p.batch <= 24 && p.vocab <= 6 * (SLICE_MOST - 4)) return launch<6>(p, SMEM_ALONE, s);
+    int rows = 0;
+    cudaError_t e = rows_alone<8>(&rows);
+    if (e != cudaSuccess) return e;
+    if (p.batch <= rows) return launch<8>(p, SMEM_ALONE, s);
+    e = rows_alone<6>(&rows);
+    if (e != cudaSuccess) return e;
+    if (p.batch <= rows && p.vocab <= 6 * (SLICE_MOST - 4)) return launch<6>(p, SMEM_ALONE, s);
     return launch<8>(p, 0, s);
 }
 

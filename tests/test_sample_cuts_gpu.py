@@ -106,3 +106,13 @@ def test_cuts_by_weight_among_near_equal_logits(vocab, spread, base):
 def test_draws_at_the_ends(u):
     rng = np.random.default_rng(3)
     _check(torch.from_numpy(rng.standard_normal((4, 32000)).astype(np.float32)), u=u, top_p=[0.3, 0.9, 0.999, 1.0])
+
+
+@pytest.mark.parametrize("vocab", [20000, 32000, 151937])
+@pytest.mark.parametrize("batch", [8, 14, 15, 16, 17, 22, 23, 24, 28, 40])
+def test_batches_about_the_changes_of_cluster_size(vocab, batch):
+    rng = np.random.default_rng([vocab, batch])
+    x = torch.from_numpy(rng.standard_normal((batch, vocab)).astype(np.float32) * 2)
+    u = torch.from_numpy(rng.random(batch).astype(np.float32))
+    _check(x, u=u, top_p=0.9)
+    _check(x, u=u, top_k=40, top_p=0.95, temperature=0.8)
