@@ -37,7 +37,9 @@ def _load():
         raise RuntimeError(f"VBQ decode binding not built: {MODULE} ({e}); "
                            "run `python -c 'import __graft_entry__ as g; g.build()'`") from e
     raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
-    current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    current_device = None                                         # asked (0.3 us a call) where there is another one
+    if torch.cuda.device_count() > 1:
+        current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     address = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
     _decode.setup(torch.float32, torch.bfloat16, torch.int16, torch.int32, raw_stream, current_device,
                   address(lib.vbq_kv_append), address(lib.vbq_kv_read), address(lib.vbq_kv_attend),

@@ -50,6 +50,7 @@ static int device_of(PyObject* t, long long* dev) {
         PyErr_SetString(PyExc_ValueError, "tensors must be on a GPU");
         return -1;
     }
+    if (current_device == Py_None) return 0;    /* a process with one GPU */
     if (long_of(PyObject_CallNoArgs(current_device), &current) < 0) return -1;
     if (*dev != current) {
         PyErr_Format(PyExc_ValueError, "tensors are on cuda:%lld, but the current device is cuda:%lld", *dev, current);
@@ -398,7 +399,7 @@ static PyObject* sample(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     return PyLong_FromLong(status);
 }
 
-/* setup(float32, bfloat16, int16, int32, raw_stream, current_device, addresses of the five functions) */
+/* setup(float32, bfloat16, int16, int32, raw_stream, current_device or None, addresses of the five functions) */
 static PyObject* setup(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     (void)self;
     NEED(11);

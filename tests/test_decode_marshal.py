@@ -52,6 +52,7 @@ def calls(monkeypatch):
         keep[name] = kind(lambda *a, name=name: log.append((name, a)) or 0)
     monkeypatch.setattr(decode._b, "load", lambda: SimpleNamespace(**keep))
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "device_count", lambda: 2)
     decode._load()
     yield log
     monkeypatch.undo()
