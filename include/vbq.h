@@ -452,9 +452,15 @@ vbq_status_t vbq_kv_read(const vbq_kv_cache* cache, const int32_t* table, int64_
  *              zero before its first use; every call leaves it ready for the
  *              next. Calls that share one must not overlap on the GPU. It
  *              serves every call that needs no more bytes, on any cache.
- * Scores, softmax statistics and sums are fp32; queries and probabilities
- * enter the tensor cores in FP16, scaled by powers of two (11 significant
- * bits: finer than the BF16 of q and out). Results do not vary between calls.
+ * Softmax statistics and sums are fp32; what enters the tensor cores is not:
+ *   - queries are FP16 there, scaled per row by a power of two: exact down to
+ *     2^-25 of the row's largest value;
+ *   - codes are used in their packed form, and a score is within 2^-15 * |scale|
+ *     * sum_i |q_i| s_i of scale * q . k (s_i: the FP16 scale that key value i
+ *     shares; |q_i| about 1, s_i 0.3, 128 of them: 1e-4);
+ *   - a probability times its value's scale is rounded to FP16: 2^-12 of it, or
+ *     2^-39 of the largest where that is more.
+ * Results do not vary between calls.
  */
 vbq_status_t vbq_kv_workspace_bytes(const vbq_kv_cache* cache, int batch, int rows, int heads, size_t* bytes);
 vbq_status_t vbq_kv_attend(const vbq_kv_cache* cache, const int32_t* table, int64_t table_stride, int table_pages,

@@ -21,7 +21,7 @@
 //     middle of the codes (8) enters as the accumulators' start, -8 times the
 //     group's sum of q; the key's scale multiplies the group's result in fp32.
 //     q enters in f16, scaled per row by a power of two so that its largest
-//     value is in [2^12, 2^13): exact for BF16 values down to 2^-27 of it.
+//     value is in [2^12, 2^13): exact for BF16 values down to 2^-25 of it.
 //   - O^T = V^T P^T: a value's word holds 8 dimensions of one key, so pairing
 //     the words of two keys (a byte permute per 4 operands) gives A fragments
 //     whose rows are dimensions. P^T is S^T's accumulators times the key's
@@ -52,20 +52,28 @@
 // and join cost a block 5 us, and a list of short ones is a run of those. A
 // small cost model picks the team's size or the list, the same in every block.
 // Only calls that can have that many segments run the variant with teams: its
-// list is 4% slower (32 sequences of 16384: 106 us, 102 without).
+// list is 4% slower (32 sequences of 16384: 106 us, 103 without).
+//
+// A key may be attended to by some rows of a tile only, or by none (before a
+// window, between the windows of distant rows, after the last token), and what
+// was never written may be any bytes. Scores are masked per row; a key without
+// rows also loses its value scale, since 0 times a NaN scale is NaN in the MMA
+// for every row. Pages at an edge only; it costs them 0.1 us a call.
 //
 // Measured (one GB300, in a graph): 8 sequences of 65536 tokens, 32 heads of 128
 // over 8: 99 us, 5.75 TB/s of cache. One of 32768: 17 us, of which 7 are the
 // pages, 3 the start and 4 the join over 19 blocks. 16 rows each of two
 // sequences, 4096 keys a row: 20 us, bound by instruction issue. 100 keys, 12
-// heads of 64: 4.9 us, a chain of loads. 1022 warp instructions a page (d = 128,
-// 8 rows); 12 warps take 103 us where 8 take 108 and 16 take 118 (8 x 65536).
-// One sequence of 32768, 16 heads over 2: 13.9 us (16.7 in parts of 7 pages
-// instead of 12). 64 sequences of up to 100 tokens, 32 heads over 8: 11 us (teams of 3; 14 by
-// single warps, 27 by blocks, 21 as a list); of up to 1000: 25 us (48, 35, 75);
-// 24 of up to 659, 5 rows, 24 heads over 12: 18 us (teams of 4; 41 as a list).
-// 8 of 9000, 8 heads of 256 over 4: 26 us (30 by 6 warps with two whole stages
-// each; 6 warps with two stages in halves take 31).
+// heads of 64: 4.9 us, a chain of loads. One sequence of 32768, 16 heads over 2:
+// 14.1 us. 64 sequences of up to 100 tokens, 32 heads over 8: 11.7 us (teams of
+// 3; 22.7 as a list); of up to 1000: 24.8 (76); 24 of up to 659, 5 rows, 24 heads
+// over 12: 17.6 (teams of 4; 41 as a list). 8 of 9000, 8 heads of 256 over 4: 26.
+// When the shapes were chosen, each pair in one build of the time: 12 warps took
+// 103 us where 8 took 108 and 16 took 118 (8 x 65536, 1022 warp instructions a
+// page); parts of 12 pages 13.9 where parts of 7 took 16.7 (32768, 16 heads over
+// 2); teams 11 and 25 where single warps took 14 and 48 and whole blocks 27 and
+// 35 (64 x up to 100 and 1000); 8 warps of halves at d = 256 26 where 6 warps with
+// two whole stages took 30 and 6 with two in halves 31 (8 x 9000).
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -1092,8 +1100,8 @@ cudaError_t launch_shape(const KvView& c, const KvAttend& a, int row_tiles, cuda
 // TEAMS where there may be more segments than blocks. SHARES where a segment may be cut into more than 2 JOIN parts and
 // its rows leave half of the threads over that join them. The code of either costs the others' loop over the pages 2 to 4%
 // (registers), and 0.5 us of instructions that come cold between the other kernels of a decode step (12 layers: 387
-// against 378 us a step), so each is a kernel of its own. 32768 keys, 4 heads of 128 over 1: 13.0 us (17.6 without SHARES), 1 over
-// 1: 11.1 (17.5), 8 of 64 over 1: 11.7 (14.8); 54384 keys of 2 sequences, 6 heads of 256 over 3: 28.5 (32.2).
+// against 378 us a step), so each is a kernel of its own. 32768 keys, 4 heads of 128 over 1: 12.2 us (13.4 without SHARES), 1 over
+// 1: 11.3 (13.5), 8 of 64 over 1: 9.9 (10.8); 54384 keys of 2 sequences, 6 heads of 256 over 3: 28.4 (32.5). Without TEAMS: above.
 template <template <Kind> class C>
 cudaError_t launch(const KvView& c, const KvAttend& a, int row_tiles, cudaStream_t s) {
     int sms = 0;

@@ -21,7 +21,7 @@
 // a round first. The draw then adds up in index order over the whole row.
 //
 // Measured (one GB300, in a graph): 32000 logits under top-k 50 and top-p 0.95:
-// 10.4 us; 16 rows of 128256 under top-p 0.9, some 25000 tokens kept: 25 us, of
+// 10.5 us; 16 rows of 128256 under top-p 0.9, some 25000 tokens kept: 25.7 us, of
 // which the pass that fills the histogram takes 6 and the one that draws 5, both
 // bound by instruction issue, and each exchange about 1.
 #include <cooperative_groups.h>
@@ -87,8 +87,11 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 __device__ __forceinline__ u64 order_of(float v, int i) { return (u64)key_of(v) << 32 | (uint32_t)~i; }
 __device__ __forceinline__ float usable(float v) { return v == v ? v + 0.f : -INFINITY; }   // NaN is never drawn; -0 ties with 0
 
-// e = 2^t for t = (l - max) log2(e) / T, with log2(e) / T as the sum of two floats: t = n + f with n whole and |f| <= 1/2,
-// f to 2^-25, then the hardware's 2^f (2 ulps) and n added to the exponent.
+// e = 2^t for t = (l - max) log2(e) / T: t = n + f with n whole and |f| <= 1/2, then the hardware's 2^f (2 ulps) and n added
+// to the exponent. The reduction is Cody and Waite's with a constant of two floats (Software Manual for the Elementary
+// Functions, 1980): log2(e) / T = hi + lo, n = round(x hi), f = (x hi - n) + x lo with fused products, so f is off by two
+// roundings of a number below 1 and not by those of t. hi is the quotient rounded; its remainder, log2(e) - hi T (log2(e)
+// itself as two floats), over T is lo.
 struct Scale {
     float top, hi, lo;                                     // the maximum; log2(e) / T
     __device__ Scale(float top_, float T) : top(top_) {
@@ -354,9 +357,10 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(Sample p, int slice)
                 clear_hist();
                 __syncthreads();
             }
-            // Tokens too light to be in the shortest prefix even if all V weighed as much, next to the largest alone
-            // (2^32; light is 64 of its multiples or more): they count towards the whole weight only. By whole bins, so that a bin's tokens are all in the
-            // histogram or all not.
+            // Tokens too light to be in the shortest prefix: below (1 - top_p) / V of the largest, all of them together
+            // leave top_p of the whole to the others. They count towards the whole weight only. By whole bins (three
+            // spare for the rounding), so that a bin's tokens are all in the histogram or all not; and not where the
+            // limit is below 64 multiples of 2^-32, of which a weight is a whole number.
             const float light = __fdiv_rn(1.f - top_p, (float)V);
             const int light_bin = light >= 0x1p-26f ? BINS - 4 + (int)floorf((float)PER_OCTAVE * __log2f(light)) : 0;
             int rest_hi = 0;
