@@ -515,6 +515,107 @@ vbq_status_t vbq_sample(const void* logits, int64_t stride, int type, int batch,
                         int32_t* tokens, float* probs, int32_t* kept, void* stream);
 
 /*
+ * ---------------------------------------------------------------------------
+ * A linear-attention layer: the token mixer of hybrid decoders, which holds a
+ * state of fixed size per sequence in place of a growing cache. Three calls
+ * stand between the packed products of such a layer: the short causal
+ * convolution over the q, k and v channels, the gated delta rule over the
+ * recurrent state, and the gated norm per head before the output product.
+ * They take single tokens and whole prompts, in one batch too.
+ *
+ * Tokens are packed: row r of every array of a call is one token, and
+ * sequence b has the rows starts[b] .. starts[b + 1] - 1 (or b * rows ..
+ * (b + 1) * rows - 1 without starts). Its state is slot slots[b] of a pool of
+ * n_slots (slot b without slots). A sequence whose fresh[b] is not 0 begins:
+ * its state counts as zeros, whatever the slot holds. A sequence with rows
+ * leaves its new state in its slot; one without any leaves its slot alone. A
+ * negative slot marks an unused sequence: its rows give zeros. A slot outside
+ * the pool counts as unused and vbq_device_status reports VBQ_ERR_RANGE. Rows
+ * of no sequence are neither read nor written. Two sequences of one call must
+ * not share a slot. The arrays may change between calls, in a captured graph
+ * too; nothing else is read from them than the call says.
+ * ---------------------------------------------------------------------------
+ */
+typedef struct vbq_sequences {
+    const int32_t* starts;  /* device, batch + 1, not decreasing, within 0..tokens (clamped to it); or NULL */
+    const int32_t* slots;   /* device, batch; or NULL */
+    const int32_t* fresh;   /* device, batch; or NULL: none is fresh */
+    int     batch;          /* 0..65535 */
+    int     rows;           /* without starts: each sequence's rows; with starts: the longest's (a longer one is
+                               computed all the same, more slowly) */
+    int64_t tokens;         /* rows of the arrays, below 2^31; batch * rows without starts */
+} vbq_sequences;
+
+/*
+ * vbq_causal_conv — a causal convolution per channel over few taps:
+ *   y_t = bias + sum_j weight[c][j] x_{t - taps + 1 + j},  out = BF16(silu(y)) or BF16(y),
+ * in fp32. What stands before a sequence's first row are its carried inputs,
+ * state[slot][0 .. taps - 2] (the oldest first); the call leaves the sequence's
+ * last taps - 1 inputs there.
+ *   x         device, row r's channels at r * x_stride elements of `type`; rows
+ *             16-byte aligned. Must not overlap out or state.
+ *   weight    device, channels x taps float, dense.
+ *   bias      device, channels float, or NULL.
+ *   taps      2..4 (VBQ_ERR_UNSUPPORTED otherwise).
+ *   channels  a multiple of 8 (VBQ_ERR_SHAPE otherwise), at most 2^20.
+ *   state     device, n_slots x (taps - 1) x channels float, n_slots in 1..2^31 - 1.
+ *   silu      1: y / (1 + e^-y); 0: y itself.
+ *   out       device, tokens x channels BF16, dense.
+ */
+vbq_status_t vbq_causal_conv(const vbq_sequences* seq, const void* x, int64_t x_stride, int type, const float* weight,
+                             const float* bias, int taps, int channels, float* state, int64_t n_slots, int silu,
+                             uint16_t* out, void* stream);
+
+/*
+ * vbq_delta_rule — the gated delta rule. Per sequence and value head, with the
+ * state S (head_k x head_v), token by token:
+ *   S <- e^g S;   u = beta (v - S^T k);   S <- S + k u^T;   out = BF16(scale * S^T q).
+ * Value head h reads query and key head h / (heads / k_heads).
+ *   state      device, n_slots x heads x head_k x head_v float, n_slots in 1..2^31 - 1.
+ *   q, k       device, row r's k_heads x head_k values at r * stride elements of
+ *              `type`, dense within the row; rows 16-byte aligned.
+ *   v          device, row r's heads x head_v values, likewise.
+ *   head_k     64 or 128; head_v 64, 128 or 256 (VBQ_ERR_SHAPE otherwise); heads
+ *              a multiple of k_heads, at most 1024.
+ *   decay, beta   device, row r's heads values at r * stride elements of
+ *              gate_type (element alignment).
+ *   a_log, dt_bias   device, heads float each: g = -exp(a_log) softplus(decay +
+ *              dt_bias) and beta's sigmoid is taken. Or both NULL: decay holds g
+ *              and beta the factor itself.
+ *              g above 0 counts as 0 and below -100 as -100 (e^-100: nothing of
+ *              the state is left that fp32 holds beside a new token).
+ *   scale      finite.
+ *   normalize  1: q and k are scaled to unit length first, x rsqrt(sum x^2 +
+ *              1e-6) per head; 0: they are taken as they are. The rule contracts
+ *              while beta |k|^2 stays within 0..2, and is meant for that.
+ *   out        device, tokens x heads x head_v BF16, dense.
+ * The state and all sums are fp32. Results do not vary between calls; a
+ * sequence's are the same to rounding however its tokens are cut into calls.
+ */
+vbq_status_t vbq_delta_rule(const vbq_sequences* seq, float* state, int64_t n_slots, const void* q, int64_t q_stride,
+                            const void* k, int64_t k_stride, const void* v, int64_t v_stride, int type, int k_heads,
+                            int head_k, int heads, int head_v, const void* decay, int64_t decay_stride,
+                            const void* beta, int64_t beta_stride, int gate_type, const float* a_log,
+                            const float* dt_bias, float scale, int normalize, uint16_t* out, void* stream);
+
+/*
+ * vbq_gated_norm — the root-mean-square norm per head with its gate:
+ *   out = BF16(x * rsqrt(mean(x^2) + eps) * weight * silu(gate)), fp32 inside,
+ * over each head's `width` values (without a gate: no last factor).
+ *   x, gate   device, row r's heads x width values at r * stride elements of
+ *             x_type (gate_type), dense within the row; rows 16-byte aligned.
+ *             gate may be NULL.
+ *   weight    device, width float, shared by the heads.
+ *   eps       >= 0 and finite (VBQ_ERR_ARG otherwise).
+ *   rows      0..2^31 - 1 (0 does nothing); heads 1..1024; width a multiple of 8
+ *             up to 256 (VBQ_ERR_SHAPE otherwise).
+ *   out       device, rows x heads x width BF16, dense; may be x where x is dense BF16.
+ */
+vbq_status_t vbq_gated_norm(const void* x, int64_t x_stride, int x_type, const void* gate, int64_t gate_stride,
+                            int gate_type, const float* weight, float eps, int64_t rows, int heads, int width,
+                            uint16_t* out, void* stream);
+
+/*
  * vbq_device_status — report (and clear) a bounded wait that gave up.
  * (The paper has no counterpart; this is the library's failure report.)
  *
@@ -525,8 +626,9 @@ vbq_status_t vbq_sample(const void* logits, int64_t stride, int type, int batch,
  * copies in flight, so the CUDA context stays usable; the affected y is
  * undefined. This call synchronises `stream`, then reads and clears the word.
  *
- * A cache call (vbq_kv_*) that met a position or page outside its cache has
- * recorded VBQ_ERR_RANGE the same way.
+ * A cache call (vbq_kv_*) that met a position or page outside its cache, or a
+ * call on sequences that met a slot outside its pool, has recorded
+ * VBQ_ERR_RANGE the same way.
  *
  *   Returns VBQ_OK, VBQ_ERR_TIMEOUT (some kernel since the last call gave
  *   up), VBQ_ERR_RANGE, or VBQ_ERR_CUDA.

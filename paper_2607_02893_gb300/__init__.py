@@ -13,3 +13,4 @@ from .decode import (  # noqa: F401
     KvCache, vbq_kv_page_bytes, vbq_kv_append, vbq_kv_read, vbq_kv_workspace_bytes, vbq_kv_workspace, vbq_kv_attend,
     vbq_residual_norm, vbq_sample,
 )
+from .delta import Sequences, vbq_causal_conv, vbq_delta_rule, vbq_gated_norm  # noqa: F401

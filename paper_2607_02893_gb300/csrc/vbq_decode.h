@@ -1,7 +1,7 @@
 // vbq_decode.h — launchers of the kernels a decode step runs around the packed
 // products (internal; called by the C ABI in vbq_decode_api.cu): the 4-bit
-// key-value cache, the residual norm and the sampler. Each returns the
-// cudaError_t of its launch.
+// key-value cache, the residual norm and the sampler, and those of a
+// linear-attention layer. Each returns the cudaError_t of its launch.
 #pragma once
 
 #include <cstdarg>
@@ -129,10 +129,60 @@ struct Sample {
 constexpr int SAMPLE_MAX_VOCAB = 1 << 18;
 cudaError_t launch_sample(const Sample& p, cudaStream_t s);
 
-// Device status words of the cache kernels (read and cleared).
-constexpr uint32_t VBQ_DEVICE_RANGE = 2u;       // a position or page outside the cache
+// ---------------------------------------------------------------------------
+// A linear-attention layer (vbq_conv.cu, vbq_delta.cu, vbq_gated.cu).
+// ---------------------------------------------------------------------------
+struct Conv {
+    vbq_sequences seq;
+    const void* x;
+    int64_t x_stride;
+    int f32;
+    const float *weight, *bias;                 // bias may be null
+    int taps, channels;
+    float* state;
+    int64_t n_slots;
+    int silu;
+    uint16_t* out;
+};
+constexpr int CONV_MAX_TAPS = 4;
+cudaError_t launch_causal_conv(const Conv& c, cudaStream_t s);
+
+struct Delta {
+    vbq_sequences seq;
+    float* state;
+    int64_t n_slots;
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    int f32;
+    int k_heads, head_k, heads, head_v;
+    const void *decay, *beta;
+    int64_t decay_stride, beta_stride;
+    int gate_f32;
+    const float *a_log, *dt_bias;               // both or none
+    float scale;
+    int normalize;
+    uint16_t* out;
+};
+cudaError_t launch_delta_rule(const Delta& d, cudaStream_t s);
+
+struct GatedNorm {
+    const void *x, *gate;                       // gate may be null
+    int64_t x_stride, gate_stride;
+    int x_f32, gate_f32;
+    const float* weight;
+    float eps;
+    int64_t rows;
+    int heads, width;
+    uint16_t* out;
+};
+cudaError_t launch_gated_norm(const GatedNorm& n, cudaStream_t s);
+
+// Device status words of the cache and sequence kernels (read and cleared).
+constexpr uint32_t VBQ_DEVICE_RANGE = 2u;       // a position or page outside the cache, a slot outside its pool
 cudaError_t read_device_status_kv(uint32_t* status);
 cudaError_t read_device_status_attend(uint32_t* status);
+cudaError_t read_device_status_conv(uint32_t* status);
+cudaError_t read_device_status_delta(uint32_t* status);
 
 // Launch with programmatic dependent launch, as the products are: the kernel
 // may start before its predecessor on the stream has finished and waits for it

@@ -81,6 +81,33 @@ vbq_status_t check_attend(const vbq_kv_cache* c, int batch, int rows, int heads)
     return VBQ_OK;
 }
 
+vbq_status_t check_sequences(const vbq_sequences* q) {
+    if (!q) return fail(VBQ_ERR_ARG, "the sequences must be non-NULL");
+    if (q->batch < 0 || q->rows < 0 || q->tokens < 0) return fail(VBQ_ERR_ARG, "batch, rows and tokens must not be negative");
+    if (q->batch > 65535) return fail(VBQ_ERR_UNSUPPORTED, "batch must be at most 65535, got %d", q->batch);
+    if (q->tokens >= (1ll << 31)) return fail(VBQ_ERR_UNSUPPORTED, "tokens must be below 2^31, got %lld", (long long)q->tokens);
+    if (!q->starts && q->tokens != (int64_t)q->batch * q->rows)
+        return fail(VBQ_ERR_ARG, "without starts, tokens (%lld) must be batch x rows (%d x %d)", (long long)q->tokens, q->batch, q->rows);
+    if (!aligned(q->starts, 4) || !aligned(q->slots, 4) || !aligned(q->fresh, 4))
+        return fail(VBQ_ERR_ALIGN, "starts, slots and fresh must be 4-byte aligned");
+    return VBQ_OK;
+}
+
+vbq_status_t check_slots(int64_t n_slots) {
+    if (n_slots < 1 || n_slots > (1ll << 31) - 1)
+        return fail(VBQ_ERR_ARG, "n_slots must be in 1..2^31 - 1, got %lld", (long long)n_slots);
+    return VBQ_OK;
+}
+
+// Rows of `width` elements of `type`, 16-byte aligned, `stride` apart.
+vbq_status_t check_strided(const char* name, const void* p, int64_t rows, int64_t width, int64_t stride, int type) {
+    if (!p) return fail(VBQ_ERR_ARG, "%s must be non-NULL", name);
+    if (rows > 1 && stride < width) return fail(VBQ_ERR_ARG, "%s's row stride is smaller than its row", name);
+    if (!aligned(p, 16) || (rows > 1 && stride % (type == VBQ_F32 ? 4 : 8)))
+        return fail(VBQ_ERR_ALIGN, "%s's rows must be 16-byte aligned", name);
+    return VBQ_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -234,6 +261,103 @@ vbq_status_t vbq_sample(const void* logits, int64_t stride, int type, int batch,
     p.temperature = temperature; p.top_k = top_k; p.top_p = top_p; p.min_p = min_p; p.u = u;
     p.tokens = tokens; p.probs = probs; p.kept = kept;
     VBQ_CUDA(vbq::launch_sample(p, static_cast<cudaStream_t>(stream)));
+    return VBQ_OK;
+}
+
+vbq_status_t vbq_causal_conv(const vbq_sequences* seq, const void* x, int64_t x_stride, int type, const float* weight,
+                             const float* bias, int taps, int channels, float* state, int64_t n_slots, int silu,
+                             uint16_t* out, void* stream) {
+    vbq::clear_error();
+    vbq_status_t st = check_sequences(seq);
+    if (!st) st = check_type(type);
+    if (!st) st = check_slots(n_slots);
+    if (st) return st;
+    if (taps < 2 || taps > vbq::CONV_MAX_TAPS)
+        return fail(VBQ_ERR_UNSUPPORTED, "taps must be in 2..%d, got %d", vbq::CONV_MAX_TAPS, taps);
+    if (channels < 8 || channels % 8 || channels > (1 << 20))
+        return fail(VBQ_ERR_SHAPE, "channels must be a multiple of 8 up to 2^20, got %d", channels);
+    if (silu != 0 && silu != 1) return fail(VBQ_ERR_ARG, "silu must be 0 or 1, got %d", silu);
+    if (seq->batch == 0 || seq->tokens == 0) return VBQ_OK;
+    if (!weight || !state || !out) return fail(VBQ_ERR_ARG, "weight, state and out must be non-NULL");
+    st = check_strided("x", x, seq->tokens, channels, x_stride, type);
+    if (st) return st;
+    if (!aligned(weight, 16) || !aligned(bias, 16) || !aligned(state, 16) || !aligned(out, 16))
+        return fail(VBQ_ERR_ALIGN, "weight, bias, state and out must be 16-byte aligned");
+    vbq::Conv c = {};
+    c.seq = *seq;
+    c.x = x; c.x_stride = x_stride; c.f32 = type == VBQ_F32;
+    c.weight = weight; c.bias = bias; c.taps = taps; c.channels = channels;
+    c.state = state; c.n_slots = n_slots; c.silu = silu; c.out = out;
+    VBQ_CUDA(vbq::launch_causal_conv(c, static_cast<cudaStream_t>(stream)));
+    return VBQ_OK;
+}
+
+vbq_status_t vbq_delta_rule(const vbq_sequences* seq, float* state, int64_t n_slots, const void* q, int64_t q_stride,
+                            const void* k, int64_t k_stride, const void* v, int64_t v_stride, int type, int k_heads,
+                            int head_k, int heads, int head_v, const void* decay, int64_t decay_stride,
+                            const void* beta, int64_t beta_stride, int gate_type, const float* a_log,
+                            const float* dt_bias, float scale, int normalize, uint16_t* out, void* stream) {
+    vbq::clear_error();
+    vbq_status_t st = check_sequences(seq);
+    if (!st) st = check_type(type);
+    if (!st) st = check_type(gate_type);
+    if (!st) st = check_slots(n_slots);
+    if (st) return st;
+    if (head_k != 64 && head_k != 128) return fail(VBQ_ERR_SHAPE, "head_k must be 64 or 128, got %d", head_k);
+    if (head_v != 64 && head_v != 128 && head_v != 256) return fail(VBQ_ERR_SHAPE, "head_v must be 64, 128 or 256, got %d", head_v);
+    if (k_heads < 1 || heads < 1 || heads > 1024 || heads % k_heads)
+        return fail(VBQ_ERR_SHAPE, "heads (%d) must be a positive multiple of k_heads (%d), at most 1024", heads, k_heads);
+    if (!std::isfinite(scale)) return fail(VBQ_ERR_ARG, "scale must be finite");
+    if (normalize != 0 && normalize != 1) return fail(VBQ_ERR_ARG, "normalize must be 0 or 1, got %d", normalize);
+    if (!a_log != !dt_bias) return fail(VBQ_ERR_ARG, "a_log and dt_bias go together");
+    if (seq->batch == 0 || seq->tokens == 0) return VBQ_OK;
+    if (!state || !decay || !beta || !out) return fail(VBQ_ERR_ARG, "state, decay, beta and out must be non-NULL");
+    st = check_strided("q", q, seq->tokens, (int64_t)k_heads * head_k, q_stride, type);
+    if (!st) st = check_strided("k", k, seq->tokens, (int64_t)k_heads * head_k, k_stride, type);
+    if (!st) st = check_strided("v", v, seq->tokens, (int64_t)heads * head_v, v_stride, type);
+    if (st) return st;
+    if (seq->tokens > 1 && (decay_stride < heads || beta_stride < heads))
+        return fail(VBQ_ERR_ARG, "decay's or beta's row stride is smaller than its row");
+    const int size = gate_type == VBQ_F32 ? 4 : 2;
+    if (!aligned(state, 16) || !aligned(out, 16) || !aligned(decay, size) || !aligned(beta, size) || !aligned(a_log, 4) ||
+        !aligned(dt_bias, 4))
+        return fail(VBQ_ERR_ALIGN, "state and out must be 16-byte aligned, the gates to their elements");
+    vbq::Delta d = {};
+    d.seq = *seq;
+    d.state = state; d.n_slots = n_slots;
+    d.q = q; d.k = k; d.v = v;
+    d.q_stride = q_stride; d.k_stride = k_stride; d.v_stride = v_stride; d.f32 = type == VBQ_F32;
+    d.k_heads = k_heads; d.head_k = head_k; d.heads = heads; d.head_v = head_v;
+    d.decay = decay; d.beta = beta; d.decay_stride = decay_stride; d.beta_stride = beta_stride;
+    d.gate_f32 = gate_type == VBQ_F32;
+    d.a_log = a_log; d.dt_bias = dt_bias; d.scale = scale; d.normalize = normalize; d.out = out;
+    VBQ_CUDA(vbq::launch_delta_rule(d, static_cast<cudaStream_t>(stream)));
+    return VBQ_OK;
+}
+
+vbq_status_t vbq_gated_norm(const void* x, int64_t x_stride, int x_type, const void* gate, int64_t gate_stride,
+                            int gate_type, const float* weight, float eps, int64_t rows, int heads, int width,
+                            uint16_t* out, void* stream) {
+    vbq::clear_error();
+    vbq_status_t st = check_type(x_type);
+    if (!st && gate) st = check_type(gate_type);
+    if (st) return st;
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(VBQ_ERR_ARG, "eps must be finite and not negative");
+    if (width < 8 || width % 8 || width > 256) return fail(VBQ_ERR_SHAPE, "width must be a multiple of 8 up to 256, got %d", width);
+    if (heads < 1 || heads > 1024) return fail(VBQ_ERR_SHAPE, "heads must be in 1..1024, got %d", heads);
+    if (rows < 0) return fail(VBQ_ERR_SHAPE, "rows must not be negative");
+    if (rows >= (1ll << 31)) return fail(VBQ_ERR_UNSUPPORTED, "rows must be below 2^31, got %lld", (long long)rows);
+    if (rows == 0) return VBQ_OK;
+    if (!weight || !out) return fail(VBQ_ERR_ARG, "weight and out must be non-NULL");
+    st = check_strided("x", x, rows, (int64_t)heads * width, x_stride, x_type);
+    if (!st && gate) st = check_strided("gate", gate, rows, (int64_t)heads * width, gate_stride, gate_type);
+    if (st) return st;
+    if (!aligned(weight, 16) || !aligned(out, 16)) return fail(VBQ_ERR_ALIGN, "weight and out must be 16-byte aligned");
+    vbq::GatedNorm n = {};
+    n.x = x; n.gate = gate; n.x_stride = x_stride; n.gate_stride = gate_stride;
+    n.x_f32 = x_type == VBQ_F32; n.gate_f32 = gate_type == VBQ_F32;
+    n.weight = weight; n.eps = eps; n.rows = rows; n.heads = heads; n.width = width; n.out = out;
+    VBQ_CUDA(vbq::launch_gated_norm(n, static_cast<cudaStream_t>(stream)));
     return VBQ_OK;
 }
 

@@ -1,5 +1,5 @@
-/* _decode.c — argument marshalling of the decode operators (decode.py) for
- * CPython. A decode step makes these calls every few microseconds; from ctypes
+/* _decode.c — argument marshalling of the decode operators (decode.py) and those
+ * of a linear-attention layer (delta.py) for CPython. A decode step makes these calls every few microseconds; from ctypes
  * a call with its checks costs more than its kernel. The checks are the ones
  * that the C ABI cannot make: a tensor's type, size, strides and device.
  *
@@ -17,6 +17,9 @@ static __typeof__(&vbq_kv_read) p_read;
 static __typeof__(&vbq_kv_attend) p_attend;
 static __typeof__(&vbq_residual_norm) p_norm;
 static __typeof__(&vbq_sample) p_sample;
+static __typeof__(&vbq_causal_conv) p_conv;
+static __typeof__(&vbq_delta_rule) p_delta;
+static __typeof__(&vbq_gated_norm) p_gated;
 
 static PyObject *dt_f32, *dt_bf16, *dt_i16, *dt_i32, *raw_stream, *current_device;
 static PyObject *s_dtype, *s_shape, *s_stride, *s_numel, *s_contiguous, *s_device, *s_ptr, *s_nbytes, *s_cuda_stream;
@@ -399,6 +402,167 @@ static PyObject* sample(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     return PyLong_FromLong(status);
 }
 
+/* ---- calls on sequences ---- */
+
+static const vbq_sequences* sequences_of(PyObject* seq, PyObject* seq_dev, long long dev) {
+    const long long a = PyLong_AsLongLong(seq), d = PyLong_AsLongLong(seq_dev);
+    if (PyErr_Occurred()) return NULL;
+    if (d >= 0 && d != dev) {
+        PyErr_SetString(PyExc_ValueError, "the sequences' tensors must be on the call's GPU");
+        return NULL;
+    }
+    return (const vbq_sequences*)(intptr_t)a;
+}
+
+/* A (rows, heads, width) tensor whose rows are dense: its address and the elements between rows. heads, width < 0: any; they
+ * are told. heads 0: a (rows, width) tensor. */
+static int token_rows(PyObject* t, long long dev, long long rows, long long* heads, long long* width, const char* name, void** p, long long* stride) {
+    long long v[DIMS], s[DIMS], d, a;
+    const int n = shape_of(t, v), flat = *heads == 0;
+    if (n < 0 || strides_of(t, s) < 0 || ask(t, s_device, &d) < 0) return -1;
+    if (n != (flat ? 2 : 3) || d != dev || (rows >= 0 && v[0] != rows) || (!flat && *heads >= 0 && v[1] != *heads) || (*width >= 0 && v[n - 1] != *width)) {
+        PyErr_Format(PyExc_ValueError, "%s has not the shape of the call's rows%s on cuda:%lld", name, flat ? "" : ", heads and width", dev);
+        return -1;
+    }
+    if ((s[n - 1] != 1 && v[n - 1] > 1) || (!flat && v[1] > 1 && s[1] != v[2])) {
+        PyErr_Format(PyExc_ValueError, "%s's rows must be dense", name);
+        return -1;
+    }
+    if (v[n - 1] > INT32_MAX || (!flat && v[1] > INT32_MAX)) {
+        PyErr_Format(PyExc_ValueError, "%s is too wide", name);
+        return -1;
+    }
+    if (!flat) *heads = v[1];
+    *width = v[n - 1];
+    *stride = s[0];
+    if (ask(t, s_ptr, &a) < 0) return -1;
+    *p = (void*)(intptr_t)a;
+    return 0;
+}
+
+/* A pool of states: a dense float32 tensor whose dimensions but the first are given. */
+static int pool_of(PyObject* t, long long dev, const long long* dims, int n, void** p, long long* slots) {
+    long long v[DIMS], count = 1;
+    const int m = shape_of(t, v);
+    if (m < 0) return -1;
+    int same = m == n + 1;
+    for (int i = 0; same && i < n; ++i) same = v[i + 1] == dims[i];
+    if (!same) {
+        PyErr_SetString(PyExc_ValueError, "state has not the shape (n_slots, ...) of the call's");
+        return -1;
+    }
+    for (int i = 0; i < m; ++i) count *= v[i];
+    *slots = v[0];
+    return dense(t, F32, count, dev, "state", p);
+}
+
+/* conv(sequences address, their device, x, weight, bias or None, state, silu, out, stream) */
+static PyObject* conv(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    (void)self;
+    NEED(9);
+    long long dev, xs, shape[DIMS], slots, flat = 0, channels = -1;
+    void *x, *w, *bias = NULL, *state, *out, *st;
+    if (device_of(a[2], &dev) < 0) return NULL;
+    const vbq_sequences* seq = sequences_of(a[0], a[1], dev);
+    const int type = seq ? type_of(a[2]) : -1;
+    if (type < 0 || token_rows(a[2], dev, seq->tokens, &flat, &channels, "x", &x, &xs) < 0) return NULL;
+    const int m = shape_of(a[3], shape);
+    if (m < 0) return NULL;
+    if (m != 2 || shape[0] != channels || shape[1] > 1024) {
+        PyErr_Format(PyExc_ValueError, "weight must have shape (%lld, taps)", channels);
+        return NULL;
+    }
+    const long long taps = shape[1], dims[2] = {taps - 1, channels};
+    const int silu = PyObject_IsTrue(a[6]);
+    if (silu < 0 || dense(a[3], F32, channels * taps, dev, "weight", &w) < 0 ||
+        (a[4] != Py_None && dense(a[4], F32, channels, dev, "bias", &bias) < 0) || pool_of(a[5], dev, dims, 2, &state, &slots) < 0 ||
+        dense(a[7], BF16, seq->tokens * channels, dev, "out", &out) < 0 || stream_of(a[8], dev, &st) < 0)
+        return NULL;
+    int status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = p_conv(seq, x, xs, type, w, bias, (int)taps, (int)channels, state, slots, silu, out, st);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(status);
+}
+
+/* delta(sequences address, their device, state, q, k, v, decay, beta, a_log, dt_bias, scale or None, normalize, out, stream) */
+static PyObject* delta(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    (void)self;
+    NEED(14);
+    long long dev, qs, ks, vs, ds, bs, slots, k_heads = -1, dk = -1, heads = -1, dv = -1, flat = 0;
+    void *state, *q, *k, *v, *decay, *beta, *a_log = NULL, *dt_bias = NULL, *out, *st;
+    if (device_of(a[5], &dev) < 0 || together(a[8], a[9], "a_log and dt_bias") < 0) return NULL;
+    const vbq_sequences* seq = sequences_of(a[0], a[1], dev);
+    if (!seq) return NULL;
+    const int type = type_of(a[5]), tq = type < 0 ? -1 : type_of(a[3]), tk = tq < 0 ? -1 : type_of(a[4]);
+    const int gate = tk < 0 ? -1 : type_of(a[6]), tb = gate < 0 ? -1 : type_of(a[7]);
+    if (tb < 0) return NULL;
+    if (tq != type || tk != type || tb != gate) {
+        PyErr_SetString(PyExc_ValueError, "q, k and v must have one type, decay and beta too");
+        return NULL;
+    }
+    if (token_rows(a[5], dev, seq->tokens, &heads, &dv, "v", &v, &vs) < 0 || token_rows(a[3], dev, seq->tokens, &k_heads, &dk, "q", &q, &qs) < 0 ||
+        token_rows(a[4], dev, seq->tokens, &k_heads, &dk, "k", &k, &ks) < 0 || token_rows(a[6], dev, seq->tokens, &flat, &heads, "decay", &decay, &ds) < 0 ||
+        token_rows(a[7], dev, seq->tokens, &flat, &heads, "beta", &beta, &bs) < 0)
+        return NULL;
+    const long long dims[3] = {heads, dk, dv};
+    double scale;
+    if (a[10] == Py_None) {
+        scale = dk == 64 ? 0.125 : 0.08838834764831845;         /* head_k ** -0.5 of 64 or 128, the sizes there are */
+    } else {
+        scale = PyFloat_AsDouble(a[10]);
+        if (scale == -1.0 && PyErr_Occurred()) return NULL;
+    }
+    const int normalize = PyObject_IsTrue(a[11]);
+    if (normalize < 0 || pool_of(a[2], dev, dims, 3, &state, &slots) < 0 || (a[8] != Py_None && dense(a[8], F32, heads, dev, "a_log", &a_log) < 0) ||
+        (a[9] != Py_None && dense(a[9], F32, heads, dev, "dt_bias", &dt_bias) < 0) ||
+        dense(a[12], BF16, seq->tokens * heads * dv, dev, "out", &out) < 0 || stream_of(a[13], dev, &st) < 0)
+        return NULL;
+    int status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = p_delta(seq, state, slots, q, qs, k, ks, v, vs, type, (int)k_heads, (int)dk, (int)heads, (int)dv, decay, ds, beta, bs, gate, a_log, dt_bias,
+                     (float)scale, normalize, out, st);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(status);
+}
+
+/* gated(x, gate or None, weight, eps, out, stream) */
+static PyObject* gated(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    (void)self;
+    NEED(6);
+    long long dev, xs, zs = 0, shape[DIMS], heads = -1, width = -1;
+    void *x, *z = NULL, *w, *out, *st;
+    if (device_of(a[0], &dev) < 0) return NULL;
+    const int xt = type_of(a[0]), m = xt < 0 ? -1 : shape_of(a[0], shape);
+    if (m < 0 || token_rows(a[0], dev, -1, &heads, &width, "x", &x, &xs) < 0) return NULL;
+    int zt = VBQ_BF16;
+    if (a[1] != Py_None && ((zt = type_of(a[1])) < 0 || token_rows(a[1], dev, shape[0], &heads, &width, "gate", &z, &zs) < 0)) return NULL;
+    const double eps = PyFloat_AsDouble(a[3]);
+    if (eps == -1.0 && PyErr_Occurred()) return NULL;
+    if (dense(a[2], F32, width, dev, "weight", &w) < 0 || dense(a[4], BF16, shape[0] * heads * width, dev, "out", &out) < 0 || stream_of(a[5], dev, &st) < 0)
+        return NULL;
+    int status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = p_gated(x, xs, xt, z, zs, zt, w, (float)eps, shape[0], (int)heads, (int)width, out, st);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(status);
+}
+
+/* setup_delta(addresses of the three functions) */
+static PyObject* setup_delta(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    (void)self;
+    NEED(3);
+    long long f[3];
+    for (int i = 0; i < 3; ++i) {
+        f[i] = PyLong_AsLongLong(a[i]);
+        if (f[i] == -1 && PyErr_Occurred()) return NULL;
+    }
+    p_conv = (__typeof__(p_conv))(intptr_t)f[0];
+    p_delta = (__typeof__(p_delta))(intptr_t)f[1];
+    p_gated = (__typeof__(p_gated))(intptr_t)f[2];
+    Py_RETURN_NONE;
+}
+
 /* setup(float32, bfloat16, int16, int32, raw_stream, current_device or None, addresses of the five functions) */
 static PyObject* setup(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     (void)self;
@@ -424,7 +588,8 @@ static PyObject* setup(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 #define FAST(f) (PyCFunction)(void (*)(void))(f), METH_FASTCALL
 static PyMethodDef methods[] = {
     {"setup", FAST(setup), NULL},   {"append", FAST(append), NULL}, {"read", FAST(read_), NULL}, {"attend", FAST(attend), NULL},
-    {"norm", FAST(norm), NULL},     {"sample", FAST(sample), NULL}, {NULL, NULL, 0, NULL}};
+    {"norm", FAST(norm), NULL},     {"sample", FAST(sample), NULL}, {"setup_delta", FAST(setup_delta), NULL}, {"conv", FAST(conv), NULL},
+    {"delta", FAST(delta), NULL},   {"gated", FAST(gated), NULL},   {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_decode", "Marshalling of the decode operators' calls.", -1, methods,
                                     NULL, NULL, NULL, NULL};

@@ -53,6 +53,10 @@ SIGNATURES = {
     "vbq_kv_attend": (_I, [_P, _P, _I64, _I, _P, _I, _I, _P, _I, ctypes.c_float, _I, _P, _P, ctypes.c_size_t, _P]),
     "vbq_residual_norm": (_I, [_P, _I, _P, _I, _P, ctypes.c_float, _I64, _I, _P, _P, _P]),
     "vbq_sample": (_I, [_P, _I64, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "vbq_causal_conv": (_I, [_P, _P, _I64, _I, _P, _P, _I, _I, _P, _I64, _I, _P, _P]),
+    "vbq_delta_rule": (_I, [_P, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _I, _I, _I, _I, _I, _P, _I64, _P, _I64, _I, _P, _P, ctypes.c_float,
+                            _I, _P, _P]),
+    "vbq_gated_norm": (_I, [_P, _I64, _I, _P, _I64, _I, _P, ctypes.c_float, _I64, _I, _I, _P, _P]),
     "vbq_device_status": (_I, [_P]),
     "vbq_selftest_timeout": (_I, [_I, _P]),
     "vbq_free": (_I, [_P]),
