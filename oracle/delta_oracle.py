@@ -43,7 +43,7 @@ def gates(decay, beta, a_log=None, dt_bias=None):
     return np.clip(g, -100.0, 0.0), b
 
 
-def delta_rule(q, k, v, g, beta, state, scale, normalize=True):
+def delta_rule(q, k, v, g, beta, state, scale, normalize=True, wide=False):
     """One sequence: q, k (rows, k_heads, dk), v (rows, heads, dv), g, beta (rows, heads), state (heads, dk, dv). Returns
     (out, state, out_bound, state_bound): the bounds are how far fp32 kernels may be off before out is rounded to BF16.
 
@@ -52,7 +52,9 @@ def delta_rule(q, k, v, g, beta, state, scale, normalize=True):
     contraction's part; 8 times is allowed): eps = 2^-16 of the column's norm and of what the token adds. From then on the
     error is carried by e^g (1 - beta k k^T), which does not stretch while beta |k|^2 is within 0..2.
     Out: the state's error through |q|, the same eps, and what a chunk rounds to FP16 for the outputs alone: the state
-    before the chunk, its scores and its corrections (2^-11 each, so 2^-10 of a product)."""
+    before the chunk, its scores and its corrections (2^-11 each, so 2^-10 of a product). BF16 queries enter exactly. fp32
+    ones (`wide`) are rounded too, by at most 2^-11 |q_i| each: in q.S that is the second of two roundings, but a score is
+    then off by up to 2^-11 sum_i |q_i k_i| besides its own rounding, and each |U_j| carries that into the output."""
     q, k, v, g, beta = (np.asarray(a, np.float64) for a in (q, k, v, g, beta))
     s = np.asarray(state, np.float64).copy()
     rows, heads, dv = v.shape
@@ -85,6 +87,9 @@ def delta_rule(q, k, v, g, beta, state, scale, normalize=True):
         score = np.exp(upto) * np.abs(np.einsum("hk,jhk->hj", q[t], np.stack(ks)))
         spread = np.einsum("hk,hkv->hv", np.abs(q[t]), before) + np.einsum("hj,jhv->hv", score, np.abs(np.stack(us)))
         out_bound[t] = np.sqrt((q[t] * q[t]).sum(-1))[:, None] * (off + eps * norm) + 2.0 ** -10 * spread
+        if wide:
+            terms = np.exp(upto) * np.einsum("hk,jhk->hj", np.abs(q[t]), np.abs(np.stack(ks)))
+            out_bound[t] += 2.0 ** -11 * np.einsum("hj,jhv->hv", terms, np.abs(np.stack(us)))
     return out, s, out_bound, np.broadcast_to(off[:, None, :], s.shape)
 
 

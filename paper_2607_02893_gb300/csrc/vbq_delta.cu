@@ -17,6 +17,7 @@ namespace {
 
 constexpr int DR_WARPS = 2;                      // of a block; 16 columns each
 constexpr int DR_COLS = 16 * DR_WARPS;
+constexpr int DELTA_ROWS = 16;                  // a sequence of more goes by chunks
 
 template <bool F32, int DK>
 __global__ void __launch_bounds__(32 * DR_WARPS) delta_rows_kernel(Delta d, int most) {
@@ -111,20 +112,37 @@ __global__ void __launch_bounds__(32 * DR_WARPS) delta_rows_kernel(Delta d, int 
     for (int i = 0; i < PER; ++i) *reinterpret_cast<float4*>(state + (int64_t)i * d.head_v) = S[i];
 }
 
-}  // namespace
-
-cudaError_t launch_delta_rule(const Delta& d, cudaStream_t s) {
+cudaError_t launch_rows(const Delta& d, int most, cudaStream_t s) {
     const dim3 grid((unsigned)((int64_t)d.seq.batch * d.heads * (d.head_v / DR_COLS)));
-    const auto go = [&](auto kernel) { return launch_dependent(kernel, grid, 32 * DR_WARPS, 0, s, d, INT32_MAX); };
+    const auto go = [&](auto kernel) { return launch_dependent(kernel, grid, 32 * DR_WARPS, 0, s, d, most); };
     if (d.f32) return d.head_k == 64 ? go(delta_rows_kernel<true, 64>) : go(delta_rows_kernel<true, 128>);
     return d.head_k == 64 ? go(delta_rows_kernel<false, 64>) : go(delta_rows_kernel<false, 128>);
 }
 
+}  // namespace
+
+// Sequences of up to DELTA_ROWS rows go token by token, longer ones by chunks. Where the call's may be of both kinds, both
+// kernels run, each over its own.
+cudaError_t launch_delta_rule(const Delta& d, cudaStream_t s) {
+    int sms = 0;
+    const int err = device_sms(&sms);
+    if (err != 0) return (cudaError_t)err;
+    if (d.seq.rows <= DELTA_ROWS) return launch_rows(d, INT32_MAX, s);
+    if (d.seq.starts && d.seq.batch > 1) {
+        const cudaError_t e = launch_rows(d, DELTA_ROWS, s);
+        return e != cudaSuccess ? e : launch_delta_chunks(d, DELTA_ROWS, sms, s);
+    }
+    return launch_delta_chunks(d, 0, sms, s);
+}
+
 cudaError_t read_device_status_delta(uint32_t* status) {
-    cudaError_t e = cudaMemcpyFromSymbol(status, g_device_status, sizeof(uint32_t));
-    if (e != cudaSuccess || *status == 0) return e;
-    const uint32_t zero = 0;
-    return cudaMemcpyToSymbol(g_device_status, &zero, sizeof(uint32_t));
+    uint32_t chunks = 0;
+    cudaError_t e = read_device_status_delta_chunks(&chunks);
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(status, g_device_status, sizeof(uint32_t));
+    if (e != cudaSuccess) return e;
+    const uint32_t mine = *status, zero = 0;
+    *status |= chunks;
+    return mine == 0 ? cudaSuccess : cudaMemcpyToSymbol(g_device_status, &zero, sizeof(uint32_t));
 }
 
 }  // namespace vbq

@@ -4,6 +4,7 @@
 #include "vbq_sequences.cuh"
 
 namespace vbq {
+namespace {
 
 constexpr float DELTA_UNIT_EPS = 1e-6f;          // of the unit length of q and k
 constexpr float DELTA_MOST_DECAY = -100.f;       // log decays below it count as it
@@ -25,7 +26,10 @@ __device__ __forceinline__ Gate gate_of(float a, float b, bool raw, float rate, 
     return r;
 }
 
-// Sequences of more than `rows` rows, 64 tokens at a time on the tensor cores (vbq_delta_chunk.cu).
+}  // namespace
+
+// Sequences of more than `above` rows, 64 tokens at a time on the tensor cores (vbq_delta_chunk.cu).
 cudaError_t launch_delta_chunks(const Delta& d, int above, int sms, cudaStream_t s);
+cudaError_t read_device_status_delta_chunks(uint32_t* status);
 
 }  // namespace vbq

@@ -9,6 +9,7 @@
 #include "vbq_device.cuh"
 
 namespace vbq {
+namespace {
 
 struct SeqRange {
     int lo, n;                       // first row, rows
@@ -65,4 +66,5 @@ __device__ __forceinline__ uint4 pack_bf16x8(const float (&x)[8]) {
 // x / (1 + e^-x), to a few ulps of fp32; below -87, where it is smaller than 1e-35, 0
 __device__ __forceinline__ float silu(float x) { return __fdividef(x, 1.f + __expf(-x)); }
 
+}  // namespace
 }  // namespace vbq

@@ -152,6 +152,7 @@ def inputs(rng, tokens, hk, h, dk, dv, dtype, raw, gate_dtype=F32, pad=16, sizes
 def check_delta(got, after, before, lens, slots, flags, first, q, k, v, a, b, a_log, dt, scale, normalize=True, lasting=()):
     got, after, before = np64(got), np64(after), np64(before)
     g, beta = o.gates(np64(a), np64(b), a_log, dt)
+    wide = v.dtype == F32
     q, k, v = np64(q), np64(k), np64(v)
     want, bound, at = before.copy(), np.zeros_like(before), first
     for i, n in enumerate(lens):
@@ -160,7 +161,7 @@ def check_delta(got, after, before, lens, slots, flags, first, q, k, v, a, b, a_
             assert not got[s].any()
         elif n:
             start = np.zeros_like(before[0]) if flags[i] else before[slots[i]]
-            out, end, ob, sb = o.delta_rule(q[s], k[s], v[s], g[s], beta[s], start, scale, normalize)
+            out, end, ob, sb = o.delta_rule(q[s], k[s], v[s], g[s], beta[s], start, scale, normalize, wide)
             off = np.abs(got[s] - out) - (ob + 2.0 ** -8 * (np.abs(out) + ob))
             assert (off <= 0).all(), f"out of sequence {i} ({n} rows): {off.max():.3g} outside"
             want[slots[i]], bound[slots[i]] = end, sb
