@@ -39,18 +39,18 @@ namespace vbq {
 namespace {
 
 constexpr int CH = 64;                           // tokens of a chunk
-constexpr int STAGES = 2;
-constexpr int LP = 68;                           // floats between rows of the fp32 scratch matrices
+constexpr int PREP = 256;                        // threads that prepare
+constexpr int DP = 20;                           // floats between rows of an fp32 block of 16 x 16
 
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" :: "r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 __device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
     uint32_t y;
@@ -62,6 +62,18 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ float exp2_fast(float x) {              // 2 ulps; below 2^-126: 0
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// 16 bytes to shared memory, zeros where `take` is false; after cp_wait all but the thread's last GROUPS groups have landed.
+__device__ __forceinline__ void cp_16(uint32_t dst, const void* src, bool take) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int GROUPS>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(GROUPS) : "memory"); }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -71,6 +83,13 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t&
     hi = pack_f16(x, y);
     const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi));
     lo = pack_f16(x - h.x, y - h.y);
+}
+// Two neighbouring tiles of 8 columns as A fragments, scaled by row: FP16 parts.
+__device__ __forceinline__ void split_a(const float (&x)[4], const float (&y)[4], float s0, float s1, uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+    split2(x[0] * s0, x[1] * s0, hi[0], lo[0]);
+    split2(x[2] * s1, x[3] * s1, hi[1], lo[1]);
+    split2(y[0] * s0, y[1] * s0, hi[2], lo[2]);
+    split2(y[2] * s1, y[3] * s1, hi[3], lo[3]);
 }
 // The power of two that takes a magnitude m to 2^14 .. 2^15 (at most 2^100), and its inverse.
 __device__ __forceinline__ float to_f16_range(float m) {
@@ -90,186 +109,213 @@ __device__ __forceinline__ uint32_t tile_at(int row, int seg) {
     return (uint32_t)(row * PITCH + ((seg ^ turn) << 4));
 }
 
-template <bool F32, int DK, int CW, int GROUPS>
+template <bool F32, int DK, int CW>
 struct Shape {
     static constexpr int VC = 16 * CW;                              // columns of a block
     static constexpr int KP = 2 * DK;                               // bytes of a key row in FP16
     static constexpr int VP = F32 ? 4 * (VC + 4) : 2 * VC;
-    static constexpr int THREADS = 32 * (CW + 4 * GROUPS);
-    // a stage
-    static constexpr int K = 0, KLO = K + CH * KP, Q = KLO + (F32 ? CH * KP : 0), V = Q + CH * KP, THI = V + CH * VP, TLO = THI + CH * 2 * CH,
-                         P = TLO + CH * 2 * CH, FAC = P + CH * 2 * CH, STAGE = FAC + (6 * CH + 4) * 4;
-    // a group's scratch: L, then the fp32 inverse's blocks
-    static constexpr int SCRATCH = STAGES * STAGE, SCRATCH_BYTES = (CH * LP + 32 * LP) * 4 + 5 * CH * 4 + 16;
-    static constexpr int BYTES = SCRATCH + GROUPS * SCRATCH_BYTES;
+    static constexpr int TP = 2 * CH;                               // bytes of a row of T, the scores and L
+    static constexpr int CHAIN = 32 * (CW < 4 ? 4 : CW);            // whole warpgroups
+    static constexpr int THREADS = CHAIN + PREP;
+    // a stage: keys (fp32 ones: the two parts of them, where their raw values land), queries, values, T, scores, factors
+    static constexpr int K = 0, KLO = K + CH * KP, Q = KLO + (F32 ? CH * KP : 0), QLO = Q + CH * KP, V = QLO + (F32 ? CH * KP : 0),
+                         THI = V + CH * VP, TLO = THI + CH * TP, P = TLO + CH * TP, FAC = P + CH * TP,
+                         STAGE = (FAC + (6 * CH + 4) * 4 + 127) / 128 * 128;
+    // scratch of the preparing warps: -L in FP16 parts, its blocks on the diagonal in fp32, factors
+    static constexpr int LHI = 0, LLO = LHI + CH * TP, DIAG = LLO + CH * TP, TOKENS = DIAG + 4 * 16 * DP * 4, SCRATCH = TOKENS + 7 * CH * 4;
+    static constexpr int STAGES = 3 * STAGE + SCRATCH <= 227 * 1024 ? 3 : 2;
+    static constexpr int OWN = STAGES * STAGE, BYTES = OWN + SCRATCH;
+    // named barriers
+    static constexpr int FULL = 1, EMPTY = FULL + STAGES, PREPARING = EMPTY + STAGES, COUNT = 32 * CW + PREP;
 };
 // what a stage tells about its tokens
 enum { F_BETA, F_STATE, F_END, F_QUERY, F_SCORE };                  // and from F_LAST on: e^G_last
 constexpr int F_LAST = 6 * CH;
 
-template <int CW, int GROUPS>
-struct Bars {
-    static constexpr int COUNT = 32 * CW + 128;
-    __device__ static int full(int stage) { return 1 + stage; }
-    __device__ static int empty(int stage) { return 1 + STAGES + stage; }
-    __device__ static int group(int g) { return 1 + 2 * STAGES + g; }
-};
-
 // ---------------------------------------------------------------------------
-// Preparing a chunk: 128 threads.
+// Preparing the chunks: 8 warps, one chunk after the other. Loops are kept rolled where registers allow: the code of both
+// roles has to stay in the instruction cache.
 // ---------------------------------------------------------------------------
 
-// 8 values of a row to FP16 by a power of two of the row's largest; returns (scale, sum of squares). LANES neighbours share the row.
-template <int LANES>
-__device__ __forceinline__ float2 row_stats(const float (&x)[8]) {
-    float m = 0.f, s = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        m = fmaxf(m, fabsf(x[e]));
-        s = fmaf(x[e], x[e], s);
-    }
-#pragma unroll
-    for (int o = LANES / 2; o; o >>= 1) {
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        s += __shfl_xor_sync(0xffffffffu, s, o);
-    }
-    return make_float2(to_f16_range(m), s);
+// The power of two for a row of this sum of squares: its largest value comes to at most 2^15, and to 2^10 at least (128
+// values); a sum that underflows (values below 2^-60 or so) gives 2^60.
+__device__ __forceinline__ float row_scale(float squares) {
+    const int e = (int)(__float_as_uint(squares) >> 23) - 127;      // the norm is below 2^((e + 2) >> 1)
+    const int up = 15 - ((e + 2) >> 1);
+    return __uint_as_float((uint32_t)((up > 60 ? 60 : up) + 127) << 23);
 }
 
-template <bool F32, int DK, int CW, int GROUPS>
-__device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r, int h, int col0, char* smem, uint32_t base, int g, int chunks) {
-    using Z = Shape<F32, DK, CW, GROUPS>;
-    using B = Bars<CW, GROUPS>;
-    constexpr int SEGS = DK / 8, ROWS = 128 / SEGS, TURNS = CH / ROWS;
-    const int tid = (threadIdx.x - 32 * CW) & 127, warp = tid >> 5, lane = tid & 31;
+template <bool F32, int DK, int CW>
+__device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r, int h, int col0, char* smem, uint32_t base, int chunks) {
+    using Z = Shape<F32, DK, CW>;
+    constexpr int SEGS = DK / 8, STEP = PREP / SEGS, SIZE = F32 ? 4 : 2;   // 8 values a thread, STEP rows at once
+    constexpr bool AHEAD = Z::STAGES > 2;                           // the next chunk is loaded while one is worked on
+    const int tid = threadIdx.x - Z::CHAIN, warp = tid >> 5, lane = tid & 31;
     const int hk = h / (d.heads / d.k_heads);
     const bool raw = d.a_log != nullptr;
     const float rate = raw ? expf(d.a_log[h]) : 0.f, bias = raw ? d.dt_bias[h] : 0.f;
-    float* L = reinterpret_cast<float*>(smem + Z::SCRATCH + g * Z::SCRATCH_BYTES);
-    float* Y = L + CH * LP;
-    float *upto_hi = Y + 32 * LP, *upto_lo = upto_hi + CH, *beta = upto_lo + CH, *ck = beta + CH, *cq = ck + CH;
+    char* own = smem + Z::OWN;
+    const uint32_t own_b = base + Z::OWN;
+    float* diag = reinterpret_cast<float*>(own + Z::DIAG);
+    float *upto_hi = reinterpret_cast<float*>(own + Z::TOKENS), *upto_lo = upto_hi + CH, *beta = upto_lo + CH, *ck = beta + CH, *cq = ck + CH,
+          *down_k = cq + CH, *down_q = down_k + CH;
     const int seg = tid % SEGS, row_in = tid / SEGS;
-    for (int c = g; c < chunks; c += GROUPS) {
-        const int stage = c % STAGES;
+    const int quad = lane & 3, r8 = lane >> 2;
+    const int b_row = (lane & 7) + ((lane >> 4) << 3), b_seg = (lane >> 3) & 1;      // B fragments of two tiles; A, transposed
+    const int a_row = lane & 15, a_seg = lane >> 4;
+    const int mt = warp & 3;                                        // this warp's 16 rows, of keys with keys or of queries with keys
+    const bool of_q = warp >= 4;
+    float ga[2] = {}, gb[2] = {};                                   // warp 7: gates of tokens 2 lane and 2 lane + 1, as the call gives them
+
+    const auto load = [&](int c) {
+        const int stage = c % Z::STAGES, live = min(CH, r.n - c * CH);
         const int64_t row0 = (int64_t)r.lo + (int64_t)c * CH;
+        const uint32_t sb = base + stage * Z::STAGE;
+        bar_sync(Z::EMPTY + stage, Z::COUNT);
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            const int64_t stride = (half ? d.q_stride : d.k_stride) * SIZE;
+            const char* p = static_cast<const char*>(half ? d.q : d.k) + row0 * stride + (hk * DK + seg * 8) * SIZE;
+            const uint32_t to = sb + (half ? Z::Q : Z::K);
+#pragma unroll
+            for (int row = row_in; row < CH; row += STEP) {
+                const bool in = row < live;
+                const char* q = in ? p + row * stride : p;
+                cp_16(to + tile_at<Z::KP>(row, seg), q, in);
+                if (F32) cp_16(to + CH * Z::KP + tile_at<Z::KP>(row, seg), q + 16, in);
+            }
+        }
+        constexpr int PER = Z::VC * SIZE / 16;
+        const int64_t stride = d.v_stride * SIZE;
+        const char* v = static_cast<const char*>(d.v) + row0 * stride + (h * d.head_v + col0) * SIZE;
+#pragma unroll 1
+        for (int i = tid; i < CH * PER; i += PREP) {
+            const int row = i / PER, part = i % PER;
+            const uint32_t dst = F32 ? (uint32_t)(row * Z::VP + part * 16) : tile_at<Z::VP>(row, part);
+            cp_16(sb + Z::V + dst, row < live ? v + row * stride + part * 16 : v, row < live);
+        }
+        cp_commit();
+        if (warp == 7) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int t = 2 * lane + e;
+                if (t < live) {
+                    ga[e] = gate_value(d.decay, d.gate_f32, (row0 + t) * d.decay_stride + h);
+                    gb[e] = gate_value(d.beta, d.gate_f32, (row0 + t) * d.beta_stride + h);
+                }
+            }
+        }
+    };
+
+    int first = AHEAD ? -1 : 0;                                     // a turn that only loads
+    asm volatile("" : "+r"(first));                                 // unknown to the compiler, which would write that turn out on its own
+#pragma unroll 1
+    for (int c = first; c < chunks; ++c) {
+        const int stage = (c + Z::STAGES) % Z::STAGES;
         const int live = min(CH, r.n - c * CH);
         char* st = smem + stage * Z::STAGE;
         const uint32_t sb = base + stage * Z::STAGE;
         float* fac = reinterpret_cast<float*>(st + Z::FAC);
-        // the gates: two neighbouring tokens a lane, their sums in 64 bits (a decay of e^-100 among slow ones would cost the others their digits)
-        double g0 = 0, g1 = 0;
-        float b0 = 0.f, b1 = 0.f;
-        if (warp == 0) {
-            const int t = 2 * lane;
-            if (t < live) {
-                const Gate x = gate_of(gate_value(d.decay, d.gate_f32, (row0 + t) * d.decay_stride + h),
-                                       gate_value(d.beta, d.gate_f32, (row0 + t) * d.beta_stride + h), raw, rate, bias);
-                g0 = x.g; b0 = x.beta;
-            }
-            if (t + 1 < live) {
-                const Gate x = gate_of(gate_value(d.decay, d.gate_f32, (row0 + t + 1) * d.decay_stride + h),
-                                       gate_value(d.beta, d.gate_f32, (row0 + t + 1) * d.beta_stride + h), raw, rate, bias);
-                g1 = x.g; b1 = x.beta;
-            }
-        }
-        if (c >= STAGES) bar_sync(B::empty(stage), B::COUNT);
-        // keys and queries
+        const float a0 = ga[0], a1 = ga[1], b0 = gb[0], b1 = gb[1];
+        const int next = AHEAD ? c + 1 : c;
+        if (next < chunks) load(next);
+        else cp_commit();
+        if (c < 0) continue;
+        cp_wait<AHEAD ? 1 : 0>();
+        // keys and queries to FP16 in their place, each segment by the thread that loaded it
+#pragma unroll 1
         for (int half = 0; half < 2; ++half) {
-            const void* src = half ? d.q : d.k;
-            const int64_t stride = half ? d.q_stride : d.k_stride;
-            float* cs = half ? cq : ck;
-            const int at = half ? Z::Q : Z::K;
-#pragma unroll
-            for (int i = 0; i < TURNS; ++i) {
-                const int row = row_in + i * ROWS;
-                float x[8] = {};
-                if (row < live) load8<F32>(x, src, (row0 + row) * stride + hk * DK + seg * 8);
-                const float2 rs = row_stats<SEGS>(x);
+            char* tile = st + (half ? Z::Q : Z::K);
+            float *down = half ? down_q : down_k, *unit = half ? cq : ck;
+#pragma unroll(F32 ? 1 : 4)
+            for (int row = row_in; row < CH; row += STEP) {
+                uint4* at = reinterpret_cast<uint4*>(tile + tile_at<Z::KP>(row, seg));
+                const uint4 x = *at;
                 uint32_t hi[4], lo[4];
+                float up;
+                if constexpr (F32) {
+                    uint4* more = reinterpret_cast<uint4*>(tile + CH * Z::KP + tile_at<Z::KP>(row, seg));
+                    const uint4 z = *more;
+                    const float y[8] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w),
+                                        __uint_as_float(z.x), __uint_as_float(z.y), __uint_as_float(z.z), __uint_as_float(z.w)};
+                    float sum = 0.f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) split2(x[2 * e] * rs.x, x[2 * e + 1] * rs.x, hi[e], lo[e]);
-                *reinterpret_cast<uint4*>(st + at + tile_at<Z::KP>(row, seg)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                if (F32 && !half) *reinterpret_cast<uint4*>(st + Z::KLO + tile_at<Z::KP>(row, seg)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                if (seg == 0) {
-                    float f = pow2_inverse(rs.x);
-                    if (d.normalize) f *= 1.f / sqrtf(rs.y + DELTA_UNIT_EPS);
-                    cs[row] = half ? f * d.scale : f;
+                    for (int e = 0; e < 8; ++e) sum = fmaf(y[e], y[e], sum);
+#pragma unroll
+                    for (int o = SEGS / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                    up = row_scale(sum);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) split2(y[2 * e] * up, y[2 * e + 1] * up, hi[e], lo[e]);
+                    *more = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    if (seg == 0) unit[row] = d.normalize ? rsqrtf(sum + DELTA_UNIT_EPS) : 1.f;
+                } else {
+                    // by the largest magnitude; the sums of squares come out of the products below
+                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                    constexpr uint32_t MAGNITUDES = 0x7fff7fffu;
+                    uint32_t m = __vmaxu2(__vmaxu2(w[0] & MAGNITUDES, w[1] & MAGNITUDES), __vmaxu2(w[2] & MAGNITUDES, w[3] & MAGNITUDES));
+#pragma unroll
+                    for (int o = SEGS / 2; o; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    m = max(m & 0xffffu, m >> 16);
+                    up = to_f16_range(__uint_as_float(m << 16));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) hi[e] = pack_f16(__uint_as_float(w[e] << 16) * up, __uint_as_float(w[e] & 0xffff0000u) * up);
                 }
+                *at = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                if (seg == 0) down[row] = pow2_inverse(up);
             }
         }
-        // values
-        if constexpr (F32) {
-            constexpr int PER = Z::VC / 4;
-            for (int i = tid; i < CH * PER; i += 128) {
-                const int row = i / PER, s = i % PER;
-                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (row < live)
-                    x = *reinterpret_cast<const float4*>(static_cast<const float*>(d.v) + (row0 + row) * d.v_stride + h * d.head_v + col0 + s * 4);
-                *reinterpret_cast<float4*>(st + Z::V + row * Z::VP + s * 16) = x;
-            }
-        } else {
-            constexpr int PER = Z::VC / 8;
-            for (int i = tid; i < CH * PER; i += 128) {
-                const int row = i / PER, s = i % PER;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (row < live)
-                    x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(d.v) + (row0 + row) * d.v_stride + h * d.head_v + col0 + s * 8);
-                *reinterpret_cast<uint4*>(st + Z::V + tile_at<Z::VP>(row, s)) = x;
-            }
-        }
-        if (warp == 0) {
+        if (warp == 7) {
+            // sums in 64 bits: a decay of e^-100 among slow ones would cost the others their digits
             constexpr double LOG2E = 1.4426950408889634;
-            double sum = g0 + g1;
-#pragma unroll
+            const int t = 2 * lane;
+            Gate x0 = gate_of(AHEAD ? a0 : ga[0], AHEAD ? b0 : gb[0], raw, rate, bias), x1 = gate_of(AHEAD ? a1 : ga[1], AHEAD ? b1 : gb[1], raw, rate, bias);
+            if (t >= live) x0 = {0.f, 0.f};
+            if (t + 1 >= live) x1 = {0.f, 0.f};
+            double sum = (double)x0.g + (double)x1.g;
+#pragma unroll 1
             for (int o = 1; o < 32; o <<= 1) {
                 const double x = __shfl_up_sync(0xffffffffu, sum, o);
                 if (lane >= o) sum += x;
             }
             const double all = __shfl_sync(0xffffffffu, sum, 31) * LOG2E;
-            const double u1 = sum * LOG2E, u0 = (sum - g1) * LOG2E;
-            const int t = 2 * lane;
-            upto_hi[t] = (float)u0; upto_hi[t + 1] = (float)u1;
-            upto_lo[t] = (float)(u0 - (float)u0); upto_lo[t + 1] = (float)(u1 - (float)u1);
-            beta[t] = b0; beta[t + 1] = b1;
-            fac[F_BETA * CH + t] = b0; fac[F_BETA * CH + t + 1] = b1;
-            fac[F_STATE * CH + t] = b0 * exp2f((float)u0); fac[F_STATE * CH + t + 1] = b1 * exp2f((float)u1);
-            fac[F_QUERY * CH + t] = exp2f((float)u0); fac[F_QUERY * CH + t + 1] = exp2f((float)u1);
-            fac[F_END * CH + t] = exp2f((float)(all - u0)); fac[F_END * CH + t + 1] = exp2f((float)(all - u1));
+            const double u1 = sum * LOG2E, u0 = (sum - (double)x1.g) * LOG2E;
+            const float h0 = (float)u0, h1 = (float)u1, q0 = exp2f(h0), q1 = exp2f(h1);
+            const auto put = [&](float* p, float x, float y) { *reinterpret_cast<float2*>(p + t) = make_float2(x, y); };
+            put(upto_hi, h0, h1);
+            put(upto_lo, (float)(u0 - h0), (float)(u1 - h1));
+            put(beta, x0.beta, x1.beta);
+            put(fac + F_BETA * CH, x0.beta, x1.beta);
+            put(fac + F_STATE * CH, x0.beta * q0, x1.beta * q1);
+            put(fac + F_QUERY * CH, q0, q1);
+            put(fac + F_END * CH, exp2f((float)(all - u0)), exp2f((float)(all - u1)));
             if (lane == 0) fac[F_LAST] = exp2f((float)all);
         }
-        bar_sync(B::group(g), 128);
-        // the tokens' other factors
-        if (tid < CH) {
-            fac[F_STATE * CH + tid] *= ck[tid];
-            fac[F_END * CH + tid] *= ck[tid];
-        } else {
-            fac[F_QUERY * CH + tid - CH] *= cq[tid - CH];
-        }
-        // keys with keys (16 rows: this warp's) and queries with keys (the rows of the warp across, so that each has ten tiles)
-        const int quad = lane & 3, r8 = lane >> 2;
-        const uint32_t b_row = (uint32_t)((lane & 7) + ((lane >> 4) << 3)), b_seg = (lane >> 3) & 1;     // B fragments of two tiles
-        const uint32_t a_row = (uint32_t)(lane & 15), a_seg = lane >> 4;
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-            const int mt = half ? 3 - warp : warp;
-            float acc[8][4];
+        bar_sync(Z::PREPARING, PREP);
+        // 16 rows of keys (warps 0..3) or of queries with all the keys up to theirs
+        float acc[8][4], squares[2][4] = {};
 #pragma unroll
-            for (int n = 0; n < 8; ++n)
+        for (int n = 0; n < 8; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[n][e] = 0.f;
-#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[n][e] = 0.f;
+        {
+            const uint32_t a_at = sb + (of_q ? Z::Q : Z::K);
+#pragma unroll(F32 ? 1 : 2)
             for (int kk = 0; kk < DK / 16; ++kk) {
-                uint32_t a[4], alo[4];
-                ldmatrix4(a, sb + (half ? Z::Q : Z::K) + tile_at<Z::KP>(16 * mt + a_row, 2 * kk + a_seg));
-                if (F32 && !half) ldmatrix4(alo, sb + Z::KLO + tile_at<Z::KP>(16 * mt + a_row, 2 * kk + a_seg));
+                uint32_t a[4], alo[4], b[4];
+                ldmatrix4(a, a_at + tile_at<Z::KP>(16 * mt + a_row, 2 * kk + a_seg));
+                if (F32) ldmatrix4(alo, a_at + CH * Z::KP + tile_at<Z::KP>(16 * mt + a_row, 2 * kk + a_seg));
+                if (!F32 && of_q) {                                 // the queries' squares, on the diagonal
+                    ldmatrix4(b, a_at + tile_at<Z::KP>(16 * mt + b_row, 2 * kk + b_seg));
+                    mma(squares[0], a, b[0], b[1]);
+                    mma(squares[1], a, b[2], b[3]);
+                }
 #pragma unroll
                 for (int n2 = 0; n2 < 4; ++n2) {
                     if (n2 > mt) break;
-                    uint32_t b[4];
                     ldmatrix4(b, sb + Z::K + tile_at<Z::KP>(16 * n2 + b_row, 2 * kk + b_seg));
                     mma(acc[2 * n2], a, b[0], b[1]);
                     mma(acc[2 * n2 + 1], a, b[2], b[3]);
-                    if (F32 && !half) {
+                    if (F32) {
                         mma(acc[2 * n2], alo, b[0], b[1]);
                         mma(acc[2 * n2 + 1], alo, b[2], b[3]);
                         ldmatrix4(b, sb + Z::KLO + tile_at<Z::KP>(16 * n2 + b_row, 2 * kk + b_seg));
@@ -278,131 +324,195 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                     }
                 }
             }
-            const int i0 = 16 * mt + r8, i1 = i0 + 8;
+        }
+        if (!F32) {
+            // unit lengths from the diagonals, which are in the rows' own powers of two
+            const auto put = [&](int row, float x) {
+                const float p = (of_q ? down_q : down_k)[row];
+                (of_q ? cq : ck)[row] = d.normalize ? rsqrtf(x * p * p + DELTA_UNIT_EPS) : 1.f;
+            };
+            if (!of_q)
+#pragma unroll
+                for (int n2 = 0; n2 < 4; ++n2)
+                    if (n2 == mt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { squares[0][e] = acc[2 * n2][e]; squares[1][e] = acc[2 * n2 + 1][e]; }
+            if (2 * quad == (r8 & ~1)) {                            // columns 2 quad + e, rows r8 and r8 + 8
+                put(16 * mt + r8, r8 & 1 ? squares[0][1] : squares[0][0]);
+                put(16 * mt + r8 + 8, r8 & 1 ? squares[1][3] : squares[1][2]);
+            }
+        }
+        bar_sync(Z::PREPARING, PREP);
+        // the tokens' other factors
+        if (tid < CH) {
+            const float f = ck[tid] * down_k[tid];
+            fac[F_STATE * CH + tid] *= f;
+            fac[F_END * CH + tid] *= f;
+        } else if (tid < 2 * CH) {
+            fac[F_QUERY * CH + tid - CH] *= cq[tid - CH] * down_q[tid - CH] * d.scale;
+        }
+        // -L and the scores: products times their tokens' factors and the decay between them
+        const int i0 = 16 * mt + r8, i1 = i0 + 8;
+        float m0 = 0.f, m1 = 0.f;
+        {
             const float h0 = upto_hi[i0], h1 = upto_hi[i1], l0 = upto_lo[i0], l1 = upto_lo[i1];
-            const float s0 = half ? cq[i0] : beta[i0] * ck[i0], s1 = half ? cq[i1] : beta[i1] * ck[i1];
-            float m0 = 0.f, m1 = 0.f;
+            const float s0 = of_q ? cq[i0] * down_q[i0] * d.scale : -beta[i0] * ck[i0] * down_k[i0];
+            const float s1 = of_q ? cq[i1] * down_q[i1] * d.scale : -beta[i1] * ck[i1] * down_k[i1];
+            const int below = of_q ? 0 : 1;                         // below the diagonal, or up to it
 #pragma unroll
             for (int n = 0; n < 8; ++n) {
                 if (n > 2 * mt + 1) break;
+                const int j0 = 8 * n + 2 * quad;
+                const float2 hj = *reinterpret_cast<const float2*>(upto_hi + j0), lj = *reinterpret_cast<const float2*>(upto_lo + j0);
+                const float2 cj = *reinterpret_cast<const float2*>(ck + j0), dj = *reinterpret_cast<const float2*>(down_k + j0);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int j = 8 * n + 2 * quad + e;
-                    const float hj = upto_hi[j], lj = upto_lo[j], cj = ck[j];
-                    const bool in0 = half ? j <= i0 : j < i0, in1 = half ? j <= i1 : j < i1;
-                    acc[n][e] = in0 ? s0 * cj * exp2f((h0 - hj) + (l0 - lj)) * acc[n][e] : 0.f;
-                    acc[n][2 + e] = in1 ? s1 * cj * exp2f((h1 - hj) + (l1 - lj)) * acc[n][2 + e] : 0.f;
+                    const int j = j0 + e + below;
+                    const float he = e ? hj.y : hj.x, le = e ? lj.y : lj.x, ce = e ? cj.y * dj.y : cj.x * dj.x;
+                    acc[n][e] = j <= i0 ? (s0 * ce) * exp2_fast((h0 - he) + (l0 - le)) * acc[n][e] : 0.f;
+                    acc[n][2 + e] = j <= i1 ? (s1 * ce) * exp2_fast((h1 - he) + (l1 - le)) * acc[n][2 + e] : 0.f;
                     m0 = fmaxf(m0, fabsf(acc[n][e]));
                     m1 = fmaxf(m1, fabsf(acc[n][2 + e]));
                 }
             }
-            if (!half) {
+        }
+        if (of_q) {
+            const float p0 = to_f16_range(quad_max(m0)), p1 = to_f16_range(quad_max(m1));
+            if (quad == 0) {
+                fac[F_SCORE * CH + i0] = pow2_inverse(p0);
+                fac[F_SCORE * CH + i1] = pow2_inverse(p1);
+            }
 #pragma unroll
-                for (int n = 0; n < 8; ++n) {
-                    if (n > 2 * mt + 1) break;
-                    *reinterpret_cast<float2*>(L + i0 * LP + 8 * n + 2 * quad) = make_float2(acc[n][0], acc[n][1]);
-                    *reinterpret_cast<float2*>(L + i1 * LP + 8 * n + 2 * quad) = make_float2(acc[n][2], acc[n][3]);
-                }
-            } else {
-                const float p0 = to_f16_range(quad_max(m0)), p1 = to_f16_range(quad_max(m1));
-                if (quad == 0) {
-                    fac[F_SCORE * CH + i0] = pow2_inverse(p0);
-                    fac[F_SCORE * CH + i1] = pow2_inverse(p1);
-                }
+            for (int n = 0; n < 8; ++n) {
+                if (n > 2 * mt + 1) break;
+                *reinterpret_cast<uint32_t*>(st + Z::P + tile_at<Z::TP>(i0, n) + 4 * quad) = pack_f16(acc[n][0] * p0, acc[n][1] * p0);
+                *reinterpret_cast<uint32_t*>(st + Z::P + tile_at<Z::TP>(i1, n) + 4 * quad) = pack_f16(acc[n][2] * p1, acc[n][3] * p1);
+            }
+        } else {
 #pragma unroll
-                for (int n = 0; n < 8; ++n) {
-                    if (n > 2 * mt + 1) break;
-                    *reinterpret_cast<uint32_t*>(st + Z::P + tile_at<2 * CH>(i0, n) + 4 * quad) = pack_f16(acc[n][0] * p0, acc[n][1] * p0);
-                    *reinterpret_cast<uint32_t*>(st + Z::P + tile_at<2 * CH>(i1, n) + 4 * quad) = pack_f16(acc[n][2] * p1, acc[n][3] * p1);
+            for (int n = 0; n < 8; ++n) {
+                if (n > 2 * mt + 1) break;
+                if (n < 2 * mt) {
+                    uint32_t hi, lo;
+                    split2(acc[n][0], acc[n][1], hi, lo);
+                    *reinterpret_cast<uint32_t*>(own + Z::LHI + tile_at<Z::TP>(i0, n) + 4 * quad) = hi;
+                    *reinterpret_cast<uint32_t*>(own + Z::LLO + tile_at<Z::TP>(i0, n) + 4 * quad) = lo;
+                    split2(acc[n][2], acc[n][3], hi, lo);
+                    *reinterpret_cast<uint32_t*>(own + Z::LHI + tile_at<Z::TP>(i1, n) + 4 * quad) = hi;
+                    *reinterpret_cast<uint32_t*>(own + Z::LLO + tile_at<Z::TP>(i1, n) + 4 * quad) = lo;
+                } else {
+                    float* o = diag + i0 * DP + 8 * (n - 2 * mt) + 2 * quad;
+                    *reinterpret_cast<float2*>(o) = make_float2(acc[n][0], acc[n][1]);
+                    *reinterpret_cast<float2*>(o + 8 * DP) = make_float2(acc[n][2], acc[n][3]);
                 }
             }
-        }
-        bar_sync(B::group(g), 128);
-        // T = (1 + L)^-1 by 32 x 32 blocks: those on the diagonal by substitution, a column a lane; then -T22 (L21 T11)
-        const auto put_t = [&](int i, int j, float x) {
-            const __half hi = __float2half_rn(x);
-            const uint32_t o = tile_at<2 * CH>(i, j >> 3) + 2 * (j & 7);
-            *reinterpret_cast<__half*>(st + Z::THI + o) = hi;
-            *reinterpret_cast<__half*>(st + Z::TLO + o) = __float2half_rn(x - __half2float(hi));
-        };
-        if (warp < 2) {
-            const float* D = L + 32 * warp * LP + 32 * warp;
-            float x[32];
+            // T's block on the diagonal (rows and columns 16 mt ..) by substitution, a column a lane
+            __syncwarp();
+            const float* D = diag + 16 * mt * DP;
+            const int col = lane & 15;
+            float x[16];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                float s0 = i == lane ? 1.f : 0.f, s1 = 0.f;
+            for (int i = 0; i < 16; ++i) {
+                float t0 = i == col ? 1.f : 0.f, t1 = 0.f;
 #pragma unroll
                 for (int m = 0; m < i; m += 4) {
-                    const float4 l = *reinterpret_cast<const float4*>(D + i * LP + m);
-                    s0 = fmaf(-l.x, x[m], s0);
-                    if (m + 1 < i) s1 = fmaf(-l.y, x[m + 1], s1);
-                    if (m + 2 < i) s0 = fmaf(-l.z, x[m + 2], s0);
-                    if (m + 3 < i) s1 = fmaf(-l.w, x[m + 3], s1);
+                    const float4 l = *reinterpret_cast<const float4*>(D + i * DP + m);
+                    t0 = fmaf(l.x, x[m], t0);
+                    if (m + 1 < i) t1 = fmaf(l.y, x[m + 1], t1);
+                    if (m + 2 < i) t0 = fmaf(l.z, x[m + 2], t0);
+                    if (m + 3 < i) t1 = fmaf(l.w, x[m + 3], t1);
                 }
-                x[i] = i < lane ? 0.f : s0 + s1;
+                x[i] = i < col ? 0.f : t0 + t1;
             }
-            __syncwarp();
-            // over L's own block, which is not read again
-            float* O = L + 32 * warp * LP + 32 * warp + lane;
+            // the first half of the lanes writes the high parts, the second the low ones
+            char* to = st + (lane < 16 ? Z::THI : Z::TLO) + 2 * (col & 7);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                O[i * LP] = x[i];
-                put_t(32 * warp + i, 32 * warp + lane, x[i]);
+            for (int i = 0; i < 16; ++i) {
+                const __half hi = __float2half_rn(x[i]);
+                *reinterpret_cast<__half*>(to + tile_at<Z::TP>(16 * mt + i, 2 * mt + (col >> 3))) = lane < 16 ? hi : __float2half_rn(x[i] - __half2float(hi));
             }
         }
-        bar_sync(B::group(g), 128);
-        {
-            const int i = tid >> 2, j = (tid & 3) * 8;
-            float y[8] = {};
-#pragma unroll 8
-            for (int m = 0; m < 32; ++m) {
-                const float l = L[(32 + i) * LP + m];
-                const float4 a = *reinterpret_cast<const float4*>(L + m * LP + j), b = *reinterpret_cast<const float4*>(L + m * LP + j + 4);
-                y[0] = fmaf(l, a.x, y[0]); y[1] = fmaf(l, a.y, y[1]); y[2] = fmaf(l, a.z, y[2]); y[3] = fmaf(l, a.w, y[3]);
-                y[4] = fmaf(l, b.x, y[4]); y[5] = fmaf(l, b.y, y[5]); y[6] = fmaf(l, b.z, y[6]); y[7] = fmaf(l, b.w, y[7]);
-            }
-            *reinterpret_cast<float4*>(Y + i * LP + j) = make_float4(y[0], y[1], y[2], y[3]);
-            *reinterpret_cast<float4*>(Y + i * LP + j + 4) = make_float4(y[4], y[5], y[6], y[7]);
-            bar_sync(B::group(g), 128);
-            float z[8] = {};
-#pragma unroll 8
-            for (int m = 0; m < 32; ++m) {
-                const float l = -L[(32 + i) * LP + 32 + m];
-                const float4 a = *reinterpret_cast<const float4*>(Y + m * LP + j), b = *reinterpret_cast<const float4*>(Y + m * LP + j + 4);
-                z[0] = fmaf(l, a.x, z[0]); z[1] = fmaf(l, a.y, z[1]); z[2] = fmaf(l, a.z, z[2]); z[3] = fmaf(l, a.w, z[3]);
-                z[4] = fmaf(l, b.x, z[4]); z[5] = fmaf(l, b.y, z[5]); z[6] = fmaf(l, b.z, z[6]); z[7] = fmaf(l, b.w, z[7]);
-            }
-            uint32_t hi[4], lo[4];
+        bar_sync(Z::PREPARING, PREP);
+        // The blocks below the diagonal, T_ba = T_bb sum_(a <= c < b) (-L_bc) T_ca, block column a by warp a, transposed: each
+        // T_ca^T is an A fragment as it comes out of the products.
+        if (warp < 3) {
+            uint32_t th[3][4], tl[3][4];
+            ldmatrix4_trans(th[0], sb + Z::THI + tile_at<Z::TP>(16 * warp + b_row, 2 * warp + b_seg));
+            ldmatrix4_trans(tl[0], sb + Z::TLO + tile_at<Z::TP>(16 * warp + b_row, 2 * warp + b_seg));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) split2(z[2 * e], z[2 * e + 1], hi[e], lo[e]);
-            const uint32_t o = tile_at<2 * CH>(32 + i, j >> 3);
-            *reinterpret_cast<uint4*>(st + Z::THI + o) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            *reinterpret_cast<uint4*>(st + Z::TLO + o) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            for (int bi = 1; bi < 4; ++bi) {
+                const int b = warp + bi;
+                if (b > 3) break;
+                float x[2][4] = {}, y[2][4] = {};
+                uint32_t f[4], e[4], hi[4], lo[4];
+#pragma unroll
+                for (int ci = 0; ci < bi; ++ci) {
+                    ldmatrix4(f, own_b + Z::LHI + tile_at<Z::TP>(16 * b + b_row, 2 * (warp + ci) + b_seg));
+                    ldmatrix4(e, own_b + Z::LLO + tile_at<Z::TP>(16 * b + b_row, 2 * (warp + ci) + b_seg));
+                    mma(x[0], th[ci], f[0], f[1]);
+                    mma(x[1], th[ci], f[2], f[3]);
+                    mma(y[0], tl[ci], f[0], f[1]);
+                    mma(y[1], tl[ci], f[2], f[3]);
+                    mma(y[0], th[ci], e[0], e[1]);
+                    mma(y[1], th[ci], e[2], e[3]);
+                }
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { x[p][i] += y[p][i]; y[p][i] = 0.f; }
+                split_a(x[0], x[1], 1.f, 1.f, hi, lo);
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[p][i] = 0.f;
+                ldmatrix4(f, sb + Z::THI + tile_at<Z::TP>(16 * b + b_row, 2 * b + b_seg));
+                ldmatrix4(e, sb + Z::TLO + tile_at<Z::TP>(16 * b + b_row, 2 * b + b_seg));
+                mma(x[0], hi, f[0], f[1]);
+                mma(x[1], hi, f[2], f[3]);
+                mma(y[0], lo, f[0], f[1]);
+                mma(y[1], lo, f[2], f[3]);
+                mma(y[0], hi, e[0], e[1]);
+                mma(y[1], hi, e[2], e[3]);
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[p][i] += y[p][i];
+                split_a(x[0], x[1], 1.f, 1.f, hi, lo);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (bi < 3) { th[bi][i] = hi[i]; tl[bi][i] = lo[i]; }
+                    const uint32_t at = tile_at<Z::TP>(16 * b + 8 * (i >> 1) + r8, 2 * warp + (i & 1)) + 4 * quad;
+                    *reinterpret_cast<uint32_t*>(st + Z::THI + at) = movmatrix_trans(hi[i]);
+                    *reinterpret_cast<uint32_t*>(st + Z::TLO + at) = movmatrix_trans(lo[i]);
+                }
+            }
         }
-        bar_arrive(B::full(stage), B::COUNT);
+        bar_arrive(Z::FULL + stage, Z::COUNT);
     }
 }
 
 // ---------------------------------------------------------------------------
 // The chain: a warp, 16 columns.
 // ---------------------------------------------------------------------------
-template <bool F32, int DK, int CW, int GROUPS>
+template <bool F32, int DK, int CW>
 __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int h, int col0, char* smem, uint32_t base, int chunks) {
-    using Z = Shape<F32, DK, CW, GROUPS>;
-    using B = Bars<CW, GROUPS>;
+    using Z = Shape<F32, DK, CW>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3, r8 = lane >> 2;
     const int vcol = 16 * warp;
-    float* state = d.state + ((int64_t)r.slot * d.heads + h) * DK * d.head_v + col0 + vcol + r8;
+    float* state = d.state + ((int64_t)r.slot * d.heads + h) * DK * d.head_v + 2 * quad * d.head_v + col0 + vcol + r8;
     float S[DK / 8][4];                                             // [8 rows of S][columns r8, r8 + 8 x two rows]
+    const float* from = state;
 #pragma unroll
-    for (int j = 0; j < DK / 8; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            S[j][e] = r.fresh ? 0.f : state[(int64_t)(8 * j + 2 * quad + (e & 1)) * d.head_v + (e >> 1) * 8];
-    const uint32_t b_row = (uint32_t)((lane & 7) + ((lane >> 4) << 3)), b_seg = (lane >> 3) & 1;       // two tiles of tokens
-    const uint32_t t_row = (uint32_t)((lane & 7) + (((lane >> 3) & 1) << 3)), t_seg = lane >> 4;       // transposed: 16 tokens, two tiles of columns
+    for (int j = 0; j < DK / 8; ++j, from += 8 * d.head_v) {
+        S[j][0] = r.fresh ? 0.f : from[0]; S[j][2] = r.fresh ? 0.f : from[8];
+        S[j][1] = r.fresh ? 0.f : from[d.head_v]; S[j][3] = r.fresh ? 0.f : from[d.head_v + 8];
+    }
+    for (int i = 0; i < Z::STAGES && i < chunks; ++i) bar_arrive(Z::EMPTY + i, Z::COUNT);
+    const int b_row = (lane & 7) + ((lane >> 4) << 3), b_seg = (lane >> 3) & 1;                        // two tiles of tokens
+    const int t_row = (lane & 7) + (((lane >> 3) & 1) << 3), t_seg = lane >> 4;                        // transposed: 16 tokens, two tiles of columns
+#pragma unroll 1
     for (int c = 0; c < chunks; ++c) {
-        const int stage = c % STAGES;
+        const int stage = c % Z::STAGES;
         const char* st = smem + stage * Z::STAGE;
         const uint32_t sb = base + stage * Z::STAGE;
         const float* fac = reinterpret_cast<const float*>(st + Z::FAC);
@@ -414,7 +524,7 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
         }
         sc0 = to_f16_range(quad_max(sc0));
         sc1 = to_f16_range(quad_max(sc1));
-        bar_sync(B::full(stage), B::COUNT);
+        bar_sync(Z::FULL + stage, Z::COUNT);
         // S^T k and S^T q of every token
         float R[8][4], O[8][4];
 #pragma unroll
@@ -423,29 +533,24 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
             for (int e = 0; e < 4; ++e) R[n][e] = O[n][e] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < DK / 16; ++kk) {
-            uint32_t hi[4], lo[4];
-            split2(S[2 * kk][0] * sc0, S[2 * kk][1] * sc0, hi[0], lo[0]);
-            split2(S[2 * kk][2] * sc1, S[2 * kk][3] * sc1, hi[1], lo[1]);
-            split2(S[2 * kk + 1][0] * sc0, S[2 * kk + 1][1] * sc0, hi[2], lo[2]);
-            split2(S[2 * kk + 1][2] * sc1, S[2 * kk + 1][3] * sc1, hi[3], lo[3]);
+            uint32_t hi[4], lo[4], b[4][4];
+            split_a(S[2 * kk], S[2 * kk + 1], sc0, sc1, hi, lo);
 #pragma unroll
-            for (int n2 = 0; n2 < 4; ++n2) {
-                const uint32_t at = tile_at<Z::KP>(16 * n2 + b_row, 2 * kk + b_seg);
-                uint32_t b[4];
-                ldmatrix4(b, sb + Z::K + at);
-                mma(R[2 * n2], hi, b[0], b[1]);
-                mma(R[2 * n2 + 1], hi, b[2], b[3]);
-                mma(R[2 * n2], lo, b[0], b[1]);
-                mma(R[2 * n2 + 1], lo, b[2], b[3]);
-                if constexpr (F32) {
-                    ldmatrix4(b, sb + Z::KLO + at);
-                    mma(R[2 * n2], hi, b[0], b[1]);
-                    mma(R[2 * n2 + 1], hi, b[2], b[3]);
-                }
-                ldmatrix4(b, sb + Z::Q + at);
-                mma(O[2 * n2], hi, b[0], b[1]);
-                mma(O[2 * n2 + 1], hi, b[2], b[3]);
+            for (int n2 = 0; n2 < 4; ++n2) ldmatrix4(b[n2], sb + Z::K + tile_at<Z::KP>(16 * n2 + b_row, 2 * kk + b_seg));
+#pragma unroll
+            for (int n = 0; n < 8; ++n) mma(R[n], hi, b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
+#pragma unroll
+            for (int n = 0; n < 8; ++n) mma(R[n], lo, b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
+            if constexpr (F32) {
+#pragma unroll
+                for (int n2 = 0; n2 < 4; ++n2) ldmatrix4(b[n2], sb + Z::KLO + tile_at<Z::KP>(16 * n2 + b_row, 2 * kk + b_seg));
+#pragma unroll
+                for (int n = 0; n < 8; ++n) mma(R[n], hi, b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
             }
+#pragma unroll
+            for (int n2 = 0; n2 < 4; ++n2) ldmatrix4(b[n2], sb + Z::Q + tile_at<Z::KP>(16 * n2 + b_row, 2 * kk + b_seg));
+#pragma unroll
+            for (int n = 0; n < 8; ++n) mma(O[n], hi, b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
         }
         // R = beta v - beta e^G (S^T k); the queries' part of the outputs
         const float is0 = pow2_inverse(sc0), is1 = pow2_inverse(sc1);
@@ -503,12 +608,7 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
         // U^T = R^T T^T, 16 tokens at a time from the last: a block of U takes the place of the block of R that no other needs
         uint32_t rh[4][4], rl[4][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float s = e & 1 ? rs1 : rs0;
-                split2(R[2 * j + (e >> 1)][2 * (e & 1)] * s, R[2 * j + (e >> 1)][2 * (e & 1) + 1] * s, rh[j][e], rl[j][e]);
-            }
+        for (int j = 0; j < 4; ++j) split_a(R[2 * j], R[2 * j + 1], rs0, rs1, rh[j], rl[j]);
         const float ir0 = pow2_inverse(rs0), ir1 = pow2_inverse(rs1);
         float u0 = 0.f, u1 = 0.f;
 #pragma unroll
@@ -516,7 +616,7 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
             float x[2][4] = {};
 #pragma unroll
             for (int j = 0; j <= i; ++j) {
-                const uint32_t at = tile_at<2 * CH>(16 * i + b_row, 2 * j + b_seg);
+                const uint32_t at = tile_at<Z::TP>(16 * i + b_row, 2 * j + b_seg);
                 uint32_t b[4];
                 ldmatrix4(b, sb + Z::THI + at);
                 mma(x[0], rh[j], b[0], b[1]);
@@ -571,7 +671,7 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
 #pragma unroll
             for (int j = 0; j <= i; ++j) {
                 uint32_t b[4];
-                ldmatrix4(b, sb + Z::P + tile_at<2 * CH>(16 * i + b_row, 2 * j + b_seg));
+                ldmatrix4(b, sb + Z::P + tile_at<Z::TP>(16 * i + b_row, 2 * j + b_seg));
                 mma(x[0], rh[j], b[0], b[1]);
                 mma(x[1], rh[j], b[2], b[3]);
             }
@@ -644,17 +744,18 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
                 if (bad1 < CH) S[j][2] = S[j][3] = nan;
             }
         }
-        if (c + STAGES < chunks) bar_arrive(B::empty(stage), B::COUNT);
+        if (c + Z::STAGES < chunks) bar_arrive(Z::EMPTY + stage, Z::COUNT);
     }
 #pragma unroll
-    for (int j = 0; j < DK / 8; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) state[(int64_t)(8 * j + 2 * quad + (e & 1)) * d.head_v + (e >> 1) * 8] = S[j][e];
+    for (int j = 0; j < DK / 8; ++j, state += 8 * d.head_v) {
+        state[0] = S[j][0]; state[8] = S[j][2];
+        state[d.head_v] = S[j][1]; state[d.head_v + 8] = S[j][3];
+    }
 }
 
-template <bool F32, int DK, int CW, int GROUPS>
-__global__ void __launch_bounds__(Shape<F32, DK, CW, GROUPS>::THREADS, 1) delta_chunk_kernel(Delta d, int above) {
-    using Z = Shape<F32, DK, CW, GROUPS>;
+template <bool F32, int DK, int CW>
+__global__ void __launch_bounds__(Shape<F32, DK, CW>::THREADS, 1) delta_chunk_kernel(Delta d, int above) {
+    using Z = Shape<F32, DK, CW>;
     extern __shared__ __align__(128) char smem[];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -671,17 +772,21 @@ __global__ void __launch_bounds__(Shape<F32, DK, CW, GROUPS>::THREADS, 1) delta_
     }
     const uint32_t base = smem_u32(smem);
     const int chunks = (r.n + CH - 1) / CH;
-    if (threadIdx.x < 32 * CW)
-        run_chain<F32, DK, CW, GROUPS>(d, r, h, col0, smem, base, chunks);
-    else
-        prepare_chunks<F32, DK, CW, GROUPS>(d, r, h, col0, smem, base, (threadIdx.x - 32 * CW) / 128, chunks);
+    // 168 registers a thread at launch; the chain takes what the preparing warps leave
+    if (threadIdx.x < Z::CHAIN) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        if (threadIdx.x < 32 * CW) run_chain<F32, DK, CW>(d, r, h, col0, smem, base, chunks);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 136;");
+        prepare_chunks<F32, DK, CW>(d, r, h, col0, smem, base, chunks);
+    }
 }
 
-template <bool F32, int DK, int CW, int GROUPS>
+template <bool F32, int DK, int CW>
 cudaError_t launch_shape(const Delta& d, int above, cudaStream_t s) {
-    using Z = Shape<F32, DK, CW, GROUPS>;
+    using Z = Shape<F32, DK, CW>;
     static_assert(Z::BYTES <= 227 * 1024, "stages must fit");
-    const auto kernel = delta_chunk_kernel<F32, DK, CW, GROUPS>;
+    const auto kernel = delta_chunk_kernel<F32, DK, CW>;
     static LaunchPrep prep;
     int sms = 0;
     const cudaError_t e = prep.get(kernel, Z::BYTES, &sms);
@@ -692,7 +797,7 @@ cudaError_t launch_shape(const Delta& d, int above, cudaStream_t s) {
 
 template <bool F32, int DK>
 cudaError_t launch_width(const Delta& d, int above, int sms, cudaStream_t s) {
-    return launch_shape<F32, DK, 2, 2>(d, above, s);
+    return launch_shape<F32, DK, 2>(d, above, s);
 }
 
 }  // namespace
