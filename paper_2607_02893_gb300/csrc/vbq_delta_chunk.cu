@@ -39,7 +39,7 @@ namespace vbq {
 namespace {
 
 constexpr int CH = 64;                           // tokens of a chunk
-constexpr int PREP = 256;                        // threads that prepare
+constexpr int STAGES = 2;
 constexpr int DP = 20;                           // floats between rows of an fp32 block of 16 x 16
 
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(threads) : "memory"); }
@@ -67,13 +67,11 @@ __device__ __forceinline__ float exp2_fast(float x) {              // 2 ulps; be
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// 16 bytes to shared memory, zeros where `take` is false; after cp_wait all but the thread's last GROUPS groups have landed.
+// 16 bytes to shared memory, zeros where `take` is false.
 __device__ __forceinline__ void cp_16(uint32_t dst, const void* src, bool take) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int GROUPS>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(GROUPS) : "memory"); }
+__device__ __forceinline__ void cp_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -109,32 +107,40 @@ __device__ __forceinline__ uint32_t tile_at(int row, int seg) {
     return (uint32_t)(row * PITCH + ((seg ^ turn) << 4));
 }
 
-template <bool F32, int DK, int CW>
+// what the gates of a chunk come to, per token, and from G_LAST on for the chunk
+enum { G_HI, G_LO, G_BETA, G_START, G_END, G_BLOCK };
+constexpr int G_LAST = 6 * CH, GATES = 6 * CH + 4;
+
+template <bool F32, int DK, int CW, int PW>
 struct Shape {
     static constexpr int VC = 16 * CW;                              // columns of a block
-    static constexpr int KP = 2 * DK;                               // bytes of a key row in FP16
-    static constexpr int VP = F32 ? 4 * (VC + 4) : 2 * VC;
+    // Bytes of a row of keys in FP16 and of values, 16 more than they hold, so that eight rows' segments fall in distinct
+    // banks (fp32 keys: turned by row instead, for want of room).
+    static constexpr int KP = 2 * DK + (F32 ? 0 : 16), VP = F32 ? 4 * (VC + 4) : 2 * VC + 16;
     static constexpr int TP = 2 * CH;                               // bytes of a row of T, the scores and L
     static constexpr int CHAIN = 32 * (CW < 4 ? 4 : CW);            // whole warpgroups
-    static constexpr int THREADS = CHAIN + PREP;
+    static constexpr int PREP = 32 * PW, THREADS = CHAIN + PREP;
     // a stage: keys (fp32 ones: the two parts of them, where their raw values land), queries, values, T, scores, factors
     static constexpr int K = 0, KLO = K + CH * KP, Q = KLO + (F32 ? CH * KP : 0), QLO = Q + CH * KP, V = QLO + (F32 ? CH * KP : 0),
-                         THI = V + CH * VP, TLO = THI + CH * TP, P = TLO + CH * TP, FAC = P + CH * TP,
-                         STAGE = (FAC + (6 * CH + 4) * 4 + 127) / 128 * 128;
+                         THI = (V + CH * VP + 127) / 128 * 128, TLO = THI + CH * TP, P = TLO + CH * TP, FAC = P + CH * TP,
+                         STAGE = (FAC + (5 * CH + 4) * 4 + 127) / 128 * 128;
     // scratch of the preparing warps: -L in FP16 parts, its blocks on the diagonal in fp32, factors
-    static constexpr int LHI = 0, LLO = LHI + CH * TP, DIAG = LLO + CH * TP, TOKENS = DIAG + 4 * 16 * DP * 4, SCRATCH = TOKENS + 7 * CH * 4;
-    static constexpr int STAGES = 3 * STAGE + SCRATCH <= 227 * 1024 ? 3 : 2;
+    static constexpr int LHI = 0, LLO = LHI + CH * TP, DIAG = LLO + CH * TP, TOKENS = DIAG + 4 * 16 * DP * 4,
+                         SCRATCH = TOKENS + (2 * CH + GATES) * 4;
     static constexpr int OWN = STAGES * STAGE, BYTES = OWN + SCRATCH;
     // named barriers
     static constexpr int FULL = 1, EMPTY = FULL + STAGES, PREPARING = EMPTY + STAGES, COUNT = 32 * CW + PREP;
+    __device__ static __forceinline__ uint32_t key_at(int row, int seg) {
+        return F32 ? tile_at<2 * DK>(row, seg) : (uint32_t)(row * KP + seg * 16);
+    }
 };
 // what a stage tells about its tokens
 enum { F_BETA, F_STATE, F_END, F_QUERY, F_SCORE };                  // and from F_LAST on: e^G_last
-constexpr int F_LAST = 6 * CH;
+constexpr int F_LAST = 5 * CH;
 
 // ---------------------------------------------------------------------------
-// Preparing the chunks: 8 warps, one chunk after the other. Loops are kept rolled where registers allow: the code of both
-// roles has to stay in the instruction cache.
+// Preparing the chunks: PW warps (4 or 8), one chunk after the other. Loops are kept rolled where registers allow: the code of both roles
+// has to stay in the instruction cache.
 // ---------------------------------------------------------------------------
 
 // The power of two for a row of this sum of squares: its largest value comes to at most 2^15, and to 2^10 at least (128
@@ -145,11 +151,22 @@ __device__ __forceinline__ float row_scale(float squares) {
     return __uint_as_float((uint32_t)((up > 60 ? 60 : up) + 127) << 23);
 }
 
-template <bool F32, int DK, int CW>
+// Sums of log2 decays in fixed point, 32 bits of fraction, as magnitudes: a decay of e^-100 among slow ones would cost the
+// others their digits in fp32 (and 64-bit floating point runs at a 64th of the rate here).
+__device__ __forceinline__ uint64_t to_fixed(float magnitude) {     // 0 .. 2^31
+    const float n = floorf(magnitude);
+    return ((uint64_t)(uint32_t)n << 32) + __float2uint_rz((magnitude - n) * 4294967296.f);
+}
+__device__ __forceinline__ float2 from_fixed(uint64_t x) {          // minus x, as a float and the rest
+    const float n = (float)(uint32_t)(x >> 32), f = (float)(uint32_t)x * 2.3283064365386963e-10f, hi = n + f;
+    return make_float2(-hi, (hi - n) - f);
+}
+
+template <bool F32, int DK, int CW, int PW>
 __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r, int h, int col0, char* smem, uint32_t base, int chunks) {
-    using Z = Shape<F32, DK, CW>;
-    constexpr int SEGS = DK / 8, STEP = PREP / SEGS, SIZE = F32 ? 4 : 2;   // 8 values a thread, STEP rows at once
-    constexpr bool AHEAD = Z::STAGES > 2;                           // the next chunk is loaded while one is worked on
+    using Z = Shape<F32, DK, CW, PW>;
+    constexpr int PREP = Z::PREP, SEGS = DK / 8, STEP = PREP / SEGS, ROWS = CH / STEP;     // 8 values a thread, STEP rows at once
+    constexpr bool AHEAD = !F32 && PW == 8;                         // there are registers for the next chunk's keys and queries
     const int tid = threadIdx.x - Z::CHAIN, warp = tid >> 5, lane = tid & 31;
     const int hk = h / (d.heads / d.k_heads);
     const bool raw = d.a_log != nullptr;
@@ -157,346 +174,384 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
     char* own = smem + Z::OWN;
     const uint32_t own_b = base + Z::OWN;
     float* diag = reinterpret_cast<float*>(own + Z::DIAG);
-    float *upto_hi = reinterpret_cast<float*>(own + Z::TOKENS), *upto_lo = upto_hi + CH, *beta = upto_lo + CH, *ck = beta + CH, *cq = ck + CH,
-          *down_k = cq + CH, *down_q = down_k + CH;
+    float *ck = reinterpret_cast<float*>(own + Z::TOKENS), *cq = ck + CH, *gate = cq + CH;
     const int seg = tid % SEGS, row_in = tid / SEGS;
     const int quad = lane & 3, r8 = lane >> 2;
     const int b_row = (lane & 7) + ((lane >> 4) << 3), b_seg = (lane >> 3) & 1;      // B fragments of two tiles; A, transposed
     const int a_row = lane & 15, a_seg = lane >> 4;
-    const int mt = warp & 3;                                        // this warp's 16 rows, of keys with keys or of queries with keys
-    const bool of_q = warp >= 4;
-    float ga[2] = {}, gb[2] = {};                                   // warp 7: gates of tokens 2 lane and 2 lane + 1, as the call gives them
+    constexpr int sync = Z::PREPARING;
 
-    const auto load = [&](int c) {
-        const int stage = c % Z::STAGES, live = min(CH, r.n - c * CH);
-        const int64_t row0 = (int64_t)r.lo + (int64_t)c * CH;
-        const uint32_t sb = base + stage * Z::STAGE;
-        bar_sync(Z::EMPTY + stage, Z::COUNT);
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-            const int64_t stride = (half ? d.q_stride : d.k_stride) * SIZE;
-            const char* p = static_cast<const char*>(half ? d.q : d.k) + row0 * stride + (hk * DK + seg * 8) * SIZE;
-            const uint32_t to = sb + (half ? Z::Q : Z::K);
+    // BF16 keys and queries: 8 values of ROWS rows of each in registers (rows past the end: the last one's).
+    uint4 keys[ROWS], queries[ROWS];
+    const auto load_rows = [&](uint4 (&x)[ROWS], const void* from, int64_t stride, int c) {
+        const int last = min(CH, r.n - c * CH) - 1;
+        const uint16_t* p = static_cast<const uint16_t*>(from) + ((int64_t)r.lo + (int64_t)c * CH) * stride + hk * DK + seg * 8;
 #pragma unroll
-            for (int row = row_in; row < CH; row += STEP) {
-                const bool in = row < live;
-                const char* q = in ? p + row * stride : p;
-                cp_16(to + tile_at<Z::KP>(row, seg), q, in);
-                if (F32) cp_16(to + CH * Z::KP + tile_at<Z::KP>(row, seg), q + 16, in);
-            }
-        }
-        constexpr int PER = Z::VC * SIZE / 16;
+        for (int i = 0; i < ROWS; ++i) x[i] = *reinterpret_cast<const uint4*>(p + min(row_in + i * STEP, last) * stride);
+    };
+    // Values, and fp32 keys and queries, 16 bytes at a time straight into the stage.
+    const auto load_values = [&](int c, uint32_t to) {
+        constexpr int SIZE = F32 ? 4 : 2, PER = Z::VC * SIZE / 16;
+        const int live = min(CH, r.n - c * CH);
         const int64_t stride = d.v_stride * SIZE;
-        const char* v = static_cast<const char*>(d.v) + row0 * stride + (h * d.head_v + col0) * SIZE;
-#pragma unroll 1
+        const char* v = static_cast<const char*>(d.v) + ((int64_t)r.lo + (int64_t)c * CH) * stride + (h * d.head_v + col0) * SIZE;
+#pragma unroll 2
         for (int i = tid; i < CH * PER; i += PREP) {
             const int row = i / PER, part = i % PER;
-            const uint32_t dst = F32 ? (uint32_t)(row * Z::VP + part * 16) : tile_at<Z::VP>(row, part);
-            cp_16(sb + Z::V + dst, row < live ? v + row * stride + part * 16 : v, row < live);
+            cp_16(to + row * Z::VP + part * 16, row < live ? v + row * stride + part * 16 : v, row < live);
         }
-        cp_commit();
-        if (warp == 7) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int t = 2 * lane + e;
-                if (t < live) {
-                    ga[e] = gate_value(d.decay, d.gate_f32, (row0 + t) * d.decay_stride + h);
-                    gb[e] = gate_value(d.beta, d.gate_f32, (row0 + t) * d.beta_stride + h);
-                }
-            }
+    };
+    const auto load_pieces = [&](const void* from, int64_t stride, int c, uint32_t to) {
+        const int live = min(CH, r.n - c * CH);
+        const float* p = static_cast<const float*>(from) + ((int64_t)r.lo + (int64_t)c * CH) * stride + hk * DK + seg * 8;
+#pragma unroll 2
+        for (int row = row_in; row < CH; row += STEP) {
+            const float* q = row < live ? p + row * stride : p;
+            cp_16(to + Z::key_at(row, seg), q, row < live);
+            cp_16(to + CH * Z::KP + Z::key_at(row, seg), q + 4, row < live);
         }
     };
 
-    int first = AHEAD ? -1 : 0;                                     // a turn that only loads
+    // A chunk's gates, two neighbouring tokens a lane of the last warp: as the call gives them, then what they come to.
+    float ga[2] = {}, gb[2] = {};
+    const auto load_gates = [&](int c) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int t = c * CH + 2 * lane + e;
+            if (t < r.n) {
+                ga[e] = gate_value(d.decay, d.gate_f32, ((int64_t)r.lo + t) * d.decay_stride + h);
+                gb[e] = gate_value(d.beta, d.gate_f32, ((int64_t)r.lo + t) * d.beta_stride + h);
+            }
+        }
+    };
+    const auto sum_gates = [&](int c) {
+        constexpr float LOG2E = 1.44269504f;
+        const int t = 2 * lane, live = r.n - c * CH;
+        Gate x0 = gate_of(ga[0], gb[0], raw, rate, bias), x1 = gate_of(ga[1], gb[1], raw, rate, bias);
+        if (t >= live) x0 = {0.f, 0.f};
+        if (t + 1 >= live) x1 = {0.f, 0.f};
+        const uint64_t f1 = to_fixed(-x1.g * LOG2E);
+        uint64_t sum = to_fixed(-x0.g * LOG2E) + f1;
+#pragma unroll 1
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint64_t x = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += x;
+        }
+        const uint64_t all = __shfl_sync(0xffffffffu, sum, 31), end = __shfl_sync(0xffffffffu, sum, lane | 7);   // of the chunk; of the token's 16
+        // A NaN decay makes NaNs of the sums that it is in.
+        const uint32_t odd = __ballot_sync(0xffffffffu, x0.g + x1.g != x0.g + x1.g);
+        const float nan0 = (odd & ((2u << lane) - 1)) && (x0.g != x0.g || (odd & ((1u << lane) - 1))) ? __int_as_float(0x7fffffff) : 0.f;
+        const float nan1 = odd & ((2u << lane) - 1) ? __int_as_float(0x7fffffff) : 0.f, nan = odd ? __int_as_float(0x7fffffff) : 0.f;
+        const float2 u0 = from_fixed(sum - f1), u1 = from_fixed(sum);
+        const auto put = [&](int what, float x, float y) { *reinterpret_cast<float2*>(gate + what * CH + t) = make_float2(x, y); };
+        put(G_HI, u0.x + nan0, u1.x + nan1);
+        put(G_LO, u0.y, u1.y);
+        put(G_BETA, x0.beta, x1.beta);
+        put(G_START, exp2f(u0.x + nan0), exp2f(u1.x + nan1));
+        put(G_END, exp2f(from_fixed(all - sum + f1).x + nan), exp2f(from_fixed(all - sum).x + nan));
+        put(G_BLOCK, exp2f(from_fixed(end - sum + f1).x + nan1), exp2f(from_fixed(end - sum).x + nan1));
+        if (lane == 0) gate[G_LAST] = exp2f(from_fixed(all).x + nan);
+    };
+
+    int first = -1;                                     // a turn that only loads
     asm volatile("" : "+r"(first));                                 // unknown to the compiler, which would write that turn out on its own
 #pragma unroll 1
     for (int c = first; c < chunks; ++c) {
-        const int stage = (c + Z::STAGES) % Z::STAGES;
-        const int live = min(CH, r.n - c * CH);
+        const int stage = c & (STAGES - 1);
         char* st = smem + stage * Z::STAGE;
         const uint32_t sb = base + stage * Z::STAGE;
         float* fac = reinterpret_cast<float*>(st + Z::FAC);
-        const float a0 = ga[0], a1 = ga[1], b0 = gb[0], b1 = gb[1];
-        const int next = AHEAD ? c + 1 : c;
-        if (next < chunks) load(next);
-        else cp_commit();
-        if (c < 0) continue;
-        cp_wait<AHEAD ? 1 : 0>();
-        // keys and queries to FP16 in their place, each segment by the thread that loaded it
+        const int next = c + 1;
+        if (warp == PW - 1 && next < chunks) load_gates(next);
+        if (c >= 0) {
+            if constexpr (!F32 && !AHEAD) load_rows(keys, d.k, d.k_stride, c);
+            bar_sync(Z::EMPTY + stage, Z::COUNT);
+            load_values(c, sb + Z::V);
+            // keys and queries to FP16 by a power of two a row; what a row's unit length makes of them
+            if constexpr (F32) {
+                load_pieces(d.k, d.k_stride, c, sb + Z::K);
+                load_pieces(d.q, d.q_stride, c, sb + Z::Q);
+                cp_wait_all();
+            }
+            const auto scaled = [&](float (&y)[8], int row, float* unit, float scale) {
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum = fmaf(y[e], y[e], sum);
+#pragma unroll
+                for (int o = SEGS / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                const float up = row_scale(sum);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] *= up;
+                if (seg == 0) unit[row] = (d.normalize ? rsqrtf(sum + DELTA_UNIT_EPS) : 1.f) * pow2_inverse(up) * scale;
+            };
+            if constexpr (F32) {
 #pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-            char* tile = st + (half ? Z::Q : Z::K);
-            float *down = half ? down_q : down_k, *unit = half ? cq : ck;
-#pragma unroll(F32 ? 1 : 4)
-            for (int row = row_in; row < CH; row += STEP) {
-                uint4* at = reinterpret_cast<uint4*>(tile + tile_at<Z::KP>(row, seg));
-                const uint4 x = *at;
-                uint32_t hi[4], lo[4];
-                float up;
-                if constexpr (F32) {
-                    uint4* more = reinterpret_cast<uint4*>(tile + CH * Z::KP + tile_at<Z::KP>(row, seg));
-                    const uint4 z = *more;
-                    const float y[8] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w),
-                                        __uint_as_float(z.x), __uint_as_float(z.y), __uint_as_float(z.z), __uint_as_float(z.w)};
-                    float sum = 0.f;
+                for (int half = 0; half < 2; ++half) {              // in place: each piece by the thread that loaded it
+                    char* tile = st + (half ? Z::Q : Z::K);
+#pragma unroll 1
+                    for (int row = row_in; row < CH; row += STEP) {
+                        uint4 *at = reinterpret_cast<uint4*>(tile + Z::key_at(row, seg)), *more = reinterpret_cast<uint4*>(tile + CH * Z::KP + Z::key_at(row, seg));
+                        const uint4 x = *at, z = *more;
+                        float y[8] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w),
+                                      __uint_as_float(z.x), __uint_as_float(z.y), __uint_as_float(z.z), __uint_as_float(z.w)};
+                        scaled(y, row, half ? cq : ck, half ? d.scale : 1.f);
+                        uint32_t hi[4], lo[4];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sum = fmaf(y[e], y[e], sum);
-#pragma unroll
-                    for (int o = SEGS / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                    up = row_scale(sum);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) split2(y[2 * e] * up, y[2 * e + 1] * up, hi[e], lo[e]);
-                    *more = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                    if (seg == 0) unit[row] = d.normalize ? rsqrtf(sum + DELTA_UNIT_EPS) : 1.f;
-                } else {
-                    // by the largest magnitude; the sums of squares come out of the products below
-                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-                    constexpr uint32_t MAGNITUDES = 0x7fff7fffu;
-                    uint32_t m = __vmaxu2(__vmaxu2(w[0] & MAGNITUDES, w[1] & MAGNITUDES), __vmaxu2(w[2] & MAGNITUDES, w[3] & MAGNITUDES));
-#pragma unroll
-                    for (int o = SEGS / 2; o; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
-                    m = max(m & 0xffffu, m >> 16);
-                    up = to_f16_range(__uint_as_float(m << 16));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) hi[e] = pack_f16(__uint_as_float(w[e] << 16) * up, __uint_as_float(w[e] & 0xffff0000u) * up);
+                        for (int e = 0; e < 4; ++e) split2(y[2 * e], y[2 * e + 1], hi[e], lo[e]);
+                        *at = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                        *more = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    }
                 }
-                *at = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                if (seg == 0) down[row] = pow2_inverse(up);
+            } else {
+                const auto convert = [&](uint4 (&x)[ROWS], char* tile, float* unit, float scale) {
+                    if (r.n - c * CH < CH)
+#pragma unroll
+                        for (int i = 0; i < ROWS; ++i)
+                            if (row_in + i * STEP >= r.n - c * CH) x[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < ROWS; ++i) {
+                        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                        float y[8];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { y[2 * e] = __uint_as_float(w[e] << 16); y[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u); }
+                        scaled(y, row_in + i * STEP, unit, scale);
+                        *reinterpret_cast<uint4*>(tile + Z::key_at(row_in + i * STEP, seg)) =
+                            make_uint4(pack_f16(y[0], y[1]), pack_f16(y[2], y[3]), pack_f16(y[4], y[5]), pack_f16(y[6], y[7]));
+                    }
+                };
+                convert(keys, st + Z::K, ck, 1.f);
+                if constexpr (!AHEAD) load_rows(keys, d.q, d.q_stride, c);
+                if constexpr (AHEAD) convert(queries, st + Z::Q, cq, d.scale);
+                else convert(keys, st + Z::Q, cq, d.scale);
             }
-        }
-        if (warp == 7) {
-            // sums in 64 bits: a decay of e^-100 among slow ones would cost the others their digits
-            constexpr double LOG2E = 1.4426950408889634;
-            const int t = 2 * lane;
-            Gate x0 = gate_of(AHEAD ? a0 : ga[0], AHEAD ? b0 : gb[0], raw, rate, bias), x1 = gate_of(AHEAD ? a1 : ga[1], AHEAD ? b1 : gb[1], raw, rate, bias);
-            if (t >= live) x0 = {0.f, 0.f};
-            if (t + 1 >= live) x1 = {0.f, 0.f};
-            double sum = (double)x0.g + (double)x1.g;
+            bar_sync(sync, PREP);
+            // the tokens' factors
+            if (tid < CH) {
+                const float f = ck[tid], g = gate[G_BETA * CH + tid];
+                fac[F_BETA * CH + tid] = g;
+                fac[F_STATE * CH + tid] = g * gate[G_START * CH + tid] * f;
+                fac[F_END * CH + tid] = gate[G_END * CH + tid] * f;
+            } else if (tid < 2 * CH) {
+                const int t = tid - CH;
+                fac[F_QUERY * CH + t] = gate[G_START * CH + t] * cq[t];
+                if (t == 0) fac[F_LAST] = gate[G_LAST];
+            }
+            // 16 rows of keys or of queries with the keys up to theirs. Four warps: of keys, then of queries, those of the warp
+            // across, so that each has five blocks of 16 x 16 in all.
 #pragma unroll 1
-            for (int o = 1; o < 32; o <<= 1) {
-                const double x = __shfl_up_sync(0xffffffffu, sum, o);
-                if (lane >= o) sum += x;
-            }
-            const double all = __shfl_sync(0xffffffffu, sum, 31) * LOG2E;
-            const double u1 = sum * LOG2E, u0 = (sum - (double)x1.g) * LOG2E;
-            const float h0 = (float)u0, h1 = (float)u1, q0 = exp2f(h0), q1 = exp2f(h1);
-            const auto put = [&](float* p, float x, float y) { *reinterpret_cast<float2*>(p + t) = make_float2(x, y); };
-            put(upto_hi, h0, h1);
-            put(upto_lo, (float)(u0 - h0), (float)(u1 - h1));
-            put(beta, x0.beta, x1.beta);
-            put(fac + F_BETA * CH, x0.beta, x1.beta);
-            put(fac + F_STATE * CH, x0.beta * q0, x1.beta * q1);
-            put(fac + F_QUERY * CH, q0, q1);
-            put(fac + F_END * CH, exp2f((float)(all - u0)), exp2f((float)(all - u1)));
-            if (lane == 0) fac[F_LAST] = exp2f((float)all);
-        }
-        bar_sync(Z::PREPARING, PREP);
-        // 16 rows of keys (warps 0..3) or of queries with all the keys up to theirs
-        float acc[8][4], squares[2][4] = {};
+            for (int turn = 0; turn < 8 / PW; ++turn) {
+                const bool of_q = PW == 8 ? warp >= 4 : turn;
+                const int mt = PW == 8 ? warp & 3 : of_q ? 3 - warp : warp;
+                float acc[8][4];
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
+                for (int n = 0; n < 8; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[n][e] = 0.f;
-        {
-            const uint32_t a_at = sb + (of_q ? Z::Q : Z::K);
+                    for (int e = 0; e < 4; ++e) acc[n][e] = 0.f;
+                const uint32_t a_at = sb + (of_q ? Z::Q : Z::K);
+                uint32_t fa[2][4], fb[2][4][4];
+                const auto load5 = [&](int i, int kk) {
+                    ldmatrix4(fa[i], a_at + Z::key_at(16 * mt + a_row, 2 * kk + a_seg));
+#pragma unroll
+                    for (int n2 = 0; n2 < 4; ++n2)
+                        if (n2 <= mt) ldmatrix4(fb[i][n2], sb + Z::K + Z::key_at(16 * n2 + b_row, 2 * kk + b_seg));
+                };
+                if (!F32) load5(0, 0);
 #pragma unroll(F32 ? 1 : 2)
-            for (int kk = 0; kk < DK / 16; ++kk) {
-                uint32_t a[4], alo[4], b[4];
-                ldmatrix4(a, a_at + tile_at<Z::KP>(16 * mt + a_row, 2 * kk + a_seg));
-                if (F32) ldmatrix4(alo, a_at + CH * Z::KP + tile_at<Z::KP>(16 * mt + a_row, 2 * kk + a_seg));
-                if (!F32 && of_q) {                                 // the queries' squares, on the diagonal
-                    ldmatrix4(b, a_at + tile_at<Z::KP>(16 * mt + b_row, 2 * kk + b_seg));
-                    mma(squares[0], a, b[0], b[1]);
-                    mma(squares[1], a, b[2], b[3]);
-                }
+                for (int kk = 0; kk < DK / 16; ++kk) {
+                    const int i = F32 ? 0 : kk & 1;
+                    if (F32) load5(0, kk);
+                    else if (kk + 1 < DK / 16) load5(i ^ 1, kk + 1);
 #pragma unroll
-                for (int n2 = 0; n2 < 4; ++n2) {
-                    if (n2 > mt) break;
-                    ldmatrix4(b, sb + Z::K + tile_at<Z::KP>(16 * n2 + b_row, 2 * kk + b_seg));
-                    mma(acc[2 * n2], a, b[0], b[1]);
-                    mma(acc[2 * n2 + 1], a, b[2], b[3]);
+                    for (int n2 = 0; n2 < 4; ++n2) {
+                        if (n2 > mt) break;
+                        mma(acc[2 * n2], fa[i], fb[i][n2][0], fb[i][n2][1]);
+                        mma(acc[2 * n2 + 1], fa[i], fb[i][n2][2], fb[i][n2][3]);
+                    }
                     if (F32) {
-                        mma(acc[2 * n2], alo, b[0], b[1]);
-                        mma(acc[2 * n2 + 1], alo, b[2], b[3]);
-                        ldmatrix4(b, sb + Z::KLO + tile_at<Z::KP>(16 * n2 + b_row, 2 * kk + b_seg));
-                        mma(acc[2 * n2], a, b[0], b[1]);
-                        mma(acc[2 * n2 + 1], a, b[2], b[3]);
+                        uint32_t alo[4], b[4];
+                        ldmatrix4(alo, a_at + CH * Z::KP + Z::key_at(16 * mt + a_row, 2 * kk + a_seg));
+#pragma unroll
+                        for (int n2 = 0; n2 < 4; ++n2) {
+                            if (n2 > mt) break;
+                            mma(acc[2 * n2], alo, fb[i][n2][0], fb[i][n2][1]);
+                            mma(acc[2 * n2 + 1], alo, fb[i][n2][2], fb[i][n2][3]);
+                            ldmatrix4(b, sb + Z::KLO + Z::key_at(16 * n2 + b_row, 2 * kk + b_seg));
+                            mma(acc[2 * n2], fa[i], b[0], b[1]);
+                            mma(acc[2 * n2 + 1], fa[i], b[2], b[3]);
+                        }
+                    }
+                }
+                // -L or the scores: products times their tokens' factors and the decay between them. Across blocks of 16 the
+                // decay is that from the column's token to its block's end times that from there on, both at most 1.
+                const int i0 = 16 * mt + r8, i1 = i0 + 8;
+                float m0 = 0.f, m1 = 0.f;
+                {
+                    const float *upto_hi = gate + G_HI * CH, *upto_lo = gate + G_LO * CH, *beta = gate + G_BETA * CH;
+                    const float h0 = upto_hi[i0], h1 = upto_hi[i1], l0 = upto_lo[i0], l1 = upto_lo[i1];
+                    const float s0 = of_q ? cq[i0] : -beta[i0] * ck[i0], s1 = of_q ? cq[i1] : -beta[i1] * ck[i1];
+                    const int below = of_q ? 0 : 1;                 // below the diagonal, or up to it
+#pragma unroll
+                    for (int n2 = 0; n2 < 4; ++n2) {
+                        if (n2 > mt) break;
+                        const float he = upto_hi[16 * n2 + 15], le = upto_lo[16 * n2 + 15];
+                        const float f0 = s0 * exp2_fast((h0 - he) + (l0 - le)), f1 = s1 * exp2_fast((h1 - he) + (l1 - le));
+#pragma unroll
+                        for (int p = 0; p < 2; ++p) {
+                            float(&x)[4] = acc[2 * n2 + p];
+                            const int j0 = 16 * n2 + 8 * p + 2 * quad;
+                            const float2 cj = *reinterpret_cast<const float2*>(ck + j0);
+                            if (n2 < mt) {
+                                const float2 ej = *reinterpret_cast<const float2*>(gate + G_BLOCK * CH + j0);
+                                const float c0 = cj.x * ej.x, c1 = cj.y * ej.y;
+                                x[0] *= c0 * f0; x[1] *= c1 * f0; x[2] *= c0 * f1; x[3] *= c1 * f1;
+                            } else {
+                                const float2 hj = *reinterpret_cast<const float2*>(upto_hi + j0), lj = *reinterpret_cast<const float2*>(upto_lo + j0);
+                                x[0] = j0 + below <= i0 ? (s0 * cj.x) * exp2_fast((h0 - hj.x) + (l0 - lj.x)) * x[0] : 0.f;
+                                x[1] = j0 + 1 + below <= i0 ? (s0 * cj.y) * exp2_fast((h0 - hj.y) + (l0 - lj.y)) * x[1] : 0.f;
+                                x[2] = j0 + below <= i1 ? (s1 * cj.x) * exp2_fast((h1 - hj.x) + (l1 - lj.x)) * x[2] : 0.f;
+                                x[3] = j0 + 1 + below <= i1 ? (s1 * cj.y) * exp2_fast((h1 - hj.y) + (l1 - lj.y)) * x[3] : 0.f;
+                            }
+                            m0 = fmaxf(m0, fmaxf(fabsf(x[0]), fabsf(x[1])));
+                            m1 = fmaxf(m1, fmaxf(fabsf(x[2]), fabsf(x[3])));
+                        }
+                    }
+                }
+                if (of_q) {
+                    const float p0 = to_f16_range(quad_max(m0)), p1 = to_f16_range(quad_max(m1));
+                    if (quad == 0) {
+                        fac[F_SCORE * CH + i0] = pow2_inverse(p0);
+                        fac[F_SCORE * CH + i1] = pow2_inverse(p1);
+                    }
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) {
+                        if (n > 2 * mt + 1) break;
+                        *reinterpret_cast<uint32_t*>(st + Z::P + tile_at<Z::TP>(i0, n) + 4 * quad) = pack_f16(acc[n][0] * p0, acc[n][1] * p0);
+                        *reinterpret_cast<uint32_t*>(st + Z::P + tile_at<Z::TP>(i1, n) + 4 * quad) = pack_f16(acc[n][2] * p1, acc[n][3] * p1);
+                    }
+                } else {
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) {
+                        if (n > 2 * mt + 1) break;
+                        if (n < 2 * mt) {
+                            uint32_t hi, lo;
+                            split2(acc[n][0], acc[n][1], hi, lo);
+                            *reinterpret_cast<uint32_t*>(own + Z::LHI + tile_at<Z::TP>(i0, n) + 4 * quad) = hi;
+                            *reinterpret_cast<uint32_t*>(own + Z::LLO + tile_at<Z::TP>(i0, n) + 4 * quad) = lo;
+                            split2(acc[n][2], acc[n][3], hi, lo);
+                            *reinterpret_cast<uint32_t*>(own + Z::LHI + tile_at<Z::TP>(i1, n) + 4 * quad) = hi;
+                            *reinterpret_cast<uint32_t*>(own + Z::LLO + tile_at<Z::TP>(i1, n) + 4 * quad) = lo;
+                        } else {
+                            float* o = diag + i0 * DP + 8 * (n - 2 * mt) + 2 * quad;
+                            *reinterpret_cast<float2*>(o) = make_float2(acc[n][0], acc[n][1]);
+                            *reinterpret_cast<float2*>(o + 8 * DP) = make_float2(acc[n][2], acc[n][3]);
+                        }
+                    }
+                    // T's block on the diagonal (rows and columns 16 mt ..) by substitution, a column a lane
+                    __syncwarp();
+                    const float* D = diag + 16 * mt * DP;
+                    const int col = lane & 15;
+                    float x[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float t0 = i == col ? 1.f : 0.f, t1 = 0.f;
+#pragma unroll
+                        for (int m = 0; m < i; m += 4) {
+                            const float4 l = *reinterpret_cast<const float4*>(D + i * DP + m);
+                            t0 = fmaf(l.x, x[m], t0);
+                            if (m + 1 < i) t1 = fmaf(l.y, x[m + 1], t1);
+                            if (m + 2 < i) t0 = fmaf(l.z, x[m + 2], t0);
+                            if (m + 3 < i) t1 = fmaf(l.w, x[m + 3], t1);
+                        }
+                        x[i] = i < col ? 0.f : t0 + t1;
+                    }
+                    // the first half of the lanes writes the high parts, the second the low ones
+                    char* to = st + (lane < 16 ? Z::THI : Z::TLO) + 2 * (col & 7);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const __half hi = __float2half_rn(x[i]);
+                        *reinterpret_cast<__half*>(to + tile_at<Z::TP>(16 * mt + i, 2 * mt + (col >> 3))) =
+                            lane < 16 ? hi : __float2half_rn(x[i] - __half2float(hi));
                     }
                 }
             }
-        }
-        if (!F32) {
-            // unit lengths from the diagonals, which are in the rows' own powers of two
-            const auto put = [&](int row, float x) {
-                const float p = (of_q ? down_q : down_k)[row];
-                (of_q ? cq : ck)[row] = d.normalize ? rsqrtf(x * p * p + DELTA_UNIT_EPS) : 1.f;
-            };
-            if (!of_q)
-#pragma unroll
-                for (int n2 = 0; n2 < 4; ++n2)
-                    if (n2 == mt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) { squares[0][e] = acc[2 * n2][e]; squares[1][e] = acc[2 * n2 + 1][e]; }
-            if (2 * quad == (r8 & ~1)) {                            // columns 2 quad + e, rows r8 and r8 + 8
-                put(16 * mt + r8, r8 & 1 ? squares[0][1] : squares[0][0]);
-                put(16 * mt + r8 + 8, r8 & 1 ? squares[1][3] : squares[1][2]);
-            }
-        }
-        bar_sync(Z::PREPARING, PREP);
-        // the tokens' other factors
-        if (tid < CH) {
-            const float f = ck[tid] * down_k[tid];
-            fac[F_STATE * CH + tid] *= f;
-            fac[F_END * CH + tid] *= f;
-        } else if (tid < 2 * CH) {
-            fac[F_QUERY * CH + tid - CH] *= cq[tid - CH] * down_q[tid - CH] * d.scale;
-        }
-        // -L and the scores: products times their tokens' factors and the decay between them
-        const int i0 = 16 * mt + r8, i1 = i0 + 8;
-        float m0 = 0.f, m1 = 0.f;
-        {
-            const float h0 = upto_hi[i0], h1 = upto_hi[i1], l0 = upto_lo[i0], l1 = upto_lo[i1];
-            const float s0 = of_q ? cq[i0] * down_q[i0] * d.scale : -beta[i0] * ck[i0] * down_k[i0];
-            const float s1 = of_q ? cq[i1] * down_q[i1] * d.scale : -beta[i1] * ck[i1] * down_k[i1];
-            const int below = of_q ? 0 : 1;                         // below the diagonal, or up to it
-#pragma unroll
-            for (int n = 0; n < 8; ++n) {
-                if (n > 2 * mt + 1) break;
-                const int j0 = 8 * n + 2 * quad;
-                const float2 hj = *reinterpret_cast<const float2*>(upto_hi + j0), lj = *reinterpret_cast<const float2*>(upto_lo + j0);
-                const float2 cj = *reinterpret_cast<const float2*>(ck + j0), dj = *reinterpret_cast<const float2*>(down_k + j0);
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int j = j0 + e + below;
-                    const float he = e ? hj.y : hj.x, le = e ? lj.y : lj.x, ce = e ? cj.y * dj.y : cj.x * dj.x;
-                    acc[n][e] = j <= i0 ? (s0 * ce) * exp2_fast((h0 - he) + (l0 - le)) * acc[n][e] : 0.f;
-                    acc[n][2 + e] = j <= i1 ? (s1 * ce) * exp2_fast((h1 - he) + (l1 - le)) * acc[n][2 + e] : 0.f;
-                    m0 = fmaxf(m0, fabsf(acc[n][e]));
-                    m1 = fmaxf(m1, fabsf(acc[n][2 + e]));
+            bar_sync(sync, PREP);
+            if constexpr (AHEAD) {
+                if (next < chunks) {
+                    load_rows(keys, d.k, d.k_stride, next);
+                    load_rows(queries, d.q, d.q_stride, next);
                 }
             }
-        }
-        if (of_q) {
-            const float p0 = to_f16_range(quad_max(m0)), p1 = to_f16_range(quad_max(m1));
-            if (quad == 0) {
-                fac[F_SCORE * CH + i0] = pow2_inverse(p0);
-                fac[F_SCORE * CH + i1] = pow2_inverse(p1);
-            }
+            // The blocks below the diagonal, T_ba = T_bb sum_(a <= c < b) (-L_bc) T_ca, block column a by warp a, transposed: each
+            // T_ca^T is an A fragment as it comes out of the products.
+            if (warp < 3) {
+                uint32_t th[3][4], tl[3][4];
+                ldmatrix4_trans(th[0], sb + Z::THI + tile_at<Z::TP>(16 * warp + b_row, 2 * warp + b_seg));
+                ldmatrix4_trans(tl[0], sb + Z::TLO + tile_at<Z::TP>(16 * warp + b_row, 2 * warp + b_seg));
 #pragma unroll
-            for (int n = 0; n < 8; ++n) {
-                if (n > 2 * mt + 1) break;
-                *reinterpret_cast<uint32_t*>(st + Z::P + tile_at<Z::TP>(i0, n) + 4 * quad) = pack_f16(acc[n][0] * p0, acc[n][1] * p0);
-                *reinterpret_cast<uint32_t*>(st + Z::P + tile_at<Z::TP>(i1, n) + 4 * quad) = pack_f16(acc[n][2] * p1, acc[n][3] * p1);
+                for (int bi = 1; bi < 4; ++bi) {
+                    const int b = warp + bi;
+                    if (b > 3) break;
+                    float x[2][4] = {}, y[2][4] = {};
+                    uint32_t f[4] = {}, e[4] = {}, hi[4], lo[4];
+                    const auto product = [&](const uint32_t (&ah)[4], const uint32_t (&al)[4]) {
+                        mma(x[0], ah, f[0], f[1]);
+                        mma(x[1], ah, f[2], f[3]);
+                        mma(y[0], al, f[0], f[1]);
+                        mma(y[1], al, f[2], f[3]);
+                        mma(y[0], ah, e[0], e[1]);
+                        mma(y[1], ah, e[2], e[3]);
+                    };
+                    const auto collect = [&] {
+#pragma unroll
+                        for (int p = 0; p < 2; ++p)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) { x[p][i] += y[p][i]; y[p][i] = 0.f; }
+                        split_a(x[0], x[1], 1.f, 1.f, hi, lo);
+#pragma unroll
+                        for (int p = 0; p < 2; ++p)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) x[p][i] = 0.f;
+                    };
+#pragma unroll
+                    for (int ci = 0; ci < bi; ++ci) {
+                        ldmatrix4(f, own_b + Z::LHI + tile_at<Z::TP>(16 * b + b_row, 2 * (warp + ci) + b_seg));
+                        ldmatrix4(e, own_b + Z::LLO + tile_at<Z::TP>(16 * b + b_row, 2 * (warp + ci) + b_seg));
+                        product(th[ci], tl[ci]);
+                    }
+                    ldmatrix4(f, sb + Z::THI + tile_at<Z::TP>(16 * b + b_row, 2 * b + b_seg));
+                    ldmatrix4(e, sb + Z::TLO + tile_at<Z::TP>(16 * b + b_row, 2 * b + b_seg));
+                    collect();
+                    product(hi, lo);
+                    collect();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (bi < 3) { th[bi][i] = hi[i]; tl[bi][i] = lo[i]; }
+                        const uint32_t at = tile_at<Z::TP>(16 * b + 8 * (i >> 1) + r8, 2 * warp + (i & 1)) + 4 * quad;
+                        *reinterpret_cast<uint32_t*>(st + Z::THI + at) = movmatrix_trans(hi[i]);
+                        *reinterpret_cast<uint32_t*>(st + Z::TLO + at) = movmatrix_trans(lo[i]);
+                    }
+                }
+            } else if (warp == PW - 1 && next < chunks) {
+                sum_gates(next);
             }
+            if constexpr (!F32) cp_wait_all();
+            bar_arrive(Z::FULL + stage, Z::COUNT);
         } else {
-#pragma unroll
-            for (int n = 0; n < 8; ++n) {
-                if (n > 2 * mt + 1) break;
-                if (n < 2 * mt) {
-                    uint32_t hi, lo;
-                    split2(acc[n][0], acc[n][1], hi, lo);
-                    *reinterpret_cast<uint32_t*>(own + Z::LHI + tile_at<Z::TP>(i0, n) + 4 * quad) = hi;
-                    *reinterpret_cast<uint32_t*>(own + Z::LLO + tile_at<Z::TP>(i0, n) + 4 * quad) = lo;
-                    split2(acc[n][2], acc[n][3], hi, lo);
-                    *reinterpret_cast<uint32_t*>(own + Z::LHI + tile_at<Z::TP>(i1, n) + 4 * quad) = hi;
-                    *reinterpret_cast<uint32_t*>(own + Z::LLO + tile_at<Z::TP>(i1, n) + 4 * quad) = lo;
-                } else {
-                    float* o = diag + i0 * DP + 8 * (n - 2 * mt) + 2 * quad;
-                    *reinterpret_cast<float2*>(o) = make_float2(acc[n][0], acc[n][1]);
-                    *reinterpret_cast<float2*>(o + 8 * DP) = make_float2(acc[n][2], acc[n][3]);
-                }
+            if constexpr (AHEAD) {
+                load_rows(keys, d.k, d.k_stride, next);
+                load_rows(queries, d.q, d.q_stride, next);
             }
-            // T's block on the diagonal (rows and columns 16 mt ..) by substitution, a column a lane
-            __syncwarp();
-            const float* D = diag + 16 * mt * DP;
-            const int col = lane & 15;
-            float x[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float t0 = i == col ? 1.f : 0.f, t1 = 0.f;
-#pragma unroll
-                for (int m = 0; m < i; m += 4) {
-                    const float4 l = *reinterpret_cast<const float4*>(D + i * DP + m);
-                    t0 = fmaf(l.x, x[m], t0);
-                    if (m + 1 < i) t1 = fmaf(l.y, x[m + 1], t1);
-                    if (m + 2 < i) t0 = fmaf(l.z, x[m + 2], t0);
-                    if (m + 3 < i) t1 = fmaf(l.w, x[m + 3], t1);
-                }
-                x[i] = i < col ? 0.f : t0 + t1;
-            }
-            // the first half of the lanes writes the high parts, the second the low ones
-            char* to = st + (lane < 16 ? Z::THI : Z::TLO) + 2 * (col & 7);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const __half hi = __float2half_rn(x[i]);
-                *reinterpret_cast<__half*>(to + tile_at<Z::TP>(16 * mt + i, 2 * mt + (col >> 3))) = lane < 16 ? hi : __float2half_rn(x[i] - __half2float(hi));
-            }
+            if (warp == PW - 1) sum_gates(next);
         }
-        bar_sync(Z::PREPARING, PREP);
-        // The blocks below the diagonal, T_ba = T_bb sum_(a <= c < b) (-L_bc) T_ca, block column a by warp a, transposed: each
-        // T_ca^T is an A fragment as it comes out of the products.
-        if (warp < 3) {
-            uint32_t th[3][4], tl[3][4];
-            ldmatrix4_trans(th[0], sb + Z::THI + tile_at<Z::TP>(16 * warp + b_row, 2 * warp + b_seg));
-            ldmatrix4_trans(tl[0], sb + Z::TLO + tile_at<Z::TP>(16 * warp + b_row, 2 * warp + b_seg));
-#pragma unroll
-            for (int bi = 1; bi < 4; ++bi) {
-                const int b = warp + bi;
-                if (b > 3) break;
-                float x[2][4] = {}, y[2][4] = {};
-                uint32_t f[4], e[4], hi[4], lo[4];
-#pragma unroll
-                for (int ci = 0; ci < bi; ++ci) {
-                    ldmatrix4(f, own_b + Z::LHI + tile_at<Z::TP>(16 * b + b_row, 2 * (warp + ci) + b_seg));
-                    ldmatrix4(e, own_b + Z::LLO + tile_at<Z::TP>(16 * b + b_row, 2 * (warp + ci) + b_seg));
-                    mma(x[0], th[ci], f[0], f[1]);
-                    mma(x[1], th[ci], f[2], f[3]);
-                    mma(y[0], tl[ci], f[0], f[1]);
-                    mma(y[1], tl[ci], f[2], f[3]);
-                    mma(y[0], th[ci], e[0], e[1]);
-                    mma(y[1], th[ci], e[2], e[3]);
-                }
-#pragma unroll
-                for (int p = 0; p < 2; ++p)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) { x[p][i] += y[p][i]; y[p][i] = 0.f; }
-                split_a(x[0], x[1], 1.f, 1.f, hi, lo);
-#pragma unroll
-                for (int p = 0; p < 2; ++p)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[p][i] = 0.f;
-                ldmatrix4(f, sb + Z::THI + tile_at<Z::TP>(16 * b + b_row, 2 * b + b_seg));
-                ldmatrix4(e, sb + Z::TLO + tile_at<Z::TP>(16 * b + b_row, 2 * b + b_seg));
-                mma(x[0], hi, f[0], f[1]);
-                mma(x[1], hi, f[2], f[3]);
-                mma(y[0], lo, f[0], f[1]);
-                mma(y[1], lo, f[2], f[3]);
-                mma(y[0], hi, e[0], e[1]);
-                mma(y[1], hi, e[2], e[3]);
-#pragma unroll
-                for (int p = 0; p < 2; ++p)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[p][i] += y[p][i];
-                split_a(x[0], x[1], 1.f, 1.f, hi, lo);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (bi < 3) { th[bi][i] = hi[i]; tl[bi][i] = lo[i]; }
-                    const uint32_t at = tile_at<Z::TP>(16 * b + 8 * (i >> 1) + r8, 2 * warp + (i & 1)) + 4 * quad;
-                    *reinterpret_cast<uint32_t*>(st + Z::THI + at) = movmatrix_trans(hi[i]);
-                    *reinterpret_cast<uint32_t*>(st + Z::TLO + at) = movmatrix_trans(lo[i]);
-                }
-            }
-        }
-        bar_arrive(Z::FULL + stage, Z::COUNT);
     }
 }
 
 // ---------------------------------------------------------------------------
 // The chain: a warp, 16 columns.
 // ---------------------------------------------------------------------------
-template <bool F32, int DK, int CW>
+template <bool F32, int DK, int CW, int PW>
 __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int h, int col0, char* smem, uint32_t base, int chunks) {
-    using Z = Shape<F32, DK, CW>;
+    using Z = Shape<F32, DK, CW, PW>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3, r8 = lane >> 2;
     const int vcol = 16 * warp;
     float* state = d.state + ((int64_t)r.slot * d.heads + h) * DK * d.head_v + 2 * quad * d.head_v + col0 + vcol + r8;
@@ -507,12 +562,12 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
         S[j][0] = r.fresh ? 0.f : from[0]; S[j][2] = r.fresh ? 0.f : from[8];
         S[j][1] = r.fresh ? 0.f : from[d.head_v]; S[j][3] = r.fresh ? 0.f : from[d.head_v + 8];
     }
-    for (int i = 0; i < Z::STAGES && i < chunks; ++i) bar_arrive(Z::EMPTY + i, Z::COUNT);
+    for (int i = 0; i < STAGES && i < chunks; ++i) bar_arrive(Z::EMPTY + i, Z::COUNT);
     const int b_row = (lane & 7) + ((lane >> 4) << 3), b_seg = (lane >> 3) & 1;                        // two tiles of tokens
     const int t_row = (lane & 7) + (((lane >> 3) & 1) << 3), t_seg = lane >> 4;                        // transposed: 16 tokens, two tiles of columns
 #pragma unroll 1
     for (int c = 0; c < chunks; ++c) {
-        const int stage = c % Z::STAGES;
+        const int stage = c & (STAGES - 1);
         const char* st = smem + stage * Z::STAGE;
         const uint32_t sb = base + stage * Z::STAGE;
         const float* fac = reinterpret_cast<const float*>(st + Z::FAC);
@@ -531,26 +586,33 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
         for (int n = 0; n < 8; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) R[n][e] = O[n][e] = 0.f;
+        // fragments one step ahead of their products
+        uint32_t fk[2][4][4], fq[4][4];
+        const auto load4 = [&](uint32_t (&f)[4][4], int tile, int kk) {
+#pragma unroll
+            for (int n2 = 0; n2 < 4; ++n2) ldmatrix4(f[n2], sb + tile + Z::key_at(16 * n2 + b_row, 2 * kk + b_seg));
+        };
+        load4(fk[0], Z::K, 0);
 #pragma unroll
         for (int kk = 0; kk < DK / 16; ++kk) {
-            uint32_t hi[4], lo[4], b[4][4];
+            uint32_t hi[4], lo[4];
+            uint32_t (&b)[4][4] = fk[kk & 1];
             split_a(S[2 * kk], S[2 * kk + 1], sc0, sc1, hi, lo);
-#pragma unroll
-            for (int n2 = 0; n2 < 4; ++n2) ldmatrix4(b[n2], sb + Z::K + tile_at<Z::KP>(16 * n2 + b_row, 2 * kk + b_seg));
+            load4(fq, Z::Q, kk);
 #pragma unroll
             for (int n = 0; n < 8; ++n) mma(R[n], hi, b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
+            if (!F32 && kk + 1 < DK / 16) load4(fk[(kk + 1) & 1], Z::K, kk + 1);
+            if (F32) load4(fk[(kk + 1) & 1], Z::KLO, kk);
 #pragma unroll
             for (int n = 0; n < 8; ++n) mma(R[n], lo, b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
             if constexpr (F32) {
+                uint32_t (&l)[4][4] = fk[(kk + 1) & 1];
 #pragma unroll
-                for (int n2 = 0; n2 < 4; ++n2) ldmatrix4(b[n2], sb + Z::KLO + tile_at<Z::KP>(16 * n2 + b_row, 2 * kk + b_seg));
-#pragma unroll
-                for (int n = 0; n < 8; ++n) mma(R[n], hi, b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
+                for (int n = 0; n < 8; ++n) mma(R[n], hi, l[n >> 1][2 * (n & 1)], l[n >> 1][2 * (n & 1) + 1]);
+                if (kk + 1 < DK / 16) load4(fk[(kk + 1) & 1], Z::K, kk + 1);
             }
 #pragma unroll
-            for (int n2 = 0; n2 < 4; ++n2) ldmatrix4(b[n2], sb + Z::Q + tile_at<Z::KP>(16 * n2 + b_row, 2 * kk + b_seg));
-#pragma unroll
-            for (int n = 0; n < 8; ++n) mma(O[n], hi, b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
+            for (int n = 0; n < 8; ++n) mma(O[n], hi, fq[n >> 1][2 * (n & 1)], fq[n >> 1][2 * (n & 1) + 1]);
         }
         // R = beta v - beta e^G (S^T k); the queries' part of the outputs
         const float is0 = pow2_inverse(sc0), is1 = pow2_inverse(sc1);
@@ -558,7 +620,7 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
 #pragma unroll
         for (int n2 = 0; n2 < 4; ++n2) {
             uint32_t v[4];
-            if constexpr (!F32) ldmatrix4_trans(v, sb + Z::V + tile_at<Z::VP>(16 * n2 + b_row, vcol / 8 + b_seg));
+            if constexpr (!F32) ldmatrix4_trans(v, sb + Z::V + (16 * n2 + b_row) * Z::VP + (vcol / 8 + b_seg) * 16);
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
                 const int n = 2 * n2 + p, t = 8 * n + 2 * quad;
@@ -709,26 +771,32 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
             }
         const float ie0 = pow2_inverse(es0), ie1 = pow2_inverse(es1);
         const float last = fac[F_LAST];
+        uint32_t fu[2][2][4];
+        const auto load2 = [&](uint32_t (&f)[2][4], int tile, int step) {           // 16 tokens by four tiles of S
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+                ldmatrix4_trans(f[p], sb + tile + Z::key_at(16 * (step & 3) + t_row, 4 * (step >> 2) + 2 * p + t_seg));
+        };
+        load2(fu[0], Z::K, 0);
 #pragma unroll
         for (int j4 = 0; j4 < DK / 32; ++j4) {                       // four tiles of S at a time
             float x[4][4] = {};
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
+            for (int kk = 0; kk < 4; ++kk) {
+                const int step = 4 * j4 + kk;
+                uint32_t (&b)[2][4] = fu[step & 1], (&next)[2][4] = fu[(step + 1) & 1];
+                if (F32) load2(next, Z::KLO, step);
+                else if (step + 1 < DK / 8) load2(next, Z::K, step + 1);
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const uint32_t at = tile_at<Z::KP>(16 * kk + t_row, 4 * j4 + 2 * p + t_seg);
-                    uint32_t b[4];
-                    ldmatrix4_trans(b, sb + Z::K + at);
-                    mma(x[2 * p], rh[kk], b[0], b[1]);
-                    mma(x[2 * p + 1], rh[kk], b[2], b[3]);
-                    mma(x[2 * p], rl[kk], b[0], b[1]);
-                    mma(x[2 * p + 1], rl[kk], b[2], b[3]);
-                    if constexpr (F32) {
-                        ldmatrix4_trans(b, sb + Z::KLO + at);
-                        mma(x[2 * p], rh[kk], b[0], b[1]);
-                        mma(x[2 * p + 1], rh[kk], b[2], b[3]);
-                    }
+                for (int p = 0; p < 4; ++p) mma(x[p], rh[kk], b[p >> 1][2 * (p & 1)], b[p >> 1][2 * (p & 1) + 1]);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) mma(x[p], rl[kk], b[p >> 1][2 * (p & 1)], b[p >> 1][2 * (p & 1) + 1]);
+                if constexpr (F32) {
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) mma(x[p], rh[kk], next[p >> 1][2 * (p & 1)], next[p >> 1][2 * (p & 1) + 1]);
+                    if (step + 1 < DK / 8) load2(next, Z::K, step + 1);
                 }
+            }
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
                 float(&s)[4] = S[4 * j4 + p];
@@ -744,7 +812,7 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
                 if (bad1 < CH) S[j][2] = S[j][3] = nan;
             }
         }
-        if (c + Z::STAGES < chunks) bar_arrive(Z::EMPTY + stage, Z::COUNT);
+        if (c + STAGES < chunks) bar_arrive(Z::EMPTY + stage, Z::COUNT);
     }
 #pragma unroll
     for (int j = 0; j < DK / 8; ++j, state += 8 * d.head_v) {
@@ -753,9 +821,9 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
     }
 }
 
-template <bool F32, int DK, int CW>
-__global__ void __launch_bounds__(Shape<F32, DK, CW>::THREADS, 1) delta_chunk_kernel(Delta d, int above) {
-    using Z = Shape<F32, DK, CW>;
+template <bool F32, int DK, int CW, int PW>
+__global__ void __launch_bounds__(Shape<F32, DK, CW, PW>::THREADS, 1) delta_chunk_kernel(Delta d, int above) {
+    using Z = Shape<F32, DK, CW, PW>;
     extern __shared__ __align__(128) char smem[];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -772,21 +840,24 @@ __global__ void __launch_bounds__(Shape<F32, DK, CW>::THREADS, 1) delta_chunk_ke
     }
     const uint32_t base = smem_u32(smem);
     const int chunks = (r.n + CH - 1) / CH;
-    // 168 registers a thread at launch; the chain takes what the preparing warps leave
+    // Three warpgroups of 168 registers a thread at launch; the chain takes what the preparing warps leave.
+    static_assert(Z::THREADS == 384);
     if (threadIdx.x < Z::CHAIN) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
-        if (threadIdx.x < 32 * CW) run_chain<F32, DK, CW>(d, r, h, col0, smem, base, chunks);
+        if (CW == 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        if (threadIdx.x < 32 * CW) run_chain<F32, DK, CW, PW>(d, r, h, col0, smem, base, chunks);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 136;");
-        prepare_chunks<F32, DK, CW>(d, r, h, col0, smem, base, chunks);
+        if (CW == 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 136;");
+        prepare_chunks<F32, DK, CW, PW>(d, r, h, col0, smem, base, chunks);
     }
 }
 
-template <bool F32, int DK, int CW>
+template <bool F32, int DK, int CW, int PW>
 cudaError_t launch_shape(const Delta& d, int above, cudaStream_t s) {
-    using Z = Shape<F32, DK, CW>;
+    using Z = Shape<F32, DK, CW, PW>;
     static_assert(Z::BYTES <= 227 * 1024, "stages must fit");
-    const auto kernel = delta_chunk_kernel<F32, DK, CW>;
+    const auto kernel = delta_chunk_kernel<F32, DK, CW, PW>;
     static LaunchPrep prep;
     int sms = 0;
     const cudaError_t e = prep.get(kernel, Z::BYTES, &sms);
@@ -797,7 +868,17 @@ cudaError_t launch_shape(const Delta& d, int above, cudaStream_t s) {
 
 template <bool F32, int DK>
 cudaError_t launch_width(const Delta& d, int above, int sms, cudaStream_t s) {
-    return launch_shape<F32, DK, 2>(d, above, s);
+        // Chain warps of a block. All blocks of a head prepare the same chunks, so fewer and wider blocks do less in all, and more
+    // and narrower ones fill the GPU: as wide as leaves every SM a block, by the sequences like the longest that the tokens
+    // make up. Five sequences of 1774 to 3001 tokens, 32 heads of 128: 1202 us with 2, 737 with 4, 695 with 8; one of 32768:
+    // 3.5, 3.6 and 6.0 ms.
+    if constexpr (!F32) {
+        const int64_t alike = d.seq.tokens / d.seq.rows, sequences = alike < 1 ? 1 : alike > d.seq.batch ? d.seq.batch : alike;
+        const int64_t columns = sequences * d.heads * d.head_v;
+        if (d.head_v % 128 == 0 && columns / 128 >= sms) return launch_shape<F32, DK, 8, 4>(d, above, s);
+        if (columns / 64 >= sms) return launch_shape<F32, DK, 4, 8>(d, above, s);
+    }
+    return launch_shape<F32, DK, 2, 8>(d, above, s);
 }
 
 }  // namespace
