@@ -17,7 +17,7 @@ namespace {
 
 constexpr int CONV_THREADS = 128;
 constexpr int CONV_ROWS = 32;        // rows of a tile
-constexpr int CONV_AHEAD = 4;        // rows loaded together
+constexpr int CONV_AHEAD = 8;        // rows loaded together, ahead of their use
 
 // Tile `t` of the call is tile *tile of sequence b. With `starts`, sequence b's tiles are among numbers starts[b] / ROWS + b
 // and on: a sequence of n rows spans at most floor(starts[b + 1] / ROWS) - floor(starts[b] / ROWS) + 1 of them, so the
@@ -50,11 +50,34 @@ __device__ __forceinline__ int find_tile(const vbq_sequences& q, int t, int* til
     return b;
 }
 
+// Four neighbouring values of a row, as they come and in fp32.
+template <bool F32>
+struct Four {
+    uint4 raw;                       // BF16: the first two words
+    __device__ __forceinline__ void load(const void* x, int64_t at) {
+        if constexpr (F32) {
+            raw = *reinterpret_cast<const uint4*>(static_cast<const float*>(x) + at);
+        } else {
+            const uint2 a = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(x) + at);
+            raw.x = a.x; raw.y = a.y;
+        }
+    }
+    __device__ __forceinline__ void values(float (&v)[4]) const {
+        if constexpr (F32) {
+            v[0] = __uint_as_float(raw.x); v[1] = __uint_as_float(raw.y); v[2] = __uint_as_float(raw.z); v[3] = __uint_as_float(raw.w);
+        } else {
+            v[0] = __uint_as_float(raw.x << 16); v[1] = __uint_as_float(raw.x & 0xffff0000u);
+            v[2] = __uint_as_float(raw.y << 16); v[3] = __uint_as_float(raw.y & 0xffff0000u);
+        }
+    }
+};
+
 template <bool F32, int TAPS>
 __global__ void __launch_bounds__(CONV_THREADS) causal_conv_kernel(Conv c) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int ch = (int)(blockIdx.y * CONV_THREADS + threadIdx.x) * 8;
+    constexpr int PAST = TAPS - 1;
+    const int ch = (int)(blockIdx.y * CONV_THREADS + threadIdx.x) * 4;
     int tile = 0;
     const int b = find_tile(c.seq, (int)blockIdx.x, &tile);
     if (b < 0 || ch >= c.channels) return;
@@ -65,82 +88,88 @@ __global__ void __launch_bounds__(CONV_THREADS) causal_conv_kernel(Conv c) {
     const int64_t row0 = r.lo + t0;
     uint16_t* out = c.out + row0 * c.channels + ch;
     if (r.slot < 0) {
-        for (int i = 0; i < rows; ++i) *reinterpret_cast<uint4*>(out + (int64_t)i * c.channels) = make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < rows; ++i) *reinterpret_cast<uint2*>(out + (int64_t)i * c.channels) = make_uint2(0, 0);
         return;
     }
-    float w[TAPS][8], bias[8] = {}, win[TAPS - 1][8];                // win[j]: the input TAPS - 1 - j rows before
+    const int64_t at = row0 * c.x_stride + ch;
+    Four<F32> next[CONV_AHEAD];
+#pragma unroll
+    for (int i = 0; i < CONV_AHEAD; ++i) next[i].load(c.x, at + min(i, rows - 1) * c.x_stride);
+    float w[TAPS][4], bias[4] = {}, line[PAST + CONV_AHEAD][4];      // line: the inputs before the rows worked on, and theirs
     {
-        float wide[TAPS * 8];
+        float wide[TAPS * 4];
         const float4* p = reinterpret_cast<const float4*>(c.weight + (int64_t)ch * TAPS);
 #pragma unroll
-        for (int i = 0; i < 2 * TAPS; ++i) {
+        for (int i = 0; i < TAPS; ++i) {
             const float4 v = p[i];
             wide[4 * i] = v.x; wide[4 * i + 1] = v.y; wide[4 * i + 2] = v.z; wide[4 * i + 3] = v.w;
         }
 #pragma unroll
         for (int j = 0; j < TAPS; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[j][e] = wide[e * TAPS + j];
+            for (int e = 0; e < 4; ++e) w[j][e] = wide[e * TAPS + j];
     }
-    if (c.bias) load8<true>(bias, c.bias, ch);
-    const int64_t at = row0 * c.x_stride + ch;
+    if (c.bias) {
+        const float4 v = *reinterpret_cast<const float4*>(c.bias + ch);
+        bias[0] = v.x; bias[1] = v.y; bias[2] = v.z; bias[3] = v.w;
+    }
     if (tile > 0) {
 #pragma unroll
-        for (int j = 0; j < TAPS - 1; ++j) load8<F32>(win[j], c.x, at - (int64_t)(TAPS - 1 - j) * c.x_stride);
-    } else {
-        float* carried = c.state + (int64_t)r.slot * (TAPS - 1) * c.channels + ch;
-#pragma unroll
-        for (int j = 0; j < TAPS - 1; ++j) {
-            if (r.fresh) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) win[j][e] = 0.f;
-            } else {
-                load8<true>(win[j], carried, (int64_t)j * c.channels);
-            }
+        for (int j = 0; j < PAST; ++j) {
+            Four<F32> x;
+            x.load(c.x, at - (int64_t)(PAST - j) * c.x_stride);
+            x.values(line[j]);
         }
-        // the sequence's last TAPS - 1 inputs: of x, or for a shorter one of what was carried
+    } else {
+        float* carried = c.state + (int64_t)r.slot * PAST * c.channels + ch;
 #pragma unroll
-        for (int j = 0; j < TAPS - 1; ++j) {
-            float last[8];
-            if (r.n + j >= TAPS - 1) {
-                load8<F32>(last, c.x, at + (int64_t)(r.n + j - (TAPS - 1)) * c.x_stride);
+        for (int j = 0; j < PAST; ++j) {
+            Four<true> x = {make_uint4(0, 0, 0, 0)};
+            if (!r.fresh) x.load(carried, (int64_t)j * c.channels);
+            x.values(line[j]);
+        }
+        // the sequence's last PAST inputs: of x, or for a shorter one of what was carried
+#pragma unroll
+        for (int j = 0; j < PAST; ++j) {
+            float last[4];
+            if (r.n + j >= PAST) {
+                Four<F32> x;
+                x.load(c.x, at + (int64_t)(r.n + j - PAST) * c.x_stride);
+                x.values(last);
             } else {
 #pragma unroll
-                for (int m = 0; m < TAPS - 1; ++m)
+                for (int m = 0; m < PAST; ++m)
                     if (m == r.n + j)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) last[e] = win[m][e];
+                        for (int e = 0; e < 4; ++e) last[e] = line[m][e];
             }
-            float4* p = reinterpret_cast<float4*>(carried + (int64_t)j * c.channels);
-            p[0] = make_float4(last[0], last[1], last[2], last[3]);
-            p[1] = make_float4(last[4], last[5], last[6], last[7]);
+            *reinterpret_cast<float4*>(carried + (int64_t)j * c.channels) = make_float4(last[0], last[1], last[2], last[3]);
         }
     }
+#pragma unroll 1
     for (int i0 = 0; i0 < rows; i0 += CONV_AHEAD) {
-        float x[CONV_AHEAD][8];
 #pragma unroll
-        for (int i = 0; i < CONV_AHEAD; ++i)
-            if (i0 + i < rows) load8<F32>(x[i], c.x, at + (int64_t)(i0 + i) * c.x_stride);
+        for (int i = 0; i < CONV_AHEAD; ++i) next[i].values(line[PAST + i]);
+        if (i0 + CONV_AHEAD < rows)
+#pragma unroll
+            for (int i = 0; i < CONV_AHEAD; ++i) next[i].load(c.x, at + min(i0 + CONV_AHEAD + i, rows - 1) * c.x_stride);
+        uint16_t* o = out + (int64_t)i0 * c.channels;
 #pragma unroll
         for (int i = 0; i < CONV_AHEAD; ++i) {
-            if (i0 + i >= rows) break;
-            float y[8];
+            float y[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 4; ++e) {
                 float s = bias[e];
 #pragma unroll
-                for (int j = 0; j < TAPS - 1; ++j) s = fmaf(w[j][e], win[j][e], s);
-                s = fmaf(w[TAPS - 1][e], x[i][e], s);
+                for (int j = 0; j < TAPS; ++j) s = fmaf(w[j][e], line[i + j][e], s);
                 y[e] = c.silu ? silu(s) : s;
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-#pragma unroll
-                for (int j = 0; j + 1 < TAPS - 1; ++j) win[j][e] = win[j + 1][e];
-                win[TAPS - 2][e] = x[i][e];
-            }
-            *reinterpret_cast<uint4*>(out + (int64_t)(i0 + i) * c.channels) = pack_bf16x8(y);
+            if (i0 + i < rows) *reinterpret_cast<uint2*>(o + (int64_t)i * c.channels) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
         }
+#pragma unroll
+        for (int j = 0; j < PAST; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) line[j][e] = line[CONV_AHEAD + j][e];
     }
 }
 
@@ -149,7 +178,7 @@ __global__ void __launch_bounds__(CONV_THREADS) causal_conv_kernel(Conv c) {
 cudaError_t launch_causal_conv(const Conv& c, cudaStream_t s) {
     const vbq_sequences& q = c.seq;
     const int64_t tiles = q.starts ? q.tokens / CONV_ROWS + q.batch : (int64_t)((q.rows + CONV_ROWS - 1) / CONV_ROWS) * q.batch;
-    const dim3 grid((unsigned)tiles, (unsigned)((c.channels / 8 + CONV_THREADS - 1) / CONV_THREADS));
+    const dim3 grid((unsigned)tiles, (unsigned)((c.channels / 4 + CONV_THREADS - 1) / CONV_THREADS));
     const auto go = [&](auto kernel) { return launch_dependent(kernel, grid, CONV_THREADS, 0, s, c); };
     if (c.f32) return c.taps == 2 ? go(causal_conv_kernel<true, 2>) : c.taps == 3 ? go(causal_conv_kernel<true, 3>) : go(causal_conv_kernel<true, 4>);
     return c.taps == 2 ? go(causal_conv_kernel<false, 2>) : c.taps == 3 ? go(causal_conv_kernel<false, 3>) : go(causal_conv_kernel<false, 4>);

@@ -868,15 +868,16 @@ cudaError_t launch_shape(const Delta& d, int above, cudaStream_t s) {
 
 template <bool F32, int DK>
 cudaError_t launch_width(const Delta& d, int above, int sms, cudaStream_t s) {
-        // Chain warps of a block. All blocks of a head prepare the same chunks, so fewer and wider blocks do less in all, and more
-    // and narrower ones fill the GPU: as wide as leaves every SM a block, by the sequences like the longest that the tokens
-    // make up. Five sequences of 1774 to 3001 tokens, 32 heads of 128: 1202 us with 2, 737 with 4, 695 with 8; one of 32768:
-    // 3.5, 3.6 and 6.0 ms.
+    // Columns of a block. All blocks of a head prepare the same chunks, so fewer and wider ones do less in all, and more and
+    // narrower ones fill the GPU. A chunk takes a block of 32, 64 or 128 columns about 6.7, 7.1 and 11.5 us; the rounds of
+    // blocks are counted by the sequences like the longest that the tokens make up. Five sequences of 1774 to 3001 tokens, 32
+    // heads of 128: 1202, 737 and 695 us; one of 32768: 3.5, 3.6 and 6.0 ms.
     if constexpr (!F32) {
-        const int64_t alike = d.seq.tokens / d.seq.rows, sequences = alike < 1 ? 1 : alike > d.seq.batch ? d.seq.batch : alike;
-        const int64_t columns = sequences * d.heads * d.head_v;
-        if (d.head_v % 128 == 0 && columns / 128 >= sms) return launch_shape<F32, DK, 8, 4>(d, above, s);
-        if (columns / 64 >= sms) return launch_shape<F32, DK, 4, 8>(d, above, s);
+        const int64_t alike = (d.seq.tokens + d.seq.rows / 2) / d.seq.rows, sequences = alike < 1 ? 1 : alike > d.seq.batch ? d.seq.batch : alike;
+        const auto cost = [&](int columns, int64_t each) { return (sequences * d.heads * d.head_v / columns + sms - 1) / sms * each; };
+        const int64_t narrow = cost(32, 67), middle = cost(64, 71), wide = d.head_v % 128 == 0 ? cost(128, 115) : INT64_MAX;
+        if (wide < narrow && wide < middle) return launch_shape<F32, DK, 8, 4>(d, above, s);
+        if (middle < narrow) return launch_shape<F32, DK, 4, 8>(d, above, s);
     }
     return launch_shape<F32, DK, 2, 8>(d, above, s);
 }
