@@ -30,6 +30,7 @@
 // NaN and infinities must not reach earlier tokens through the zeros above the
 // diagonal: a column whose R is not finite at some token is computed without it
 // and gets NaN from that token on.
+#include <type_traits>
 #include <cuda_fp16.h>
 
 #include "vbq_delta.cuh"
@@ -273,17 +274,6 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 load_pieces(d.q, d.q_stride, c, sb + Z::Q);
                 cp_wait_all();
             }
-            const auto scaled = [&](float (&y)[8], int row, float* unit, float scale) {
-                float sum = 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum = fmaf(y[e], y[e], sum);
-#pragma unroll
-                for (int o = SEGS / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                const float up = row_scale(sum);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] *= up;
-                if (seg == 0) unit[row] = (d.normalize ? rsqrtf(sum + DELTA_UNIT_EPS) : 1.f) * pow2_inverse(up) * scale;
-            };
             if constexpr (F32) {
 #pragma unroll 1
                 for (int half = 0; half < 2; ++half) {              // in place: each piece by the thread that loaded it
@@ -294,48 +284,49 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                         const uint4 x = *at, z = *more;
                         float y[8] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w),
                                       __uint_as_float(z.x), __uint_as_float(z.y), __uint_as_float(z.z), __uint_as_float(z.w)};
-                        scaled(y, row, half ? cq : ck, half ? d.scale : 1.f);
+                        float sum = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sum = fmaf(y[e], y[e], sum);
+#pragma unroll
+                        for (int o = SEGS / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                        const float up = row_scale(sum);
+                        if (seg == 0) (half ? cq : ck)[row] = (d.normalize ? rsqrtf(sum + DELTA_UNIT_EPS) : 1.f) * pow2_inverse(up);
                         uint32_t hi[4], lo[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) split2(y[2 * e], y[2 * e + 1], hi[e], lo[e]);
+                        for (int e = 0; e < 4; ++e) split2(y[2 * e] * up, y[2 * e + 1] * up, hi[e], lo[e]);
                         *at = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                         *more = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                     }
                 }
             } else {
-                const auto convert = [&](uint4 (&x)[ROWS], char* tile, float* unit, float scale) {
+                // one power of two for a thread's rows, by their largest magnitude: what is below 2^-32 of it loses digits
+                const auto convert = [&](uint4 (&x)[ROWS], char* tile, float* down) {
                     if (r.n - c * CH < CH)
 #pragma unroll
                         for (int i = 0; i < ROWS; ++i)
                             if (row_in + i * STEP >= r.n - c * CH) x[i] = make_uint4(0, 0, 0, 0);
+                    constexpr uint32_t MAGNITUDES = 0x7fff7fffu;
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int i = 0; i < ROWS; ++i)
+                        m = __vmaxu2(__vmaxu2(m, __vmaxu2(x[i].x & MAGNITUDES, x[i].y & MAGNITUDES)), __vmaxu2(x[i].z & MAGNITUDES, x[i].w & MAGNITUDES));
+#pragma unroll
+                    for (int o = SEGS / 2; o; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    const float up = to_f16_range(__uint_as_float(max(m & 0xffffu, m >> 16) << 16)), inverse = pow2_inverse(up);
+                    const auto two = [&](uint32_t w) { return pack_f16(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up); };
+                    char* to = tile + Z::key_at(row_in, seg);
 #pragma unroll
                     for (int i = 0; i < ROWS; ++i) {
-                        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-                        float y[8];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) { y[2 * e] = __uint_as_float(w[e] << 16); y[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u); }
-                        scaled(y, row_in + i * STEP, unit, scale);
-                        *reinterpret_cast<uint4*>(tile + Z::key_at(row_in + i * STEP, seg)) =
-                            make_uint4(pack_f16(y[0], y[1]), pack_f16(y[2], y[3]), pack_f16(y[4], y[5]), pack_f16(y[6], y[7]));
+                        *reinterpret_cast<uint4*>(to + i * STEP * Z::KP) = make_uint4(two(x[i].x), two(x[i].y), two(x[i].z), two(x[i].w));
+                        if (seg == 0) down[row_in + i * STEP] = inverse;
                     }
                 };
-                convert(keys, st + Z::K, ck, 1.f);
+                convert(keys, st + Z::K, ck);
                 if constexpr (!AHEAD) load_rows(keys, d.q, d.q_stride, c);
-                if constexpr (AHEAD) convert(queries, st + Z::Q, cq, d.scale);
-                else convert(keys, st + Z::Q, cq, d.scale);
+                if constexpr (AHEAD) convert(queries, st + Z::Q, cq);
+                else convert(keys, st + Z::Q, cq);
             }
             bar_sync(sync, PREP);
-            // the tokens' factors
-            if (tid < CH) {
-                const float f = ck[tid], g = gate[G_BETA * CH + tid];
-                fac[F_BETA * CH + tid] = g;
-                fac[F_STATE * CH + tid] = g * gate[G_START * CH + tid] * f;
-                fac[F_END * CH + tid] = gate[G_END * CH + tid] * f;
-            } else if (tid < 2 * CH) {
-                const int t = tid - CH;
-                fac[F_QUERY * CH + t] = gate[G_START * CH + t] * cq[t];
-                if (t == 0) fac[F_LAST] = gate[G_LAST];
-            }
             // 16 rows of keys or of queries with the keys up to theirs. Four warps: of keys, then of queries, those of the warp
             // across, so that each has five blocks of 16 x 16 in all.
 #pragma unroll 1
@@ -347,40 +338,77 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 for (int n = 0; n < 8; ++n)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[n][e] = 0.f;
-                const uint32_t a_at = sb + (of_q ? Z::Q : Z::K);
-                uint32_t fa[2][4], fb[2][4][4];
-                const auto load5 = [&](int i, int kk) {
-                    ldmatrix4(fa[i], a_at + Z::key_at(16 * mt + a_row, 2 * kk + a_seg));
+                float squares[2][4] = {};                           // the rows' own block, for its diagonal
+                const uint32_t a_at = sb + (of_q ? Z::Q : Z::K), a_in = Z::key_at(16 * mt + a_row, a_seg), own_in = Z::key_at(16 * mt + b_row, b_seg),
+                               b_in = Z::key_at(b_row, b_seg);
+                const auto products = [&](auto blocks) {            // with the keys of blocks 0 .. mt
+                    constexpr int N = decltype(blocks)::value;
+#pragma unroll(F32 ? 1 : DK / 16)
+                    for (int kk = 0; kk < DK / 16; ++kk) {
+                        uint32_t a[4], alo[4], b[N][4], l[4];
+                        if constexpr (F32) {
+                            ldmatrix4(a, a_at + Z::key_at(16 * mt + a_row, 2 * kk + a_seg));
+                            ldmatrix4(alo, a_at + CH * Z::KP + Z::key_at(16 * mt + a_row, 2 * kk + a_seg));
+                        } else {
+                            ldmatrix4(a, a_at + a_in + 32 * kk);
+                            if (of_q) ldmatrix4(l, a_at + own_in + 32 * kk);
+                        }
 #pragma unroll
-                    for (int n2 = 0; n2 < 4; ++n2)
-                        if (n2 <= mt) ldmatrix4(fb[i][n2], sb + Z::K + Z::key_at(16 * n2 + b_row, 2 * kk + b_seg));
-                };
-                if (!F32) load5(0, 0);
-#pragma unroll(F32 ? 1 : 2)
-                for (int kk = 0; kk < DK / 16; ++kk) {
-                    const int i = F32 ? 0 : kk & 1;
-                    if (F32) load5(0, kk);
-                    else if (kk + 1 < DK / 16) load5(i ^ 1, kk + 1);
+                        for (int n2 = 0; n2 < N; ++n2)
+                            ldmatrix4(b[n2], sb + Z::K + (F32 ? Z::key_at(16 * n2 + b_row, 2 * kk + b_seg) : b_in + 16 * n2 * Z::KP + 32 * kk));
+                        if (!F32 && of_q) {
+                            mma(squares[0], a, l[0], l[1]);
+                            mma(squares[1], a, l[2], l[3]);
+                        }
 #pragma unroll
-                    for (int n2 = 0; n2 < 4; ++n2) {
-                        if (n2 > mt) break;
-                        mma(acc[2 * n2], fa[i], fb[i][n2][0], fb[i][n2][1]);
-                        mma(acc[2 * n2 + 1], fa[i], fb[i][n2][2], fb[i][n2][3]);
-                    }
-                    if (F32) {
-                        uint32_t alo[4], b[4];
-                        ldmatrix4(alo, a_at + CH * Z::KP + Z::key_at(16 * mt + a_row, 2 * kk + a_seg));
+                        for (int n2 = 0; n2 < N; ++n2) {
+                            mma(acc[2 * n2], a, b[n2][0], b[n2][1]);
+                            mma(acc[2 * n2 + 1], a, b[n2][2], b[n2][3]);
+                        }
+                        if constexpr (F32) {
 #pragma unroll
-                        for (int n2 = 0; n2 < 4; ++n2) {
-                            if (n2 > mt) break;
-                            mma(acc[2 * n2], alo, fb[i][n2][0], fb[i][n2][1]);
-                            mma(acc[2 * n2 + 1], alo, fb[i][n2][2], fb[i][n2][3]);
-                            ldmatrix4(b, sb + Z::KLO + Z::key_at(16 * n2 + b_row, 2 * kk + b_seg));
-                            mma(acc[2 * n2], fa[i], b[0], b[1]);
-                            mma(acc[2 * n2 + 1], fa[i], b[2], b[3]);
+                            for (int n2 = 0; n2 < N; ++n2) {
+                                mma(acc[2 * n2], alo, b[n2][0], b[n2][1]);
+                                mma(acc[2 * n2 + 1], alo, b[n2][2], b[n2][3]);
+                                ldmatrix4(l, sb + Z::KLO + Z::key_at(16 * n2 + b_row, 2 * kk + b_seg));
+                                mma(acc[2 * n2], a, l[0], l[1]);
+                                mma(acc[2 * n2 + 1], a, l[2], l[3]);
+                            }
                         }
                     }
+                    if (!F32 && !of_q)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { squares[0][e] = acc[2 * N - 2][e]; squares[1][e] = acc[2 * N - 1][e]; }
+                };
+                switch (mt) {
+                    case 0: products(std::integral_constant<int, 1>()); break;
+                    case 1: products(std::integral_constant<int, 2>()); break;
+                    case 2: products(std::integral_constant<int, 3>()); break;
+                    default: products(std::integral_constant<int, 4>());
                 }
+                // the rows' factors, their unit lengths among them (BF16: from the diagonals, in the rows' own powers of two)
+                const auto put = [&](int row, float x) {
+                    float* unit = (of_q ? cq : ck) + row;
+                    float f = *unit;
+                    if (!F32) f *= d.normalize ? rsqrtf(x * f * f + DELTA_UNIT_EPS) : 1.f;
+                    if (of_q) {
+                        f *= d.scale;
+                        fac[F_QUERY * CH + row] = gate[G_START * CH + row] * f;
+                    } else {
+                        const float g = gate[G_BETA * CH + row];
+                        fac[F_BETA * CH + row] = g;
+                        fac[F_STATE * CH + row] = g * gate[G_START * CH + row] * f;
+                        fac[F_END * CH + row] = gate[G_END * CH + row] * f;
+                    }
+                    *unit = f;
+                };
+                if (2 * quad == (r8 & ~1)) {                        // columns 2 quad + e, rows r8 and r8 + 8
+                    put(16 * mt + r8, r8 & 1 ? squares[0][1] : squares[0][0]);
+                    put(16 * mt + r8 + 8, r8 & 1 ? squares[1][3] : squares[1][2]);
+                }
+                if (tid == 0) fac[F_LAST] = gate[G_LAST];
+                if (PW == 8 || !of_q) bar_sync(sync, PREP);
+                else __syncwarp();
                 // -L or the scores: products times their tokens' factors and the decay between them. Across blocks of 16 the
                 // decay is that from the column's token to its block's end times that from there on, both at most 1.
                 const int i0 = 16 * mt + r8, i1 = i0 + 8;
@@ -825,7 +853,6 @@ template <bool F32, int DK, int CW, int PW>
 __global__ void __launch_bounds__(Shape<F32, DK, CW, PW>::THREADS, 1) delta_chunk_kernel(Delta d, int above) {
     using Z = Shape<F32, DK, CW, PW>;
     extern __shared__ __align__(128) char smem[];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int slices = d.head_v / Z::VC;
     const int unit = (int)(blockIdx.x / slices), slice = (int)(blockIdx.x - unit * slices);
