@@ -35,7 +35,11 @@
 // token, which BF16 values survive unchanged (8 bits of 11, 39 binades down from
 // the largest); S, R, U and T enter as two FP16 parts, x = hi + lo, with a power
 // of two per column of S, so a product is good to 2^-22 (fp32 keys are two parts
-// as well). What reaches the outputs alone, which are rounded to BF16, enters as
+// as well). T and L are up by 2^10, so that what a strong decay leaves of an
+// earlier token's R keeps its digits (parts end at 2^-35, not 2^-25, which had an
+// element of 2e-5 off by 2e-8); they overflow from 64 on, and where the rule
+// contracts |T_ij| is at most |beta_i| |k_i| |k_j|, 2 for keys of unit length.
+// What reaches the outputs alone, which are rounded to BF16, enters as
 // one part (2^-12): queries, scores, and S and U beside them.
 //
 // NaN and infinities must not reach earlier tokens through the zeros above the
@@ -52,6 +56,7 @@ namespace {
 
 constexpr int CH = 64;                           // tokens of a chunk
 constexpr int STAGES = 2;
+constexpr float T_UP = 1024.f;                   // T and L in FP16 parts are up by this: see above
 constexpr int DP = 20;                           // floats between rows of an fp32 block of 16 x 16
 
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(threads) : "memory"); }
@@ -370,6 +375,16 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                         for (int i = 0; i < ROWS; ++i)
                             m = __vmaxu2(__vmaxu2(m, __vmaxu2(x[i].x & MAGNITUDES, x[i].y & MAGNITUDES)), __vmaxu2(x[i].z & MAGNITUDES, x[i].w & MAGNITUDES));
                         m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+                        if (m >= 0x7f80) {                          // infinities and NaN have no say in the others' power of two
+                            m = 0;
+                            const auto finite = [&](uint32_t w) { m = max(m, (w & 0x7fff) < 0x7f80 ? w & 0x7fff : 0u); };
+#pragma unroll
+                            for (int i = 0; i < ROWS; ++i) {
+                                finite(x[i].x); finite(x[i].x >> 16); finite(x[i].y); finite(x[i].y >> 16);
+                                finite(x[i].z); finite(x[i].z >> 16); finite(x[i].w); finite(x[i].w >> 16);
+                            }
+                            m = __reduce_max_sync(0xffffffffu, m);
+                        }
                         const float up = to_f16_range(__uint_as_float(m << 16)), inverse = pow2_inverse(up);
                         const auto two = [&](uint32_t w) { return pack_f16(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up); };
                         char* to = st + (half ? Z::Q : Z::K) + Z::key_at(row, seg);
@@ -497,16 +512,16 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 {
                     const float *upto_hi = gate + G_HI * CH, *upto_lo = gate + G_LO * CH, *beta = gate + G_BETA * CH;
                     const float h0 = upto_hi[i0], h1 = upto_hi[i1], l0 = upto_lo[i0], l1 = upto_lo[i1];
-                    const float s0 = of_q ? cq[i0] : -beta[i0] * ck[i0], s1 = of_q ? cq[i1] : -beta[i1] * ck[i1];
+                    const float s0 = of_q ? cq[i0] : -beta[i0] * ck[i0], s1 = of_q ? cq[i1] : -beta[i1] * ck[i1], up = of_q ? 1.f : T_UP;
                     const auto largest = [&](const float (&x)[4]) {
-                        m0 = fmaxf(m0, fmaxf(fabsf(x[0]), fabsf(x[1])));
-                        m1 = fmaxf(m1, fmaxf(fabsf(x[2]), fabsf(x[3])));
+                        m0 = max_of(m0, x[0], x[1]);
+                        m1 = max_of(m1, x[2], x[3]);
                     };
 #pragma unroll
                     for (int n2 = 0; n2 < 3; ++n2) {
                         if (n2 >= mt) break;
                         const float he = upto_hi[16 * n2 + 15], le = upto_lo[16 * n2 + 15];
-                        const float f0 = s0 * exp2_fast((h0 - he) + (l0 - le)), f1 = s1 * exp2_fast((h1 - he) + (l1 - le));
+                        const float f0 = s0 * up * exp2_fast((h0 - he) + (l0 - le)), f1 = s1 * up * exp2_fast((h1 - he) + (l1 - le));
 #pragma unroll
                         for (int p = 0; p < 2; ++p) {
                             float(&x)[4] = acc[2 * n2 + p];
@@ -550,6 +565,21 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                     put_scores(own_acc[0], 2 * mt);
                     put_scores(own_acc[1], 2 * mt + 1);
                 } else {
+                    // Rows that are not finite, of keys or gates that are not: T would carry them to earlier tokens through zeros. They
+                    // count as 0 there, and their tokens' R as NaN, which the chain deals with.
+                    if (__any_sync(0xffffffffu, !(max_of(m0, m1, 0.f) < __int_as_float(0x7f800000)))) {
+                        const auto clean = [](float (&x)[4]) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (!(fabsf(x[e]) < __int_as_float(0x7f800000))) x[e] = 0.f;
+                        };
+#pragma unroll
+                        for (int n = 0; n < 6; ++n) clean(acc[n]);
+                        clean(own_acc[0]);
+                        clean(own_acc[1]);
+                        if (!(m0 < __int_as_float(0x7f800000))) fac[F_STATE * CH + i0] = __int_as_float(0x7fffffff);
+                        if (!(m1 < __int_as_float(0x7f800000))) fac[F_STATE * CH + i1] = __int_as_float(0x7fffffff);
+                    }
 #pragma unroll
                     for (int n = 0; n < 6; ++n) {
                         if (n >= 2 * mt) break;
@@ -612,10 +642,11 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                         const float4 a = *reinterpret_cast<const float4*>(D + row * DP + 8 * half), b = *reinterpret_cast<const float4*>(D + row * DP + 8 * half + 4);
                         const bool above = half && row < 8;         // zeros, whatever stood there
                         uint32_t hi[4], lo[4];
-                        split2(above ? 0.f : a.x, above ? 0.f : a.y, hi[0], lo[0]);
-                        split2(above ? 0.f : a.z, above ? 0.f : a.w, hi[1], lo[1]);
-                        split2(above ? 0.f : b.x, above ? 0.f : b.y, hi[2], lo[2]);
-                        split2(above ? 0.f : b.z, above ? 0.f : b.w, hi[3], lo[3]);
+                        const auto two = [&](float x, float y, int i) { split2(above ? 0.f : x * T_UP, above ? 0.f : y * T_UP, hi[i], lo[i]); };
+                        two(a.x, a.y, 0);
+                        two(a.z, a.w, 1);
+                        two(b.x, b.y, 2);
+                        two(b.z, b.w, 3);
                         const uint32_t at = tile_at<Z::TP>(16 * mt + row, 2 * mt + half);
                         *reinterpret_cast<uint4*>(st + Z::THI + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                         *reinterpret_cast<uint4*>(st + Z::TLO + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
@@ -653,7 +684,7 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 for (int p = 0; p < 2; ++p)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s.x[p][i] += s.y[p][i];
-                split_a(s.x[0], s.x[1], 1.f, 1.f, hi, lo);
+                split_a(s.x[0], s.x[1], 1.f / T_UP, 1.f / T_UP, hi, lo);        // up by T_UP once, not twice
             };
             const auto put = [&](const uint32_t (&hi)[4], const uint32_t (&lo)[4], int b, int a) {
                 const uint32_t at = tile_at<Z::TP>(16 * b + 8 * (lane >> 4) + (lane & 7), 2 * a + ((lane >> 3) & 1));
@@ -827,7 +858,7 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
         uint32_t rh[4][4], rl[4][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) split_a(R[2 * j], R[2 * j + 1], rs0, rs1, rh[j], rl[j]);
-        const float ir0 = pow2_inverse(rs0), ir1 = pow2_inverse(rs1);
+        const float ir0 = pow2_inverse(rs0) * (1.f / T_UP), ir1 = pow2_inverse(rs1) * (1.f / T_UP);
         float u0 = 0.f, u1 = 0.f;
 #pragma unroll
         for (int i = 3; i >= 0; --i) {

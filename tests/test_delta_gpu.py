@@ -307,6 +307,39 @@ def test_delta_nan_stays_in_its_head_and_column(rows):
     del first
 
 
+@pytest.mark.parametrize("rows,at", [(1, 0), (20, 5), (130, 0), (130, 5), (130, 22), (130, 77), (130, 127)])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_delta_nan_reaches_no_earlier_token(rows, at, dtype):
+    """One token's key, query, decay or factor is NaN or infinite, a head each: what comes before is as without it, what comes
+    after is NaN (of a query: that token alone)."""
+    rng = np.random.default_rng(at)
+    h, dk, dv = 6, 128, 64
+    q, k, v, a, b, _, _ = inputs(rng, rows, h, h, dk, dv, dtype, False)
+    q, k, v, a, b = (t.clone() for t in (q, k, v, a, b))
+    clean = [np64(t) for t in (q, k, v, a, b)]
+    k[at, 0, 3], k[at, 1, 100], q[at, 2, 64], a[at, 3], b[at, 4], k[at, 5, 7] = (float(x) for x in ("nan", "inf", "nan", "nan", "inf", "-inf"))
+    state = torch.randn(1, h, dk, dv, device=DEV)
+    before = np64(state)[0]
+    got = np64(vbq.vbq_delta_rule(vbq.Sequences(1, rows), state, q, k, v, a, b))
+    after = np64(state)[0]
+    g, beta = o.gates(clean[3], clean[4], None, None)
+    want, end, bound, sb = o.delta_rule(clean[0], clean[1], clean[2], g, beta, before, dk ** -0.5, True, dtype == F32)
+    off = np.abs(got - want) - (bound + 2.0 ** -8 * (np.abs(want) + bound))
+    assert (off[:at] <= 0).all(), f"heads {np.unique(np.argwhere(~(off[:at] <= 0))[:, 1])}"
+    assert (off[at + 1:, 2] <= 0).all() and (np.abs(after[2] - end[2]) <= sb[2]).all() and np.isnan(got[at, 2]).all()
+    lost = [0, 1, 3, 4, 5]
+    assert not np.isfinite(got[at:, lost]).any() and not np.isfinite(after[lost]).any()
+
+
+# Sequences and heads so many that 64 columns of a state go to a block instead of 32 (where a head's 32 would take a second
+# round of blocks and its 64 do not), idle, fresh and empty ones among them.
+@pytest.mark.parametrize("lens,hk,h,dk,dv", [([130, 129, 1, 0, 140, 130, 128], 8, 16, 128, 128), ([65, 64, 90, 63, 80], 16, 16, 64, 128),
+                                             ([200, 170], 16, 32, 128, 128), ([100] * 11, 8, 8, 64, 64)], ids=str)
+def test_delta_of_wide_blocks(lens, hk, h, dk, dv):
+    run_delta(lens, hk, h, dk, dv, idle=(1,), fresh=(0, len(lens) - 1))
+    run_delta(lens, hk, h, dk, dv, raw=False, gate_dtype=BF16, fresh=(0,))
+
+
 def test_delta_cut_anywhere_is_the_same_to_rounding():
     rng = np.random.default_rng(8)
     n, hk, h, d = 333, 1, 2, 128
