@@ -588,9 +588,12 @@ vbq_status_t vbq_causal_conv(const vbq_sequences* seq, const void* x, int64_t x_
  *   normalize  1: q and k are scaled to unit length first, x rsqrt(sum x^2 +
  *              1e-6) per head; 0: they are taken as they are. The rule contracts
  *              while beta |k|^2 stays within 0..2, and is meant for that.
+ *              (Sequences of more than 24 rows also need |beta_i| |k_i| |k_j| below
+ *              64 between tokens; beyond that their outputs may be NaN.)
  *   out        device, tokens x heads x head_v BF16, dense.
  * The state and all sums are fp32. Results do not vary between calls; a
  * sequence's are the same to rounding however its tokens are cut into calls.
+ * What is NaN or infinite in a token reaches no token before it.
  */
 vbq_status_t vbq_delta_rule(const vbq_sequences* seq, float* state, int64_t n_slots, const void* q, int64_t q_stride,
                             const void* k, int64_t k_stride, const void* v, int64_t v_stride, int type, int k_heads,

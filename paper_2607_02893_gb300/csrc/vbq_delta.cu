@@ -174,13 +174,22 @@ struct Staged {
 };
 
 template <bool F32, int DK>
-__global__ void __launch_bounds__(32 * RW_WARPS) delta_rows_kernel(Delta d, int most) {
+__global__ void __launch_bounds__(32 * RW_WARPS) delta_rows_kernel(Delta d, int most, bool beside) {
     using In = Staged<F32, DK>;
     __shared__ __align__(16) In in[2];
     __shared__ float4 token[BATCH];              // keep; beta; the unit key's factor; the scaled unit query's
     __shared__ float product[BATCH];             // q.k of these
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // Beside the kernel before it, which lets this one start when what came before both is done (the fence: no line that the
+    // SM still has is read): block 0 waits for that one at its end instead, so that this grid does not count as done before it.
+    if (beside) {
+        asm volatile("fence.acq_rel.gpu;" ::: "memory");
+    } else {
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+    }
+    const auto leave = [&] {
+        if (beside && blockIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+    };
     constexpr int PER = DK / 8;                  // rows of the state in a lane
     const int slices = d.head_v / DR_COLS;
     const int unit = (int)(blockIdx.x / slices), slice = (int)(blockIdx.x - unit * slices);
@@ -188,12 +197,12 @@ __global__ void __launch_bounds__(32 * RW_WARPS) delta_rows_kernel(Delta d, int 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, part = lane >> 2, quad = lane & 3;
     const int col = slice * DR_COLS + warp * 8 + quad * 2;
     const SeqRange r = seq_range(d.seq, b, d.n_slots, h == 0 && slice == 0 && tid == 0);
-    if (r.n == 0 || r.n > most) return;
+    if (r.n == 0 || r.n > most) return leave();
     const int64_t out_row = (int64_t)d.heads * d.head_v;
     uint16_t* out = d.out + r.lo * out_row + h * d.head_v + col;
     if (r.slot < 0) {
         for (int t = part; t < r.n; t += 8) *reinterpret_cast<uint32_t*>(out + t * out_row) = 0;
-        return;
+        return leave();
     }
     const int hk = h / (d.heads / d.k_heads);
     constexpr int SIZE = F32 ? 4 : 2, SEGS = DK * SIZE / 16, VSEGS = DR_COLS * SIZE / 16;
@@ -295,6 +304,7 @@ __global__ void __launch_bounds__(32 * RW_WARPS) delta_rows_kernel(Delta d, int 
     }
 #pragma unroll
     for (int i = 0; i < PER; ++i) *reinterpret_cast<float2*>(state + i * d.head_v) = S[i];
+    leave();
 }
 
 dim3 grid_of(const Delta& d) { return dim3((unsigned)((int64_t)d.seq.batch * d.heads * (d.head_v / DR_COLS))); }
@@ -304,8 +314,8 @@ cudaError_t launch_tokens(const Delta& d, cudaStream_t s) {
     if (d.f32) return d.head_k == 64 ? go(delta_token_kernel<true, 64>) : go(delta_token_kernel<true, 128>);
     return d.head_k == 64 ? go(delta_token_kernel<false, 64>) : go(delta_token_kernel<false, 128>);
 }
-cudaError_t launch_rows(const Delta& d, int most, cudaStream_t s) {
-    const auto go = [&](auto kernel) { return launch_dependent(kernel, grid_of(d), 32 * RW_WARPS, 0, s, d, most); };
+cudaError_t launch_rows(const Delta& d, int most, bool beside, cudaStream_t s) {
+    const auto go = [&](auto kernel) { return launch_dependent(kernel, grid_of(d), 32 * RW_WARPS, 0, s, d, most, beside); };
     if (d.f32) return d.head_k == 64 ? go(delta_rows_kernel<true, 64>) : go(delta_rows_kernel<true, 128>);
     return d.head_k == 64 ? go(delta_rows_kernel<false, 64>) : go(delta_rows_kernel<false, 128>);
 }
@@ -313,16 +323,17 @@ cudaError_t launch_rows(const Delta& d, int most, cudaStream_t s) {
 }  // namespace
 
 // Sequences of up to DELTA_ROWS rows go token by token, longer ones by chunks. Where the call's may be of both kinds, both
-// kernels run, each over its own.
+// kernels run, each over its own and side by side (24 single tokens and a prompt of 2000, 32 heads of 128: 185 us one after
+// the other, 165 so).
 cudaError_t launch_delta_rule(const Delta& d, cudaStream_t s) {
     int sms = 0;
     const int err = device_sms(&sms);
     if (err != 0) return (cudaError_t)err;
     if (d.seq.rows <= 1) return launch_tokens(d, s);
-    if (d.seq.rows <= DELTA_ROWS) return launch_rows(d, INT32_MAX, s);
+    if (d.seq.rows <= DELTA_ROWS) return launch_rows(d, INT32_MAX, false, s);
     if (d.seq.starts && d.seq.batch > 1) {
-        const cudaError_t e = launch_rows(d, DELTA_ROWS, s);
-        return e != cudaSuccess ? e : launch_delta_chunks(d, DELTA_ROWS, sms, s);
+        const cudaError_t e = launch_delta_chunks(d, DELTA_ROWS, sms, s);
+        return e != cudaSuccess ? e : launch_rows(d, DELTA_ROWS, true, s);
     }
     return launch_delta_chunks(d, 0, sms, s);
 }

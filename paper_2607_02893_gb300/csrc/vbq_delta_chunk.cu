@@ -23,13 +23,15 @@
 // keys and makes T: blocks of 16 on the diagonal by substitution in fp32, the
 // ones below them by products. Named barriers hand the stages over.
 //
-// What bounds it is neither memory nor the tensor cores but the instructions: a
-// chunk's code, written out, is twice the 32 KB that an SM keeps of it, and both
-// roles run through all of it per chunk, about one instruction in two clocks for
-// each new one. Hence rolled loops wherever registers need no index, two floats
-// at a time (fma2), and nothing twice. One sequence of 32768 tokens, 32 heads of
-// 128 by 128, blocks of 32 columns: 2.42 ms, 4.7 us a chunk, 123 us of it what
-// memory needs; the bytes of a block's two stages stay on the chip throughout.
+// What bounds it is neither memory nor the tensor cores (a third busy) but the
+// chain of instructions a chunk takes: 14 thousand of ten warps, 0.39 an issue slot,
+// each waiting for the one before it or for the other group. Two blocks do not
+// fit in the registers of an SM. The code of both roles is twice the 32 KB that
+// an SM keeps of it, so what a chunk does not need twice is not written out
+// twice: loops are rolled wherever registers need no index. One sequence of 32768
+// tokens, 32 heads of 128 by 128, blocks of 32 columns: 2.45 ms, 4.8 us a chunk
+// (the chain alone, with three of four chunks not prepared: 3.4); memory needs
+// 0.12 ms of it.
 //
 // fp32 through the tensor cores. Keys are taken to FP16 by a power of two per
 // token, which BF16 values survive unchanged (8 bits of 11, 39 binades down from
@@ -986,6 +988,7 @@ __global__ void __launch_bounds__(Shape<F32, DK, CW>::THREADS, 1) delta_chunk_ke
     using Z = Shape<F32, DK, CW>;
     extern __shared__ __align__(128) char smem[];
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (above > 0) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");     // the kernel of the shorter sequences
     const int slices = d.head_v / Z::VC;
     const int unit = (int)(blockIdx.x / slices), slice = (int)(blockIdx.x - unit * slices);
     const int b = unit / d.heads, h = unit - b * d.heads, col0 = slice * Z::VC;
