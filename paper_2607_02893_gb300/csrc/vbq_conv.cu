@@ -62,12 +62,13 @@ struct Four {
             raw.x = a.x; raw.y = a.y;
         }
     }
-    __device__ __forceinline__ void values(float (&v)[4]) const {
+    __device__ __forceinline__ void values(float2 (&v)[2]) const {
         if constexpr (F32) {
-            v[0] = __uint_as_float(raw.x); v[1] = __uint_as_float(raw.y); v[2] = __uint_as_float(raw.z); v[3] = __uint_as_float(raw.w);
+            v[0] = make_float2(__uint_as_float(raw.x), __uint_as_float(raw.y));
+            v[1] = make_float2(__uint_as_float(raw.z), __uint_as_float(raw.w));
         } else {
-            v[0] = __uint_as_float(raw.x << 16); v[1] = __uint_as_float(raw.x & 0xffff0000u);
-            v[2] = __uint_as_float(raw.y << 16); v[3] = __uint_as_float(raw.y & 0xffff0000u);
+            v[0] = make_float2(__uint_as_float(raw.x << 16), __uint_as_float(raw.x & 0xffff0000u));
+            v[1] = make_float2(__uint_as_float(raw.y << 16), __uint_as_float(raw.y & 0xffff0000u));
         }
     }
 };
@@ -95,7 +96,7 @@ __global__ void __launch_bounds__(CONV_THREADS) causal_conv_kernel(Conv c) {
     Four<F32> next[CONV_AHEAD];
 #pragma unroll
     for (int i = 0; i < CONV_AHEAD; ++i) next[i].load(c.x, at + min(i, rows - 1) * c.x_stride);
-    float w[TAPS][4], bias[4] = {}, line[PAST + CONV_AHEAD][4];      // line: the inputs before the rows worked on, and theirs
+    float2 w[TAPS][2], bias[2] = {}, line[PAST + CONV_AHEAD][2];     // line: the inputs before the rows worked on, and theirs
     {
         float wide[TAPS * 4];
         const float4* p = reinterpret_cast<const float4*>(c.weight + (int64_t)ch * TAPS);
@@ -107,11 +108,12 @@ __global__ void __launch_bounds__(CONV_THREADS) causal_conv_kernel(Conv c) {
 #pragma unroll
         for (int j = 0; j < TAPS; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[j][e] = wide[e * TAPS + j];
+            for (int e = 0; e < 2; ++e) w[j][e] = make_float2(wide[2 * e * TAPS + j], wide[(2 * e + 1) * TAPS + j]);
     }
     if (c.bias) {
         const float4 v = *reinterpret_cast<const float4*>(c.bias + ch);
-        bias[0] = v.x; bias[1] = v.y; bias[2] = v.z; bias[3] = v.w;
+        bias[0] = make_float2(v.x, v.y);
+        bias[1] = make_float2(v.z, v.w);
     }
     if (tile > 0) {
 #pragma unroll
@@ -131,7 +133,7 @@ __global__ void __launch_bounds__(CONV_THREADS) causal_conv_kernel(Conv c) {
         // the sequence's last PAST inputs: of x, or for a shorter one of what was carried
 #pragma unroll
         for (int j = 0; j < PAST; ++j) {
-            float last[4];
+            float2 last[2];
             if (r.n + j >= PAST) {
                 Four<F32> x;
                 x.load(c.x, at + (int64_t)(r.n + j - PAST) * c.x_stride);
@@ -141,9 +143,9 @@ __global__ void __launch_bounds__(CONV_THREADS) causal_conv_kernel(Conv c) {
                 for (int m = 0; m < PAST; ++m)
                     if (m == r.n + j)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) last[e] = line[m][e];
+                        for (int e = 0; e < 2; ++e) last[e] = line[m][e];
             }
-            *reinterpret_cast<float4*>(carried + (int64_t)j * c.channels) = make_float4(last[0], last[1], last[2], last[3]);
+            *reinterpret_cast<float4*>(carried + (int64_t)j * c.channels) = make_float4(last[0].x, last[0].y, last[1].x, last[1].y);
         }
     }
 #pragma unroll 1
@@ -156,20 +158,20 @@ __global__ void __launch_bounds__(CONV_THREADS) causal_conv_kernel(Conv c) {
         uint16_t* o = out + (int64_t)i0 * c.channels;
 #pragma unroll
         for (int i = 0; i < CONV_AHEAD; ++i) {
-            float y[4];
+            uint32_t y[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float s = bias[e];
+            for (int e = 0; e < 2; ++e) {
+                float2 s = bias[e];
 #pragma unroll
-                for (int j = 0; j < TAPS; ++j) s = fmaf(w[j][e], line[i + j][e], s);
-                y[e] = c.silu ? silu(s) : s;
+                for (int j = 0; j < TAPS; ++j) s = fma2(w[j][e], line[i + j][e], s);
+                y[e] = c.silu ? pack_bf16(silu(s.x), silu(s.y)) : pack_bf16(s.x, s.y);
             }
-            if (i0 + i < rows) *reinterpret_cast<uint2*>(o + (int64_t)i * c.channels) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+            if (i0 + i < rows) *reinterpret_cast<uint2*>(o + (int64_t)i * c.channels) = make_uint2(y[0], y[1]);
         }
 #pragma unroll
         for (int j = 0; j < PAST; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) line[j][e] = line[CONV_AHEAD + j][e];
+            for (int e = 0; e < 2; ++e) line[j][e] = line[CONV_AHEAD + j][e];
     }
 }
 

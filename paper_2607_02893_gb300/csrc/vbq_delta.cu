@@ -149,18 +149,6 @@ __global__ void __launch_bounds__(32 * DR_WARPS, 8) delta_token_kernel(Delta d) 
     for (int i = 0; i < PER; ++i) *reinterpret_cast<float4*>(state + (int64_t)i * d.head_v) = S[i];
 }
 
-// Pairs of neighbouring columns: two fp32 operations an instruction.
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)));
-    return *reinterpret_cast<float2*>(&r);
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)), "l"(*reinterpret_cast<uint64_t*>(&c)));
-    return *reinterpret_cast<float2*>(&r);
-}
-
 // A few tokens of a sequence: BATCH at a time through shared memory, copies of the next ones under way. What does not depend
 // on the state (unit lengths, q.k, gates) is worked out for all of them first, so a token's chain is its two products with
 // the state, a reduction over the 8 groups of lanes and the update.

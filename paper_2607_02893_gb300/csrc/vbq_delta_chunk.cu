@@ -111,19 +111,6 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-// two floats at a time
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 y;
-    asm("{.reg .b64 a, b, y; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mul.rn.f32x2 y, a, b; mov.b64 {%0, %1}, y;}"
-        : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return y;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 y;
-    asm("{.reg .b64 a, b, c, y; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mov.b64 c, {%6, %7}; fma.rn.f32x2 y, a, b, c; mov.b64 {%0, %1}, y;}"
-        : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return y;
-}
 __device__ __forceinline__ float2 twice(float x) { return make_float2(x, x); }
 // max(m, |x|, |y|); a NaN stays
 __device__ __forceinline__ float max_of(float m, float x, float y) {
