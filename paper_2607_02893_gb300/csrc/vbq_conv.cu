@@ -2,10 +2,13 @@
 // y_t = bias + sum_j w_j x_{t - taps + 1 + j} per channel, its silu, BF16 out;
 // the last taps - 1 inputs of a sequence are carried between calls.
 //
-// Two to four multiplications a value: bytes bound it. A thread takes 8
-// channels (a 16-byte load of BF16) of a tile of rows and carries the window in
-// registers, so a row is read once, but for the taps - 1 before a tile, which
-// the tile before has just brought into L2. A sequence's first tile reads its
+// Bytes bound it, instructions next (4 multiply-adds and a silu a value). A
+// thread takes 4 channels of a tile of rows, two an instruction, loads 8 rows
+// ahead and carries the window in registers, so a row is read once, but for the
+// taps - 1 before a tile, which the tile before has just brought into L2. 14145
+// rows of 8192 channels, BF16, 4 taps: 81 us, 5.75 TB/s; 4 rows ahead 84, tiles
+// of 64 rows 80, but half the blocks for a short prompt, blocks of 256 threads
+// 90, registers for 6 blocks an SM 113. A sequence's first tile reads its
 // carried inputs and also writes the new ones: nobody else touches its slot,
 // so no order between blocks is needed, and a tile is never shorter than the
 // window (CONV_ROWS >= taps - 1), so no other tile reaches back to them.

