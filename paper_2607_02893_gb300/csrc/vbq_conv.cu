@@ -78,7 +78,6 @@ struct Four {
 
 template <bool F32, int TAPS>
 __global__ void __launch_bounds__(CONV_THREADS) causal_conv_kernel(Conv c) {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr int PAST = TAPS - 1;
     const int ch = (int)(blockIdx.y * CONV_THREADS + threadIdx.x) * 4;

@@ -8,6 +8,11 @@
 // products are taken of the state before the token, o = e^g S^T q + (q.k) u, so
 // their sums go through the shuffles together.
 //
+// Neither kernel lets the next one start early, nor do the convolution and the
+// norm: waiting blocks take places on the SMs where the first ones end, so the
+// next call's are spread unevenly (the three of a layer, 32 heads, in a graph:
+// 6.3 against 7.3 us a token, 18.6 against 23.3 for 4 x 16 tokens).
+//
 // A single token is bound by the state's bytes, 128 KB a head of 128 x 128: 64
 // sequences of 32 heads, 272 MB, 48 us, 5.65 TB/s.
 #include <type_traits>
@@ -27,7 +32,6 @@ constexpr int DELTA_ROWS = 16, DELTA_ROWS_FULL = 28;
 
 template <bool F32, int DK>
 __global__ void __launch_bounds__(32 * DR_WARPS, 8) delta_token_kernel(Delta d) {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr int PER = DK / 8;                  // rows of the state in a lane
     const int slices = d.head_v / DR_COLS;
@@ -171,12 +175,8 @@ __global__ void __launch_bounds__(32 * RW_WARPS) delta_rows_kernel(Delta d, int 
     __shared__ float product[BATCH];             // q.k of these
     // Beside the kernel before it, which lets this one start when what came before both is done (the fence: no line that the
     // SM still has is read): block 0 waits for that one at its end instead, so that this grid does not count as done before it.
-    if (beside) {
-        asm volatile("fence.acq_rel.gpu;" ::: "memory");
-    } else {
-        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-        asm volatile("griddepcontrol.wait;" ::: "memory");
-    }
+    if (beside) asm volatile("fence.acq_rel.gpu;" ::: "memory");
+    else asm volatile("griddepcontrol.wait;" ::: "memory");
     const auto leave = [&] {
         if (beside && blockIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
     };

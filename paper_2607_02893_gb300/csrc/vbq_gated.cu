@@ -16,7 +16,6 @@ constexpr int GN_THREADS = 256;
 // LANES: threads of a head, a power of two at least width / 8.
 template <bool XF32, bool ZF32, int LANES>
 __global__ void __launch_bounds__(GN_THREADS) gated_norm_kernel(GatedNorm n) {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int64_t total = n.rows * n.heads, step = (int64_t)gridDim.x * (GN_THREADS / LANES);
     const int l = threadIdx.x & (LANES - 1);
