@@ -588,7 +588,7 @@ vbq_status_t vbq_causal_conv(const vbq_sequences* seq, const void* x, int64_t x_
  *   normalize  1: q and k are scaled to unit length first, x rsqrt(sum x^2 +
  *              1e-6) per head; 0: they are taken as they are. The rule contracts
  *              while beta |k|^2 stays within 0..2, and is meant for that.
- *              (Sequences of more than 16 rows also need |beta_i| |k_i| |k_j| below
+ *              (Sequences of more than 22 rows also need |beta_i| |k_i| |k_j| below
  *              64 between tokens; beyond that their outputs may be NaN.)
  *   out        device, tokens x heads x head_v BF16, dense.
  * The state and all sums are fp32. Results do not vary between calls; a

@@ -14,7 +14,7 @@
 // 6.3 against 7.3 us a token, 18.6 against 23.3 for 4 x 16 tokens).
 //
 // A single token is bound by the state's bytes, 128 KB a head of 128 x 128: 64
-// sequences of 32 heads, 272 MB, 48 us, 5.65 TB/s.
+// sequences of 32 heads, 270 MB, 47.4 us, 5.7 TB/s.
 #include <type_traits>
 
 #include "vbq_delta.cuh"
@@ -25,10 +25,10 @@ namespace {
 
 constexpr int DR_WARPS = 2;                      // of a block; 16 columns each
 constexpr int DR_COLS = 16 * DR_WARPS;
-// A sequence of more rows goes by chunks. Token by token 1 x 32 heads of 128 take 3.0 us and 0.36 a token, 4 x 16 heads 4.0
-// and 0.43, 16 x 32 heads 9.7 and 1.9; one chunk takes them 9.5, 11.5 and 67 us: the first two, whose blocks of 64 columns
-// the GPU holds at once, change over at 17 rows, the third at 31.
-constexpr int DELTA_ROWS = 16, DELTA_ROWS_FULL = 28;
+// A sequence of more rows goes by chunks. Token by token 1 x 32 heads of 128 take 2.8 us and 0.29 a token, 4 x 16 heads 3.1
+// and 0.36, 16 x 32 heads 9.6 and 1.9; one chunk takes them 9.4, 11.4 and 67 us: the first two, whose blocks of 64 columns
+// the GPU holds at once, change over at 23 rows, the third at 30.
+constexpr int DELTA_ROWS = 22, DELTA_ROWS_FULL = 28;
 
 template <bool F32, int DK>
 __global__ void __launch_bounds__(32 * DR_WARPS, 8) delta_token_kernel(Delta d) {
