@@ -29,7 +29,7 @@
 // fit in the registers of an SM. The code of both roles is twice the 32 KB that
 // an SM keeps of it, so what a chunk does not need twice is not written out
 // twice: loops are rolled wherever registers need no index. One sequence of 32768
-// tokens, 32 heads of 128 by 128, blocks of 32 columns: 2.45 ms, 4.8 us a chunk
+// tokens, 32 heads of 128 by 128, blocks of 32 columns: 2.30 ms, 4.5 us a chunk
 // (the chain alone, with three of four chunks not prepared: 3.4); memory needs
 // 0.12 ms of it.
 //
@@ -308,7 +308,7 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
         const uint32_t sb = base + stage * Z::STAGE;
         float* fac = reinterpret_cast<float*>(st + Z::FAC);
         float *ck = reinterpret_cast<float*>(own + Z::TOKENS) + stage * Z::FACTORS, *cq = ck + CH, *gate = cq + CH;
-        const bool gates = !of_q && warp == 3 && next < chunks;
+        const bool gates = !of_q && warp == (CW == 2 ? 0 : 3) && next < chunks;
         if (gates) load_gates(next);
         if (c >= 0) {
             if (of_q) {
@@ -389,7 +389,9 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
             bar_sync(Z::PREPARING, PREP);
             // 16 rows of keys or of queries with the keys up to theirs
             {
-                const int mt = of_q ? 3 - warp : warp;
+                // The four parts of an SM take the warps in turn, so two chain warps leave two parts to themselves: those get the
+                // rows with most columns and T (2.44 -> 2.30 ms for 32768 tokens). Four: rows balanced over keys and queries.
+                const int mt = of_q && CW != 2 ? 3 - warp : warp;
                 float acc[8][4];
 #pragma unroll
                 for (int n = 0; n < 8; ++n)
@@ -681,8 +683,9 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 stmatrix4_trans(sb + Z::TLO + at, lo);
             };
             uint32_t hi[4], lo[4];
-            if (warp < 2) {
-                const int a = 2 * warp;
+            const int side = CW == 2 ? warp - 2 : warp;             // (see `mt`)
+            if (side >= 0 && side < 2) {
+                const int a = 2 * side;
                 Sum s = {}, t = {};
                 get(hi, lo, a, a);
                 times_n(s, hi, lo, a + 1, a);
@@ -692,11 +695,11 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 put(hi, lo, a + 1, a);
             }
             bar_sync(Z::KEYS, Z::HALF);
-            if (warp < 2) {
+            if (side >= 0 && side < 2) {
                 Sum s2 = {}, s3 = {}, t2 = {}, t3 = {};
 #pragma unroll 1
-                for (int k = warp; k < 2; ++k) {
-                    get(hi, lo, k, warp);
+                for (int k = side; k < 2; ++k) {
+                    get(hi, lo, k, side);
                     times_n(s2, hi, lo, 2, k);
                     times_n(s3, hi, lo, 3, k);
                 }
@@ -708,8 +711,8 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 times_t(t3, hi3, lo3, 3, 3);
                 parts(t2, hi, lo);
                 parts(t3, hi3, lo3);
-                put(hi, lo, 2, warp);
-                put(hi3, lo3, 3, warp);
+                put(hi, lo, 2, side);
+                put(hi3, lo3, 3, side);
             }
         }
         if (gates) sum_gates(next, reinterpret_cast<float*>(own + Z::TOKENS) + (next & (STAGES - 1)) * Z::FACTORS + 2 * CH);
@@ -1016,14 +1019,14 @@ cudaError_t launch_shape(const Delta& d, int above, cudaStream_t s) {
 template <bool F32, int DK>
 cudaError_t launch_width(const Delta& d, int above, int sms, cudaStream_t s) {
     // Columns of a block. All blocks of a head prepare the same chunks, so fewer and wider ones do less in all, and more and
-    // narrower ones fill the GPU. A chunk takes a block of 32 or 64 columns about 4.7 and 4.9 us; the rounds of blocks are
+    // narrower ones fill the GPU. A chunk takes a block of 32 or 64 columns about 4.5 and 4.9 us; the rounds of blocks are
     // counted by the sequences like the longest that the tokens make up. Five sequences of 1774 to 3001 tokens, 32 heads of
-    // 128: 862 and 520 us; one of 32768: 2420 and 2503. (128 columns, which leave the preparing warps half the registers,
+    // 128: 820 and 525 us; one of 32768: 2303 and 2510. (128 columns, which leave the preparing warps half the registers,
     // took 11.2 us a chunk.) fp32 values leave no room for the wider one.
     if constexpr (!F32) {
         const int64_t alike = (d.seq.tokens + d.seq.rows / 2) / d.seq.rows, sequences = alike < 1 ? 1 : alike > d.seq.batch ? d.seq.batch : alike;
         const auto cost = [&](int columns, int64_t each) { return (sequences * d.heads * d.head_v / columns + sms - 1) / sms * each; };
-        if (cost(64, 49) < cost(32, 47)) return launch_shape<F32, DK, 4>(d, above, s);
+        if (cost(64, 49) < cost(32, 45)) return launch_shape<F32, DK, 4>(d, above, s);
     }
     return launch_shape<F32, DK, 2>(d, above, s);
 }
