@@ -715,11 +715,11 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 put(hi3, lo3, 3, side);
             }
         }
-        if (gates) sum_gates(next, reinterpret_cast<float*>(own + Z::TOKENS) + (next & (STAGES - 1)) * Z::FACTORS + 2 * CH);
         if (c >= 0) {
             cp_wait_but_one();                                      // the values, not what comes for the next chunk
             bar_arrive(Z::FULL + stage, Z::FULL_COUNT);
         }
+        if (gates) sum_gates(next, reinterpret_cast<float*>(own + Z::TOKENS) + (next & (STAGES - 1)) * Z::FACTORS + 2 * CH);
     }
 }
 
