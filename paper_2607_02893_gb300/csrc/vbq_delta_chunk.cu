@@ -33,11 +33,11 @@
 // (the chain alone, with three of four chunks not prepared: 3.4); memory needs
 // 0.12 ms of it.
 //
-// fp32 through the tensor cores. Keys are taken to FP16 by a power of two per
-// token, which BF16 values survive unchanged (8 bits of 11, 39 binades down from
-// the largest); S, R, U and T enter as two FP16 parts, x = hi + lo, with a power
-// of two per column of S, so a product is good to 2^-22 (fp32 keys are two parts
-// as well). T and L are up by 2^10, so that what a strong decay leaves of an
+// fp32 through the tensor cores. BF16 keys are taken to FP16 by a power of two for
+// 8 or 16 tokens, which they survive unchanged (8 bits of 11) down to 2^-31 of the
+// largest; S, R, U and T enter as two FP16 parts, x = hi + lo, with a power of two
+// per column of S, so a product is good to 2^-22 (fp32 keys, with a power of two a
+// token, are two parts as well). T and L are up by 2^10, so that what a strong decay leaves of an
 // earlier token's R keeps its digits (parts end at 2^-35, not 2^-25, which had an
 // element of 2e-5 off by 2e-8); they overflow from 64 on, and where the rule
 // contracts |T_ij| is at most |beta_i| |k_i| |k_j|, 2 for keys of unit length.
@@ -145,8 +145,7 @@ __device__ __forceinline__ float quad_max(float m) {              // over the fo
 // Byte offset of 16-byte segment `seg` of row `row` in a tile of PITCH-byte rows; eight rows' segments fall in distinct banks.
 template <int PITCH>
 __device__ __forceinline__ uint32_t tile_at(int row, int seg) {
-    const int turn = PITCH == 64 ? (row >> 1) & 3 : row & 7;
-    return (uint32_t)(row * PITCH + ((seg ^ turn) << 4));
+    return (uint32_t)(row * PITCH + ((seg ^ (row & 7)) << 4));
 }
 
 // what the gates of a chunk come to, per token: log2 of the decay from the chunk's start (and what a float of it leaves out),
