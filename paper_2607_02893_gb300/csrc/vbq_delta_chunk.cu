@@ -16,21 +16,23 @@
 // head_k) over the whole sequence. Everything is computed transposed: what comes
 // out of one product is, in the same registers, the A operand of the next, so
 // the chain has no exchange between warps and nothing but key, query, T and
-// score fragments is read from shared memory. Eight other warps prepare the next
-// chunk meanwhile, in two groups that work side by side. The one for queries
-// takes keys and queries to FP16, multiplies queries with keys, makes the scores
-// and goes on to the next chunk's rows; the one for keys multiplies keys with
-// keys and makes T: blocks of 16 on the diagonal by substitution in fp32, the
-// ones below them by products. Named barriers hand the stages over.
+// score fragments is read from shared memory. Where there are two chain warps, two
+// more make the outputs, from the parts of S and U that they are handed (2.30 ->
+// 2.16 ms for 32768 tokens). Eight other warps prepare the next chunk meanwhile, in
+// two groups that work side by side. The one for queries takes keys and queries to
+// FP16, multiplies queries with keys, makes the scores and goes on to the next
+// chunk's rows; the one for keys multiplies keys with keys and makes T: blocks of
+// 16 on the diagonal by substitution in fp32, the ones below them by products.
+// Named barriers hand the stages over.
 //
 // What bounds it is neither memory nor the tensor cores (a third busy) but the
-// chain of instructions a chunk takes: 14 thousand of ten warps, 0.39 an issue slot,
-// each waiting for the one before it or for the other group. Two blocks do not
+// chain of instructions a chunk takes: 14 thousand of twelve warps, 0.4 an issue slot,
+// each waiting for the one before it or for another group. Two blocks do not
 // fit in the registers of an SM. The code of both roles is twice the 32 KB that
 // an SM keeps of it, so what a chunk does not need twice is not written out
 // twice: loops are rolled wherever registers need no index. One sequence of 32768
-// tokens, 32 heads of 128 by 128, blocks of 32 columns: 2.30 ms, 4.5 us a chunk
-// (the chain alone, with three of four chunks not prepared: 3.4); memory needs
+// tokens, 32 heads of 128 by 128, blocks of 32 columns: 2.16 ms, 4.2 us a chunk
+// (with three of four chunks not prepared: 3.4); memory needs
 // 0.12 ms of it.
 //
 // fp32 through the tensor cores. BF16 keys are taken to FP16 by a power of two for
@@ -170,10 +172,16 @@ struct Shape {
     // chunk's keys and queries as they come (fp32: the second parts of this one's queries)
     static constexpr int LHI = 0, LLO = LHI + CH * TP, DIAG = LLO + CH * TP, TOKENS = DIAG + 4 * 16 * DP * 4,
                          FACTORS = 2 * CH + GATES, RAW = TOKENS + 2 * FACTORS * 4, SCRATCH = RAW + (F32 ? CH * KP : 2 * CH * 2 * DK);
-    static constexpr int OWN = STAGES * STAGE, BYTES = OWN + SCRATCH;
+    static constexpr int OWN = STAGES * STAGE;
+    // Two chain warps leave two of their warpgroup to the outputs. What they are handed, each lane by the one at its place: the
+    // parts of S and U that enter the outputs, their scales, where a column is lost.
+    static constexpr bool APART = CW == 2;
+    static constexpr int HANDED = (OWN + SCRATCH + 127) / 128 * 128, HAND_U = DK / 16 * 512, HAND_SCALES = HAND_U + 4 * 512, HAND = HAND_SCALES + 3 * 256,
+                         BYTES = HANDED + (APART ? CW * HAND : 0);
     static_assert(RAW % 16 == 0);
     // named barriers
-    static constexpr int FULL = 1, EMPTY = FULL + STAGES, PREPARING = EMPTY + STAGES, KEYS = PREPARING + 1, FULL_COUNT = 32 * CW + PREP, EMPTY_COUNT = 32 * CW + HALF;
+    static constexpr int FULL = 1, EMPTY = FULL + STAGES, PREPARING = EMPTY + STAGES, KEYS = PREPARING + 1, S_READY = KEYS + 1, U_READY = S_READY + CW, TAKEN = U_READY + CW;
+    static constexpr int CONSUMERS = 32 * CW * (APART ? 2 : 1), FULL_COUNT = CONSUMERS + PREP, EMPTY_COUNT = CONSUMERS + HALF;
     __device__ static __forceinline__ uint32_t key_at(int row, int seg) {
         return F32 ? tile_at<2 * DK>(row, seg) : (uint32_t)(row * KP + seg * 16);
     }
@@ -307,7 +315,7 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
         const uint32_t sb = base + stage * Z::STAGE;
         float* fac = reinterpret_cast<float*>(st + Z::FAC);
         float *ck = reinterpret_cast<float*>(own + Z::TOKENS) + stage * Z::FACTORS, *cq = ck + CH, *gate = cq + CH;
-        const bool gates = !of_q && warp == (CW == 2 ? 0 : 3) && next < chunks;
+        const bool gates = !of_q && warp == 3 && next < chunks;
         if (gates) load_gates(next);
         if (c >= 0) {
             if (of_q) {
@@ -388,8 +396,8 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
             bar_sync(Z::PREPARING, PREP);
             // 16 rows of keys or of queries with the keys up to theirs
             {
-                // The four parts of an SM take the warps in turn, so two chain warps leave two parts to themselves: those get the
-                // rows with most columns and T (2.44 -> 2.30 ms for 32768 tokens). Four: rows balanced over keys and queries.
+                // The four parts of an SM take the warps in turn, so two chain warps leave two parts to the others: those get the
+                // rows with most columns (balanced over keys and queries: 2.18 against 2.16 ms for 32768 tokens). Four: balanced.
                 const int mt = of_q && CW != 2 ? 3 - warp : warp;
                 float acc[8][4];
 #pragma unroll
@@ -682,9 +690,8 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 stmatrix4_trans(sb + Z::TLO + at, lo);
             };
             uint32_t hi[4], lo[4];
-            const int side = CW == 2 ? warp - 2 : warp;             // (see `mt`)
-            if (side >= 0 && side < 2) {
-                const int a = 2 * side;
+            if (warp < 2) {
+                const int a = 2 * warp;
                 Sum s = {}, t = {};
                 get(hi, lo, a, a);
                 times_n(s, hi, lo, a + 1, a);
@@ -694,11 +701,11 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 put(hi, lo, a + 1, a);
             }
             bar_sync(Z::KEYS, Z::HALF);
-            if (side >= 0 && side < 2) {
+            if (warp < 2) {
                 Sum s2 = {}, s3 = {}, t2 = {}, t3 = {};
 #pragma unroll 1
-                for (int k = side; k < 2; ++k) {
-                    get(hi, lo, k, side);
+                for (int k = warp; k < 2; ++k) {
+                    get(hi, lo, k, warp);
                     times_n(s2, hi, lo, 2, k);
                     times_n(s3, hi, lo, 3, k);
                 }
@@ -710,8 +717,8 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 times_t(t3, hi3, lo3, 3, 3);
                 parts(t2, hi, lo);
                 parts(t3, hi3, lo3);
-                put(hi, lo, 2, side);
-                put(hi3, lo3, 3, side);
+                put(hi, lo, 2, warp);
+                put(hi3, lo3, 3, warp);
             }
         }
         if (c >= 0) {
@@ -723,6 +730,108 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
 }
 
 // ---------------------------------------------------------------------------
+// Outputs: e^G S^T q of a chunk's tokens, scaled, and what the scores add. By the chain warps, or by two others.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ float2 get2(const float (&x)[4], int i) { return make_float2(x[i], x[i + 1]); }
+__device__ __forceinline__ void put2(float (&x)[4], int i, float2 y) { x[i] = y.x; x[i + 1] = y.y; }
+
+// The products with the state by their tokens' factors; NaN from a lost column's token on.
+__device__ __forceinline__ void scale_outputs(float (&O)[8][4], const float* fac, float is0, float is1, bool odd, int bad0, int bad1) {
+    const int quad = threadIdx.x & 3;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+        const float2 f = *reinterpret_cast<const float2*>(fac + F_QUERY * CH + 8 * n + 2 * quad);
+        put2(O[n], 0, mul2(mul2(f, twice(is0)), get2(O[n], 0)));
+        put2(O[n], 2, mul2(mul2(f, twice(is1)), get2(O[n], 2)));
+    }
+    if (odd)
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int t = 8 * n + 2 * quad + e;
+                if (t >= bad0) O[n][e] = __int_as_float(0x7fffffff);
+                if (t >= bad1) O[n][2 + e] = __int_as_float(0x7fffffff);
+            }
+}
+// O^T + U^T P^T, to where row r8's values of the lane's columns are; `live`: rows from there on.
+template <class Z>
+__device__ __forceinline__ void put_outputs(const float (&O)[8][4], const uint32_t (&u)[4][4], float iu0, float iu1, uint32_t scores, const float* fac, uint16_t* o, int64_t step,
+                                            int live) {
+    const int lane = threadIdx.x & 31, quad = lane & 3, b_row = (lane & 7) + ((lane >> 4) << 3), b_seg = (lane >> 3) & 1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float x[2][4];
+#pragma unroll
+        for (int j = 0; j <= i; ++j) {
+            uint32_t b[4];
+            ldmatrix4(b, scores + tile_at<Z::TP>(16 * i + b_row, 2 * j + b_seg));
+            mma_from(j == 0, x[0], u[j], b[0], b[1]);
+            mma_from(j == 0, x[1], u[j], b[2], b[3]);
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int n = 2 * i + p;
+            const float2 fp = *reinterpret_cast<const float2*>(fac + F_SCORE * CH + 8 * n + 2 * quad);
+            float y[4];
+            put2(y, 0, fma2(get2(x[p], 0), mul2(fp, twice(iu0)), get2(O[n], 0)));
+            put2(y, 2, fma2(get2(x[p], 2), mul2(fp, twice(iu1)), get2(O[n], 2)));
+            const uint32_t a = movmatrix_trans(pack_bf16(y[0], y[1])), b = movmatrix_trans(pack_bf16(y[2], y[3]));
+            store_if(o, a, b, 8 * n < live);
+            o += step;
+        }
+    }
+}
+
+template <bool F32, int DK, int CW>
+__device__ __forceinline__ void run_outputs(const Delta& d, const SeqRange& r, int h, int col0, char* smem, uint32_t base, int chunks) {
+    using Z = Shape<F32, DK, CW>;
+    const int warp = (threadIdx.x >> 5) - CW, lane = threadIdx.x & 31, r8 = lane >> 2;                 // for chain warp `warp`
+    const int64_t step = 8 * (int64_t)d.heads * d.head_v;
+    uint16_t* out = d.out + (((int64_t)r.lo + r8) * d.heads + h) * d.head_v + col0 + 16 * warp + 2 * (lane & 3);
+    const char* hand = smem + Z::HANDED + warp * Z::HAND;
+    const uint4* from = reinterpret_cast<const uint4*>(hand) + lane;
+    const int b_row = (lane & 7) + ((lane >> 4) << 3), b_seg = (lane >> 3) & 1;
+    for (int i = 0; i < STAGES && i < chunks; ++i) bar_arrive(Z::EMPTY + i, Z::EMPTY_COUNT);
+#pragma unroll 1
+    for (int c = 0; c < chunks; ++c, out += CH / 8 * step) {
+        const int stage = c & (STAGES - 1);
+        const uint32_t sb = base + stage * Z::STAGE;
+        const float* fac = reinterpret_cast<const float*>(smem + stage * Z::STAGE + Z::FAC);
+        float O[8][4];
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) O[n][e] = 0.f;
+        bar_sync(Z::FULL + stage, Z::FULL_COUNT);
+        bar_sync(Z::S_READY + warp, 64);
+#pragma unroll 2
+        for (int kk = 0; kk < DK / 16; ++kk) {
+            uint32_t f[4][4];
+#pragma unroll
+            for (int n2 = 0; n2 < 4; ++n2) ldmatrix4(f[n2], sb + Z::Q + Z::key_at(16 * n2 + b_row, 2 * kk + b_seg));
+            const uint4 x = from[kk * 32];
+            const uint32_t hi[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int n = 0; n < 8; ++n) mma(O[n], hi, f[n >> 1][2 * (n & 1)], f[n >> 1][2 * (n & 1) + 1]);
+        }
+        bar_sync(Z::U_READY + warp, 64);
+        uint32_t u[4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint4 x = from[(DK / 16 + j) * 32];
+            u[j][0] = x.x; u[j][1] = x.y; u[j][2] = x.z; u[j][3] = x.w;
+        }
+        const float4 scales = *reinterpret_cast<const float4*>(hand + Z::HAND_SCALES + lane * 16);
+        const int2 bad = *reinterpret_cast<const int2*>(hand + Z::HAND_SCALES + 512 + lane * 8);
+        if (c + 1 < chunks) bar_arrive(Z::TAKEN + warp, 64);
+        scale_outputs(O, fac, scales.x, scales.y, bad.x < CH || bad.y < CH, bad.x, bad.y);
+        put_outputs<Z>(O, u, scales.z, scales.w, sb + Z::P, fac, out, step, r.n - c * CH - r8);
+        if (c + STAGES < chunks) bar_arrive(Z::EMPTY + stage, Z::EMPTY_COUNT);
+    }
+}
+
+// ---------------------------------------------------------------------------
 // The chain: a warp, 16 columns.
 // ---------------------------------------------------------------------------
 template <bool F32, int DK, int CW>
@@ -730,10 +839,10 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
     using Z = Shape<F32, DK, CW>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3, r8 = lane >> 2;
     const int vcol = 16 * warp;
-    const auto get2 = [](const float (&x)[4], int i) { return make_float2(x[i], x[i + 1]); };
-    const auto put2 = [](float (&x)[4], int i, float2 y) { x[i] = y.x; x[i + 1] = y.y; };
     float* state = d.state + ((int64_t)r.slot * d.heads + h) * DK * d.head_v + 2 * quad * d.head_v + col0 + vcol + r8;
     uint16_t* out = d.out + (((int64_t)r.lo + r8) * d.heads + h) * d.head_v + col0 + vcol + 2 * quad;
+    char* hand = smem + Z::HANDED + warp * Z::HAND;
+    uint4* to = reinterpret_cast<uint4*>(hand) + lane;
     float S[DK / 8][4];                                             // [8 rows of S][columns r8, r8 + 8 x two rows]
     const float* from = state;
 #pragma unroll
@@ -759,7 +868,8 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
         sc0 = to_f16_range(quad_max(sc0));
         sc1 = to_f16_range(quad_max(sc1));
         bar_sync(Z::FULL + stage, Z::FULL_COUNT);
-        // S^T k and S^T q of every token
+        if (Z::APART && c > 0) bar_sync(Z::TAKEN + warp, 64);
+        // S^T k and (but for outputs elsewhere) S^T q of every token
         float R[8][4], O[8][4];
         // fragments one step ahead of their products
         uint32_t fk[4][4], fq[4][4];
@@ -772,7 +882,8 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
         for (int kk = 0; kk < DK / 16; ++kk) {
             uint32_t hi[4], lo[4];
             split_a(S[2 * kk], S[2 * kk + 1], sc0, sc1, hi, lo);
-            load4(fq, Z::Q, kk);
+            if constexpr (Z::APART) to[kk * 32] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            else load4(fq, Z::Q, kk);
 #pragma unroll
             for (int n = 0; n < 8; ++n) mma_from(kk == 0, R[n], hi, fk[n >> 1][2 * (n & 1)], fk[n >> 1][2 * (n & 1) + 1]);
 #pragma unroll
@@ -783,10 +894,12 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
                 for (int n = 0; n < 8; ++n) mma(R[n], hi, fk[n >> 1][2 * (n & 1)], fk[n >> 1][2 * (n & 1) + 1]);
             }
             if (kk + 1 < DK / 16) load4(fk, Z::K, kk + 1);
+            if constexpr (!Z::APART)
 #pragma unroll
-            for (int n = 0; n < 8; ++n) mma_from(kk == 0, O[n], hi, fq[n >> 1][2 * (n & 1)], fq[n >> 1][2 * (n & 1) + 1]);
+                for (int n = 0; n < 8; ++n) mma_from(kk == 0, O[n], hi, fq[n >> 1][2 * (n & 1)], fq[n >> 1][2 * (n & 1) + 1]);
         }
-        // R = beta v - beta e^G (S^T k); the queries' part of the outputs
+        if constexpr (Z::APART) bar_arrive(Z::S_READY + warp, 64);
+        // R = beta v - beta e^G (S^T k)
         const float is0 = pow2_inverse(sc0), is1 = pow2_inverse(sc1);
         const float2 down0 = twice(-is0), down1 = twice(-is1);
         float m0 = 0.f, m1 = 0.f;
@@ -808,12 +921,9 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
                     v0[0] = __uint_as_float(v[2 * p] << 16); v0[1] = __uint_as_float(v[2 * p] & 0xffff0000u);
                     v1[0] = __uint_as_float(v[2 * p + 1] << 16); v1[1] = __uint_as_float(v[2 * p + 1] & 0xffff0000u);
                 }
-                const float2 fb = *reinterpret_cast<const float2*>(fac + F_BETA * CH + t), fs = *reinterpret_cast<const float2*>(fac + F_STATE * CH + t),
-                             fq = *reinterpret_cast<const float2*>(fac + F_QUERY * CH + t);
+                const float2 fb = *reinterpret_cast<const float2*>(fac + F_BETA * CH + t), fs = *reinterpret_cast<const float2*>(fac + F_STATE * CH + t);
                 put2(R[n], 0, fma2(mul2(fs, down0), get2(R[n], 0), mul2(fb, make_float2(v0[0], v0[1]))));
                 put2(R[n], 2, fma2(mul2(fs, down1), get2(R[n], 2), mul2(fb, make_float2(v1[0], v1[1]))));
-                put2(O[n], 0, mul2(mul2(fq, twice(is0)), get2(O[n], 0)));
-                put2(O[n], 2, mul2(mul2(fq, twice(is1)), get2(O[n], 2)));
                 m0 = max_of(m0, R[n][0], R[n][1]);
                 m1 = max_of(m1, R[n][2], R[n][3]);
             }
@@ -835,15 +945,8 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
                 }
             bad0 = min(bad0, __shfl_xor_sync(0xffffffffu, bad0, 1)); bad0 = min(bad0, __shfl_xor_sync(0xffffffffu, bad0, 2));
             bad1 = min(bad1, __shfl_xor_sync(0xffffffffu, bad1, 1)); bad1 = min(bad1, __shfl_xor_sync(0xffffffffu, bad1, 2));
-#pragma unroll
-            for (int n = 0; n < 8; ++n)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int t = 8 * n + 2 * quad + e;
-                    if (t >= bad0) O[n][e] = nan;
-                    if (t >= bad1) O[n][2 + e] = nan;
-                }
         }
+        if constexpr (!Z::APART) scale_outputs(O, fac, is0, is1, odd, bad0, bad1);
         const float rs0 = to_f16_range(quad_max(m0)), rs1 = to_f16_range(quad_max(m1));
         // U^T = R^T T^T, 16 tokens at a time from the last: a block of U takes the place of the block of R that no other needs
         uint32_t rh[4][4], rl[4][4];
@@ -885,7 +988,7 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
         }
         const float us0 = to_f16_range(quad_max(u0)), us1 = to_f16_range(quad_max(u1));
         const float es0 = to_f16_range(quad_max(e0)), es1 = to_f16_range(quad_max(e1));
-        // O^T += U^T P^T
+        // U as the outputs take it
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -894,30 +997,15 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
                 rh[j][e] = pack_f16(x.x, x.y);
             }
         const float iu0 = pow2_inverse(us0), iu1 = pow2_inverse(us1);
-        const int live = r.n - c * CH - r8;
-        const int64_t step = 8 * (int64_t)d.heads * d.head_v;
-        uint16_t* o = out + c * (CH / 8) * step;
+        if constexpr (Z::APART) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float x[2][4];
-#pragma unroll
-            for (int j = 0; j <= i; ++j) {
-                uint32_t b[4];
-                ldmatrix4(b, sb + Z::P + tile_at<Z::TP>(16 * i + b_row, 2 * j + b_seg));
-                mma_from(j == 0, x[0], rh[j], b[0], b[1]);
-                mma_from(j == 0, x[1], rh[j], b[2], b[3]);
-            }
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                const int n = 2 * i + p, t = 8 * n + 2 * quad;
-                const float2 fp = *reinterpret_cast<const float2*>(fac + F_SCORE * CH + t);
-                float y[4];
-                put2(y, 0, fma2(get2(x[p], 0), mul2(fp, twice(iu0)), get2(O[n], 0)));
-                put2(y, 2, fma2(get2(x[p], 2), mul2(fp, twice(iu1)), get2(O[n], 2)));
-                const uint32_t a = movmatrix_trans(pack_bf16(y[0], y[1])), b = movmatrix_trans(pack_bf16(y[2], y[3]));
-                store_if(o, a, b, 8 * n < live);
-                o += step;
-            }
+            for (int j = 0; j < 4; ++j) to[(DK / 16 + j) * 32] = make_uint4(rh[j][0], rh[j][1], rh[j][2], rh[j][3]);
+            *reinterpret_cast<float4*>(hand + Z::HAND_SCALES + lane * 16) = make_float4(is0, is1, iu0, iu1);
+            *reinterpret_cast<int2*>(hand + Z::HAND_SCALES + 512 + lane * 8) = make_int2(bad0, bad1);
+            bar_arrive(Z::U_READY + warp, 64);
+        } else {
+            const int64_t step = 8 * (int64_t)d.heads * d.head_v;
+            put_outputs<Z>(O, rh, iu0, iu1, sb + Z::P, fac, out + c * (CH / 8) * step, step, r.n - c * CH - r8);
         }
         // S^T <- e^G S^T + U^T k
 #pragma unroll
@@ -996,6 +1084,7 @@ __global__ void __launch_bounds__(Shape<F32, DK, CW>::THREADS, 1) delta_chunk_ke
     if (threadIdx.x < Z::CHAIN) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
         if (threadIdx.x < 32 * CW) run_chain<F32, DK, CW>(d, r, h, col0, smem, base, chunks);
+        else if constexpr (Z::APART) run_outputs<F32, DK, CW>(d, r, h, col0, smem, base, chunks);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 136;");
         prepare_chunks<F32, DK, CW>(d, r, h, col0, smem, base, chunks);
@@ -1018,14 +1107,14 @@ cudaError_t launch_shape(const Delta& d, int above, cudaStream_t s) {
 template <bool F32, int DK>
 cudaError_t launch_width(const Delta& d, int above, int sms, cudaStream_t s) {
     // Columns of a block. All blocks of a head prepare the same chunks, so fewer and wider ones do less in all, and more and
-    // narrower ones fill the GPU. A chunk takes a block of 32 or 64 columns about 4.5 and 4.9 us; the rounds of blocks are
+    // narrower ones fill the GPU. A chunk takes a block of 32 or 64 columns about 4.2 and 4.9 us; the rounds of blocks are
     // counted by the sequences like the longest that the tokens make up. Five sequences of 1774 to 3001 tokens, 32 heads of
-    // 128: 820 and 525 us; one of 32768: 2303 and 2510. (128 columns, which leave the preparing warps half the registers,
+    // 128: 770 and 515 us; one of 32768: 2160 and 2510. (128 columns, which leave the preparing warps half the registers,
     // took 11.2 us a chunk.) fp32 values leave no room for the wider one.
     if constexpr (!F32) {
         const int64_t alike = (d.seq.tokens + d.seq.rows / 2) / d.seq.rows, sequences = alike < 1 ? 1 : alike > d.seq.batch ? d.seq.batch : alike;
         const auto cost = [&](int columns, int64_t each) { return (sequences * d.heads * d.head_v / columns + sms - 1) / sms * each; };
-        if (cost(64, 49) < cost(32, 45)) return launch_shape<F32, DK, 4>(d, above, s);
+        if (cost(64, 49) < cost(32, 42)) return launch_shape<F32, DK, 4>(d, above, s);
     }
     return launch_shape<F32, DK, 2>(d, above, s);
 }
