@@ -26,7 +26,7 @@
 // Named barriers hand the stages over.
 //
 // What bounds it is neither memory nor the tensor cores (a third busy) but the
-// chain of instructions a chunk takes: 14 thousand of twelve warps, 0.4 an issue slot,
+// chain of instructions a chunk takes: 14 thousand of twelve warps, 0.42 an issue slot,
 // each waiting for the one before it or for another group. Two blocks do not
 // fit in the registers of an SM. The code of both roles is twice the 32 KB that
 // an SM keeps of it, so what a chunk does not need twice is not written out
