@@ -51,10 +51,10 @@ def delta_rule(q, k, v, g, beta, state, scale, normalize=True, wide=False):
     a chunk's products enter the tensor cores as pairs of FP16 parts, 2^-22), through the solve of a chunk (its inverse is a
     contraction's part; 8 times is allowed): eps = 2^-16 of the column's norm and of what the token adds. From then on the
     error is carried by e^g (1 - beta k k^T), which does not stretch while beta |k|^2 is within 0..2.
-    Out: the state's error through |q|, the same eps, and what a chunk rounds to FP16 for the outputs alone: the state
-    before the chunk, its scores and its corrections (2^-11 each, so 2^-10 of a product). BF16 queries enter exactly. fp32
-    ones (`wide`) are rounded too, by at most 2^-11 |q_i| each: in q.S that is the second of two roundings, but a score is
-    then off by up to 2^-11 sum_i |q_i k_i| besides its own rounding, and each |U_j| carries that into the output."""
+    Out: the state's error through |q|, the same eps, and the products' own, relative to the magnitudes that are added,
+    |q_i| times the state before the chunk and |q_i k_i| |U_j|: operands are fp32 or pairs of FP16 parts (2^-22 each, at most
+    two), their decay is good to 2^-21, and a sum of up to 128 and 64 terms takes the tensor cores at most 3 x 12 steps of
+    2^-23: 2^-17 in all. (`wide`, for fp32 queries and keys, makes no difference: they are pairs too.)"""
     q, k, v, g, beta = (np.asarray(a, np.float64) for a in (q, k, v, g, beta))
     s = np.asarray(state, np.float64).copy()
     rows, heads, dv = v.shape
@@ -84,12 +84,9 @@ def delta_rule(q, k, v, g, beta, state, scale, normalize=True, wide=False):
         us.append(add)
         ks.append(k[t])
         upto = np.concatenate((upto + g[t][:, None], np.zeros((heads, 1))), 1)
-        score = np.exp(upto) * np.abs(np.einsum("hk,jhk->hj", q[t], np.stack(ks)))
-        spread = np.einsum("hk,hkv->hv", np.abs(q[t]), before) + np.einsum("hj,jhv->hv", score, np.abs(np.stack(us)))
-        out_bound[t] = np.sqrt((q[t] * q[t]).sum(-1))[:, None] * (off + eps * norm) + 2.0 ** -10 * spread
-        if wide:
-            terms = np.exp(upto) * np.einsum("hk,jhk->hj", np.abs(q[t]), np.abs(np.stack(ks)))
-            out_bound[t] += 2.0 ** -11 * np.einsum("hj,jhv->hv", terms, np.abs(np.stack(us)))
+        terms = np.exp(upto) * np.einsum("hk,jhk->hj", np.abs(q[t]), np.abs(np.stack(ks)))
+        spread = np.einsum("hk,hkv->hv", np.abs(q[t]), before) + np.einsum("hj,jhv->hv", terms, np.abs(np.stack(us)))
+        out_bound[t] = np.sqrt((q[t] * q[t]).sum(-1))[:, None] * (off + eps * norm) + 2.0 ** -17 * spread
     return out, s, out_bound, np.broadcast_to(off[:, None, :], s.shape)
 
 

@@ -37,14 +37,16 @@
 //
 // fp32 through the tensor cores. BF16 keys are taken to FP16 by a power of two for
 // 8 or 16 tokens, which they survive unchanged (8 bits of 11) down to 2^-31 of the
-// largest; S, R, U and T enter as two FP16 parts, x = hi + lo, with a power of two
-// per column of S, so a product is good to 2^-22 (fp32 keys, with a power of two a
-// token, are two parts as well). T and L are up by 2^10, so that what a strong decay leaves of an
-// earlier token's R keeps its digits (parts end at 2^-35, not 2^-25, which had an
-// element of 2e-5 off by 2e-8); they overflow from 64 on, and where the rule
+// largest; S, R, U, T and the scores enter as two FP16 parts, x = hi + lo, with a
+// power of two per column of S (the scores: per row), so a product is good to 2^-22
+// (fp32 keys and queries, with a power of two a token, are two parts as well). That
+// holds for the outputs too, which are rounded once: with one part (2^-12) of S, U,
+// the scores and fp32 queries they were off by many steps of BF16 where terms cancel
+// (32768 tokens in 2.16 ms against 2.28, five prompts in 515 us against 555). T and L
+// are up by 2^10, so that what a strong decay leaves of an earlier token's R keeps
+// its digits (parts end at 2^-35, not 2^-25, which had an element of 2e-5 off by
+// 2e-8); they overflow from 64 on, and where the rule
 // contracts |T_ij| is at most |beta_i| |k_i| |k_j|, 2 for keys of unit length.
-// What reaches the outputs alone, which are rounded to BF16, enters as
-// one part (2^-12): queries, scores, and S and U beside them.
 //
 // NaN and infinities must not reach earlier tokens through the zeros above the
 // diagonal: a column whose R is not finite at some token is computed without it
@@ -155,6 +157,9 @@ __device__ __forceinline__ uint32_t tile_at(int row, int seg) {
 enum { G_HI, G_LO, G_BETA, G_BLOCK };
 constexpr int GATES = 4 * CH;
 
+// The same in a tile of two segments a row.
+__device__ __forceinline__ uint32_t beside_at(int row, int seg) { return (uint32_t)(32 * row + ((seg ^ ((row >> 2) & 1)) << 4)); }
+
 template <bool F32, int DK, int CW>
 struct Shape {
     static constexpr int VC = 16 * CW;                              // columns of a block
@@ -164,19 +169,20 @@ struct Shape {
     static constexpr int TP = 2 * CH;                               // bytes of a row of T, the scores and L
     static constexpr int CHAIN = 128;                               // a whole warpgroup
     static constexpr int HALF = 128, PREP = 2 * HALF, THREADS = CHAIN + PREP;     // warps for keys, for queries
-    // a stage: keys (fp32 ones: the two parts of them, where their raw values land), queries, values, T, scores, factors
-    static constexpr int K = 0, KLO = K + CH * KP, Q = KLO + (F32 ? CH * KP : 0), V = Q + CH * KP,
-                         THI = (V + CH * VP + 127) / 128 * 128, TLO = THI + CH * TP, P = TLO + CH * TP, FAC = P + CH * TP,
+    // a stage: keys and queries (fp32 ones: the two parts of each, where their raw values land), values, T in two parts (below the
+    // diagonal -L, until T takes its place, but for two blocks), scores in two parts, factors
+    static constexpr int K = 0, KLO = K + CH * KP, Q = KLO + (F32 ? CH * KP : 0), QLO = Q + CH * KP, V = QLO + (F32 ? CH * KP : 0),
+                         THI = (V + CH * VP + 127) / 128 * 128, TLO = THI + CH * TP, P = TLO + CH * TP, PLO = P + CH * TP, FAC = PLO + CH * TP,
                          STAGE = (FAC + (5 * CH + 4) * 4 + 127) / 128 * 128;
-    // scratch of the preparing warps: -L in FP16 parts, its blocks on the diagonal in fp32, factors of two chunks; the next
-    // chunk's keys and queries as they come (fp32: the second parts of this one's queries)
-    static constexpr int LHI = 0, LLO = LHI + CH * TP, DIAG = LLO + CH * TP, TOKENS = DIAG + 4 * 16 * DP * 4,
-                         FACTORS = 2 * CH + GATES, RAW = TOKENS + 2 * FACTORS * 4, SCRATCH = RAW + (F32 ? CH * KP : 2 * CH * 2 * DK);
+    // scratch of the preparing warps: -L's blocks (2, 1) and (3, 1) in FP16 parts, which are still read when T's are written; its
+    // blocks on the diagonal in fp32; factors of two chunks; the next chunk's BF16 keys and queries as they come
+    static constexpr int BESIDE = 0, PART = 32 * 32, DIAG = BESIDE + 2 * PART, TOKENS = DIAG + 4 * 16 * DP * 4, FACTORS = 2 * CH + GATES, RAW = TOKENS + 2 * FACTORS * 4,
+                         SCRATCH = RAW + (F32 ? 0 : 2 * CH * 2 * DK);
     static constexpr int OWN = STAGES * STAGE;
-    // Two chain warps leave two of their warpgroup to the outputs. What they are handed, each lane by the one at its place: the
-    // parts of S and U that enter the outputs, their scales, where a column is lost.
-    static constexpr bool APART = CW == 2;
-    static constexpr int HANDED = (OWN + SCRATCH + 127) / 128 * 128, HAND_U = DK / 16 * 512, HAND_SCALES = HAND_U + 4 * 512, HAND = HAND_SCALES + 3 * 256,
+    // Two chain warps leave two of their warpgroup to the outputs (fp32 heads of 128 have no room left to hand things over). What
+    // they are handed, each lane by the one at its place: the parts of S and U, their scales, where a column is lost.
+    static constexpr bool APART = CW == 2 && !(F32 && DK == 128);
+    static constexpr int HANDED = (OWN + SCRATCH + 127) / 128 * 128, HAND_U = DK / 16 * 1024, HAND_SCALES = HAND_U + 4 * 1024, HAND = HAND_SCALES + 3 * 256,
                          BYTES = HANDED + (APART ? CW * HAND : 0);
     static_assert(RAW % 16 == 0);
     // named barriers
@@ -322,7 +328,7 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 bar_sync(Z::EMPTY + stage, Z::EMPTY_COUNT);
                 if constexpr (F32) {
                     load_pieces(d.k, d.k_stride, c, sb + Z::K, sb + Z::KLO);
-                    load_pieces(d.q, d.q_stride, c, sb + Z::Q, own_b + Z::RAW);
+                    load_pieces(d.q, d.q_stride, c, sb + Z::Q, sb + Z::QLO);
                 }
                 cp_wait_all();
                 load_values(c, sb + Z::V);
@@ -335,7 +341,7 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
 #pragma unroll 1
                         for (int row = row_in; row < CH; row += STEP) {
                             uint4 *at = reinterpret_cast<uint4*>(tile + Z::key_at(row, seg)),
-                                  *more = reinterpret_cast<uint4*>((half ? own + Z::RAW : st + Z::KLO) + Z::key_at(row, seg));
+                                  *more = reinterpret_cast<uint4*>(st + (half ? Z::QLO : Z::KLO) + Z::key_at(row, seg));
                             const uint4 x = *at, z = *more;
                             float y[8] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w),
                                           __uint_as_float(z.x), __uint_as_float(z.y), __uint_as_float(z.z), __uint_as_float(z.w)};
@@ -412,7 +418,7 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                     for (int kk = 0; kk < DK / 16; ++kk) {
                         uint32_t a[4], alo[4], b[4], l[4];
                         ldmatrix4(a, a_at + Z::key_at(16 * mt + a_row, 2 * kk + a_seg));
-                        ldmatrix4(alo, (of_q ? own_b + Z::RAW : sb + Z::KLO) + Z::key_at(16 * mt + a_row, 2 * kk + a_seg));
+                        ldmatrix4(alo, sb + (of_q ? Z::QLO : Z::KLO) + Z::key_at(16 * mt + a_row, 2 * kk + a_seg));
 #pragma unroll
                         for (int n2 = 0; n2 < 4; ++n2) {
                             if (n2 > mt) break;
@@ -545,16 +551,22 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                     }
                 }
                 const uint32_t to0 = tile_at<Z::TP>(i0, 0) + 4 * quad, to1 = tile_at<Z::TP>(i1, 0) + 4 * quad;       // segment n: turned by 16 n
+                const auto put_parts = [&](const float (&x)[4], float p0, float p1, char* to0, char* to1, int part) {
+                    uint32_t hi, lo;
+                    split2(x[0] * p0, x[1] * p0, hi, lo);
+                    *reinterpret_cast<uint32_t*>(to0) = hi;
+                    *reinterpret_cast<uint32_t*>(to0 + part) = lo;
+                    split2(x[2] * p1, x[3] * p1, hi, lo);
+                    *reinterpret_cast<uint32_t*>(to1) = hi;
+                    *reinterpret_cast<uint32_t*>(to1 + part) = lo;
+                };
                 if (of_q) {
                     const float p0 = to_f16_range(quad_max(m0)), p1 = to_f16_range(quad_max(m1));
                     if (quad == 0) {
                         fac[F_SCORE * CH + i0] = pow2_inverse(p0);
                         fac[F_SCORE * CH + i1] = pow2_inverse(p1);
                     }
-                    const auto put_scores = [&](const float (&x)[4], int n) {
-                        *reinterpret_cast<uint32_t*>(st + Z::P + (to0 ^ (n << 4))) = pack_f16(x[0] * p0, x[1] * p0);
-                        *reinterpret_cast<uint32_t*>(st + Z::P + (to1 ^ (n << 4))) = pack_f16(x[2] * p1, x[3] * p1);
-                    };
+                    const auto put_scores = [&](const float (&x)[4], int n) { put_parts(x, p0, p1, st + Z::P + (to0 ^ (n << 4)), st + Z::P + (to1 ^ (n << 4)), Z::PLO - Z::P); };
 #pragma unroll
                     for (int n = 0; n < 6; ++n) {
                         if (n >= 2 * mt) break;
@@ -581,13 +593,10 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
 #pragma unroll
                     for (int n = 0; n < 6; ++n) {
                         if (n >= 2 * mt) break;
-                        uint32_t hi, lo;
-                        split2(acc[n][0], acc[n][1], hi, lo);
-                        *reinterpret_cast<uint32_t*>(own + Z::LHI + (to0 ^ (n << 4))) = hi;
-                        *reinterpret_cast<uint32_t*>(own + Z::LLO + (to0 ^ (n << 4))) = lo;
-                        split2(acc[n][2], acc[n][3], hi, lo);
-                        *reinterpret_cast<uint32_t*>(own + Z::LHI + (to1 ^ (n << 4))) = hi;
-                        *reinterpret_cast<uint32_t*>(own + Z::LLO + (to1 ^ (n << 4))) = lo;
+                        if (n >> 1 == 1 && mt >= 2)
+                            put_parts(acc[n], 1.f, 1.f, own + Z::BESIDE + beside_at(i0 - 32, n & 1) + 4 * quad, own + Z::BESIDE + beside_at(i1 - 32, n & 1) + 4 * quad, Z::PART);
+                        else
+                            put_parts(acc[n], 1.f, 1.f, st + Z::THI + (to0 ^ (n << 4)), st + Z::THI + (to1 ^ (n << 4)), Z::TLO - Z::THI);
                     }
                     // T's block on the diagonal, in fp32: its two blocks of 8 by substitution, a column a lane, then the one below
                     // them, -C^-1 B A^-1 (with B as it stands here, of -L, the sign is gone).
@@ -653,16 +662,16 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
             }
             if (!of_q) bar_sync(Z::KEYS, Z::HALF);
         }
-        // The blocks below the diagonal, N for -L: T_10 and T_32, T_bb N_ba T_aa, a warp each; then, a warp for each of the columns
+        // The blocks below the diagonal, N for -L, whose places they take: T_10 and T_32, T_bb N_ba T_aa, a warp each; then, a warp for each of the columns
         // a = 0, 1, X_b = sum_(k <= 1) N_bk T_ka for b = 2, 3, T_2a = T_22 X_2 and T_3a = T_32 X_2 + T_33 X_3. Transposed: T_ka^T,
         // read transposed, is an A fragment, and so is what comes out of the products.
         if (c >= 0 && !of_q) {
             struct Sum { float x[2][4], y[2][4]; };
-            const auto times = [&](Sum& s, const uint32_t (&hi)[4], const uint32_t (&lo)[4], uint32_t high, uint32_t low, int b, int k) {
+            const auto times = [&](Sum& s, const uint32_t (&hi)[4], const uint32_t (&lo)[4], int b, int k, bool beside = false) {       // by block (b, k) of N or T
                 uint32_t f[4], e[4];
-                const uint32_t at = tile_at<Z::TP>(16 * b + b_row, 2 * k + b_seg);
-                ldmatrix4(f, high + at);
-                ldmatrix4(e, low + at);
+                const uint32_t at = beside ? own_b + Z::BESIDE + beside_at(16 * (b - 2) + b_row, b_seg) : sb + Z::THI + tile_at<Z::TP>(16 * b + b_row, 2 * k + b_seg);
+                ldmatrix4(f, at);
+                ldmatrix4(e, at + (beside ? Z::PART : Z::TLO - Z::THI));
                 mma(s.x[0], hi, f[0], f[1]);
                 mma(s.x[1], hi, f[2], f[3]);
                 mma(s.y[0], lo, f[0], f[1]);
@@ -670,8 +679,6 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 mma(s.y[0], hi, e[0], e[1]);
                 mma(s.y[1], hi, e[2], e[3]);
             };
-            const auto times_n = [&](Sum& s, const uint32_t (&hi)[4], const uint32_t (&lo)[4], int b, int k) { times(s, hi, lo, own_b + Z::LHI, own_b + Z::LLO, b, k); };
-            const auto times_t = [&](Sum& s, const uint32_t (&hi)[4], const uint32_t (&lo)[4], int b, int k) { times(s, hi, lo, sb + Z::THI, sb + Z::TLO, b, k); };
             const auto get = [&](uint32_t (&hi)[4], uint32_t (&lo)[4], int k, int a) {
                 const uint32_t at = tile_at<Z::TP>(16 * k + b_row, 2 * a + b_seg);
                 ldmatrix4_trans(hi, sb + Z::THI + at);
@@ -694,9 +701,9 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                 const int a = 2 * warp;
                 Sum s = {}, t = {};
                 get(hi, lo, a, a);
-                times_n(s, hi, lo, a + 1, a);
+                times(s, hi, lo, a + 1, a);
                 parts(s, hi, lo);
-                times_t(t, hi, lo, a + 1, a + 1);
+                times(t, hi, lo, a + 1, a + 1);
                 parts(t, hi, lo);
                 put(hi, lo, a + 1, a);
             }
@@ -706,15 +713,15 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
 #pragma unroll 1
                 for (int k = warp; k < 2; ++k) {
                     get(hi, lo, k, warp);
-                    times_n(s2, hi, lo, 2, k);
-                    times_n(s3, hi, lo, 3, k);
+                    times(s2, hi, lo, 2, k, k == 1);
+                    times(s3, hi, lo, 3, k, k == 1);
                 }
                 uint32_t hi3[4], lo3[4];
                 parts(s2, hi, lo);
                 parts(s3, hi3, lo3);
-                times_t(t2, hi, lo, 2, 2);
-                times_t(t3, hi, lo, 3, 2);
-                times_t(t3, hi3, lo3, 3, 3);
+                times(t2, hi, lo, 2, 2);
+                times(t3, hi, lo, 3, 2);
+                times(t3, hi3, lo3, 3, 3);
                 parts(t2, hi, lo);
                 parts(t3, hi3, lo3);
                 put(hi, lo, 2, warp);
@@ -756,18 +763,24 @@ __device__ __forceinline__ void scale_outputs(float (&O)[8][4], const float* fac
 }
 // O^T + U^T P^T, to where row r8's values of the lane's columns are; `live`: rows from there on.
 template <class Z>
-__device__ __forceinline__ void put_outputs(const float (&O)[8][4], const uint32_t (&u)[4][4], float iu0, float iu1, uint32_t scores, const float* fac, uint16_t* o, int64_t step,
-                                            int live) {
+__device__ __forceinline__ void put_outputs(const float (&O)[8][4], const uint32_t (&u)[4][4], const uint32_t (&ulo)[4][4], float iu0, float iu1, uint32_t scores, const float* fac,
+                                            uint16_t* o, int64_t step, int live) {
     const int lane = threadIdx.x & 31, quad = lane & 3, b_row = (lane & 7) + ((lane >> 4) << 3), b_seg = (lane >> 3) & 1;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float x[2][4];
 #pragma unroll
         for (int j = 0; j <= i; ++j) {
-            uint32_t b[4];
-            ldmatrix4(b, scores + tile_at<Z::TP>(16 * i + b_row, 2 * j + b_seg));
+            uint32_t b[4], l[4];
+            const uint32_t at = scores + tile_at<Z::TP>(16 * i + b_row, 2 * j + b_seg);
+            ldmatrix4(b, at);
+            ldmatrix4(l, at + Z::PLO - Z::P);
             mma_from(j == 0, x[0], u[j], b[0], b[1]);
             mma_from(j == 0, x[1], u[j], b[2], b[3]);
+            mma(x[0], ulo[j], b[0], b[1]);
+            mma(x[1], ulo[j], b[2], b[3]);
+            mma(x[0], u[j], l[0], l[1]);
+            mma(x[1], u[j], l[2], l[3]);
         }
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
@@ -810,23 +823,32 @@ __device__ __forceinline__ void run_outputs(const Delta& d, const SeqRange& r, i
             uint32_t f[4][4];
 #pragma unroll
             for (int n2 = 0; n2 < 4; ++n2) ldmatrix4(f[n2], sb + Z::Q + Z::key_at(16 * n2 + b_row, 2 * kk + b_seg));
-            const uint4 x = from[kk * 32];
-            const uint32_t hi[4] = {x.x, x.y, x.z, x.w};
+            const uint4 x = from[2 * kk * 32], y = from[(2 * kk + 1) * 32];
+            const uint32_t hi[4] = {x.x, x.y, x.z, x.w}, lo[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
             for (int n = 0; n < 8; ++n) mma(O[n], hi, f[n >> 1][2 * (n & 1)], f[n >> 1][2 * (n & 1) + 1]);
+#pragma unroll
+            for (int n = 0; n < 8; ++n) mma(O[n], lo, f[n >> 1][2 * (n & 1)], f[n >> 1][2 * (n & 1) + 1]);
+            if constexpr (F32) {
+#pragma unroll
+                for (int n2 = 0; n2 < 4; ++n2) ldmatrix4(f[n2], sb + Z::QLO + Z::key_at(16 * n2 + b_row, 2 * kk + b_seg));
+#pragma unroll
+                for (int n = 0; n < 8; ++n) mma(O[n], hi, f[n >> 1][2 * (n & 1)], f[n >> 1][2 * (n & 1) + 1]);
+            }
         }
         bar_sync(Z::U_READY + warp, 64);
-        uint32_t u[4][4];
+        uint32_t u[4][4], ulo[4][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint4 x = from[(DK / 16 + j) * 32];
+            const uint4 x = from[2 * (DK / 16 + j) * 32], y = from[(2 * (DK / 16 + j) + 1) * 32];
             u[j][0] = x.x; u[j][1] = x.y; u[j][2] = x.z; u[j][3] = x.w;
+            ulo[j][0] = y.x; ulo[j][1] = y.y; ulo[j][2] = y.z; ulo[j][3] = y.w;
         }
         const float4 scales = *reinterpret_cast<const float4*>(hand + Z::HAND_SCALES + lane * 16);
         const int2 bad = *reinterpret_cast<const int2*>(hand + Z::HAND_SCALES + 512 + lane * 8);
         if (c + 1 < chunks) bar_arrive(Z::TAKEN + warp, 64);
         scale_outputs(O, fac, scales.x, scales.y, bad.x < CH || bad.y < CH, bad.x, bad.y);
-        put_outputs<Z>(O, u, scales.z, scales.w, sb + Z::P, fac, out, step, r.n - c * CH - r8);
+        put_outputs<Z>(O, u, ulo, scales.z, scales.w, sb + Z::P, fac, out, step, r.n - c * CH - r8);
         if (c + STAGES < chunks) bar_arrive(Z::EMPTY + stage, Z::EMPTY_COUNT);
     }
 }
@@ -882,8 +904,12 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
         for (int kk = 0; kk < DK / 16; ++kk) {
             uint32_t hi[4], lo[4];
             split_a(S[2 * kk], S[2 * kk + 1], sc0, sc1, hi, lo);
-            if constexpr (Z::APART) to[kk * 32] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            else load4(fq, Z::Q, kk);
+            if constexpr (Z::APART) {
+                to[2 * kk * 32] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                to[(2 * kk + 1) * 32] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            } else {
+                load4(fq, Z::Q, kk);
+            }
 #pragma unroll
             for (int n = 0; n < 8; ++n) mma_from(kk == 0, R[n], hi, fk[n >> 1][2 * (n & 1)], fk[n >> 1][2 * (n & 1) + 1]);
 #pragma unroll
@@ -894,9 +920,17 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
                 for (int n = 0; n < 8; ++n) mma(R[n], hi, fk[n >> 1][2 * (n & 1)], fk[n >> 1][2 * (n & 1) + 1]);
             }
             if (kk + 1 < DK / 16) load4(fk, Z::K, kk + 1);
-            if constexpr (!Z::APART)
+            if constexpr (!Z::APART) {
 #pragma unroll
                 for (int n = 0; n < 8; ++n) mma_from(kk == 0, O[n], hi, fq[n >> 1][2 * (n & 1)], fq[n >> 1][2 * (n & 1) + 1]);
+#pragma unroll
+                for (int n = 0; n < 8; ++n) mma(O[n], lo, fq[n >> 1][2 * (n & 1)], fq[n >> 1][2 * (n & 1) + 1]);
+                if constexpr (F32) {
+                    load4(fq, Z::QLO, kk);
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) mma(O[n], hi, fq[n >> 1][2 * (n & 1)], fq[n >> 1][2 * (n & 1) + 1]);
+                }
+            }
         }
         if constexpr (Z::APART) bar_arrive(Z::S_READY + warp, 64);
         // R = beta v - beta e^G (S^T k)
@@ -994,18 +1028,21 @@ __device__ __forceinline__ void run_chain(const Delta& d, const SeqRange& r, int
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float2 x = mul2(get2(R[2 * j + (e >> 1)], 2 * (e & 1)), twice(e & 1 ? us1 : us0));
-                rh[j][e] = pack_f16(x.x, x.y);
+                split2(x, rh[j][e], rl[j][e]);
             }
         const float iu0 = pow2_inverse(us0), iu1 = pow2_inverse(us1);
         if constexpr (Z::APART) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) to[(DK / 16 + j) * 32] = make_uint4(rh[j][0], rh[j][1], rh[j][2], rh[j][3]);
+            for (int j = 0; j < 4; ++j) {
+                to[2 * (DK / 16 + j) * 32] = make_uint4(rh[j][0], rh[j][1], rh[j][2], rh[j][3]);
+                to[(2 * (DK / 16 + j) + 1) * 32] = make_uint4(rl[j][0], rl[j][1], rl[j][2], rl[j][3]);
+            }
             *reinterpret_cast<float4*>(hand + Z::HAND_SCALES + lane * 16) = make_float4(is0, is1, iu0, iu1);
             *reinterpret_cast<int2*>(hand + Z::HAND_SCALES + 512 + lane * 8) = make_int2(bad0, bad1);
             bar_arrive(Z::U_READY + warp, 64);
         } else {
             const int64_t step = 8 * (int64_t)d.heads * d.head_v;
-            put_outputs<Z>(O, rh, iu0, iu1, sb + Z::P, fac, out + c * (CH / 8) * step, step, r.n - c * CH - r8);
+            put_outputs<Z>(O, rh, rl, iu0, iu1, sb + Z::P, fac, out + c * (CH / 8) * step, step, r.n - c * CH - r8);
         }
         // S^T <- e^G S^T + U^T k
 #pragma unroll
