@@ -589,9 +589,9 @@ vbq_status_t vbq_causal_conv(const vbq_sequences* seq, const void* x, int64_t x_
  *              1e-6) per head; 0: they are taken as they are. The rule contracts
  *              while beta |k|^2 stays within 0..2, and is meant for that.
  *              (Sequences of more than 22 rows also need |beta_i| |k_i| |k_j| below
- *              64 between tokens; beyond that their outputs may be NaN. BF16
- *              keys and queries below 2^-31 of the largest among 16 neighbouring
- *              tokens lose digits there.)
+ *              64 between tokens; beyond that their outputs may be NaN. What of a
+ *              BF16 key or query is below 2^-31 of the largest of the same key or
+ *              query loses digits there.)
  *   out        device, tokens x heads x head_v BF16, dense.
  * The state and all sums are fp32. Results do not vary between calls; a
  * sequence's are the same to rounding however its tokens are cut into calls.

@@ -35,9 +35,9 @@
 // (with three of four chunks not prepared: 3.4); memory needs
 // 0.12 ms of it.
 //
-// fp32 through the tensor cores. BF16 keys are taken to FP16 by a power of two for
-// 8 or 16 tokens, which they survive unchanged (8 bits of 11) down to 2^-31 of the
-// largest; S, R, U, T and the scores enter as two FP16 parts, x = hi + lo, with a
+// fp32 through the tensor cores. BF16 keys and queries are taken to FP16 by a power
+// of two a token, which they survive unchanged (8 bits of 11) down to 2^-31 of their
+// token's largest; S, R, U, T and the scores enter as two FP16 parts, x = hi + lo, with a
 // power of two per column of S (the scores: per row), so a product is good to 2^-22
 // (fp32 keys and queries, with a power of two a token, are two parts as well). That
 // holds for the outputs too, which are rounded once: with one part (2^-12) of S, U,
@@ -360,8 +360,7 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                         }
                     }
                 } else {
-                    // one power of two for a warp's rows of a turn (8; 64 values: 16), by their largest magnitude: what is below 2^-32 of
-                    // it loses digits
+                    // a power of two per row, by its largest magnitude: the others have no say in it (two rows' magnitudes in a word)
                     constexpr int ROWS = 4, TURNS = CH / STEP / ROWS;
 #pragma unroll 1
                     for (int turn = 0; turn < 2 * TURNS; ++turn) {
@@ -372,29 +371,26 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
 #pragma unroll
                         for (int i = 0; i < ROWS; ++i) x[i] = from[i * Z::HALF];
                         constexpr uint32_t MAGNITUDES = 0x7fff7fffu;
-                        uint32_t m = 0;
+                        uint32_t m[ROWS];
 #pragma unroll
                         for (int i = 0; i < ROWS; ++i)
-                            m = __vmaxu2(__vmaxu2(m, __vmaxu2(x[i].x & MAGNITUDES, x[i].y & MAGNITUDES)), __vmaxu2(x[i].z & MAGNITUDES, x[i].w & MAGNITUDES));
-                        m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
-                        if (m >= 0x7f80) {                          // infinities and NaN have no say in the others' power of two
-                            m = 0;
-                            const auto finite = [&](uint32_t w) { m = max(m, (w & 0x7fff) < 0x7f80 ? w & 0x7fff : 0u); };
+                            m[i] = __vmaxu2(__vmaxu2(x[i].x & MAGNITUDES, x[i].y & MAGNITUDES), __vmaxu2(x[i].z & MAGNITUDES, x[i].w & MAGNITUDES));
 #pragma unroll
-                            for (int i = 0; i < ROWS; ++i) {
-                                finite(x[i].x); finite(x[i].x >> 16); finite(x[i].y); finite(x[i].y >> 16);
-                                finite(x[i].z); finite(x[i].z >> 16); finite(x[i].w); finite(x[i].w >> 16);
-                            }
-                            m = __reduce_max_sync(0xffffffffu, m);
+                        for (int i = 0; i < ROWS; i += 2) {
+                            uint32_t both = __vmaxu2(__byte_perm(m[i], m[i + 1], 0x5410), __byte_perm(m[i], m[i + 1], 0x7632));
+#pragma unroll
+                            for (int o = SEGS / 2; o; o >>= 1) both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, o));
+                            m[i] = both << 16;
+                            m[i + 1] = both & 0xffff0000u;
                         }
-                        const float up = to_f16_range(__uint_as_float(m << 16)), inverse = pow2_inverse(up);
-                        const auto two = [&](uint32_t w) { return pack_f16(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up); };
                         char* to = st + (half ? Z::Q : Z::K) + Z::key_at(row, seg);
                         float* down = (half ? cq : ck) + row;
 #pragma unroll
                         for (int i = 0; i < ROWS; ++i) {
+                            const float up = to_f16_range(__uint_as_float(m[i]));
+                            const auto two = [&](uint32_t w) { return pack_f16(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up); };
                             *reinterpret_cast<uint4*>(to + i * STEP * Z::KP) = make_uint4(two(x[i].x), two(x[i].y), two(x[i].z), two(x[i].w));
-                            if (seg == 0) down[i * STEP] = inverse;
+                            if (seg == 0) down[i * STEP] = pow2_inverse(up);
                         }
                     }
                 }

@@ -105,3 +105,34 @@ def test_layer_tokens_of_each_sequence():
         rows = np.stack(got[s])
         for part in (slice(0, lens[s]), slice(lens[s], None)):
             assert np.linalg.norm(rows[part] - ref[part]) <= 0.02 * np.linalg.norm(ref[part])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("dk", [64, 128])
+@pytest.mark.parametrize("size", [1e14, 1e-14], ids=str)
+def test_keys_of_all_sizes_beside_each_other(size, dk, dtype):
+    """Unit length takes a key's and a query's size away, whatever its neighbours' are: single tokens 1e14 times as large, or
+    as small, as those of the same chunk (their smallness counts: 1e-14 squared is nothing beside the epsilon)."""
+    rng = np.random.default_rng(dk)
+    rows, h, dv = 90, 2, 64
+    q, k, v, a, b, _, _ = inputs(rng, rows, h, h, dk, dv, dtype, False)
+    q, k = q.clone(), k.clone()
+    for t in (1, 17, 48, 70):
+        k[t] = (k[t].float() * size).to(dtype)
+        q[t + 3] = (q[t + 3].float() * size).to(dtype)
+    state = torch.randn(1, h, dk, dv, device=DEV)
+    before = state.clone()
+    out = vbq.vbq_delta_rule(vbq.Sequences(1, rows), state, q, k, v, a, b)
+    check_delta(out, state, before, [rows], [0], [0], 0, q, k, v, a, b, None, None, dk ** -0.5)
+
+
+def test_a_large_key_leaves_earlier_tokens_alone():
+    """Bit for bit: a key that comes later, as large as they get, has no say in what is computed before it."""
+    rng = np.random.default_rng(5)
+    for dk, at in ((64, 48), (128, 24), (64, 63)):
+        q, k, v, a, b, _, _ = inputs(rng, 64, 1, 1, dk, 64, BF16, False)
+        k, state = k.clone(), torch.randn(1, 1, dk, 64, device=DEV)
+        run = lambda: vbq.vbq_delta_rule(vbq.Sequences(1, 64), state.clone(), q, k, v, a, b)  # noqa: E731
+        want = run()
+        k[at] *= 2.0 ** 46
+        assert torch.equal(run()[:at], want[:at])
