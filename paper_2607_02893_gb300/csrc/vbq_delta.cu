@@ -312,9 +312,10 @@ cudaError_t launch_rows(const Delta& d, int most, bool beside, cudaStream_t s) {
 
 }  // namespace
 
-// Sequences of a few rows go token by token, longer ones by chunks. Where the call's may be of both kinds, both
-// kernels run, each over its own and side by side (24 single tokens and a prompt of 2000, 32 heads of 128: 185 us one after
-// the other, 165 so).
+// Sequences of a few rows go token by token, longer ones by chunks: with `starts` by the rows that they turn out to have, not
+// by what the call says of the longest, since up to 22 rows keys may be of any sizes. Where the call's may be of both kinds,
+// both kernels run, each over its own and side by side (24 single tokens and a prompt of 2000, 32 heads of 128: 185 us one
+// after the other, 165 so).
 cudaError_t launch_delta_rule(const Delta& d, cudaStream_t s) {
     int sms = 0;
     const int err = device_sms(&sms);
@@ -322,7 +323,7 @@ cudaError_t launch_delta_rule(const Delta& d, cudaStream_t s) {
     if (d.seq.rows <= 1) return launch_tokens(d, s);
     const int few = (int64_t)d.seq.batch * d.heads * (d.head_v / 64) <= sms ? DELTA_ROWS : DELTA_ROWS_FULL;
     if (d.seq.rows <= few) return launch_rows(d, INT32_MAX, false, s);
-    if (d.seq.starts && d.seq.batch > 1) {
+    if (d.seq.starts) {
         const cudaError_t e = launch_delta_chunks(d, few, sms, s);
         return e != cudaSuccess ? e : launch_rows(d, few, true, s);
     }

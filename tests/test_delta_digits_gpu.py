@@ -136,3 +136,26 @@ def test_a_large_key_leaves_earlier_tokens_alone():
         want = run()
         k[at] *= 2.0 ** 46
         assert torch.equal(run()[:at], want[:at])
+
+
+@pytest.mark.parametrize("batch", [1, 2])
+@pytest.mark.parametrize("rows", [1, 5, 22])
+def test_few_rows_in_a_call_that_may_have_many(rows, batch):
+    """One place of a captured step: `rows` says 200, starts say fewer. Up to 22 rows a sequence's keys may be of any sizes:
+    here |k_i| |k_j| beta is 100 between tokens while beta |k|^2 stays within 0..2."""
+    rng = np.random.default_rng(rows)
+    h, d = 2, 128
+    lens = [rows] * batch
+    q, k, v, a, b, _, _ = inputs(rng, rows * batch, h, h, d, d, BF16, False)
+    k, b = k.clone(), b.clone()
+    k[:], b[:] = 0, 1.0
+    k[:, :, 0] = 1.0
+    k[:, :, 1:9] = 0.25 * torch.randn(rows * batch, h, 8, device=DEV).to(BF16)
+    for i in range(batch):
+        k[i * rows], b[i * rows] = 0, 1e-4
+        k[i * rows, :, 0] = 100.0
+    state = torch.randn(batch, h, d, d, device=DEV)
+    before = state.clone()
+    seq = sequences(lens, list(range(batch)), rows=200)
+    out = vbq.vbq_delta_rule(seq, state, q, k, v, a, b, normalize=False)
+    check_delta(out, state, before, lens, list(range(batch)), [0] * batch, 0, q, k, v, a, b, None, None, d ** -0.5, normalize=False)
