@@ -22,13 +22,16 @@ constexpr int CONV_THREADS = 128;
 constexpr int CONV_ROWS = 32;        // rows of a tile
 constexpr int CONV_AHEAD = 8;        // rows loaded together, ahead of their use
 
+// Up to 2^31 - 1 rows: no sum here passes 32 bits.
+__host__ __device__ __forceinline__ int tiles_of(int rows) { return rows / CONV_ROWS + (rows % CONV_ROWS != 0); }
+
 // Tile `t` of the call is tile *tile of sequence b. With `starts`, sequence b's tiles are among numbers starts[b] / ROWS + b
 // and on: a sequence of n rows spans at most floor(starts[b + 1] / ROWS) - floor(starts[b] / ROWS) + 1 of them, so the
 // numbers of two sequences are apart and no prefix sum over the batch is needed. Each round of the search narrows b to a
 // 32nd, a lane each.
 __device__ __forceinline__ int find_tile(const vbq_sequences& q, int t, int* tile) {
     if (!q.starts) {
-        const int per = (q.rows + CONV_ROWS - 1) / CONV_ROWS, b = t / per;
+        const int per = tiles_of(q.rows), b = t / per;
         *tile = t - b * per;
         return b;
     }
@@ -136,14 +139,14 @@ __global__ void __launch_bounds__(CONV_THREADS) causal_conv_kernel(Conv c) {
 #pragma unroll
         for (int j = 0; j < PAST; ++j) {
             float2 last[2];
-            if (r.n + j >= PAST) {
+            if (r.n >= PAST - j) {
                 Four<F32> x;
-                x.load(c.x, at + (int64_t)(r.n + j - PAST) * c.x_stride);
+                x.load(c.x, at + (int64_t)(r.n - (PAST - j)) * c.x_stride);
                 x.values(last);
             } else {
 #pragma unroll
                 for (int m = 0; m < PAST; ++m)
-                    if (m == r.n + j)
+                    if (m - j == r.n)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) last[e] = line[m][e];
             }
@@ -181,7 +184,7 @@ __global__ void __launch_bounds__(CONV_THREADS) causal_conv_kernel(Conv c) {
 
 cudaError_t launch_causal_conv(const Conv& c, cudaStream_t s) {
     const vbq_sequences& q = c.seq;
-    const int64_t tiles = q.starts ? q.tokens / CONV_ROWS + q.batch : (int64_t)((q.rows + CONV_ROWS - 1) / CONV_ROWS) * q.batch;
+    const int64_t tiles = q.starts ? q.tokens / CONV_ROWS + q.batch : (int64_t)tiles_of(q.rows) * q.batch;
     const dim3 grid((unsigned)tiles, (unsigned)((c.channels / 4 + CONV_THREADS - 1) / CONV_THREADS));
     const auto go = [&](auto kernel) { return launch_dependent(kernel, grid, CONV_THREADS, 0, s, c); };
     if (c.f32) return c.taps == 2 ? go(causal_conv_kernel<true, 2>) : c.taps == 3 ? go(causal_conv_kernel<true, 3>) : go(causal_conv_kernel<true, 4>);
