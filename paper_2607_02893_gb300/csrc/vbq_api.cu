@@ -513,17 +513,15 @@ vbq_status_t vbq_chain_free(vbq_chain* C) {
 vbq_status_t vbq_device_status(void* stream) {
     g_err[0] = 0;
     uint32_t word = 0;
-    uint32_t kv = 0, attend = 0, conv = 0, delta = 0;
+    uint32_t kv = 0, attend = 0;
     VBQ_CUDA(vbq::read_device_status(&word, static_cast<cudaStream_t>(stream)));
     VBQ_CUDA(vbq::read_device_status_kv(&kv));
     VBQ_CUDA(vbq::read_device_status_attend(&attend));
-    VBQ_CUDA(vbq::read_device_status_conv(&conv));
-    VBQ_CUDA(vbq::read_device_status_delta(&delta));
     word |= kv | attend;
-    if ((word | conv | delta) == vbq::VBQ_DEVICE_RANGE)
-        return word ? fail(VBQ_ERR_RANGE, "a position or page of a cache call lay outside the cache")
-                    : fail(VBQ_ERR_RANGE, "a slot of a call on sequences lay outside its pool");
-    word |= conv | delta;
+    constexpr uint32_t ranges = vbq::VBQ_DEVICE_RANGE | vbq::VBQ_DEVICE_SLOT;
+    if (word && !(word & ~ranges))
+        return word & vbq::VBQ_DEVICE_RANGE ? fail(VBQ_ERR_RANGE, "a position or page of a cache call lay outside the cache")
+                                            : fail(VBQ_ERR_RANGE, "a slot of a call on sequences lay outside its pool");
     if (word) return fail(VBQ_ERR_TIMEOUT, "a bounded device wait gave up (status word 0x%x)", word);
     return VBQ_OK;
 }

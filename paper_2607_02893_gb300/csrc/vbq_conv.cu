@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(CONV_THREADS) causal_conv_kernel(Conv c) {
     int tile = 0;
     const int b = find_tile(c.seq, (int)blockIdx.x, &tile);
     if (b < 0 || ch >= c.channels) return;
-    const SeqRange r = seq_range(c.seq, b, c.n_slots, ch == 0 && tile == 0);
+    const SeqRange r = seq_range(c.seq, b, c.n_slots, ch == 0 && tile == 0, c.status);
     const int64_t t0 = (int64_t)tile * CONV_ROWS;
     if (t0 >= r.n) return;
     const int rows = min(CONV_ROWS, (int)(r.n - t0));
@@ -189,13 +189,6 @@ cudaError_t launch_causal_conv(const Conv& c, cudaStream_t s) {
     const auto go = [&](auto kernel) { return launch_dependent(kernel, grid, CONV_THREADS, 0, s, c); };
     if (c.f32) return c.taps == 2 ? go(causal_conv_kernel<true, 2>) : c.taps == 3 ? go(causal_conv_kernel<true, 3>) : go(causal_conv_kernel<true, 4>);
     return c.taps == 2 ? go(causal_conv_kernel<false, 2>) : c.taps == 3 ? go(causal_conv_kernel<false, 3>) : go(causal_conv_kernel<false, 4>);
-}
-
-cudaError_t read_device_status_conv(uint32_t* status) {
-    cudaError_t e = cudaMemcpyFromSymbol(status, g_device_status, sizeof(uint32_t));
-    if (e != cudaSuccess || *status == 0) return e;
-    const uint32_t zero = 0;
-    return cudaMemcpyToSymbol(g_device_status, &zero, sizeof(uint32_t));
 }
 
 }  // namespace vbq

@@ -143,6 +143,7 @@ struct Conv {
     int64_t n_slots;
     int silu;
     uint16_t* out;
+    uint32_t* status;                           // sequence_status's word
 };
 constexpr int CONV_MAX_TAPS = 4;
 cudaError_t launch_causal_conv(const Conv& c, cudaStream_t s);
@@ -162,6 +163,7 @@ struct Delta {
     float scale;
     int normalize;
     uint16_t* out;
+    uint32_t* status;
 };
 cudaError_t launch_delta_rule(const Delta& d, cudaStream_t s);
 
@@ -177,12 +179,13 @@ struct GatedNorm {
 };
 cudaError_t launch_gated_norm(const GatedNorm& n, cudaStream_t s);
 
-// Device status words of the cache and sequence kernels (read and cleared).
-constexpr uint32_t VBQ_DEVICE_RANGE = 2u;       // a position or page outside the cache, a slot outside its pool
+// Device status words of the cache kernels (read and cleared). Those on sequences report into the first, whose address on the
+// current device they are given: a word of their own would be a copy more, which waits for the device, in every report.
+constexpr uint32_t VBQ_DEVICE_RANGE = 2u;       // a position or page outside the cache
+constexpr uint32_t VBQ_DEVICE_SLOT = 4u;        // a slot of a call on sequences outside its pool
 cudaError_t read_device_status_kv(uint32_t* status);
 cudaError_t read_device_status_attend(uint32_t* status);
-cudaError_t read_device_status_conv(uint32_t* status);
-cudaError_t read_device_status_delta(uint32_t* status);
+cudaError_t sequence_status(uint32_t** word);
 
 // Launch with programmatic dependent launch, as the products are: the kernel
 // may start before its predecessor on the stream has finished and waits for it

@@ -288,6 +288,7 @@ vbq_status_t vbq_causal_conv(const vbq_sequences* seq, const void* x, int64_t x_
     c.x = x; c.x_stride = x_stride; c.f32 = type == VBQ_F32;
     c.weight = weight; c.bias = bias; c.taps = taps; c.channels = channels;
     c.state = state; c.n_slots = n_slots; c.silu = silu; c.out = out;
+    VBQ_CUDA(vbq::sequence_status(&c.status));
     VBQ_CUDA(vbq::launch_causal_conv(c, static_cast<cudaStream_t>(stream)));
     return VBQ_OK;
 }
@@ -331,6 +332,7 @@ vbq_status_t vbq_delta_rule(const vbq_sequences* seq, float* state, int64_t n_sl
     d.decay = decay; d.beta = beta; d.decay_stride = decay_stride; d.beta_stride = beta_stride;
     d.gate_f32 = gate_type == VBQ_F32;
     d.a_log = a_log; d.dt_bias = dt_bias; d.scale = scale; d.normalize = normalize; d.out = out;
+    VBQ_CUDA(vbq::sequence_status(&d.status));
     VBQ_CUDA(vbq::launch_delta_rule(d, static_cast<cudaStream_t>(stream)));
     return VBQ_OK;
 }

@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(32 * DR_WARPS, 8) delta_token_kernel(Delta d) 
     const int b = unit / d.heads, h = unit - b * d.heads;
     const int lane = threadIdx.x & 31, part = lane >> 2;
     const int col = slice * DR_COLS + (threadIdx.x >> 5) * 16 + (lane & 3) * 4;
-    const SeqRange r = seq_range(d.seq, b, d.n_slots, h == 0 && slice == 0 && threadIdx.x == 0);
+    const SeqRange r = seq_range(d.seq, b, d.n_slots, h == 0 && slice == 0 && threadIdx.x == 0, d.status);
     if (r.n == 0) return;
     const int64_t out_row = (int64_t)d.heads * d.head_v;
     uint16_t* out = d.out + r.lo * out_row + h * d.head_v + col;
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(32 * RW_WARPS) delta_rows_kernel(Delta d, int 
     const int b = unit / d.heads, h = unit - b * d.heads;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, part = lane >> 2, quad = lane & 3;
     const int col = slice * DR_COLS + warp * 8 + quad * 2;
-    const SeqRange r = seq_range(d.seq, b, d.n_slots, h == 0 && slice == 0 && tid == 0);
+    const SeqRange r = seq_range(d.seq, b, d.n_slots, h == 0 && slice == 0 && tid == 0, d.status);
     if (r.n == 0 || r.n > most) return leave();
     const int64_t out_row = (int64_t)d.heads * d.head_v;
     uint16_t* out = d.out + r.lo * out_row + h * d.head_v + col;
@@ -328,16 +328,6 @@ cudaError_t launch_delta_rule(const Delta& d, cudaStream_t s) {
         return e != cudaSuccess ? e : launch_rows(d, few, true, s);
     }
     return launch_delta_chunks(d, 0, sms, s);
-}
-
-cudaError_t read_device_status_delta(uint32_t* status) {
-    uint32_t chunks = 0;
-    cudaError_t e = read_device_status_delta_chunks(&chunks);
-    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(status, g_device_status, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
-    const uint32_t mine = *status, zero = 0;
-    *status |= chunks;
-    return mine == 0 ? cudaSuccess : cudaMemcpyToSymbol(g_device_status, &zero, sizeof(uint32_t));
 }
 
 }  // namespace vbq

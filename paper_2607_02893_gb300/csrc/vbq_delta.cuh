@@ -30,6 +30,5 @@ __device__ __forceinline__ Gate gate_of(float a, float b, bool raw, float rate, 
 
 // Sequences of more than `above` rows, 64 tokens at a time on the tensor cores (vbq_delta_chunk.cu).
 cudaError_t launch_delta_chunks(const Delta& d, int above, int sms, cudaStream_t s);
-cudaError_t read_device_status_delta_chunks(uint32_t* status);
 
 }  // namespace vbq

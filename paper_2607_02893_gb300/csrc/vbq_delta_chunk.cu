@@ -1102,7 +1102,7 @@ __global__ void __launch_bounds__(Shape<F32, DK, CW>::THREADS, 1) delta_chunk_ke
     const int slices = d.head_v / Z::VC;
     const int unit = (int)(blockIdx.x / slices), slice = (int)(blockIdx.x - unit * slices);
     const int b = unit / d.heads, h = unit - b * d.heads, col0 = slice * Z::VC;
-    const SeqRange r = seq_range(d.seq, b, d.n_slots, h == 0 && slice == 0 && threadIdx.x == 0);
+    const SeqRange r = seq_range(d.seq, b, d.n_slots, h == 0 && slice == 0 && threadIdx.x == 0, d.status);
     if (r.n <= above) return;
     if (r.slot < 0) {
         constexpr int PER = Z::VC / 8;
@@ -1157,13 +1157,6 @@ cudaError_t launch_width(const Delta& d, int above, int sms, cudaStream_t s) {
 cudaError_t launch_delta_chunks(const Delta& d, int above, int sms, cudaStream_t s) {
     if (d.f32) return d.head_k == 64 ? launch_width<true, 64>(d, above, sms, s) : launch_width<true, 128>(d, above, sms, s);
     return d.head_k == 64 ? launch_width<false, 64>(d, above, sms, s) : launch_width<false, 128>(d, above, sms, s);
-}
-
-cudaError_t read_device_status_delta_chunks(uint32_t* status) {
-    cudaError_t e = cudaMemcpyFromSymbol(status, g_device_status, sizeof(uint32_t));
-    if (e != cudaSuccess || *status == 0) return e;
-    const uint32_t zero = 0;
-    return cudaMemcpyToSymbol(g_device_status, &zero, sizeof(uint32_t));
 }
 
 }  // namespace vbq

@@ -247,4 +247,27 @@ cudaError_t read_device_status_kv(uint32_t* status) {
     return cudaMemcpyToSymbol(g_device_status, &zero, sizeof(uint32_t));
 }
 
+cudaError_t sequence_status(uint32_t** word) {
+    constexpr int MAX_DEVICES = LaunchPrep::MAX_DEVICES;
+    static std::mutex mu;
+    static uint32_t* words[MAX_DEVICES] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= MAX_DEVICES) return cudaErrorInvalidDevice;
+    std::lock_guard<std::mutex> lock(mu);
+    if (!words[dev]) {
+        // the first call on a device may be one that a graph captures; the address may have to load the code first
+        cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+        if ((e = cudaThreadExchangeStreamCaptureMode(&mode)) != cudaSuccess) return e;
+        void* p = nullptr;
+        e = cudaGetSymbolAddress(&p, g_device_status);
+        const cudaError_t back = cudaThreadExchangeStreamCaptureMode(&mode);
+        if (e != cudaSuccess || (e = back) != cudaSuccess) return e;
+        words[dev] = static_cast<uint32_t*>(p);
+    }
+    *word = words[dev];
+    return cudaSuccess;
+}
+
 }  // namespace vbq

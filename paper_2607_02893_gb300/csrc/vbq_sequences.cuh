@@ -18,7 +18,7 @@ struct SeqRange {
 };
 
 // Whatever `starts` holds, the rows are within 0..tokens. `report`: this thread records a slot outside the pool.
-__device__ __forceinline__ SeqRange seq_range(const vbq_sequences& q, int b, int64_t n_slots, bool report) {
+__device__ __forceinline__ SeqRange seq_range(const vbq_sequences& q, int b, int64_t n_slots, bool report, uint32_t* status) {
     SeqRange r;
     const int tokens = (int)q.tokens;
     r.slot = q.slots ? q.slots[b] : b;
@@ -31,7 +31,7 @@ __device__ __forceinline__ SeqRange seq_range(const vbq_sequences& q, int b, int
         r.n = q.rows;
     }
     if (r.slot >= n_slots) {
-        if (report) atomicOr(&g_device_status, VBQ_DEVICE_RANGE);
+        if (report) atomicOr(status, VBQ_DEVICE_SLOT);
         r.slot = -1;
     }
     return r;
