@@ -53,7 +53,10 @@ class Sequences:
             tokens = batch * rows
         elif tokens is None:
             raise ValueError("starts needs tokens, the rows of the calls' arrays")
-        self.batch, self.rows, self.tokens = batch, rows, int(tokens)
+        tokens = int(tokens)
+        if not 0 <= tokens < 1 << 63:
+            raise ValueError("tokens must be within 0..2^63 - 1")
+        self.batch, self.rows, self.tokens = batch, rows, tokens
         self.starts, self.slots, self.fresh = starts, slots, fresh
         self.device = -1                                          # any
         for name, t, n in (("starts", starts, batch + 1), ("slots", slots, batch), ("fresh", fresh, batch)):
