@@ -575,6 +575,7 @@ vbq_status_t vbq_causal_conv(const vbq_sequences* seq, const void* x, int64_t x_
  *   q, k       device, row r's k_heads x head_k values at r * stride elements of
  *              `type`, dense within the row; rows 16-byte aligned.
  *   v          device, row r's heads x head_v values, likewise.
+ *   seq        at most 2^31 - 64 tokens (VBQ_ERR_UNSUPPORTED otherwise).
  *   head_k     64 or 128; head_v 64, 128 or 256 (VBQ_ERR_SHAPE otherwise); heads
  *              a multiple of k_heads, at most 1024.
  *   decay, beta   device, row r's heads values at r * stride elements of

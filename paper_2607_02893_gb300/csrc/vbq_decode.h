@@ -165,6 +165,7 @@ struct Delta {
     uint16_t* out;
     uint32_t* status;
 };
+constexpr int64_t DELTA_MAX_TOKENS = (1ll << 31) - 64;   // row numbers rounded up to a chunk's end are ints
 cudaError_t launch_delta_rule(const Delta& d, cudaStream_t s);
 
 struct GatedNorm {

@@ -311,6 +311,8 @@ vbq_status_t vbq_delta_rule(const vbq_sequences* seq, float* state, int64_t n_sl
     if (!std::isfinite(scale)) return fail(VBQ_ERR_ARG, "scale must be finite");
     if (normalize != 0 && normalize != 1) return fail(VBQ_ERR_ARG, "normalize must be 0 or 1, got %d", normalize);
     if (!a_log != !dt_bias) return fail(VBQ_ERR_ARG, "a_log and dt_bias go together");
+    if (seq->tokens > vbq::DELTA_MAX_TOKENS)
+        return fail(VBQ_ERR_UNSUPPORTED, "tokens must be at most 2^31 - 64, got %lld", (long long)seq->tokens);
     if (seq->batch == 0 || seq->tokens == 0) return VBQ_OK;
     if (!state || !decay || !beta || !out) return fail(VBQ_ERR_ARG, "state, decay, beta and out must be non-NULL");
     st = check_strided("q", q, seq->tokens, (int64_t)k_heads * head_k, q_stride, type);

@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(32 * DR_WARPS, 8) delta_token_kernel(Delta d) 
     const int64_t out_row = (int64_t)d.heads * d.head_v;
     uint16_t* out = d.out + r.lo * out_row + h * d.head_v + col;
     if (r.slot < 0) {
-        for (int64_t t = part; t < r.n; t += 8) *reinterpret_cast<uint2*>(out + t * out_row) = make_uint2(0, 0);
+        for (int t = part; t < r.n; t += 8) *reinterpret_cast<uint2*>(out + t * out_row) = make_uint2(0, 0);
         return;
     }
     float* state = d.state + ((int64_t)r.slot * d.heads + h) * DK * d.head_v + (int64_t)part * PER * d.head_v + col;
@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(32 * DR_WARPS, 8) delta_token_kernel(Delta d) 
     // Gates of 32 tokens, one a lane.
     float keep_of = 0.f, beta_of = 0.f;
     const auto gates = [&](int t) {
-        if (lane >= r.n - t) return;
+        if (t + lane >= r.n) return;
         const int64_t row = (int64_t)r.lo + t + lane;
         const Gate g = gate_of(gate_value(d.decay, d.gate_f32, row * d.decay_stride + h), gate_value(d.beta, d.gate_f32, row * d.beta_stride + h),
                                raw, rate, bias);
@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(32 * RW_WARPS) delta_rows_kernel(Delta d, int 
     const int64_t out_row = (int64_t)d.heads * d.head_v;
     uint16_t* out = d.out + r.lo * out_row + h * d.head_v + col;
     if (r.slot < 0) {
-        for (int64_t t = part; t < r.n; t += 8) *reinterpret_cast<uint32_t*>(out + t * out_row) = 0;
+        for (int t = part; t < r.n; t += 8) *reinterpret_cast<uint32_t*>(out + t * out_row) = 0;
         return leave();
     }
     const int hk = h / (d.heads / d.k_heads);
@@ -225,10 +225,10 @@ __global__ void __launch_bounds__(32 * RW_WARPS) delta_rows_kernel(Delta d, int 
         return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
     };
 #pragma unroll 1
-    for (uint32_t t0 = 0; t0 < (uint32_t)r.n; t0 += BATCH) {          // r.n: up to 2^31 - 1
+    for (int t0 = 0; t0 < r.n; t0 += BATCH) {
         const In& now = in[(t0 / BATCH) & 1];
-        const int n = min(BATCH, r.n - (int)t0);
-        if (r.n - (int)t0 > BATCH) {
+        const int n = min(BATCH, r.n - t0);
+        if (t0 + BATCH < r.n) {
             copy(t0 + BATCH);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
         } else {

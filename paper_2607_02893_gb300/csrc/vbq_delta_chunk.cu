@@ -1111,7 +1111,7 @@ __global__ void __launch_bounds__(Shape<F32, DK, CW>::THREADS, 1) delta_chunk_ke
         return;
     }
     const uint32_t base = smem_u32(smem);
-    const int chunks = (r.n - 1) / CH + 1;                          // r.n: up to 2^31 - 1
+    const int chunks = (r.n + CH - 1) / CH;
     // Three warpgroups of 168 registers a thread at launch; the chain takes what the preparing warps leave.
     static_assert(Z::THREADS == 384);
     if (threadIdx.x < Z::CHAIN) {
