@@ -593,9 +593,14 @@ vbq_status_t vbq_causal_conv(const vbq_sequences* seq, const void* x, int64_t x_
  *              64 between tokens; beyond that their outputs may be NaN. What of a
  *              BF16 key or query is below 2^-31 of the largest of the same key or
  *              query loses digits there.)
- *   out        device, tokens x heads x head_v BF16, dense.
- * The state and all sums are fp32. Results do not vary between calls; a
- * sequence's are the same to rounding however its tokens are cut into calls.
+ *   out        device, tokens x heads x head_v BF16, dense. Must not overlap q, k,
+ *              v, the gates or the state.
+ * The state and all sums are fp32. Sequences of more than 22 rows (28 where the
+ * call's others fill the GPU) are taken 64 tokens at a time; operands of their
+ * products, those of the outputs too, are pairs of FP16 parts there, good to
+ * 2^-22 of the largest of their column or token. Results do not vary between
+ * calls; a sequence's are the same to rounding however its tokens are cut into
+ * calls.
  * What is NaN or infinite in a token reaches no token before it.
  */
 vbq_status_t vbq_delta_rule(const vbq_sequences* seq, float* state, int64_t n_slots, const void* q, int64_t q_stride,

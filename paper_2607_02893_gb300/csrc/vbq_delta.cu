@@ -25,9 +25,11 @@ namespace {
 
 constexpr int DR_WARPS = 2;                      // of a block; 16 columns each
 constexpr int DR_COLS = 16 * DR_WARPS;
-// A sequence of more rows goes by chunks. Token by token 1 x 32 heads of 128 take 2.8 us and 0.29 a token, 4 x 16 heads 3.1
-// and 0.36, 16 x 32 heads 9.6 and 1.9; one chunk takes them 9.4, 11.4 and 67 us: the first two, whose blocks of 64 columns
-// the GPU holds at once, change over at 23 rows, the third at 30.
+// A sequence of more rows goes by chunks. Measured with BF16 heads of 128 by 128: token by token 22 and 28 rows take 1 x 32
+// heads 8.8 and 10.3 us, 4 x 16 heads 11.1 and 13.1, 16 x 32 heads 54 and 65; one chunk takes them 9.0, 10.6 and 69: the
+// first two, whose blocks of 64 columns the GPU holds at once, change over near 22 rows, the third at 30. Others would change
+// over elsewhere: fp32 heads of 128 by 128, whose chunks are slower, at more than 64 rows (16 x 32: 132 us against 245 there),
+// fp32 heads of 64 by 64 at 34 (3 x 12) or more than 64 (16 x 32), BF16 heads of 64 by 64 at 27 (4 x 16) or 38 (16 x 32).
 constexpr int DELTA_ROWS = 22, DELTA_ROWS_FULL = 28;
 
 template <bool F32, int DK>
@@ -173,8 +175,11 @@ __global__ void __launch_bounds__(32 * RW_WARPS) delta_rows_kernel(Delta d, int 
     __shared__ __align__(16) In in[2];
     __shared__ float4 token[BATCH];              // keep; beta; the unit key's factor; the scaled unit query's
     __shared__ float product[BATCH];             // q.k of these
-    // Beside the kernel before it, which lets this one start when what came before both is done (the fence: no line that the
-    // SM still has is read): block 0 waits for that one at its end instead, so that this grid does not count as done before it.
+    // Beside the chunk kernel: that one's blocks let this one start, each after its own griddepcontrol.wait, and no block here
+    // starts before the last of them has. So what the kernels before both wrote is complete and in global memory by then: the
+    // wait's promise to the chunk kernel, which holds for whatever starts later and has no older copies of a line (the fence
+    // drops those that the SM may have). Of the chunk kernel itself nothing is read: each leaves the other's sequences alone.
+    // Block 0 waits for it at the end, so that this grid does not count as done before it and what waits for this one has both.
     if (beside) asm volatile("fence.acq_rel.gpu;" ::: "memory");
     else asm volatile("griddepcontrol.wait;" ::: "memory");
     const auto leave = [&] {
@@ -314,8 +319,8 @@ cudaError_t launch_rows(const Delta& d, int most, bool beside, cudaStream_t s) {
 
 // Sequences of a few rows go token by token, longer ones by chunks: with `starts` by the rows that they turn out to have, not
 // by what the call says of the longest, since up to 22 rows keys may be of any sizes. Where the call's may be of both kinds,
-// both kernels run, each over its own and side by side (24 single tokens and a prompt of 2000, 32 heads of 128: 185 us one
-// after the other, 165 so).
+// both kernels run, each over its own and side by side (24 single tokens and a prompt of 2000, 32 heads of 128, when it was
+// added: 185 us one after the other, 165 so).
 cudaError_t launch_delta_rule(const Delta& d, cudaStream_t s) {
     int sms = 0;
     const int err = device_sms(&sms);

@@ -11,42 +11,44 @@
 // Only R, U, o and the new state depend on the state; T and the scores do not.
 //
 // The chunks are a chain, and the columns of S do not meet. So a block takes one
-// sequence, one head and 16 columns for each of its chain warps, and a chain
-// warp holds S^T for its 16 columns in the accumulators of m16n8k16 (columns x
-// head_k) over the whole sequence. Everything is computed transposed: what comes
-// out of one product is, in the same registers, the A operand of the next, so
-// the chain has no exchange between warps and nothing but key, query, T and
-// score fragments is read from shared memory. Where there are two chain warps, two
-// more make the outputs, from the parts of S and U that they are handed (2.30 ->
-// 2.16 ms for 32768 tokens). Eight other warps prepare the next chunk meanwhile, in
-// two groups that work side by side. The one for queries takes keys and queries to
+// sequence, one head and 16 columns for each of its chain warps, and a chain warp
+// holds S^T for its 16 columns in the accumulators of m16n8k16 (columns x head_k)
+// over the whole sequence. Everything is computed transposed: what comes out of one
+// product is, in the same registers, the A operand of the next, so the chain has no
+// exchange between warps and nothing but key, query, T and score fragments is read
+// from shared memory. Where there are two chain warps, two more make the outputs,
+// from the parts of S and U that they are handed (when it was added, 2.30 -> 2.16
+// ms for 32768 tokens). Eight other warps prepare the next chunk meanwhile, in two
+// groups that work side by side. The one for queries takes keys and queries to
 // FP16, multiplies queries with keys, makes the scores and goes on to the next
 // chunk's rows; the one for keys multiplies keys with keys and makes T: blocks of
 // 16 on the diagonal by substitution in fp32, the ones below them by products.
 // Named barriers hand the stages over.
 //
-// What bounds it is neither memory nor the tensor cores (a third busy) but the
-// chain of instructions a chunk takes: 14 thousand of twelve warps, 0.42 an issue slot,
+// What bounds it is neither memory nor the tensor cores (39% busy) but the chain of
+// instructions a chunk takes: 15.6 thousand of twelve warps, 0.43 an issue slot,
 // each waiting for the one before it or for another group. Two blocks do not
 // fit in the registers of an SM. The code of both roles is twice the 32 KB that
 // an SM keeps of it, so what a chunk does not need twice is not written out
 // twice: loops are rolled wherever registers need no index. One sequence of 32768
-// tokens, 32 heads of 128 by 128, blocks of 32 columns: 2.16 ms, 4.2 us a chunk
-// (with three of four chunks not prepared: 3.4); memory needs
-// 0.12 ms of it.
+// tokens, 32 heads of 128 by 128, blocks of 32 columns: 2.29 ms, 4.5 us a chunk
+// (before the outputs took both parts of their operands 4.2, and with three of four
+// chunks not prepared 3.4); memory needs 0.12 ms of it.
 //
 // fp32 through the tensor cores. BF16 keys and queries are taken to FP16 by a power
-// of two a token, which they survive unchanged (8 bits of 11) down to 2^-31 of their
-// token's largest; S, R, U, T and the scores enter as two FP16 parts, x = hi + lo, with a
-// power of two per column of S (the scores: per row), so a product is good to 2^-22
-// (fp32 keys and queries, with a power of two a token, are two parts as well). That
-// holds for the outputs too, which are rounded once: with one part (2^-12) of S, U,
-// the scores and fp32 queries they were off by many steps of BF16 where terms cancel
-// (32768 tokens in 2.16 ms against 2.28, five prompts in 515 us against 555). T and L
-// are up by 2^10, so that what a strong decay leaves of an earlier token's R keeps
-// its digits (parts end at 2^-35, not 2^-25, which had an element of 2e-5 off by
-// 2e-8); they overflow from 64 on, and where the rule
-// contracts |T_ij| is at most |beta_i| |k_i| |k_j|, 2 for keys of unit length.
+// of two a token, which they survive unchanged (8 bits of 11) down to 2^-31 of
+// their token's largest; S, R, U, T and the scores enter as two FP16 parts, x = hi
+// + lo, with a power of two per column of S (the scores: per row), so a product is
+// good to 2^-22 (fp32 keys and queries, with a power of two a token, are two parts
+// as well). That holds for the outputs too, which are rounded once: with one part
+// (2^-11) of S, U, the scores and fp32 queries they were off by many steps of BF16
+// where terms cancel (32768 tokens in 2.16 ms against 2.28, five prompts in 515 us
+// against 555). A power of two for the rows of a warp together instead of one a
+// token cost tokens their digits beside larger ones, and saved 1%. T and L are up
+// by 2^10, so that what a strong decay leaves of an earlier token's R keeps its
+// digits (parts end at 2^-35, not 2^-25, which had an element of 2e-5 off by 2e-8);
+// they overflow from 64 on, and where the rule contracts |T_ij| is at most |beta_i|
+// |k_i| |k_j|, 2 for keys of unit length.
 //
 // NaN and infinities must not reach earlier tokens through the zeros above the
 // diagonal: a column whose R is not finite at some token is computed without it
@@ -399,7 +401,7 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
             // 16 rows of keys or of queries with the keys up to theirs
             {
                 // The four parts of an SM take the warps in turn, so two chain warps leave two parts to the others: those get the
-                // rows with most columns (balanced over keys and queries: 2.18 against 2.16 ms for 32768 tokens). Four: balanced.
+                // rows with most columns (balanced over keys and queries 1% more time for 32768 tokens). Four: balanced.
                 const int mt = of_q && CW != 2 ? 3 - warp : warp;
                 float acc[8][4];
 #pragma unroll
@@ -429,30 +431,24 @@ __device__ __forceinline__ void prepare_chunks(const Delta& d, const SeqRange& r
                         }
                     }
                 } else {
-                    uint32_t a[2][4], l[2][4], b[2][4][4];          // one step ahead
-                    const auto load = [&](int to, int kk) {
-                        ldmatrix4(a[to], a_at + a_in + 32 * kk);
-                        if (of_q) ldmatrix4(l[to], a_at + own_in + 32 * kk);
+#pragma unroll 1
+                    for (int kk = 0; kk < DK / 16; ++kk) {
+                        uint32_t a[4], l[4], b[4][4];
+                        ldmatrix4(a, a_at + a_in + 32 * kk);
+                        if (of_q) ldmatrix4(l, a_at + own_in + 32 * kk);
 #pragma unroll
                         for (int n2 = 0; n2 < 4; ++n2)
-                            if (n2 <= mt) ldmatrix4(b[to][n2], sb + Z::K + b_in + 16 * n2 * Z::KP + 32 * kk);
-                    };
-                    const auto multiply = [&](int at) {
+                            if (n2 <= mt) ldmatrix4(b[n2], sb + Z::K + b_in + 16 * n2 * Z::KP + 32 * kk);
                         if (of_q) {
-                            mma(squares[0], a[at], l[at][0], l[at][1]);
-                            mma(squares[1], a[at], l[at][2], l[at][3]);
+                            mma(squares[0], a, l[0], l[1]);
+                            mma(squares[1], a, l[2], l[3]);
                         }
 #pragma unroll
                         for (int n2 = 0; n2 < 4; ++n2)
                             if (n2 <= mt) {
-                                mma(acc[2 * n2], a[at], b[at][n2][0], b[at][n2][1]);
-                                mma(acc[2 * n2 + 1], a[at], b[at][n2][2], b[at][n2][3]);
+                                mma(acc[2 * n2], a, b[n2][0], b[n2][1]);
+                                mma(acc[2 * n2 + 1], a, b[n2][2], b[n2][3]);
                             }
-                    };
-#pragma unroll 1
-                    for (int kk = 0; kk < DK / 16; ++kk) {
-                        load(0, kk);
-                        multiply(0);
                     }
                 }
                 float own_acc[2][4];                                // the block on the diagonal
@@ -1140,14 +1136,14 @@ cudaError_t launch_shape(const Delta& d, int above, cudaStream_t s) {
 template <bool F32, int DK>
 cudaError_t launch_width(const Delta& d, int above, int sms, cudaStream_t s) {
     // Columns of a block. All blocks of a head prepare the same chunks, so fewer and wider ones do less in all, and more and
-    // narrower ones fill the GPU. A chunk takes a block of 32 or 64 columns about 4.2 and 4.9 us; the rounds of blocks are
+    // narrower ones fill the GPU. A chunk takes a block of 32 or 64 columns about 4.5 and 5.2 us; the rounds of blocks are
     // counted by the sequences like the longest that the tokens make up. Five sequences of 1774 to 3001 tokens, 32 heads of
-    // 128: 770 and 515 us; one of 32768: 2160 and 2510. (128 columns, which leave the preparing warps half the registers,
-    // took 11.2 us a chunk.) fp32 values leave no room for the wider one.
+    // 128: 859 and 550 us; one of 32768: 2290 and 2650. (128 columns, which leave the preparing warps half the registers,
+    // took 11.2 us a chunk.) Measured with BF16 heads of 128 by 128. fp32 values leave no room for the wider one.
     if constexpr (!F32) {
         const int64_t alike = (d.seq.tokens + d.seq.rows / 2) / d.seq.rows, sequences = alike < 1 ? 1 : alike > d.seq.batch ? d.seq.batch : alike;
         const auto cost = [&](int columns, int64_t each) { return (sequences * d.heads * d.head_v / columns + sms - 1) / sms * each; };
-        if (cost(64, 49) < cost(32, 42)) return launch_shape<F32, DK, 4>(d, above, s);
+        if (cost(64, 52) < cost(32, 45)) return launch_shape<F32, DK, 4>(d, above, s);
     }
     return launch_shape<F32, DK, 2>(d, above, s);
 }
